@@ -249,7 +249,7 @@ def _prepare_verify(c, seed):
     drafts = (dp.float() / torch.empty_like(dp, dtype=torch.float32).exponential_(generator=g).clamp_min(1e-20)).argmax(1).int()
     s = {"c": c, "tp": tp, "dp": dp if c["sampled"] else None, "drafts": drafts, "cu": cu,
          "u": torch.rand(n, device=DEV, generator=g),
-         "noise": torch.empty(B, V, device=DEV).exponential_(generator=g).clamp_min(1e-20), "max_draft": max(lens)}
+         "noise": torch.empty(B, V, device=DEV).exponential_(generator=g).clamp_min(1e-20)}
     if own:
         from paper_2608_02691_gb300 import optr
         i32 = torch.int32
@@ -257,7 +257,6 @@ def _prepare_verify(c, seed):
         s["p"] = _params({"h_kv": 8, **G32}, rot)
         s["accepted"] = torch.empty(B, device=DEV, dtype=i32)
         s["tokens"] = torch.empty(n + B, device=DEV, dtype=i32)
-        s["ws"] = optr.new_verify_workspace(B)
     return s
 
 
@@ -280,7 +279,7 @@ def run(s):
         optr.optr_kv_read(s["p"], s["cu"], s["pos0"], s["table"], s["pool"], s["k"], s["v"])
         return s["k"], s["v"]
     optr.optr_verify_drafts(s["p"], s["tp"], s["dp"], s["drafts"], s["u"], s["noise"], s["cu"],
-                            s["accepted"], s["tokens"], s["ws"])
+                            s["accepted"], s["tokens"])
     return s["accepted"], s["tokens"]
 
 
