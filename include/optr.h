@@ -164,6 +164,7 @@ typedef enum {
 #define OPTR_DEVERR_TIMEOUT 32u  /* internal: a kernel's bounded wait gave up */
 #define OPTR_DEVERR_WIN_SLOT 64u /* window slot of a sequence < 0 or >= n_slots */
 #define OPTR_DEVERR_CALIB_RANGE 128u /* calibration: generator norm past exp's scaling range */
+#define OPTR_DEVERR_TOKEN 256u   /* draft token < 0 or >= vocab */
 
 /* Kernel variants (for measurement; 0 picks the library default). */
 #define OPTR_VARIANT_DEFAULT 0
@@ -204,7 +205,7 @@ typedef struct {
  *   mu    host float32 [h_kv][D]: per-channel key mean (Appendix, key-mean
  *         estimation).  Pass all zeros for no centering.
  *   out   host; receives the new handle, or NULL on error.
- * Allocates device memory on the current device (about h_kv * 200 KB) and
+ * Allocates device memory on the current device (about h_kv * 450 KB) and
  * copies synchronously.  Returns OPTR_OK or a negative status.
  */
 optr_status optr_params_create(const optr_config* cfg, const float* R_k,
@@ -419,6 +420,120 @@ optr_status optr_decode_step_win(const optr_params* p, const void* q,
                                  const int32_t* win_slot, int n_slots,
                                  float* out, void* workspace, size_t ws_bytes,
                                  cudaStream_t stream);
+
+/*
+ * Attention of a chunk of new tokens over the paged cache: the step of a
+ * prefill whose earlier tokens are cached already (or of a whole prompt, with
+ * nothing cached), and of a batch of drafted tokens.  Sequence b holds
+ * n = pos0[b] cached tokens and gets the new tokens t = cu_new[b] ..
+ * cu_new[b+1]-1 (rows of q, k and v); with query head j, KV head
+ * h = j / (h_q / h_kv), and i = t - cu_new[b]:
+ *      l_s = <q_j R_k[h], khat_R,s> / sqrt(D)      cached INT2 positions s of a
+ *                                                 sequence of n tokens
+ *      l_s = <q_j, k_s - mu[h]> / sqrt(D)         its BF16-window positions, and
+ *                                                 the chunk's own tokens 0 .. i
+ *      p   = softmax over all of them
+ *      out_j = (sum_INT2 p_s vhat_R,s) R_v[h]^T + sum_others p_s v_s    (bf16)
+ * The chunk's own keys and values are taken exactly as given; the cache is
+ * only read, whatever its pages hold from position n on.  Call it before the
+ * tokens are written (optr_kv_append_win turns the window ring over), and write
+ * only those that stay: rejected drafts then leave no trace.  With R_v = NULL
+ * at create, v and out are in the folded basis.
+ *   q, out      device bf16 [n_tok][h_q][D].
+ *   k, v        device bf16 [n_tok][h_kv][D].
+ *   n_tok       host; new tokens of all sequences (0 is a no-op).
+ *   cu_new      device int32 [B+1], as in optr_kv_append.
+ *   pos0        device int32 [B]: cached tokens per sequence, 0 .. max_pages*16.
+ *   max_new     host; no sequence gets more new tokens than this.
+ *   block_table device int32 [B][max_pages], pool as in optr_decode_attention
+ *               (read only).
+ *   workspace   device, optr_chunk_workspace_size bytes, 256-byte aligned,
+ *               scratch as in optr_decode_attention.
+ * Softmax, sums and accumulators are float32; out is rounded once to bf16.
+ * Inputs must be finite; a sequence's rows depend on no other sequence's.  A
+ * sequence with pos0 out of range (OPTR_DEVERR_SEQ_LEN), more than max_new
+ * tokens or inconsistent cu_new (OPTR_DEVERR_CU_NEW) gets zero rows; keys of an
+ * out-of-range page (OPTR_DEVERR_PAGE_ID) or window slot
+ * (OPTR_DEVERR_WIN_SLOT) are left out.  Nothing is allocated or synchronised.
+ */
+size_t optr_chunk_workspace_size(const optr_params* p, int n_tok, int B, int max_new);
+
+optr_status optr_chunk_attention(const optr_params* p, const void* q,
+                                 const void* k, const void* v, int n_tok,
+                                 const int32_t* cu_new, const int32_t* pos0,
+                                 int max_new, const int32_t* block_table, int B,
+                                 int max_pages, const uint8_t* pool,
+                                 int num_pages, void* out, void* workspace,
+                                 size_t ws_bytes, cudaStream_t stream);
+
+/* The same with the BF16 windows of p (see "BF16 windows"); with
+ * sink = recent = 0 exactly the plain call. */
+optr_status optr_chunk_attention_win(const optr_params* p, const void* q,
+                                     const void* k, const void* v, int n_tok,
+                                     const int32_t* cu_new, const int32_t* pos0,
+                                     int max_new, const int32_t* block_table,
+                                     int B, int max_pages, const uint8_t* pool,
+                                     int num_pages, const void* win,
+                                     const int32_t* win_slot, int n_slots,
+                                     void* out, void* workspace,
+                                     size_t ws_bytes, cudaStream_t stream);
+
+/*
+ * Read the cache back: the INT2 records of positions pos0[b] ..
+ * pos0[b] + cu_read[b+1] - cu_read[b] - 1 of each sequence as rows
+ * cu_read[b] .. cu_read[b+1]-1 of k and v in the model's basis,
+ *      k = khat_R R_k[h]^T + mu[h],   v = vhat_R R_v[h]^T   (R_v = NULL: vhat)
+ * rounded once to bf16 (float32 accumulation; the dequantized value is rounded
+ * to fp16 before it is rotated).  For moving a sequence to other rotations, to
+ * another cache or to an attention of one's own.  Window positions too are
+ * read from their records (their exact rows are in the window store).
+ *   k, v        device bf16 [n_tok][h_kv][D], written.
+ *   n_tok       host; rows (0 is a no-op).  The rest as in optr_kv_append.
+ * A row whose position, page or cu_read entry is out of range is flagged
+ * (OPTR_DEVERR_*) and reads as the row of an all-zero record.
+ */
+optr_status optr_kv_read(const optr_params* p, int n_tok,
+                         const int32_t* cu_read, const int32_t* pos0,
+                         const int32_t* block_table, int B, int max_pages,
+                         const uint8_t* pool, int num_pages, void* k, void* v,
+                         cudaStream_t stream);
+
+/*
+ * Verification of drafted tokens against the target's probabilities, from
+ * given random numbers.  Sequence b has the drafts x = drafts[cu_draft[b] ..
+ * cu_draft[b+1]-1], n of them (n may be 0), a target row p_i after each prefix,
+ * rows cu_draft[b] + b + i (i = 0 .. n) of target_probs, and a draft row q_i
+ * for each draft, rows cu_draft[b] + i of draft_probs.  Draft i is accepted
+ * while u_i q_i(x_i) < p_i(x_i) (one float32 product); a of them are.  The next
+ * token is the first maximum over the vocabulary of r(v) / e(v) in float32,
+ *      r = max(p_a - q_a, 0)  (a < n)     or  r = p_n  (a = n),
+ * and r = p_a where that residual is zero everywhere: a draw from r / sum r
+ * when the numbers e of the sequence are independent and exponential.
+ *   target_probs device [n_draft + B][vocab], float32 or bf16 (probs_dtype).
+ *   draft_probs  device [n_draft][vocab] of the same type, or NULL: drafted
+ *                without probabilities (q_i is 1 at x_i and 0 elsewhere).
+ *   drafts       device int32 [n_draft].
+ *   uniform      device float32 [n_draft]: u, in [0, 1).
+ *   noise        device float32 [B][vocab]: e, positive.
+ *   cu_draft     device int32 [B+1], cu_draft[B] = n_draft.
+ *   accepted     device int32 [B]: a.
+ *   tokens       device int32 [n_draft + B], rows as target_probs': the
+ *                accepted drafts, the next token, then -1.
+ * Probabilities are finite and not negative; a row need not sum to exactly 1.
+ * A draft out of 0 .. vocab-1 is rejected and sets OPTR_DEVERR_TOKEN; a
+ * sequence whose cu_draft is out of range gets accepted = -1 and sets
+ * OPTR_DEVERR_CU_NEW (p serves the device error word only).  Nothing is
+ * allocated or synchronised.
+ */
+#define OPTR_PROBS_F32 0
+#define OPTR_PROBS_BF16 1
+optr_status optr_verify_drafts(const optr_params* p, const void* target_probs,
+                               const void* draft_probs, int probs_dtype,
+                               const int32_t* drafts, const float* uniform,
+                               const float* noise, const int32_t* cu_draft,
+                               int n_draft, int B, int vocab,
+                               int32_t* accepted, int32_t* tokens,
+                               cudaStream_t stream);
 
 /* Static description of a status code. */
 const char* optr_strerror(optr_status s);

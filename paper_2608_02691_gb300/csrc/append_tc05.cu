@@ -44,23 +44,24 @@
 // The quantizer is quant.cuh's float32 formula.
 #include "append_common.cuh"
 #include "decode_common.cuh"
+#include "dequant.cuh"
 #include "f32x2.cuh"
 #include "quant.cuh"
 #include "tc05.cuh"
+#include "tmap.cuh"
 #include "window.cuh"
 
-#include <cudaTypedefs.h>
-#include <mutex>
 #include <type_traits>
 
 namespace optr {
 
-// Host: B operand of one rotation for tcgen05 (f16, K-major, no swizzle):
-// out[term][n][k] = (hi, lo) fp16 parts of 64 R[k][n] at element offset
+// Host: B operand of a product on tcgen05 (f16, K-major, no swizzle):
+// out[term][n][k] = (hi, lo) fp16 parts of 64 x(n, k) at element offset
 // ((n / 8) * 2048 + (k / 8) * 128 + (n % 8) * 16 + (k % 8) * 2) / 2 of the
-// term's 32 KB, i.e. core matrices of 8 output channels x 8 input channels,
-// 128 B apart along k (LBO) and 2048 B apart along n (SBO).
-void build_rotation_tc05(const float* R, uint16_t* out) {
+// term's 32 KB, i.e. core matrices of 8 columns n x 8 inner indices k, 128 B
+// apart along k (LBO) and 2048 B apart along n (SBO).
+template <typename F>
+static void build_operand_tc05(F x, uint16_t* out) {
   auto h16 = [](float x) -> uint16_t {
     __half_raw r = __half(__float2half_rn(x));
     return r.x;
@@ -72,12 +73,20 @@ void build_rotation_tc05(const float* R, uint16_t* out) {
   };
   for (int n = 0; n < kD; ++n)
     for (int k = 0; k < kD; ++k) {
-      const float x = R[(size_t)k * kD + n] * 64.0f;
-      const uint16_t hi = h16(x), lo = h16(x - f16(hi));
+      const float y = x(n, k) * 64.0f;
+      const uint16_t hi = h16(y), lo = h16(y - f16(hi));
       const size_t off = ((size_t)(n / 8) * 2048 + (k / 8) * 128 + (n % 8) * 16 + (k % 8) * 2) / 2;
       out[off] = hi;
       out[(size_t)kD * kD + off] = lo;
     }
+}
+
+void build_rotation_tc05(const float* R, uint16_t* out) {
+  build_operand_tc05([R](int n, int k) { return R[(size_t)k * kD + n]; }, out);
+}
+
+void build_back_rotation_tc05(const float* R, uint16_t* out) {
+  build_operand_tc05([R](int n, int k) { return R[(size_t)n * kD + row_channel(k)]; }, out);
 }
 
 namespace {
@@ -601,36 +610,6 @@ append_tc05_kernel(const __grid_constant__ CUtensorMap tmap_k,
 
 }  // namespace
 
-// cuTensorMapEncodeTiled from the driver, looked up once.
-static PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
-  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000,
-                                         cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
-  });
-  return fn;
-}
-
-// Tensor map of x[n_tok][h_kv][128] bf16: box of 64 channels x 1 head x 128
-// tokens, 128-byte swizzle, zero fill past the end.
-static bool token_rows_map(CUtensorMap* m, const __nv_bfloat16* x, int n_tok, int h_kv) {
-  PFN_cuTensorMapEncodeTiled_v12000 fn = encode_fn();
-  if (!fn) return false;
-  const cuuint64_t dims[3] = {(cuuint64_t)kD, (cuuint64_t)h_kv, (cuuint64_t)n_tok};
-  const cuuint64_t strides[2] = {(cuuint64_t)kD * 2, (cuuint64_t)h_kv * kD * 2};
-  const cuuint32_t box[3] = {64, 1, (cuuint32_t)kRows};
-  const cuuint32_t estr[3] = {1, 1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(x), dims,
-            strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
-         CUDA_SUCCESS;
-}
-
 cudaError_t launch_append_tc05(const optr_params* p, const __nv_bfloat16* k,
                                const __nv_bfloat16* v, int n_tok,
                                const int32_t* cu_new, const int32_t* pos0,
@@ -652,7 +631,7 @@ cudaError_t launch_append_tc05(const optr_params* p, const __nv_bfloat16* k,
   if (e != cudaSuccess) return e;
   const int h_kv = p->cfg.h_kv;
   CUtensorMap mk, mv;
-  if (!token_rows_map(&mk, k, n_tok, h_kv) || !token_rows_map(&mv, v, n_tok, h_kv))
+  if (!token_rows_map(&mk, k, n_tok, h_kv, kRows) || !token_rows_map(&mv, v, n_tok, h_kv, kRows))
     return cudaErrorInvalidValue;
   const int tiles = (n_tok + kRows - 1) / kRows;
   // one CTA per SM (the shared memory admits no second one, so tensor

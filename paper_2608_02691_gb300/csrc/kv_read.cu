@@ -1,0 +1,322 @@
+// Cache read-back (include/optr.h, "optr_kv_read"): the INT2 records of given
+// positions as bf16 rows in the model's basis,
+//   k = khat R_k^T + mu,   v = vhat R_v^T.
+//
+// The mirror of the tcgen05 cache write (append_tc05.cu): per KV head and kind
+// a product Y[tok][128] = Z[tok][128] R^T[128][128] of 128-token tiles, Z the
+// dequantized rows (exact codes, scales and minima, rounded once to fp16;
+// dequant.cuh), R^T as fp16 hi + lo parts of 64 R^T, which keep ~22 bits of it
+// under a float32 accumulator.
+//
+// One CTA per SM works on one (KV head, kind) and loops over its tiles:
+//   8 converter warps  two groups of 4 take alternate tiles, a thread per row:
+//                   table entry requested two of its tiles ahead, record one
+//                   tile ahead, then 128 values into tensor memory (A operand);
+//   MMA warp        one thread issues a tile's 16 tcgen05.mma;
+//   8 epilogue warps  two groups likewise: accumulator rows back, mu, bf16,
+//                   into a swizzled shared-memory tile that two TMA copies
+//                   store.
+// Bound by memory: 96 B (G = 32) or 72 B read and 512 B written per token and
+// KV head.
+#include "append_common.cuh"
+#include "decode_common.cuh"
+#include "dequant.cuh"
+#include "tc05.cuh"
+#include "tmap.cuh"
+
+namespace optr {
+namespace {
+
+constexpr int kRows = 128;
+constexpr int kCuCache = 512;
+constexpr int kConvWarps = 8, kEpiWarps = 8;
+constexpr int kEpiWarp = kConvWarps, kMmaWarp = kConvWarps + kEpiWarps;
+constexpr int kThreads = (kMmaWarp + 1) * 32;
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kColD = 0, kColA = 256;  // D[g] at 128 g, A[g] at 256 + 64 g
+constexpr uint32_t kTileBytes = kRows * kD * 2;
+
+struct Smem {
+  uint16_t b[2][kD * kD];
+  // output rows, bf16: [channel half][row][128 B], TMA 128-byte swizzle
+  uint8_t stage[2][kTileBytes];
+  alignas(16) float add[kD];  // mu (keys) or 0 (values)
+  int cu[kCuCache + 1];
+  int p0[kCuCache];
+  uint64_t aready[2], adone[2], dready[2], dfree[2];
+  uint32_t tmem;
+  int abort;
+};
+
+__device__ __forceinline__ void group_sync(int id) {
+  asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory");
+}
+
+// group_sync, and whether x held in any thread of the group.
+__device__ __forceinline__ bool group_any(int id, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.u32 p, %2, 0;\n"
+      " barrier.cta.red.or.pred q, %1, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+      : "=r"(r) : "r"(id), "r"((uint32_t)x) : "memory");
+  return r != 0;
+}
+
+__device__ __forceinline__ void tma_store_3d(const void* tmap, int c0, int c1, int c2,
+                                             const void* src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
+               ::"l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2),
+                 "r"(tc05::smem_addr(src))
+               : "memory");
+}
+
+// A row's record as read: codes and {scale, min} words.
+struct RawRow {
+  uint4 c0, c1, m;
+};
+
+template <bool kG128>
+__global__ void __launch_bounds__(kThreads, 1)
+kv_read_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+               int n_tok, const int32_t* __restrict__ cu_read, const int32_t* __restrict__ pos0,
+               const int32_t* __restrict__ bt, int B, int max_pages,
+               const uint8_t* __restrict__ pool, int num_pages, int h_kv,
+               const uint16_t* __restrict__ Rk_back, const uint16_t* __restrict__ Rv_back,
+               const float* __restrict__ mu, unsigned* err) {
+  extern __shared__ __align__(1024) unsigned char dsm_[];
+  Smem& S = *reinterpret_cast<Smem*>(dsm_);
+  const int h = blockIdx.y, kind = blockIdx.z;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tiles = (n_tok + kRows - 1) / kRows;
+  const int my_tiles =
+      tiles > (int)blockIdx.x ? (tiles - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0;
+
+  {
+    const uint4* src = reinterpret_cast<const uint4*>(kind ? Rv_back : Rk_back) +
+                       (size_t)h * (2 * kD * kD * 2 / 16);
+    uint4* dst = reinterpret_cast<uint4*>(&S.b[0][0]);
+    for (int i = tid; i < 2 * kD * kD * 2 / 16; i += kThreads) cp_async16_zfill(dst + i, src + i, true);
+    cp_async_commit();
+  }
+  if (tid < kD) S.add[tid] = kind ? 0.f : __ldg(mu + h * kD + tid);
+  if (tid == 0) {
+    for (int g = 0; g < 2; ++g) {
+      tc05::bar_init(&S.aready[g], 128);
+      tc05::bar_init(&S.adone[g], 1);
+      tc05::bar_init(&S.dready[g], 1);
+      tc05::bar_init(&S.dfree[g], 128);
+    }
+    S.abort = (tc05::smem_addr(S.stage[0]) & 1023u) != 0;  // the swizzle's alignment
+    tc05::bar_init_fence();
+  }
+  if (warp == kMmaWarp) tc05::tmem_alloc(&S.tmem, kTmemCols);
+  pdl_wait();
+  pdl_trigger();
+  const bool cached = B <= kCuCache;
+  if (cached) {
+    for (int i = tid; i <= B; i += kThreads) S.cu[i] = __ldcg(cu_read + i);
+    for (int i = tid; i < B; i += kThreads) S.p0[i] = __ldcg(pos0 + i);
+  }
+  cp_async_wait<0>();
+  tc05::fence_proxy_async();
+  tc05::fence_before();
+  __syncthreads();
+  tc05::fence_after();
+  const uint32_t tmem = S.tmem;
+  volatile int* abort = &S.abort;
+
+  if (warp < kConvWarps) {
+    // -------------------------------------------------------- converters
+    const int g = warp >> 2, q = warp & 3, row = 32 * q + lane;
+    const uint32_t tA = tmem + ((uint32_t)(32 * q) << 16) + kColA + 64u * g;
+    auto cu = [&](int b) { return cached ? S.cu[b] : __ldcg(cu_read + b); };
+    // the record's page is requested a tile before the record itself
+    int page = -1, slot = 0;
+    auto request = [&](int i) {
+      page = -1;
+      const int tok = ((int)blockIdx.x + i * (int)gridDim.x) * kRows + row;
+      if (i >= my_tiles || tok >= n_tok) return;
+      int lo = 0, hi = B;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (cu(mid) <= tok) lo = mid; else hi = mid;
+      }
+      const int c0 = cu(lo);
+      if (!(c0 <= tok && tok < cu(lo + 1))) {
+        atomicOr(err, OPTR_DEVERR_CU_NEW);
+        return;
+      }
+      const long long pos = (long long)(cached ? S.p0[lo] : __ldcg(pos0 + lo)) + (tok - c0);
+      if (pos < 0 || pos >= (long long)max_pages * kPage) {
+        atomicOr(err, OPTR_DEVERR_POSITION);
+        return;
+      }
+      slot = (int)(pos % kPage);
+      page = __ldcg(bt + (size_t)lo * max_pages + pos / kPage);
+      if (page < 0) page = num_pages;  // flagged where it is used
+    };
+    auto fetch = [&](RawRow& r) {
+      r.c0 = r.c1 = r.m = make_uint4(0u, 0u, 0u, 0u);
+      if (page < 0) return;
+      if (page >= num_pages) {
+        atomicOr(err, OPTR_DEVERR_PAGE_ID);
+        return;
+      }
+      const uint8_t* rec = pool + ((size_t)page * h_kv + h) * chunk_bytes(kG128);
+      const uint4* c = reinterpret_cast<const uint4*>(
+          rec + (kind ? OPTR_V_CODES_OFFSET : OPTR_K_CODES_OFFSET) + slot * 32);
+      const uint8_t* m = rec + (kind ? vmeta_offset(kG128) : OPTR_K_META_OFFSET) +
+                         slot * meta_stride(kG128);
+      r.c0 = __ldcg(c);
+      r.c1 = __ldcg(c + 1);
+      if (kG128)
+        r.m.x = __ldcg(reinterpret_cast<const uint32_t*>(m));
+      else
+        r.m = __ldcg(reinterpret_cast<const uint4*>(m));
+    };
+    RawRow next;
+    request(g);
+    fetch(next);
+    request(g + 2);
+    for (int i = g, k = 0; i < my_tiles; i += 2, ++k) {
+      const RawRow cur = next;
+      fetch(next);
+      request(i + 4);
+      if (k > 0 && !__all_sync(0xffffffffu, tc05::bar_wait(&S.adone[g], (k - 1) & 1, abort))) break;
+      const SlotMeta m = kG128 ? slot_meta(cur.m.x, cur.m.x, cur.m.x, cur.m.x)
+                               : slot_meta(cur.m.x, cur.m.y, cur.m.z, cur.m.w);
+      const uint32_t word[8] = {cur.c0.x, cur.c0.y, cur.c0.z, cur.c0.w,
+                                cur.c1.x, cur.c1.y, cur.c1.z, cur.c1.w};
+      tc05::fence_after();
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t a[32];
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          dequant_word(word[4 * half + w], m, reinterpret_cast<uint32_t(&)[8]>(a[8 * w]));
+        tc05::tmem_st32(tA + 32u * half, a);
+      }
+      tc05::tmem_wait_st();
+      tc05::fence_before();
+      tc05::bar_arrive(&S.aready[g]);
+    }
+  } else if (warp == kMmaWarp) {
+    // --------------------------------------------------------------- MMA
+    int last = -1;
+    if (lane == 0) {
+      const uint32_t b0 = tc05::smem_addr(&S.b[0][0]);
+      for (int i = 0; i < my_tiles; ++i) {
+        const int g = i & 1, k = i >> 1;
+        if (!tc05::bar_wait(&S.aready[g], k & 1, abort)) break;
+        if (k > 0 && !tc05::bar_wait(&S.dfree[g], (k - 1) & 1, abort)) break;
+        tc05::fence_after();
+        const uint32_t d = tmem + kColD + 128u * g, a = tmem + kColA + 64u * g;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+          for (int term = 0; term < 2; ++term)
+            tc05::mma_ts(d, a + 8u * ks,
+                         tc05::smem_desc(b0 + term * kD * kD * 2 + ks * 256, 128, 2048),
+                         tc05::idesc_f16(128, 128), (ks | term) != 0);
+        tc05::mma_commit(&S.dready[g]);
+        tc05::mma_commit(&S.adone[g]);
+        last = i;
+      }
+      if (last >= 0) {  // the tensor core is done with tensor memory before it is freed
+        tc05::bar_wait_drain(&S.dready[last & 1], (last >> 1) & 1);
+        tc05::bar_wait_drain(&S.adone[last & 1], (last >> 1) & 1);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---------------------------------------------------------- epilogue
+    const int g = (warp - kEpiWarp) >> 2, q = warp & 3, row = 32 * q + lane;
+    const uint32_t tD = tmem + ((uint32_t)(32 * q) << 16) + kColD + 128u * g;
+    uint8_t* out = S.stage[g];
+    const bool leader = q == 0 && lane == 0;
+    const CUtensorMap* tmap = kind ? &tmap_v : &tmap_k;
+    for (int i = g, k = 0; i < my_tiles; i += 2, ++k) {
+      const bool ok = __all_sync(0xffffffffu, tc05::bar_wait(&S.dready[g], k & 1, abort));
+      // the group's previous copies have read the stage
+      if (leader) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      group_sync(1 + g);
+      if (ok) {
+        tc05::fence_after();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t d[32];
+          tc05::tmem_ld32(tD + 32u * c, d);
+          tc05::tmem_wait_ld();
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int ch = 32 * c + 8 * j + 2 * e;
+              const float2 add = *reinterpret_cast<const float2*>(&S.add[ch]);
+              const __nv_bfloat162 z = __floats2bfloat162_rn(
+                  fmaf(__uint_as_float(d[8 * j + 2 * e]), 1.f / 64.f, add.x),
+                  fmaf(__uint_as_float(d[8 * j + 2 * e + 1]), 1.f / 64.f, add.y));
+              y[e] = *reinterpret_cast<const uint32_t*>(&z);
+            }
+            const int chunk = 4 * (c & 1) + j;  // of the channel half c / 2
+            *reinterpret_cast<uint4*>(out + (c >> 1) * (kTileBytes / 2) + row * 128 +
+                                      ((chunk ^ (row & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+          }
+        }
+        tc05::fence_before();
+        tc05::bar_arrive(&S.dfree[g]);
+        tc05::fence_proxy_async();
+      }
+      if (group_any(1 + g, !ok)) break;  // the group leaves together
+      if (leader) {
+        const int tok0 = ((int)blockIdx.x + i * (int)gridDim.x) * kRows;
+        tma_store_3d(tmap, 0, h, tok0, out);
+        tma_store_3d(tmap, 64, h, tok0, out + kTileBytes / 2);
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+      }
+    }
+    if (leader) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+
+  tc05::fence_before();
+  __syncthreads();
+  if (S.abort && tid == 0) atomicOr(err, OPTR_DEVERR_TIMEOUT);
+  if (warp == kMmaWarp) {
+    tc05::fence_after();
+    tc05::tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+}  // namespace
+}  // namespace optr
+
+extern "C" optr_status optr_kv_read(const optr_params* p, int n_tok, const int32_t* cu_read,
+                                    const int32_t* pos0, const int32_t* block_table, int B,
+                                    int max_pages, const uint8_t* pool, int num_pages, void* k,
+                                    void* v, cudaStream_t stream) {
+  using namespace optr;
+  if (!p || n_tok < 0 || B <= 0 || max_pages <= 0 || num_pages <= 0) return OPTR_ERR_INVALID_ARG;
+  if (n_tok == 0) return OPTR_OK;
+  if (!cu_read || !pos0 || !block_table || !pool || !k || !v) return OPTR_ERR_INVALID_ARG;
+  if (!aligned(pool, 16) || !aligned(k, 16) || !aligned(v, 16)) return OPTR_ERR_INVALID_ARG;
+  const void *kd = nullptr, *vd = nullptr;
+  bool k_host = false, v_host = false;
+  // the rows are stored by TMA: device memory only
+  if (!io_pointer(k, &kd, &k_host) || !io_pointer(v, &vd, &v_host) || k_host || v_host)
+    return OPTR_ERR_INVALID_ARG;
+  if ((long long)max_pages * kPage > (1LL << 30)) return OPTR_ERR_OUT_OF_RANGE;
+  const int h_kv = p->cfg.h_kv;
+  auto fn = p->cfg.group == 4 * kG ? kv_read_kernel<true> : kv_read_kernel<false>;
+  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), sizeof(Smem));
+  if (e != cudaSuccess) return OPTR_ERR_CUDA;
+  CUtensorMap mk, mv;
+  if (!token_rows_map(&mk, kd, n_tok, h_kv, kRows) || !token_rows_map(&mv, vd, n_tok, h_kv, kRows))
+    return OPTR_ERR_CUDA;
+  const int tiles = (n_tok + kRows - 1) / kRows;
+  const int per = max(1, min(tiles, p->num_sms / (2 * h_kv)));
+  return cuda_status(launch_pdl(fn, dim3(per, h_kv, 2), dim3(kThreads), sizeof(Smem), stream, mk, mv,
+                                n_tok, cu_read, pos0, block_table, B, max_pages, pool, num_pages,
+                                h_kv, (const uint16_t*)p->Rk_back, (const uint16_t*)p->Rv_back,
+                                (const float*)p->mu, p->err));
+}

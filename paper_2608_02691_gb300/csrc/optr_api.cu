@@ -18,24 +18,11 @@ using namespace optr;
 
 namespace {
 
-bool aligned(const void* ptr, size_t a) {
-  return (reinterpret_cast<uintptr_t>(ptr) % a) == 0;
-}
-
-optr_status cuda_status(cudaError_t e) {
-  return e == cudaSuccess ? OPTR_OK : OPTR_ERR_CUDA;
-}
-
 size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-// A per-step activation (k, v, q or out) as the kernels address it: device
-// or managed memory as given; page-locked host memory through its device
-// mapping (*host set), which the kernels then read or write in place over
-// the host link.  Pageable host memory, or a pointer the runtime does not
-// know, is refused (false), so no kernel ever dereferences it.
-//
-// Device memory is the common answer and the driver gives it alone faster
-// than cudaPointerGetAttributes gives every attribute.
+// The driver's pointer query: device memory is the common answer and the
+// driver gives it alone faster than cudaPointerGetAttributes gives every
+// attribute.
 PFN_cuPointerGetAttribute_v4000 pointer_attribute_fn() {
   static PFN_cuPointerGetAttribute_v4000 fn = nullptr;
   static std::once_flag once;
@@ -49,6 +36,10 @@ PFN_cuPointerGetAttribute_v4000 pointer_attribute_fn() {
   });
   return fn;
 }
+
+}  // namespace
+
+namespace optr {
 
 bool io_pointer(const void* ptr, const void** dev, bool* host) {
   unsigned type = 0;
@@ -77,10 +68,6 @@ bool io_pointer(const void* ptr, const void** dev, bool* host) {
   }
   return false;
 }
-
-}  // namespace
-
-namespace optr {
 
 cudaError_t ensure_dynamic_smem(const void* kernel, size_t bytes) {
   struct Entry {
@@ -283,20 +270,17 @@ optr_status optr_params_create(const optr_config* cfg, const float* R_k,
   if (e == cudaSuccess) e = cudaMalloc(&p->mu, sizeof(float) * H * kD);
   if (e == cudaSuccess) e = cudaMalloc(&p->err, sizeof(unsigned));
   std::vector<uint16_t> t5((size_t)H * kRT5Halves);
-  if (e == cudaSuccess) e = cudaMalloc(&p->Rk_t5, sizeof(uint16_t) * t5.size());
-  if (e == cudaSuccess) e = cudaMalloc(&p->Rv_t5, sizeof(uint16_t) * t5.size());
-  if (e == cudaSuccess) {
-    for (int h = 0; h < H; ++h)
-      build_rotation_tc05(R_k + h * mat, t5.data() + (size_t)h * kRT5Halves);
-    e = cudaMemcpy(p->Rk_t5, t5.data(), sizeof(uint16_t) * t5.size(),
-                   cudaMemcpyHostToDevice);
-  }
-  if (e == cudaSuccess) {
-    for (int h = 0; h < H; ++h)
-      build_rotation_tc05(R_v + h * mat, t5.data() + (size_t)h * kRT5Halves);
-    e = cudaMemcpy(p->Rv_t5, t5.data(), sizeof(uint16_t) * t5.size(),
-                   cudaMemcpyHostToDevice);
-  }
+  auto operand = [&](uint16_t** dev, const float* R, void (*build)(const float*, uint16_t*)) {
+    if (e != cudaSuccess) return;
+    e = cudaMalloc(dev, sizeof(uint16_t) * t5.size());
+    if (e != cudaSuccess) return;
+    for (int h = 0; h < H; ++h) build(R + h * mat, t5.data() + (size_t)h * kRT5Halves);
+    e = cudaMemcpy(*dev, t5.data(), sizeof(uint16_t) * t5.size(), cudaMemcpyHostToDevice);
+  };
+  operand(&p->Rk_t5, R_k, build_rotation_tc05);
+  operand(&p->Rv_t5, R_v, build_rotation_tc05);
+  operand(&p->Rk_back, R_k, build_back_rotation_tc05);
+  operand(&p->Rv_back, R_v, build_back_rotation_tc05);
   if (e == cudaSuccess)
     e = cudaMemcpy(p->R_k, R_k, sizeof(float) * H * mat, cudaMemcpyHostToDevice);
   if (e == cudaSuccess)
@@ -331,6 +315,8 @@ void optr_params_destroy(optr_params* p) {
   cudaFree(p->mu);
   cudaFree(p->Rk_t5);
   cudaFree(p->Rv_t5);
+  cudaFree(p->Rk_back);
+  cudaFree(p->Rv_back);
   cudaFree(p->err);
   free(p);
 }

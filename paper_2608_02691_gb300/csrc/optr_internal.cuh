@@ -52,6 +52,8 @@ struct optr_params {
   float* mu;           // device [h_kv][D], the key mean (window logits)
   uint16_t* Rk_t5;     // device tcgen05 B operands of R_k (append_tc05.cu)
   uint16_t* Rv_t5;     // device tcgen05 B operands of R_v
+  uint16_t* Rk_back;   // the same of R_k^T and R_v^T, for dequantized rows
+  uint16_t* Rv_back;   // (inner index in the order of dequant.cuh)
   unsigned* err;       // device error word
   // device address of the fixed scratch array of
   // optr_decode_attention_noalloc on this params' device (noalloc.cu),
@@ -67,6 +69,21 @@ struct optr_params {
 };
 
 namespace optr {
+inline bool aligned(const void* ptr, size_t a) {
+  return (reinterpret_cast<uintptr_t>(ptr) % a) == 0;
+}
+
+inline optr_status cuda_status(cudaError_t e) {
+  return e == cudaSuccess ? OPTR_OK : OPTR_ERR_CUDA;
+}
+
+// A per-step activation (k, v, q or out) as the kernels address it: device
+// or managed memory as given; page-locked host memory through its device
+// mapping (*host set), which the kernels then read or write in place over
+// the host link.  Pageable host memory, or a pointer the runtime does not
+// know, is refused (false), so no kernel ever dereferences it.
+bool io_pointer(const void* ptr, const void** dev, bool* host);
+
 // Argument and range checks shared by every decode entry point (null or
 // misaligned pointers, sizes): OPTR_OK or the status the call returns.
 optr_status decode_args_status(const optr_params* p, const void* q,
@@ -203,6 +220,8 @@ cudaError_t launch_append_cuda_core(const optr_params* p, const __nv_bfloat16* k
 // tcgen05 append operand: [hi, lo][128 x 128] fp16 per head, see append_tc05.cu.
 constexpr int kRT5Halves = 2 * kD * kD;
 void build_rotation_tc05(const float* R /*[D][D]*/, uint16_t* out);
+// The same of the inverse rotation z R^T, z a dequantized row (dequant.cuh).
+void build_back_rotation_tc05(const float* R /*[D][D]*/, uint16_t* out);
 cudaError_t launch_append_tc05(const optr_params* p, const __nv_bfloat16* k,
                                const __nv_bfloat16* v, int n_tok,
                                const int32_t* cu_new, const int32_t* pos0,

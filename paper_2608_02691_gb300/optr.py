@@ -34,6 +34,10 @@ OPTR_DEVERR_CU_NEW = 8
 OPTR_DEVERR_FP16_RANGE = 16
 OPTR_DEVERR_TIMEOUT = 32
 OPTR_DEVERR_WIN_SLOT = 64
+OPTR_DEVERR_TOKEN = 256
+# types of probabilities (optr_verify_drafts)
+OPTR_PROBS_F32 = 0
+OPTR_PROBS_BF16 = 1
 
 
 class OptrError(RuntimeError):
@@ -93,6 +97,13 @@ _SIG = {
     "optr_decode_step_win": (_I, [_V, _V, _V, _V, _I, _V, _V, _V, _V, _I, _I,
                                   _V, _I, _V, _V, _I, _V, _V, ctypes.c_size_t,
                                   _V]),
+    "optr_chunk_workspace_size": (ctypes.c_size_t, [_V, _I, _I, _I]),
+    "optr_chunk_attention": (_I, [_V, _V, _V, _V, _I, _V, _V, _I, _V, _I, _I, _V, _I, _V,
+                                  _V, ctypes.c_size_t, _V]),
+    "optr_chunk_attention_win": (_I, [_V, _V, _V, _V, _I, _V, _V, _I, _V, _I, _I, _V, _I,
+                                      _V, _V, _I, _V, _V, ctypes.c_size_t, _V]),
+    "optr_kv_read": (_I, [_V, _I, _V, _V, _V, _I, _I, _V, _I, _V, _V, _V]),
+    "optr_verify_drafts": (_I, [_V, _V, _V, _I, _V, _V, _V, _V, _I, _I, _I, _V, _V, _V]),
     "optr_profile_enable": (_I, [_V, _I]),
     "optr_profile_last": (_I, [_V, ctypes.POINTER(ctypes.c_float)]),
 }
@@ -163,6 +174,13 @@ def _dev(t, dtype, name):
         return t.data_ptr()
     kind = "CUDA or pinned host" if name in _IO else "CUDA"
     raise ValueError(f"{name} must be a contiguous {kind} {dtype} tensor")
+
+
+def _cuda(t, dtype, name):
+    """_dev for the activations of calls that take device memory only."""
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor")
 
 
 def _act(t, dtype, name):
@@ -377,6 +395,108 @@ def optr_decode_attention_noalloc(p: Params, q, block_table, seq_lens, pool,
         pool.shape[0], _act(out, torch.float32, "out"), _stream(stream))
     if st:
         _done(st, "optr_decode_attention_noalloc", (q, "q"), (out, "out"))
+
+
+def optr_chunk_workspace_size(p: Params, n_tok: int, B: int, max_new: int) -> int:
+    return int(lib().optr_chunk_workspace_size(p.handle, n_tok, B, max_new))
+
+
+def new_chunk_workspace(p: Params, n_tok: int, B: int, max_new: int, device="cuda"):
+    n = optr_chunk_workspace_size(p, n_tok, B, max_new)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _chunk_rows(p, q, k, v, cu_new, pos0, block_table, pool, out):
+    """The pointers of a chunk attention's arguments, with the shapes that the
+    library cannot see checked."""
+    bf16, i32 = torch.bfloat16, torch.int32
+    n, B = k.shape[0], block_table.shape[0]
+    if tuple(q.shape) != (n, p.h_q, HEAD_DIM) or q.shape != out.shape or \
+            tuple(k.shape) != (n, p.h_kv, HEAD_DIM) or k.shape != v.shape or \
+            cu_new.numel() != B + 1 or pos0.numel() != B:
+        raise ValueError("q, out must be [n_tok][h_q][128], k, v [n_tok][h_kv][128], "
+                         "cu_new [B+1], pos0 [B]")
+    return (_cuda(q, bf16, "q"), _cuda(k, bf16, "k"), _cuda(v, bf16, "v"), n,
+            _dev(cu_new, i32, "cu_new"), _dev(pos0, i32, "pos0"),
+            _dev(block_table, i32, "block_table"), _dev(pool, torch.uint8, "pool"),
+            _cuda(out, bf16, "out"))
+
+
+def optr_chunk_attention(p: Params, q, k, v, cu_new, pos0, max_new: int, block_table, pool,
+                         out, workspace, stream=None) -> None:
+    """Attention of each sequence's new tokens (rows cu_new[b] .. cu_new[b+1]-1
+    of q, k, v; at most max_new per sequence) over its pos0[b] cached tokens
+    and, causally, over themselves.  q, out bf16 [n_tok][h_q][128], k, v bf16
+    [n_tok][h_kv][128], CUDA tensors.  The cache is only read: write the tokens
+    that stay with optr_kv_append afterwards."""
+    qp, kp, vp, n, cu, p0, bt, pl, op = _chunk_rows(p, q, k, v, cu_new, pos0, block_table,
+                                                    pool, out)
+    B, max_pages = block_table.shape
+    st = lib().optr_chunk_attention(p.handle, qp, kp, vp, n, cu, p0, max_new, bt, B, max_pages,
+                                    pl, pool.shape[0], op, _dev(workspace, torch.uint8, "workspace"),
+                                    workspace.numel(), _stream(stream))
+    if st:
+        raise OptrError(st, "optr_chunk_attention")
+
+
+def optr_chunk_attention_win(p: Params, q, k, v, cu_new, pos0, max_new: int, block_table, pool,
+                             win, win_slot, out, workspace, stream=None) -> None:
+    """optr_chunk_attention with the cached tokens' BF16 windows read from win."""
+    qp, kp, vp, n, cu, p0, bt, pl, op = _chunk_rows(p, q, k, v, cu_new, pos0, block_table,
+                                                    pool, out)
+    w, ws_, n_slots = _win_args(p, win, win_slot)
+    B, max_pages = block_table.shape
+    st = lib().optr_chunk_attention_win(p.handle, qp, kp, vp, n, cu, p0, max_new, bt, B,
+                                        max_pages, pl, pool.shape[0], w, ws_, n_slots, op,
+                                        _dev(workspace, torch.uint8, "workspace"),
+                                        workspace.numel(), _stream(stream))
+    if st:
+        raise OptrError(st, "optr_chunk_attention_win")
+
+
+def optr_kv_read(p: Params, cu_read, pos0, block_table, pool, k, v, stream=None) -> None:
+    """Cached rows back in the model's basis: k, v bf16 [n_tok][h_kv][128] (CUDA
+    tensors, written), row cu_read[b] + i from position pos0[b] + i of sequence
+    b."""
+    bf16, i32 = torch.bfloat16, torch.int32
+    B, max_pages = block_table.shape
+    if tuple(k.shape) != (k.shape[0], p.h_kv, HEAD_DIM) or k.shape != v.shape or \
+            cu_read.numel() != B + 1 or pos0.numel() != B:
+        raise ValueError("k, v must be [n_tok][h_kv][128], cu_read [B+1], pos0 [B]")
+    st = lib().optr_kv_read(p.handle, k.shape[0], _dev(cu_read, i32, "cu_read"),
+                            _dev(pos0, i32, "pos0"), _dev(block_table, i32, "block_table"), B,
+                            max_pages, _dev(pool, torch.uint8, "pool"), pool.shape[0],
+                            _cuda(k, bf16, "k"), _cuda(v, bf16, "v"), _stream(stream))
+    if st:
+        raise OptrError(st, "optr_kv_read")
+
+
+def optr_verify_drafts(p: Params, target_probs, draft_probs, drafts, uniform, noise, cu_draft,
+                       accepted, tokens, stream=None) -> None:
+    """Verify drafts int32 [n_draft] against target_probs [n_draft + B][vocab]
+    (float32 or bf16) with draft_probs [n_draft][vocab] (the same type, or
+    None), uniform float32 [n_draft] and exponential noise float32 [B][vocab];
+    cu_draft int32 [B+1].  Writes accepted int32 [B] and tokens int32
+    [n_draft + B] (accepted drafts, the next token, then -1)."""
+    f32, i32 = torch.float32, torch.int32
+    n, B = drafts.numel(), cu_draft.numel() - 1
+    vocab = target_probs.shape[1] if target_probs.dim() == 2 else 0
+    if target_probs.shape[0] != n + B or tuple(noise.shape) != (B, vocab) or uniform.numel() != n \
+            or (draft_probs is not None and tuple(draft_probs.shape) != (n, vocab)) \
+            or accepted.numel() != B or tokens.numel() != n + B:
+        raise ValueError("target_probs must be [n_draft + B][vocab], draft_probs [n_draft][vocab], "
+                         "noise [B][vocab], uniform [n_draft], accepted [B], tokens [n_draft + B]")
+    dtype = target_probs.dtype
+    if dtype not in (f32, torch.bfloat16):
+        raise ValueError("target_probs must be float32 or bfloat16")
+    st = lib().optr_verify_drafts(
+        p.handle, _dev(target_probs, dtype, "target_probs"),
+        None if draft_probs is None else _dev(draft_probs, dtype, "draft_probs"),
+        OPTR_PROBS_F32 if dtype is f32 else OPTR_PROBS_BF16, _dev(drafts, i32, "drafts"),
+        _dev(uniform, f32, "uniform"), _dev(noise, f32, "noise"), _dev(cu_draft, i32, "cu_draft"),
+        n, B, vocab, _dev(accepted, i32, "accepted"), _dev(tokens, i32, "tokens"), _stream(stream))
+    if st:
+        raise OptrError(st, "optr_verify_drafts")
 
 
 def optr_device_error(p: Params) -> int:
