@@ -44,7 +44,6 @@
 // The quantizer is quant.cuh's float32 formula.
 #include "append_common.cuh"
 #include "decode_common.cuh"
-#include "dequant.cuh"
 #include "f32x2.cuh"
 #include "quant.cuh"
 #include "tc05.cuh"
@@ -54,40 +53,6 @@
 #include <type_traits>
 
 namespace optr {
-
-// Host: B operand of a product on tcgen05 (f16, K-major, no swizzle):
-// out[term][n][k] = (hi, lo) fp16 parts of 64 x(n, k) at element offset
-// ((n / 8) * 2048 + (k / 8) * 128 + (n % 8) * 16 + (k % 8) * 2) / 2 of the
-// term's 32 KB, i.e. core matrices of 8 columns n x 8 inner indices k, 128 B
-// apart along k (LBO) and 2048 B apart along n (SBO).
-template <typename F>
-static void build_operand_tc05(F x, uint16_t* out) {
-  auto h16 = [](float x) -> uint16_t {
-    __half_raw r = __half(__float2half_rn(x));
-    return r.x;
-  };
-  auto f16 = [](uint16_t bits) -> float {
-    __half_raw r;
-    r.x = bits;
-    return __half2float(__half(r));
-  };
-  for (int n = 0; n < kD; ++n)
-    for (int k = 0; k < kD; ++k) {
-      const float y = x(n, k) * 64.0f;
-      const uint16_t hi = h16(y), lo = h16(y - f16(hi));
-      const size_t off = ((size_t)(n / 8) * 2048 + (k / 8) * 128 + (n % 8) * 16 + (k % 8) * 2) / 2;
-      out[off] = hi;
-      out[(size_t)kD * kD + off] = lo;
-    }
-}
-
-void build_rotation_tc05(const float* R, uint16_t* out) {
-  build_operand_tc05([R](int n, int k) { return R[(size_t)k * kD + n]; }, out);
-}
-
-void build_back_rotation_tc05(const float* R, uint16_t* out) {
-  build_operand_tc05([R](int n, int k) { return R[(size_t)n * kD + row_channel(k)]; }, out);
-}
 
 namespace {
 

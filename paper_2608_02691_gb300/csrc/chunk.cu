@@ -1,148 +1,763 @@
 // Attention of a chunk of new tokens over the paged INT2 cache
 // (include/optr.h, "optr_chunk_attention").
+//
+// Three launches.  chunk_prologue_kernel rotates the queries and lays out the
+// work; chunk_kernel attends; chunk_combine_kernel joins the segments that more
+// than one CTA worked on.
+//
+// Work.  A query block is 64 new tokens of one sequence with the 4 query heads
+// of one KV head: 256 rows, two tensor-core tiles of 32 tokens x 4 heads.  It
+// goes over its keys in tiles of 128: the cached INT2 positions, the windows'
+// rows, then the chunk's own tokens up to its diagonal.  All tiles of all
+// (sequence, KV head, query block) segments are put into one line that is cut
+// into equal ranges, one per SM: a long context of one sequence, a ragged batch
+// and a causal prompt (whose blocks see between one tile and all) fill the GPU
+// alike, and a CTA leaves at most two partial results.
+//
+// A row's softmax runs over the tiles with a running maximum m and sum l
+// (float32, log2 domain); O and m, l of different ranges merge exactly.
+// The INT2 keys and values live in their rotated bases, all others in the
+// model's.  Keys: the query operand changes with the tile's kind (q R_k in fp16,
+// scaled by a power of two per row; q itself in bf16, and the constant <q, mu>
+// taken off).  Values: O is normalised and multiplied by R_v^T once, after the
+// last INT2 tile, and the other tiles go on from there.
 #include "append_common.cuh"
-#include "optr_internal.cuh"
+#include "chunk.cuh"
+#include "dequant.cuh"
+#include "tc05.cuh"
+#include "tmap.cuh"
+
+#include <algorithm>
 
 namespace optr {
 namespace {
 
-constexpr int kKeys = 16;  // keys per tile: one page
+// ------------------------------------------------------------ prologue
 
-struct ChunkArgs {
-  const __nv_bfloat16 *q, *k, *v;
-  int n_tok;
-  const int32_t *cu, *pos0;
-  int max_new;
-  const int32_t* bt;
-  int B, max_pages;
-  const uint8_t* pool;
-  int num_pages;
-  WinArgs win;
-  int sink, recent, h_kv, fold_v, compact;
-  const float *R_k, *R_vT, *mu;
-  __nv_bfloat16* out;
-  unsigned* err;
-};
+constexpr int kProThreads = 256;
 
-// A block per (new token, KV head): thread = channel, warp = query head.
-__global__ void __launch_bounds__(128) chunk_simple_kernel(const ChunkArgs A) {
-  __shared__ float qx[4][kD], qr[4][kD], K[kKeys][kD + 1], V[kKeys][kD], P[4][kKeys], alpha[4], L[4];
-  const int t = blockIdx.x, h = blockIdx.y, c = threadIdx.x, w = c >> 5, lane = c & 31;
-  pdl_wait();
-  pdl_trigger();
-  const float scale = 1.44269504f * 0.08838834764831845f;
-  const int b = find_seq(A.cu, A.B, t);
-  const int c0 = __ldcg(A.cu + b), c1 = __ldcg(A.cu + b + 1), n = __ldcg(A.pos0 + b);
-  __nv_bfloat16* out = A.out + ((size_t)t * 4 * A.h_kv + 4 * h) * kD;
-  unsigned bad = 0;
-  if (!(c0 <= t && t < c1 && c0 >= 0 && c1 <= A.n_tok && c1 - c0 <= A.max_new)) bad = OPTR_DEVERR_CU_NEW;
-  if (n < 0 || n > A.max_pages * kPage) bad = OPTR_DEVERR_SEQ_LEN;
-  if (bad) {
-    if (c == 0) atomicOr(A.err, bad);
-    for (int j = 0; j < 4; ++j) out[j * kD + c] = __float2bfloat16(0.f);
+__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
+                                         uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 "
+      "{%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ float bf_lo(uint32_t x) { return __uint_as_float(x << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
+
+// The plan (one CTA): tiles of one head of the sequences before b, for all b.
+__device__ void chunk_plan(const ChunkArgs& A) {
+  __shared__ long long warp_sum[kProThreads / 32];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  long long carry = 0;
+  if (tid == 0) A.pref[0] = 0;
+  for (int b0 = 0; b0 < A.B; b0 += kProThreads) {
+    const int b = b0 + tid;
+    long long x = 0;
+    if (b < A.B) {
+      const SeqWork s = seq_work(A, b);
+      unsigned bad = s.bad;
+      if (!bad && A.win.win && (s.slot < 0 || s.slot >= A.win.n_slots)) bad = OPTR_DEVERR_WIN_SLOT;
+      if (bad) atomicOr(A.err, bad);
+      if (s.n_new > 0)
+        x = block_tiles((s.n_new + kQTok - 1) / kQTok, tiles_of(s.n_int) + tiles_of(s.n_win));
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) warp_sum[warp] = x;
+    __syncthreads();
+    for (int w = 0; w < kProThreads / 32; ++w) {
+      if (w < warp) x += warp_sum[w];
+    }
+    x += carry;
+    if (b < A.B) A.pref[b + 1] = x;
+    for (int w = 0; w < kProThreads / 32; ++w) carry += warp_sum[w];
+    __syncthreads();
+  }
+}
+
+// CTA 0 plans; the others rotate the queries of `per` tokens (a multiple of 4)
+// and one KV head: warp w makes 16 of the 128 columns, 16 rows (4 tokens) at a
+// time, mma.sync on bf16 q and R_k as bf16 hi + lo.  q R_k is stored as fp16
+// over the power of two 2^E > sqrt(128) max |q| >= |q R_k| of its row.
+__global__ void __launch_bounds__(kProThreads) chunk_prologue_kernel(const ChunkArgs A, int per) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (blockIdx.x == 0) {
+    pdl_wait();
+    pdl_trigger();
+    chunk_plan(A);
     return;
   }
-  for (int j = 0; j < 4; ++j)
-    qx[j][c] = scale * __bfloat162float(A.q[((size_t)t * 4 * A.h_kv + 4 * h + j) * kD + c]);
-  __syncthreads();
-  float r[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < kD; ++i) {
-    const float x = A.R_k[((size_t)h * kD + i) * kD + c];
-    for (int j = 0; j < 4; ++j) r[j] = fmaf(qx[j][i], x, r[j]);
-  }
-  for (int j = 0; j < 4; ++j) qr[j][c] = r[j];
-  float acc[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-
-  // one tile of `cnt` keys in K and V, logits with the queries Q
-  auto tile = [&](const float (*Q)[kD], int cnt) {
-    __syncthreads();
-    const int s = lane & 15, half = lane >> 4;
-    float x = 0.f;
-    for (int i = 64 * half; i < 64 * half + 64; ++i) x = fmaf(Q[w][i], K[s][i], x);
-    x += __shfl_xor_sync(0xffffffffu, x, 16);
-    if (s >= cnt) x = -INFINITY;
-    float mx = x;
-    for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    const float mn = fmaxf(m, mx);
-    const float al = m == -INFINITY ? 0.f : exp2f(m - mn);
-    const float p = mn == -INFINITY ? 0.f : exp2f(x - mn);
-    float sum = p;
-    for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    l = l * al + sum;
-    m = mn;
-    if (half == 0) P[w][s] = p;
-    if (lane == 0) alpha[w] = al;
-    __syncthreads();
-    for (int j = 0; j < 4; ++j) {
-      acc[j] *= alpha[j];
-      for (int s2 = 0; s2 < cnt; ++s2) acc[j] = fmaf(P[j][s2], V[s2][c], acc[j]);
-    }
-    __syncthreads();
-  };
-
-  // cached INT2 positions
-  const int e = int2_end(n, A.sink, A.recent);
-  const int ms = meta_stride(A.compact), g = A.compact ? 0 : c >> 5;
-  const int byte = 4 * (c % 32 / 4) + c / 32, bit = 2 * (c % 4);
-  for (int s0 = A.sink; s0 < min(e, n); s0 += kKeys) {
-    const int page = __ldcg(A.bt + (size_t)b * A.max_pages + s0 / kPage);
-    if (page < 0 || page >= A.num_pages) {
-      if (c == 0) atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
-      continue;
-    }
-    const uint8_t* rec = A.pool + ((size_t)page * A.h_kv + h) * chunk_bytes(A.compact);
-    const int cnt = min(kKeys, min(e, n) - s0);
-    for (int s = 0; s < kKeys; ++s) {
-      const __half2 mk = *reinterpret_cast<const __half2*>(rec + OPTR_K_META_OFFSET + s * ms + 4 * g);
-      const __half2 mv = *reinterpret_cast<const __half2*>(rec + vmeta_offset(A.compact) + s * ms + 4 * g);
-      const int ck = rec[OPTR_K_CODES_OFFSET + 32 * s + byte] >> bit & 3;
-      const int cv = rec[OPTR_V_CODES_OFFSET + 32 * s + byte] >> bit & 3;
-      K[s][c] = s < cnt ? ck * __low2float(mk) + __high2float(mk) : 0.f;
-      V[s][c] = s < cnt ? cv * __low2float(mv) + __high2float(mv) : 0.f;
-    }
-    tile(qr, cnt);
-  }
-  if (!A.fold_v) {  // the INT2 part into the model's basis
-    for (int j = 0; j < 4; ++j) K[j][c] = acc[j];
-    __syncthreads();
-    for (int j = 0; j < 4; ++j) acc[j] = 0.f;
-    for (int i = 0; i < kD; ++i) {
-      const float x = A.R_vT[((size_t)h * kD + i) * kD + c];
-      for (int j = 0; j < 4; ++j) acc[j] = fmaf(K[j][i], x, acc[j]);
-    }
-    __syncthreads();
-  }
-  const float mu = A.mu[h * kD + c];
-  // the past's windows: the store's rows, all of them once n >= sink + recent
-  if (A.win.win) {
-    const int rows = A.sink + A.recent, slot = __ldcg(A.win.slot + b);
-    if (slot < 0 || slot >= A.win.n_slots) {
-      if (c == 0) atomicOr(A.err, OPTR_DEVERR_WIN_SLOT);
-    } else {
-      const __nv_bfloat16* wk = A.win.win + ((size_t)slot * A.h_kv + h) * 2 * rows * kD;
-      const int have = min(n, rows);
-      for (int s0 = 0; s0 < have; s0 += kKeys) {
-        const int cnt = min(kKeys, have - s0);
-        for (int s = 0; s < kKeys; ++s) {
-          K[s][c] = s < cnt ? __bfloat162float(wk[(size_t)(s0 + s) * kD + c]) - mu : 0.f;
-          V[s][c] = s < cnt ? __bfloat162float(wk[(size_t)(rows + s0 + s) * kD + c]) : 0.f;
-        }
-        tile(qx, cnt);
+  const int h = (blockIdx.x - 1) % A.h_kv, h_q = 4 * A.h_kv;
+  const int t0 = (blockIdx.x - 1) / A.h_kv * per, t1 = min(A.n_tok, t0 + per);
+  uint4 bf[8][2];
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+      bf[ks][nt] = __ldg(A.Rk_frag + (((size_t)h * 8 + warp) * 16 + 2 * ks + nt) * 32 + lane);
+  pdl_wait();
+  pdl_trigger();
+  for (int t = t0; t < t1; t += 4) {
+    // tokens t .. t + 3: outside every sequence (zero rows), or of one that
+    // has INT2 positions
+    bool need = false;
+    if (lane < 4 && t + lane < t1) {
+      const int b = find_seq(A.cu, A.B, t + lane);
+      const SeqWork s = seq_work(A, b);
+      const bool in = !s.bad && s.c0 <= t + lane && t + lane < s.c0 + s.n_new;
+      need = in && s.n_int > 0;
+      if (!in && warp == 0) {
+        if (!s.bad) atomicOr(A.err, OPTR_DEVERR_CU_NEW);
+        uint4* o = reinterpret_cast<uint4*>(A.out + ((size_t)(t + lane) * h_q + 4 * h) * kD);
+        for (int i = 0; i < 4 * kD / 8; ++i) o[i] = make_uint4(0u, 0u, 0u, 0u);
       }
     }
-  }
-  for (int s0 = c0; s0 <= t; s0 += kKeys) {
-    const int cnt = min(kKeys, t + 1 - s0);
-    for (int s = 0; s < kKeys; ++s) {
-      const size_t at = ((size_t)(s0 + s) * A.h_kv + h) * kD + c;
-      K[s][c] = s < cnt ? __bfloat162float(A.k[at]) - mu : 0.f;
-      V[s][c] = s < cnt ? __bfloat162float(A.v[at]) : 0.f;
+    if (!__any_sync(0xffffffffu, need)) continue;
+    // rows g and g + 8 of the tile: token row / 4, head row % 4
+    const int g = lane >> 2, c = 2 * (lane & 3);
+    const uint32_t* row[2];
+    bool ok[2];
+    size_t at[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = g + 8 * i;
+      ok[i] = t + r / 4 < t1;
+      at[i] = (size_t)(t + r / 4) * h_q + 4 * h + r % 4;
+      row[i] = reinterpret_cast<const uint32_t*>(A.q + at[i] * kD + c);
     }
-    tile(qx, cnt);
+    uint32_t a[8][4];
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        a[ks][j] = ok[j & 1] ? __ldcg(row[j & 1] + 8 * ks + 4 * (j >> 1)) : 0u;
+    float amax[2] = {0.f, 0.f}, qmu[2] = {0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float x = bf_lo(a[ks][j]), y = bf_hi(a[ks][j]);
+        amax[j & 1] = fmaxf(amax[j & 1], fmaxf(fabsf(x), fabsf(y)));
+        if (warp == 0) {
+          const float2 m = __ldg(reinterpret_cast<const float2*>(A.mu + h * kD + 16 * ks +
+                                                                 8 * (j >> 1) + c));
+          qmu[j & 1] = fmaf(x, m.x, fmaf(y, m.y, qmu[j & 1]));
+        }
+      }
+    float d[2][4] = {};
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+        mma_bf16(d[nt], a[ks], bf[ks][nt].x, bf[ks][nt].y);
+        mma_bf16(d[nt], a[ks], bf[ks][nt].z, bf[ks][nt].w);
+      }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        amax[i] = fmaxf(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], o));
+        qmu[i] += __shfl_xor_sync(0xffffffffu, qmu[i], o);
+      }
+      // 2^E, E = exponent(amax) + 5 within float's range
+      const int E = min(max((int)(__float_as_uint(amax[i]) >> 23) - 127 + 5, -120), 120);
+      const float up = __uint_as_float((uint32_t)(127 + E) << 23);
+      const float down = __uint_as_float((uint32_t)(127 - E) << 23);
+      if (!ok[i]) continue;
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+        *reinterpret_cast<__half2*>(A.qrot + at[i] * kD + 8 * (2 * warp + nt) + c) =
+            __floats2half2_rn(d[nt][2 * i] * down, d[nt][2 * i + 1] * down);
+      if (warp == 0 && (lane & 3) == 0) A.qinfo[at[i]] = make_float2(up * kLogit, qmu[i] * kLogit);
+    }
   }
-  if (lane == 0) L[w] = l;
+}
+
+// ----------------------------------------------------------- attention
+
+constexpr int kDeqWarp = 8, kTmaWarp = 12, kMmaWarp = 13;
+constexpr int kThreads = 14 * 32;
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kColS = 0, kColO = 256;  // S[g] (and P[g]) at 128 g, O[g] at 256 + 128 g
+constexpr int kRing = 2;
+constexpr uint32_t kHalf = kTile * 128;      // 64 channels of 128 rows
+constexpr uint32_t kOperand = 2 * kHalf;     // 128 x 128 of 16 bits
+constexpr int kPrefCache = 256;
+constexpr float kSlack = 8.f;  // a row's maximum may grow by 2^8 before O is rescaled
+
+struct Smem {
+  uint8_t q[2][kOperand];            // the query operand, by tile
+  uint8_t ring[kRing][2][kOperand];  // keys, values
+  alignas(16) uint32_t mask[kRing][4];  // keys of the tile that count
+  long long pref[kPrefCache + 1];
+  uint64_t kv_full[kRing], kv_tma[kRing], kv_empty[kRing];
+  uint64_t s_full[2], p_ready[2], o_full[2], q_full, q_empty, drained;
+  uint32_t tmem;
+  int abort;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+template <bool kBf16>
+__device__ __forceinline__ uint32_t pack16(float a, float b) {  // a in the low half
+  uint32_t r;
+  if (kBf16)
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  else
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+
+// One row of a logit tile: S (128 columns of tensor memory at tS) becomes P =
+// 2^(S scale - off - m) in 16 bits over its first 64 columns; m, l and O are
+// brought along.  Bits of `mask` and the first `lim` columns count.
+template <bool kBf16>
+__device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, float scale, float off,
+                                             uint4 mask, int lim, bool fresh, float& m, float& l) {
+  const uint32_t word[4] = {mask.x, mask.y, mask.z, mask.w};
+  const bool whole = __all_sync(0xffffffffu, lim >= kTile) &&
+                     (mask.x & mask.y & mask.z & mask.w) == 0xffffffffu;
+  auto keep = [&](int c) {  // the columns of chunk c that count
+    const int n = lim - 32 * c;
+    return word[c] & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u);
+  };
+  uint32_t s[32];
+  float top = -INFINITY;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    tc05::tmem_ld32(tS + 32 * c, s);
+    tc05::tmem_wait_ld();
+    if (!whole) {
+      const uint32_t k = keep(c);
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (!(k >> j & 1)) s[j] = 0xff800000u;
+    }
+    float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int j = 0; j < 32; j += 8)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        x[i] = fmaxf(x[i], fmaxf(__uint_as_float(s[j + i]), __uint_as_float(s[j + 4 + i])));
+    top = fmaxf(top, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
+  }
+  const float t = fmaf(top, scale, -off);
+  if (fresh) {
+    m = fmaxf(m, t);
+  } else if (__any_sync(0xffffffffu, t > m + kSlack)) {
+    const float mn = t > m + kSlack ? t : m, al = ex2(m - mn);
+    m = mn;
+    l *= al;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      tc05::tmem_ld32(tO + 32 * c, s);
+      tc05::tmem_wait_ld();
+#pragma unroll
+      for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) * al);
+      tc05::tmem_st32(tO + 32 * c, s);
+    }
+  }
+  const float sub = off + m;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    tc05::tmem_ld32(tS + 32 * c, s);
+    tc05::tmem_wait_ld();
+    if (!whole) {
+      const uint32_t k = keep(c);
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (!(k >> j & 1)) s[j] = 0xff800000u;
+    }
+    uint32_t p[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const float a = ex2(fmaf(__uint_as_float(s[2 * j]), scale, -sub));
+      const float b = ex2(fmaf(__uint_as_float(s[2 * j + 1]), scale, -sub));
+      sum[j & 3] += a + b;
+      p[j] = pack16<kBf16>(a, b);
+    }
+    tc05::tmem_st16(tS + 16 * c, p);
+  }
+  l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  tc05::tmem_wait_st();
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_qrot,
+             const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+             const __grid_constant__ CUtensorMap tm_win, const __grid_constant__ ChunkArgs A) {
+  extern __shared__ __align__(1024) unsigned char dsm_[];
+  Smem& S = *reinterpret_cast<Smem*>(dsm_);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int s = 0; s < kRing; ++s) {
+      tc05::bar_init(&S.kv_full[s], 128);
+      tc05::bar_init(&S.kv_tma[s], 1);
+      tc05::bar_init(&S.kv_empty[s], 1);
+    }
+    for (int g = 0; g < 2; ++g) {
+      tc05::bar_init(&S.s_full[g], 1);
+      tc05::bar_init(&S.p_ready[g], 128);
+      tc05::bar_init(&S.o_full[g], 1);
+    }
+    tc05::bar_init(&S.q_full, 1);
+    tc05::bar_init(&S.q_empty, 1);
+    tc05::bar_init(&S.drained, 1);
+    S.abort = (tc05::smem_addr(S.q[0]) & 1023u) != 0;  // the swizzle's alignment
+    tc05::bar_init_fence();
+  }
+  if (warp == kMmaWarp) tc05::tmem_alloc(&S.tmem, kTmemCols);
+  pdl_wait();
+  pdl_trigger();
+  const bool cached = A.B <= kPrefCache;
+  if (cached)
+    for (int i = tid; i <= A.B; i += kThreads) S.pref[i] = __ldcg(A.pref + i);
+  tc05::fence_before();
   __syncthreads();
-  for (int j = 0; j < 4; ++j) out[j * kD + c] = __float2bfloat16(acc[j] / L[j]);
+  tc05::fence_after();
+  auto pref = [&](int b) { return cached ? S.pref[b] : __ldcg(A.pref + b); };
+  const uint32_t tmem = S.tmem;
+  volatile int* abort = &S.abort;
+  const long long F = pref(A.B) * A.h_kv;
+  const int w = blockIdx.x;
+  const long long f0 = F * w / A.W, f1 = F * (w + 1) / A.W;
+
+  if (warp < kDeqWarp) {
+    // ------------------------------------------------------------- softmax
+    const int g = warp >> 2, row = 32 * (warp & 3) + lane;
+    const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
+    const uint32_t tS = tmem + lanes + kColS + 128u * g, tO = tmem + lanes + kColO + 128u * g;
+    uint32_t step = 0, ns = 0, no = 0;  // ring entries, S and O phases seen
+    bool dead = false;
+    auto wait = [&](uint64_t* bar, uint32_t phase) {
+      if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
+      tc05::fence_after();
+      return !dead;
+    };
+    for (long long f = f0; f < f1 && !dead;) {
+      const Piece p = locate_piece(A, pref, f, f1);
+      f += p.t1 - p.t0;
+      const int nint = max(0, min(p.t1, p.I) - p.t0), nother = p.t1 - p.t0 - nint;
+      const uint32_t base = step;
+      step += p.t1 - p.t0 + (nint > 0);
+      const int i0 = p.qb * kQTok + 32 * g;  // the tile's first token
+      if (i0 >= p.s.n_new) continue;
+      const int i = i0 + (row >> 2), j = row & 3;
+      const bool valid = i < p.s.n_new;
+      const size_t at = ((size_t)p.s.c0 + i) * 4 * A.h_kv + 4 * p.h + j;
+      float scale = kLogit, off = 0.f, m = -1e30f, l = 0.f;
+      if (p.I > 0 && valid) {
+        const float2 x = __ldcg(A.qinfo + at);
+        scale = x.x;
+        off = x.y;
+      }
+      bool fresh = true;
+      for (int t = 0; t < nint; ++t) {
+        if (!wait(&S.s_full[g], ns++)) break;
+        const uint4 mask = *reinterpret_cast<const uint4*>(S.mask[(base + t) % kRing]);
+        softmax_tile<false>(tS, tO, scale, 0.f, mask, kTile, fresh, m, l);
+        fresh = false;
+        tc05::fence_before();
+        tc05::bar_arrive(&S.p_ready[g]);
+      }
+      if (dead) break;
+      if (nint > 0) {
+        // O / l into the model's basis: the A operand of the product with 64
+        // R_v^T takes P's place
+        if (!wait(&S.o_full[g], no++)) break;
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t o[32], a[16];
+          tc05::tmem_ld32(tO + 32 * c, o);
+          tc05::tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            a[e] = pack16<false>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
+          tc05::tmem_st16(tS + 16 * c, a);
+        }
+        tc05::tmem_wait_st();
+        if (l > 0.f) {  // O is now 64 of weight 2^m l / 64
+          m += __log2f(l) - 6.f;
+          l = 64.f;
+        }
+        tc05::fence_before();
+        tc05::bar_arrive(&S.p_ready[g]);
+      }
+      const float sub = p.I > 0 ? off : 0.f;
+      for (int t = 0; t < nother; ++t) {
+        if (!wait(&S.s_full[g], ns++)) break;
+        const uint4 mask = *reinterpret_cast<const uint4*>(
+            S.mask[(base + nint + (nint > 0) + t) % kRing]);
+        // own tiles: causal
+        const int own = p.t0 + nint + t - p.I - p.Wt;
+        const int lim = own < 0 ? kTile : i + 1 - kTile * own;
+        softmax_tile<true>(tS, tO, kLogit, sub, mask, lim, fresh, m, l);
+        fresh = false;
+        tc05::fence_before();
+        tc05::bar_arrive(&S.p_ready[g]);
+      }
+      if (dead || !wait(&S.o_full[g], no++)) break;
+      if (p.t1 - p.t0 == p.total) {
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t o[32];
+          tc05::tmem_ld32(tO + 32 * c, o);
+          tc05::tmem_wait_ld();
+          if (valid)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t y[4];
+#pragma unroll
+              for (int z = 0; z < 4; ++z)
+                y[z] = pack16<true>(__uint_as_float(o[8 * e + 2 * z]) * inv,
+                                    __uint_as_float(o[8 * e + 2 * z + 1]) * inv);
+              reinterpret_cast<uint4*>(A.out + at * kD + 32 * c)[e] = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+        }
+      } else {
+        float* part = part_of(A, w, p.t0 > 0);
+        const int r = 128 * g + row;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t o[32];
+          tc05::tmem_ld32(tO + 32 * c, o);
+          tc05::tmem_wait_ld();
+          if (valid)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              reinterpret_cast<uint4*>(part)[(size_t)(8 * c + e) * A.rows + r] =
+                  make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+        }
+        if (valid) {
+          part[(size_t)A.rows * kD + r] = m;
+          part[(size_t)A.rows * (kD + 1) + r] = l;
+        }
+      }
+      tc05::fence_before();
+    }
+  } else if (warp < kTmaWarp) {
+    // --------------------------------------------------- keys and values
+    // thread = key: dequantizes its key and value of an INT2 tile; of the other
+    // tiles, which TMA brings, it clears the values that do not count (0 times
+    // what lies there need not be 0)
+    const int key = tid - 32 * kDeqWarp;
+    uint32_t step = 0, tma[kRing] = {0, 0};
+    bool dead = false;
+    auto wait = [&](uint64_t* bar, uint32_t phase) {
+      if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
+      return !dead;
+    };
+    const int ms = meta_stride(A.compact);
+    for (long long f = f0; f < f1 && !dead;) {
+      const Piece p = locate_piece(A, pref, f, f1);
+      f += p.t1 - p.t0;
+      const int nint = max(0, min(p.t1, p.I) - p.t0), nother = p.t1 - p.t0 - nint;
+      for (int t = 0; t < nint && !dead; ++t, ++step) {
+        const int st = step % kRing;
+        const int n = (p.t0 + t) * kTile + key;  // INT2 position, from `sink` on
+        const int pos = A.sink + n;
+        bool ok = n < p.s.n_int;
+        uint4 kc[2] = {}, vc[2] = {}, km = {}, vm = {};
+        if (ok) {
+          const int page = __ldcg(A.bt + (size_t)p.b * A.max_pages + pos / kPage);
+          if (page < 0 || page >= A.num_pages) {
+            atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
+            ok = false;
+          } else {
+            const uint8_t* rec = A.pool + ((size_t)page * A.h_kv + p.h) * chunk_bytes(A.compact);
+            const int slot = pos % kPage;
+            const uint4* k4 = reinterpret_cast<const uint4*>(rec + OPTR_K_CODES_OFFSET + 32 * slot);
+            const uint4* v4 = reinterpret_cast<const uint4*>(rec + OPTR_V_CODES_OFFSET + 32 * slot);
+            const uint8_t* mk = rec + OPTR_K_META_OFFSET + ms * slot;
+            const uint8_t* mv = rec + vmeta_offset(A.compact) + ms * slot;
+            kc[0] = __ldcg(k4);
+            kc[1] = __ldcg(k4 + 1);
+            vc[0] = __ldcg(v4);
+            vc[1] = __ldcg(v4 + 1);
+            if (A.compact) {
+              km.x = km.y = km.z = km.w = __ldcg(reinterpret_cast<const uint32_t*>(mk));
+              vm.x = vm.y = vm.z = vm.w = __ldcg(reinterpret_cast<const uint32_t*>(mv));
+            } else {
+              km = __ldcg(reinterpret_cast<const uint4*>(mk));
+              vm = __ldcg(reinterpret_cast<const uint4*>(mv));
+            }
+          }
+        }
+        if (step >= kRing && !wait(&S.kv_empty[st], step / kRing - 1)) break;
+        const uint32_t bits = __ballot_sync(0xffffffffu, ok);
+        if (lane == 0) S.mask[st][key >> 5] = bits;
+        auto put = [&](uint8_t* dst, const uint4 (&c)[2], const uint4& mm) {
+          const SlotMeta sm = slot_meta(mm.x, mm.y, mm.z, mm.w);
+          const uint32_t word[8] = {c[0].x, c[0].y, c[0].z, c[0].w, c[1].x, c[1].y, c[1].z, c[1].w};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            uint32_t x[8];
+            dequant_word(word[i], sm, x);
+            uint8_t* r = dst + (i >> 2) * kHalf + key * 128;
+            const int c0 = 2 * (i & 3);
+            *reinterpret_cast<uint4*>(r + ((c0 ^ (key & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<uint4*>(r + (((c0 + 1) ^ (key & 7)) << 4)) = make_uint4(x[4], x[5], x[6], x[7]);
+          }
+        };
+        put(S.ring[st][0], kc, km);
+        put(S.ring[st][1], vc, vm);
+        tc05::fence_proxy_async();
+        tc05::bar_arrive(&S.kv_full[st]);
+      }
+      if (dead) break;
+      for (int t = nint > 0 ? -1 : 0; t < nother; ++t, ++step) {  // -1: R_v^T
+        const int st = step % kRing;
+        if (!wait(&S.kv_tma[st], tma[st]++)) break;
+        if (t >= 0) {
+          const int tile = p.t0 + nint + t - p.I;
+          const int n = tile < p.Wt ? p.s.n_win - kTile * tile : p.s.n_new - kTile * (tile - p.Wt);
+          const bool ok = key < n;
+          const uint32_t bits = __ballot_sync(0xffffffffu, ok);
+          if (lane == 0) S.mask[st][key >> 5] = bits;
+          if (!ok) {
+            uint8_t* r = S.ring[st][1] + key * 128;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              *reinterpret_cast<uint4*>(r + 16 * c) = make_uint4(0u, 0u, 0u, 0u);
+              *reinterpret_cast<uint4*>(r + kHalf + 16 * c) = make_uint4(0u, 0u, 0u, 0u);
+            }
+          }
+          tc05::fence_proxy_async();
+        }
+        tc05::bar_arrive(&S.kv_full[st]);
+      }
+    }
+  } else if (warp == kTmaWarp) {
+    // ------------------------------------------------------------ TMA
+    uint32_t step = 0, nq = 0, pending[kRing] = {0, 0};
+    if (lane == 0) {
+      bool dead = false;
+      auto load_q = [&](const CUtensorMap* map, const Piece& p) {
+        if (nq > 0 && !tc05::bar_wait_spin(&S.q_empty, (nq - 1) & 1, abort)) {
+          dead = true;
+          return;
+        }
+        const int tiles = p.s.n_new - p.qb * kQTok > 32 ? 2 : 1;
+        tc05::bar_arrive_expect_tx(&S.q_full, tiles * kOperand);
+        for (int g = 0; g < tiles; ++g)
+          for (int c = 0; c < 2; ++c)
+            tc05::tma_load_3d(S.q[g] + c * kHalf, map, 64 * c, 4 * p.h,
+                              p.s.c0 + p.qb * kQTok + 32 * g, &S.q_full);
+        ++nq;
+      };
+      for (long long f = f0; f < f1 && !dead;) {
+        const Piece p = locate_piece(A, pref, f, f1);
+        f += p.t1 - p.t0;
+        const int nint = max(0, min(p.t1, p.I) - p.t0), nother = p.t1 - p.t0 - nint;
+        if (nint > 0) {
+          load_q(&tm_qrot, p);
+          // every phase of kv_empty is waited for, those of the other warps'
+          // tiles too: a wait for a phase tells it from the next but one only
+          for (int t = 0; t < nint && !dead; ++t, ++step)
+            if (step >= kRing &&
+                !tc05::bar_wait_spin(&S.kv_empty[step % kRing], (step / kRing - 1) & 1, abort))
+              dead = true;
+        }
+        for (int t = nint > 0 ? -1 : 0; t < nother && !dead; ++t, ++step) {
+          const int st = step % kRing;
+          if (t == 0) load_q(&tm_q, p);
+          if (dead || (step >= kRing && !tc05::bar_wait_spin(&S.kv_empty[st], (step / kRing - 1) & 1, abort))) {
+            dead = true;
+            break;
+          }
+          if (t < 0) {  // 64 R_v^T, fp16
+            tc05::bar_arrive_expect_tx(&S.kv_tma[st], kOperand);
+            tc05::bulk_g2s(S.ring[st][0], A.Rv_back + (size_t)p.h * kRT5Halves, kOperand, &S.kv_tma[st]);
+          } else {
+            const int tile = p.t0 + nint + t - p.I;
+            tc05::bar_arrive_expect_tx(&S.kv_tma[st], 2 * kOperand);
+            for (int kind = 0; kind < 2; ++kind)
+              for (int c = 0; c < 2; ++c) {
+                uint8_t* dst = S.ring[st][kind] + c * kHalf;
+                if (tile < p.Wt)
+                  tc05::tma_load_3d(dst, &tm_win, 64 * c, 0,
+                                    ((p.s.slot * A.h_kv + p.h) * 2 + kind) * (A.sink + A.recent) +
+                                        kTile * tile, &S.kv_tma[st]);
+                else
+                  tc05::tma_load_3d(dst, kind ? &tm_v : &tm_k, 64 * c, p.h,
+                                    p.s.c0 + kTile * (tile - p.Wt), &S.kv_tma[st]);
+              }
+          }
+          ++pending[st];
+        }
+      }
+      // copies in flight land before the CTA exits (after an abort nobody else
+      // waits for them)
+      for (int s = 0; s < kRing; ++s)
+        if (pending[s]) tc05::bar_wait_drain(&S.kv_tma[s], (pending[s] - 1) & 1);
+      if (nq) tc05::bar_wait_drain(&S.q_full, (nq - 1) & 1);
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------ MMA
+    if (lane == 0) {
+      constexpr uint32_t kId = tc05::idesc_f16(128, 128);
+      const uint32_t sq = tc05::smem_addr(S.q[0]), sr = tc05::smem_addr(S.ring[0][0]);
+      uint32_t step = 0, nq = 0, np[2] = {0, 0};
+      bool dead = false, used = false;
+      auto wait = [&](uint64_t* bar, uint32_t phase) {
+        if (!tc05::bar_wait_spin(bar, phase & 1, abort)) dead = true;
+        tc05::fence_after();
+        return !dead;
+      };
+      auto qk = [&](int g, uint32_t st, uint32_t type) {
+        const uint32_t a = sq + g * kOperand, b = sr + st * 2 * kOperand;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+          const uint32_t o = (ks >> 2) * kHalf + (ks & 3) * 32;
+          tc05::mma_ss(tmem + kColS + 128u * g, tc05::smem_desc_sw128(a + o, 16),
+                       tc05::smem_desc_sw128(b + o, 16), kId | type, ks != 0);
+        }
+        tc05::mma_commit(&S.s_full[g]);
+      };
+      auto pv = [&](int g, uint32_t st, uint32_t type, bool add) {
+        const uint32_t b = sr + (st * 2 + 1) * kOperand;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+          tc05::mma_ts(tmem + kColO + 128u * g, tmem + kColS + 128u * g + 8u * ks,
+                       tc05::smem_desc_sw128(b + ks * 2048, kHalf),
+                       kId | type | tc05::kIdescMajorMnB, add || ks != 0);
+      };
+      for (long long f = f0; f < f1 && !dead;) {
+        const Piece p = locate_piece(A, pref, f, f1);
+        f += p.t1 - p.t0;
+        const int nint = max(0, min(p.t1, p.I) - p.t0), nother = p.t1 - p.t0 - nint;
+        const int G = p.s.n_new - p.qb * kQTok > 32 ? 2 : 1;
+        bool add = false;
+        for (int phase = 0; phase < 2 && !dead; ++phase) {
+          const int n = phase ? nother : nint;
+          const uint32_t type = phase ? tc05::kIdescBf16 : 0u;
+          if (n == 0) continue;
+          used = true;
+          if (!wait(&S.q_full, nq++)) break;
+          if (!wait(&S.kv_full[step % kRing], step / kRing)) break;
+          for (int g = 0; g < G; ++g) qk(g, step % kRing, type);
+          if (n == 1) tc05::mma_commit(&S.q_empty);
+          for (int t = 0; t < n && !dead; ++t, ++step) {
+            for (int g = 0; g < G; ++g) {
+              if (!wait(&S.p_ready[g], np[g]++)) break;
+              pv(g, step % kRing, type, add);
+              if (t == n - 1) tc05::mma_commit(&S.o_full[g]);
+              if (g == G - 1) tc05::mma_commit(&S.kv_empty[step % kRing]);
+              if (t + 1 < n) {
+                if (g == 0 && !wait(&S.kv_full[(step + 1) % kRing], (step + 1) / kRing)) break;
+                qk(g, (step + 1) % kRing, type);
+              }
+            }
+            if (t + 2 == n) tc05::mma_commit(&S.q_empty);
+            add = true;
+          }
+          if (dead || phase) continue;
+          if (!wait(&S.kv_full[step % kRing], step / kRing)) break;
+          for (int g = 0; g < G; ++g) {
+            if (!wait(&S.p_ready[g], np[g]++)) break;
+            const uint32_t b = sr + (step % kRing) * 2 * kOperand;
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+              tc05::mma_ts(tmem + kColO + 128u * g, tmem + kColS + 128u * g + 8u * ks,
+                           tc05::smem_desc(b + ks * 256, 128, 2048), kId, ks != 0);
+            if (nother == 0) tc05::mma_commit(&S.o_full[g]);
+          }
+          tc05::mma_commit(&S.kv_empty[step % kRing]);
+          ++step;
+        }
+      }
+      if (used) {  // the tensor core is done with tensor memory before it is freed
+        tc05::mma_commit(&S.drained);
+        tc05::bar_wait_drain(&S.drained, 0);
+      }
+    }
+    __syncwarp();
+  }
+
+  tc05::fence_before();
+  __syncthreads();
+  if (S.abort && tid == 0) atomicOr(A.err, OPTR_DEVERR_TIMEOUT);
+  if (warp == kMmaWarp) {
+    tc05::fence_after();
+    tc05::tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// ------------------------------------------------------------- combine
+
+// Joins the partials of the segments that several CTAs of chunk_kernel worked
+// on.  CTA (w, y) takes the segment that spans the end of range w, if its first
+// tile lies in range w, and rows 8 y .. 8 y + 7 of it: thread = 4 channels of a
+// row.
+__global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
+  pdl_wait();
+  pdl_trigger();
+  auto pref = [&](int b) { return __ldcg(A.pref + b); };
+  const long long F = pref(A.B) * A.h_kv;
+  const int w = blockIdx.x, tid = threadIdx.x;
+  const long long f0 = F * w / A.W, f1 = F * (w + 1) / A.W;
+  if (f0 == f1 || f1 == F) return;
+  const Piece p = locate_piece(A, pref, f1, f1 + 1);
+  if (p.t0 == 0 || p.f_seg < f0) return;
+  const int r = 8 * blockIdx.y + (tid & 7), cg = tid >> 3;
+  const int i = p.qb * kQTok + r / 4;
+  if (r >= A.rows || i >= p.s.n_new) return;
+  const long long end = p.f_seg + p.total;
+  float M = -INFINITY, L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int x = w; x < A.W; ++x) {
+    const long long a = F * x / A.W, b = F * (x + 1) / A.W;
+    if (a >= end) break;
+    if (a == b) continue;
+    const float* part = part_of(A, x, x != w);
+    const float m = __ldcg(part + (size_t)A.rows * kD + r), l = __ldcg(part + (size_t)A.rows * (kD + 1) + r);
+    const float4 y = __ldcg(reinterpret_cast<const float4*>(part) + (size_t)cg * A.rows + r);
+    if (l == 0.f) continue;  // a part whose keys were all left out
+    const float mn = fmaxf(M, m), u = ex2(M - mn), v = ex2(m - mn);
+    M = mn;
+    L = L * u + l * v;
+    o = make_float4(o.x * u + y.x * v, o.y * u + y.y * v, o.z * u + y.z * v, o.w * u + y.w * v);
+  }
+  const float inv = L > 0.f ? 1.f / L : 0.f;
+  const size_t at = ((size_t)p.s.c0 + i) * 4 * A.h_kv + 4 * p.h + r % 4;
+  *reinterpret_cast<uint2*>(A.out + at * kD + 4 * cg) =
+      make_uint2(pack16<true>(o.x * inv, o.y * inv), pack16<true>(o.z * inv, o.w * inv));
+}
+
+size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
+
+// Offsets of a call's workspace, bytes.
+struct ChunkLayout {
+  size_t pref, qrot, qinfo, part, total;
+  int rows, W;
+};
+
+ChunkLayout chunk_layout(const optr_params* p, int n_tok, int B, int max_new) {
+  ChunkLayout l;
+  const size_t rows = (size_t)n_tok * p->cfg.h_q;
+  l.rows = max_new > 32 ? 256 : 128;
+  l.W = p->num_sms;
+  l.pref = 0;
+  l.qrot = round_up(sizeof(long long) * ((size_t)B + 1));
+  l.qinfo = l.qrot + round_up(rows * kD * sizeof(__half));
+  l.part = l.qinfo + round_up(rows * sizeof(float2));
+  l.total = l.part + round_up(2 * (size_t)l.W * part_floats(l.rows) * sizeof(float));
+  return l;
 }
 
 }  // namespace
@@ -152,7 +767,7 @@ using namespace optr;
 
 extern "C" size_t optr_chunk_workspace_size(const optr_params* p, int n_tok, int B, int max_new) {
   if (!p || n_tok < 0 || B <= 0 || max_new <= 0) return 0;
-  return 256;
+  return chunk_layout(p, n_tok, B, max_new).total;
 }
 
 extern "C" optr_status optr_chunk_attention_win(
@@ -171,19 +786,42 @@ extern "C" optr_status optr_chunk_attention_win(
   if (!q || !k || !v || !cu_new || !pos0 || !block_table || !pool || !out) return OPTR_ERR_INVALID_ARG;
   if (!aligned(pool, 16) || !aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16))
     return OPTR_ERR_INVALID_ARG;
-  const void* dev[4] = {q, k, v, out};
-  for (const void*& x : dev) {
+  for (const void* x : {q, k, v, (const void*)out}) {  // TMA reads device memory
     bool host = false;
     if (!io_pointer(x, &x, &host) || host) return OPTR_ERR_INVALID_ARG;
   }
   if ((long long)max_pages * kPage > (1LL << 30) || B > (1 << 24)) return OPTR_ERR_OUT_OF_RANGE;
-  if (!workspace || ws_bytes < optr_chunk_workspace_size(p, n_tok, B, max_new) || !aligned(workspace, 256))
-    return OPTR_ERR_WORKSPACE;
-  const ChunkArgs A{(const __nv_bfloat16*)q, (const __nv_bfloat16*)k, (const __nv_bfloat16*)v, n_tok,
-                    cu_new, pos0, max_new, block_table, B, max_pages, pool, num_pages, w,
-                    p->cfg.sink, p->cfg.recent, p->cfg.h_kv, p->fold_v, p->cfg.group == 4 * kG,
-                    p->R_k, p->R_vT, p->mu, (__nv_bfloat16*)out, p->err};
-  return cuda_status(launch_pdl(chunk_simple_kernel, dim3(n_tok, p->cfg.h_kv), dim3(128), 0, stream, A));
+  const int h_kv = p->cfg.h_kv, win_rows = p->cfg.sink + p->cfg.recent;
+  // token and window rows are counted with 32 bits
+  if ((long long)n_slots * h_kv * 2 * win_rows >= (1LL << 31)) return OPTR_ERR_OUT_OF_RANGE;
+  const ChunkLayout l = chunk_layout(p, n_tok, B, max_new);
+  if (!workspace || ws_bytes < l.total || !aligned(workspace, 256)) return OPTR_ERR_WORKSPACE;
+  char* ws = static_cast<char*>(workspace);
+  const ChunkArgs A{(const __nv_bfloat16*)q, n_tok, cu_new, pos0, max_new, block_table, B, max_pages,
+                    pool, num_pages, w, p->cfg.sink, p->cfg.recent, h_kv, p->cfg.group == 4 * kG,
+                    p->Rk_frag, p->Rv_back, p->mu, (__nv_bfloat16*)out, p->err,
+                    (long long*)(ws + l.pref), (__half*)(ws + l.qrot), (float2*)(ws + l.qinfo),
+                    (float*)(ws + l.part), l.rows, l.W};
+  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(chunk_kernel), sizeof(Smem));
+  if (e != cudaSuccess) return OPTR_ERR_CUDA;
+  CUtensorMap mq, mr, mk, mv, mw;
+  if (!token_rows_map(&mq, q, n_tok, 4 * h_kv, 32, 4) ||
+      !token_rows_map(&mr, A.qrot, n_tok, 4 * h_kv, 32, 4) ||
+      !token_rows_map(&mk, k, n_tok, h_kv, kTile) || !token_rows_map(&mv, v, n_tok, h_kv, kTile) ||
+      !(w.win ? token_rows_map(&mw, w.win, n_slots * h_kv * 2 * win_rows, 1, kTile)
+              : token_rows_map(&mw, k, n_tok, h_kv, kTile)))
+    return OPTR_ERR_CUDA;
+  // tokens per rotating CTA: about two CTAs per SM, at most 64 tokens each
+  const long long heads = (long long)n_tok * h_kv;
+  const int per = (int)std::min<long long>(64, std::max<long long>(4, heads / (2 * p->num_sms) / 4 * 4));
+  const long long rot = (n_tok + per - 1) / per * (long long)h_kv;
+  e = launch_pdl(chunk_prologue_kernel, dim3((unsigned)(rot + 1)), dim3(kProThreads), 0, stream, A, per);
+  if (e == cudaSuccess)
+    e = launch_pdl(chunk_kernel, dim3(l.W), dim3(kThreads), sizeof(Smem), stream, mq, mr, mk, mv, mw, A);
+  if (e == cudaSuccess)
+    e = launch_pdl(chunk_combine_kernel, dim3(l.W - 1, (std::min(l.rows, 4 * max_new) + 7) / 8),
+                   dim3(256), 0, stream, A);
+  return cuda_status(e);
 }
 
 extern "C" optr_status optr_chunk_attention(const optr_params* p, const void* q, const void* k,

@@ -269,18 +269,6 @@ optr_status optr_params_create(const optr_config* cfg, const float* R_k,
   if (e == cudaSuccess) e = cudaMalloc(&p->muR, sizeof(float) * H * kD);
   if (e == cudaSuccess) e = cudaMalloc(&p->mu, sizeof(float) * H * kD);
   if (e == cudaSuccess) e = cudaMalloc(&p->err, sizeof(unsigned));
-  std::vector<uint16_t> t5((size_t)H * kRT5Halves);
-  auto operand = [&](uint16_t** dev, const float* R, void (*build)(const float*, uint16_t*)) {
-    if (e != cudaSuccess) return;
-    e = cudaMalloc(dev, sizeof(uint16_t) * t5.size());
-    if (e != cudaSuccess) return;
-    for (int h = 0; h < H; ++h) build(R + h * mat, t5.data() + (size_t)h * kRT5Halves);
-    e = cudaMemcpy(*dev, t5.data(), sizeof(uint16_t) * t5.size(), cudaMemcpyHostToDevice);
-  };
-  operand(&p->Rk_t5, R_k, build_rotation_tc05);
-  operand(&p->Rv_t5, R_v, build_rotation_tc05);
-  operand(&p->Rk_back, R_k, build_back_rotation_tc05);
-  operand(&p->Rv_back, R_v, build_back_rotation_tc05);
   if (e == cudaSuccess)
     e = cudaMemcpy(p->R_k, R_k, sizeof(float) * H * mat, cudaMemcpyHostToDevice);
   if (e == cudaSuccess)
@@ -294,6 +282,7 @@ optr_status optr_params_create(const optr_config* cfg, const float* R_k,
   if (e == cudaSuccess)
     e = cudaMemcpy(p->mu, mu, sizeof(float) * H * kD, cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaMemset(p->err, 0, sizeof(unsigned));
+  if (e == cudaSuccess) e = build_operands(p);
   if (e == cudaSuccess) e = noalloc_scratch_address(&p->noalloc_ws);
   if (e == cudaSuccess && cfg->decode_variant != OPTR_VARIANT_CUDA_CORE)
     e = decode_one_limits(p, p->one_clusters);
@@ -317,6 +306,7 @@ void optr_params_destroy(optr_params* p) {
   cudaFree(p->Rv_t5);
   cudaFree(p->Rk_back);
   cudaFree(p->Rv_back);
+  cudaFree(p->Rk_frag);
   cudaFree(p->err);
   free(p);
 }

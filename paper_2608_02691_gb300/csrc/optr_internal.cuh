@@ -54,6 +54,7 @@ struct optr_params {
   uint16_t* Rv_t5;     // device tcgen05 B operands of R_v
   uint16_t* Rk_back;   // the same of R_k^T and R_v^T, for dequantized rows
   uint16_t* Rv_back;   // (inner index in the order of dequant.cuh)
+  uint4* Rk_frag;      // mma.sync fragments of R_k (operands.cu)
   unsigned* err;       // device error word
   // device address of the fixed scratch array of
   // optr_decode_attention_noalloc on this params' device (noalloc.cu),
@@ -217,11 +218,10 @@ cudaError_t launch_append_cuda_core(const optr_params* p, const __nv_bfloat16* k
                                     const int32_t* bt, int B, int max_pages,
                                     uint8_t* pool, int num_pages,
                                     cudaStream_t s);
-// tcgen05 append operand: [hi, lo][128 x 128] fp16 per head, see append_tc05.cu.
+// Halves of a rotation's tcgen05 operand: [hi, lo][128 x 128] fp16 per head.
 constexpr int kRT5Halves = 2 * kD * kD;
-void build_rotation_tc05(const float* R /*[D][D]*/, uint16_t* out);
-// The same of the inverse rotation z R^T, z a dequantized row (dequant.cuh).
-void build_back_rotation_tc05(const float* R /*[D][D]*/, uint16_t* out);
+// The tensor-core operands of p's rotations, from R_k and R_v (operands.cu).
+cudaError_t build_operands(optr_params* p);
 cudaError_t launch_append_tc05(const optr_params* p, const __nv_bfloat16* k,
                                const __nv_bfloat16* v, int n_tok,
                                const int32_t* cu_new, const int32_t* pos0,

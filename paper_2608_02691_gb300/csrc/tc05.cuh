@@ -28,6 +28,19 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t saddr, uint32_t lbo,
          ((uint64_t)((sbo >> 4) & 0x3FFFu) << 32) | ((uint64_t)1 << 46);
 }
 
+// The same with the 128-byte swizzle (layout type 2: 16-byte piece c of a
+// 128-byte row r at piece c ^ (r % 8), rows 128 B apart, 1024-byte aligned;
+// what TMA writes).  K-major: rows along M/N, 8 of them SBO = 1024 B; a K step
+// of 16 starts 32 B further.  MN-major (bit 15 or 16 of the instruction
+// descriptor): rows along K, 8 of them SBO = 1024 B; LBO from 64 elements of
+// M/N to the next 64; a K step of 16 starts 2048 B further.
+__device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t saddr, uint32_t lbo) {
+  return smem_desc(saddr, lbo, 1024) | ((uint64_t)2 << 61);
+}
+
+constexpr uint32_t kIdescBf16 = (1u << 7) | (1u << 10);  // A and B bf16
+constexpr uint32_t kIdescMajorMnB = 1u << 16;
+
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N) {
   return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
@@ -103,6 +116,27 @@ __device__ __forceinline__ bool bar_wait_drain(uint64_t* bar, uint32_t parity) {
   }
 }
 
+// bar_wait without sleeping between the polls (each of which the hardware
+// suspends for a while itself): for waits of a few hundred cycles on the
+// critical path.
+__device__ __forceinline__ bool bar_wait_spin(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  if (bar_try_wait(bar, parity)) return true;
+  uint64_t t0;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+  for (uint32_t it = 1;; ++it) {
+    if (bar_try_wait(bar, parity)) return true;
+    if ((it & 63u) == 0) {
+      if (*abort) return false;
+      uint64_t t;
+      asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+      if (t - t0 > 2000000000ull) {
+        *abort = 1;
+        return false;
+      }
+    }
+  }
+}
+
 // Bulk copy of `bytes` (multiple of 16; both addresses 16-byte aligned)
 // from global to shared memory, completing on bar's transaction count.
 __device__ __forceinline__ void bulk_g2s(void* dst, const void* src,
@@ -161,6 +195,15 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b,
       ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
+// The same with A in shared memory.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
+                                       uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
 // Arrive on bar once every tcgen05.mma issued so far by this thread is done.
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
   asm volatile(
@@ -196,6 +239,16 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
         "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
         "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr)
+      : "memory");
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,"
+      "%9,%10,%11,%12,%13,%14,%15,%16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
+        "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
 
