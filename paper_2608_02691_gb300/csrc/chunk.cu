@@ -24,6 +24,7 @@
 #include "append_common.cuh"
 #include "chunk.cuh"
 #include "dequant.cuh"
+#include "f32x2.cuh"
 #include "tc05.cuh"
 #include "tmap.cuh"
 
@@ -182,8 +183,13 @@ __global__ void __launch_bounds__(kProThreads) chunk_prologue_kernel(const Chunk
 
 // ----------------------------------------------------------- attention
 
+// Warpgroups: two of softmax, one of keys and values, one with the TMA and the
+// MMA warp.  Registers a thread after the split (65536 in all, as launched):
+// a softmax thread holds a whole row of 128 logits.
 constexpr int kDeqWarp = 8, kTmaWarp = 12, kMmaWarp = 13;
-constexpr int kThreads = 14 * 32;
+constexpr int kThreads = 512;
+constexpr int kRegSoftmax = 192, kRegDeq = 72, kRegIssue = 56;
+static_assert(2 * kRegSoftmax + kRegDeq + kRegIssue == 4 * 128, "registers of the launch");
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 0, kColO = 256;  // S[g] (and P[g]) at 128 g, O[g] at 256 + 128 g
 constexpr int kRing = 2;
@@ -195,6 +201,7 @@ constexpr float kSlack = 8.f;  // a row's maximum may grow by 2^8 before O is re
 struct Smem {
   uint8_t q[2][kOperand];            // the query operand, by tile
   uint8_t ring[kRing][2][kOperand];  // keys, values
+  uint4 raw[2][6][128];              // INT2 records as read: codes and metadata, by key
   alignas(16) uint32_t mask[kRing][4];  // keys of the tile that count
   long long pref[kPrefCache + 1];
   uint64_t kv_full[kRing], kv_tma[kRing], kv_empty[kRing];
@@ -232,26 +239,27 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, float sca
     const int n = lim - 32 * c;
     return word[c] & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u);
   };
-  uint32_t s[32];
-  float top = -INFINITY;
+  uint32_t s[kTile];
+  auto chunk = [&](int c) -> uint32_t (&)[32] { return reinterpret_cast<uint32_t(&)[32]>(s[32 * c]); };
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    tc05::tmem_ld32(tS + 32 * c, s);
-    tc05::tmem_wait_ld();
-    if (!whole) {
+  for (int c = 0; c < 4; ++c) tc05::tmem_ld32(tS + 32 * c, chunk(c));
+  tc05::tmem_wait_ld();
+  if (!whole) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
       const uint32_t k = keep(c);
 #pragma unroll
       for (int j = 0; j < 32; ++j)
-        if (!(k >> j & 1)) s[j] = 0xff800000u;
+        if (!(k >> j & 1)) s[32 * c + j] = 0xff800000u;
     }
-    float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-    for (int j = 0; j < 32; j += 8)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        x[i] = fmaxf(x[i], fmaxf(__uint_as_float(s[j + i]), __uint_as_float(s[j + 4 + i])));
-    top = fmaxf(top, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
   }
+  float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+  for (int j = 0; j < kTile; j += 8)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      x[i] = fmaxf(x[i], fmaxf(__uint_as_float(s[j + i]), __uint_as_float(s[j + 4 + i])));
+  const float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
   const float t = fmaf(top, scale, -off);
   if (fresh) {
     m = fmaxf(m, t);
@@ -260,37 +268,32 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, float sca
     m = mn;
     l *= al;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      tc05::tmem_ld32(tO + 32 * c, s);
+    for (int c = 0; c < 8; ++c) {
+      uint32_t o[16];
+      tc05::tmem_ld16(tO + 16 * c, o);
       tc05::tmem_wait_ld();
 #pragma unroll
-      for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) * al);
-      tc05::tmem_st32(tO + 32 * c, s);
+      for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * al);
+      tc05::tmem_st16(tO + 16 * c, o);
     }
   }
-  const float sub = off + m;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  const float2 scale2 = make_float2(scale, scale), sub2 = make_float2(-(off + m), -(off + m));
+  float2 sum[2] = {};
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    tc05::tmem_ld32(tS + 32 * c, s);
-    tc05::tmem_wait_ld();
-    if (!whole) {
-      const uint32_t k = keep(c);
-#pragma unroll
-      for (int j = 0; j < 32; ++j)
-        if (!(k >> j & 1)) s[j] = 0xff800000u;
-    }
     uint32_t p[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-      const float a = ex2(fmaf(__uint_as_float(s[2 * j]), scale, -sub));
-      const float b = ex2(fmaf(__uint_as_float(s[2 * j + 1]), scale, -sub));
-      sum[j & 3] += a + b;
-      p[j] = pack16<kBf16>(a, b);
+      const float2 y = fma2(make_float2(__uint_as_float(s[32 * c + 2 * j]),
+                                        __uint_as_float(s[32 * c + 2 * j + 1])), scale2, sub2);
+      const float2 e = make_float2(ex2(y.x), ex2(y.y));
+      sum[j & 1] = add2(sum[j & 1], e);
+      p[j] = pack16<kBf16>(e.x, e.y);
     }
     tc05::tmem_st16(tS + 16 * c, p);
   }
-  l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  const float2 total = add2(sum[0], sum[1]);
+  l += total.x + total.y;
   tc05::tmem_wait_st();
 }
 
@@ -334,6 +337,12 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
   const int w = blockIdx.x;
   const long long f0 = F * w / A.W, f1 = F * (w + 1) / A.W;
 
+  if (warp < kDeqWarp)
+    tc05::reg_inc<kRegSoftmax>();
+  else if (warp < kTmaWarp)
+    tc05::reg_dec<kRegDeq>();
+  else
+    tc05::reg_dec<kRegIssue>();
   if (warp < kDeqWarp) {
     // ------------------------------------------------------------- softmax
     const int g = warp >> 2, row = 32 * (warp & 3) + lane;
@@ -462,41 +471,65 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
       return !dead;
     };
     const int ms = meta_stride(A.compact);
+    // Records are copied into shared memory two tiles ahead (each thread reads
+    // only what it copied itself), their pages looked up three tiles ahead.
+    auto request = [&](const Piece& p, int t) {
+      const int n = t * kTile + key;
+      return n < p.s.n_int && t < p.t1
+                 ? __ldcg(A.bt + (size_t)p.b * A.max_pages + (A.sink + n) / kPage) : -1;
+    };
+    auto copy = [&](const Piece& p, int t, int page) {
+      bool ok = t * kTile + key < p.s.n_int && t < p.t1;
+      if (ok && (page < 0 || page >= A.num_pages)) {
+        atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
+        ok = false;
+      }
+      if (ok) {
+        const uint8_t* rec = A.pool + ((size_t)page * A.h_kv + p.h) * chunk_bytes(A.compact);
+        const int slot = (t * kTile + key) % kPage;  // (sink is a multiple of 16)
+        uint4* d = &S.raw[t & 1][0][key];
+        for (int i = 0; i < 2; ++i) {
+          cp_async16_zfill(d + i * 128, rec + OPTR_K_CODES_OFFSET + 32 * slot + 16 * i, true);
+          cp_async16_zfill(d + (2 + i) * 128, rec + OPTR_V_CODES_OFFSET + 32 * slot + 16 * i, true);
+        }
+        const uint8_t* mk = rec + OPTR_K_META_OFFSET + ms * slot;
+        const uint8_t* mv = rec + vmeta_offset(A.compact) + ms * slot;
+        if (A.compact) {
+          cp_async4(d + 4 * 128, mk);
+          cp_async4(d + 5 * 128, mv);
+        } else {
+          cp_async16_zfill(d + 4 * 128, mk, true);
+          cp_async16_zfill(d + 5 * 128, mv, true);
+        }
+      }
+      cp_async_commit();
+      return ok;
+    };
     for (long long f = f0; f < f1 && !dead;) {
       const Piece p = locate_piece(A, pref, f, f1);
       f += p.t1 - p.t0;
       const int nint = max(0, min(p.t1, p.I) - p.t0), nother = p.t1 - p.t0 - nint;
+      bool okn[2] = {false, false};
+      int page = -1;
+      if (nint > 0) {
+        const int e0 = request(p, p.t0), e1 = request(p, p.t0 + 1);
+        page = request(p, p.t0 + 2);
+        okn[0] = copy(p, p.t0, e0);
+        okn[1] = copy(p, p.t0 + 1, e1);
+      }
       for (int t = 0; t < nint && !dead; ++t, ++step) {
-        const int st = step % kRing;
-        const int n = (p.t0 + t) * kTile + key;  // INT2 position, from `sink` on
-        const int pos = A.sink + n;
-        bool ok = n < p.s.n_int;
+        const int st = step % kRing, tile = p.t0 + t;
+        cp_async_wait<1>();
+        const bool ok = okn[0];
         uint4 kc[2] = {}, vc[2] = {}, km = {}, vm = {};
         if (ok) {
-          const int page = __ldcg(A.bt + (size_t)p.b * A.max_pages + pos / kPage);
-          if (page < 0 || page >= A.num_pages) {
-            atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
-            ok = false;
-          } else {
-            const uint8_t* rec = A.pool + ((size_t)page * A.h_kv + p.h) * chunk_bytes(A.compact);
-            const int slot = pos % kPage;
-            const uint4* k4 = reinterpret_cast<const uint4*>(rec + OPTR_K_CODES_OFFSET + 32 * slot);
-            const uint4* v4 = reinterpret_cast<const uint4*>(rec + OPTR_V_CODES_OFFSET + 32 * slot);
-            const uint8_t* mk = rec + OPTR_K_META_OFFSET + ms * slot;
-            const uint8_t* mv = rec + vmeta_offset(A.compact) + ms * slot;
-            kc[0] = __ldcg(k4);
-            kc[1] = __ldcg(k4 + 1);
-            vc[0] = __ldcg(v4);
-            vc[1] = __ldcg(v4 + 1);
-            if (A.compact) {
-              km.x = km.y = km.z = km.w = __ldcg(reinterpret_cast<const uint32_t*>(mk));
-              vm.x = vm.y = vm.z = vm.w = __ldcg(reinterpret_cast<const uint32_t*>(mv));
-            } else {
-              km = __ldcg(reinterpret_cast<const uint4*>(mk));
-              vm = __ldcg(reinterpret_cast<const uint4*>(mv));
-            }
-          }
+          const uint4* d = &S.raw[tile & 1][0][key];
+          kc[0] = d[0], kc[1] = d[128], vc[0] = d[256], vc[1] = d[384], km = d[512], vm = d[640];
+          if (A.compact) km.y = km.z = km.w = km.x, vm.y = vm.z = vm.w = vm.x;
         }
+        okn[0] = okn[1];
+        okn[1] = copy(p, tile + 2, page);
+        page = request(p, tile + 3);
         if (step >= kRing && !wait(&S.kv_empty[st], step / kRing - 1)) break;
         const uint32_t bits = __ballot_sync(0xffffffffu, ok);
         if (lane == 0) S.mask[st][key >> 5] = bits;
@@ -541,6 +574,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
         tc05::bar_arrive(&S.kv_full[st]);
       }
     }
+    cp_async_wait<0>();
   } else if (warp == kTmaWarp) {
     // ------------------------------------------------------------ TMA
     uint32_t step = 0, nq = 0, pending[kRing] = {0, 0};
@@ -609,7 +643,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
     __syncwarp();
   } else {
     // ------------------------------------------------------------ MMA
-    if (lane == 0) {
+    if (warp == kMmaWarp && lane == 0) {
       constexpr uint32_t kId = tc05::idesc_f16(128, 128);
       const uint32_t sq = tc05::smem_addr(S.q[0]), sr = tc05::smem_addr(S.ring[0][0]);
       uint32_t step = 0, nq = 0, np[2] = {0, 0};

@@ -1,4 +1,4 @@
-// Packed float32 pair arithmetic: the .f32x2 forms of sub and fma (sm_100
+// Packed float32 pair arithmetic: the .f32x2 forms of add, sub and fma (sm_100
 // and later) issue one instruction for two independent float32 operations,
 // each rounded exactly as its scalar .rn counterpart (no flush of
 // subnormals).  Where a kernel is issue-bound and its values come in
@@ -22,6 +22,16 @@ __device__ __forceinline__ float2 sub2(float2 a, float2 b) {
   asm("{\n\t.reg .b64 ra, rb, rd;\n\t"
       "mov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
       "sub.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 ra, rb, rd;\n\t"
+      "mov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\t"
+      "add.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
       : "=f"(d.x), "=f"(d.y)
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return d;
