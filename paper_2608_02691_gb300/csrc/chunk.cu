@@ -49,7 +49,7 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
 __device__ __forceinline__ float bf_lo(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
 
-// The plan (one CTA): tiles of one head of the sequences before b, for all b.
+// The plan (one CTA): the cost of one head of the sequences before b, for all b.
 __device__ void chunk_plan(const ChunkArgs& A) {
   __shared__ long long warp_sum[kProThreads / 32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -64,7 +64,7 @@ __device__ void chunk_plan(const ChunkArgs& A) {
       if (!bad && A.win.win && (s.slot < 0 || s.slot >= A.win.n_slots)) bad = OPTR_DEVERR_WIN_SLOT;
       if (bad) atomicOr(A.err, bad);
       if (s.n_new > 0)
-        x = block_tiles((s.n_new + kQTok - 1) / kQTok, tiles_of(s.n_int) + tiles_of(s.n_win));
+        x = block_cost((s.n_new + kQTok - 1) / kQTok, tiles_of(s.n_int) + tiles_of(s.n_win));
     }
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -183,10 +183,10 @@ __global__ void __launch_bounds__(kProThreads) chunk_prologue_kernel(const Chunk
 
 // ----------------------------------------------------------- attention
 
-// Warpgroups: two of softmax, one of keys and values, one with the TMA and the
-// MMA warp.  Registers a thread after the split (65536 in all, as launched):
+// Warpgroups: two of softmax, one of keys and values, one of two TMA
+// warps, the MMA warp and the one that finds the CTA's pieces.  Registers a thread after the split (65536 in all, as launched):
 // a softmax thread holds a whole row of 128 logits.
-constexpr int kDeqWarp = 8, kTmaWarp = 12, kMmaWarp = 13;
+constexpr int kDeqWarp = 8, kTmaWarp = 12, kMmaWarp = 14, kPlanWarp = 15;
 constexpr int kThreads = 512;
 constexpr int kRegSoftmax = 192, kRegDeq = 72, kRegIssue = 56;
 static_assert(2 * kRegSoftmax + kRegDeq + kRegIssue == 4 * 128, "registers of the launch");
@@ -195,16 +195,24 @@ constexpr uint32_t kColS = 0, kColO = 256;  // S[g] (and P[g]) at 128 g, O[g] at
 constexpr int kRing = 2;
 constexpr uint32_t kHalf = kTile * 128;      // 64 channels of 128 rows
 constexpr uint32_t kOperand = 2 * kHalf;     // 128 x 128 of 16 bits
-constexpr int kPrefCache = 256;
+constexpr int kPieces = 3;       // pieces found ahead
 constexpr float kSlack = 8.f;  // a row's maximum may grow by 2^8 before O is rescaled
 
 struct Smem {
   uint8_t q[2][kOperand];            // the query operand, by tile
-  uint8_t ring[kRing][2][kOperand];  // keys, values
+  uint8_t k[kRing][kOperand];        // keys by tile
+  uint8_t v[kRing][kOperand];        // values by tile; R_v^T
   uint4 raw[2][6][128];              // INT2 records as read: codes and metadata, by key
-  alignas(16) uint32_t mask[kRing][4];  // keys of the tile that count
-  long long pref[kPrefCache + 1];
-  uint64_t kv_full[kRing], kv_tma[kRing], kv_empty[kRing];
+  // INT2 tiles: keys whose page is in range.  Read between the tile's logits
+  // and its probabilities: by when K of tile t + 4 may be written, the logits of
+  // t + 2 are done, so the probabilities of t + 1.
+  alignas(16) uint32_t mask[4][4];
+  Piece piece[kPieces];
+  // dequantized, brought by TMA, free again; v_full also after v_tma, once the
+  // rows that do not count are cleared
+  uint64_t k_full[kRing], k_tma[kRing], k_empty[kRing];
+  uint64_t v_full[kRing], v_tma[kRing], v_empty[kRing];
+  uint64_t piece_full[kPieces], piece_empty[kPieces];
   uint64_t s_full[2], p_ready[2], o_full[2], q_full, q_empty, drained;
   uint32_t tmem;
   int abort;
@@ -224,6 +232,18 @@ __device__ __forceinline__ uint32_t pack16(float a, float b) {  // a in the low 
   else
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
   return r;
+}
+
+// 32 bytes of a row, in one piece where the rows are aligned so: a thread
+// writes its own row, so every store of the warp touches 32 lines.
+__device__ __forceinline__ void store32(void* p, const uint32_t (&y)[8], bool whole) {
+  if (whole) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(y[0]), "r"(y[1]),
+                 "r"(y[2]), "r"(y[3]), "r"(y[4]), "r"(y[5]), "r"(y[6]), "r"(y[7]) : "memory");
+  } else {
+    static_cast<uint4*>(p)[0] = make_uint4(y[0], y[1], y[2], y[3]);
+    static_cast<uint4*>(p)[1] = make_uint4(y[4], y[5], y[6], y[7]);
+  }
 }
 
 // One row of a logit tile: S (128 columns of tensor memory at tS) becomes P =
@@ -303,16 +323,24 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
              const __grid_constant__ CUtensorMap tm_win, const __grid_constant__ ChunkArgs A) {
   extern __shared__ __align__(1024) unsigned char dsm_[];
   Smem& S = *reinterpret_cast<Smem*>(dsm_);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);  // uniform, as the compiler sees it
   if (tid == 0) {
     for (int s = 0; s < kRing; ++s) {
-      tc05::bar_init(&S.kv_full[s], 128);
-      tc05::bar_init(&S.kv_tma[s], 1);
-      tc05::bar_init(&S.kv_empty[s], 1);
+      tc05::bar_init(&S.k_full[s], 128);
+      tc05::bar_init(&S.k_tma[s], 1);
+      tc05::bar_init(&S.k_empty[s], 1);
+      tc05::bar_init(&S.v_full[s], 128);
+      tc05::bar_init(&S.v_tma[s], 1);
+      tc05::bar_init(&S.v_empty[s], 1);
+    }
+    for (int i = 0; i < kPieces; ++i) {
+      tc05::bar_init(&S.piece_full[i], 1);
+      tc05::bar_init(&S.piece_empty[i], kPlanWarp);
     }
     for (int g = 0; g < 2; ++g) {
       tc05::bar_init(&S.s_full[g], 1);
-      tc05::bar_init(&S.p_ready[g], 128);
+      tc05::bar_init(&S.p_ready[g], 4);
       tc05::bar_init(&S.o_full[g], 1);
     }
     tc05::bar_init(&S.q_full, 1);
@@ -324,19 +352,22 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
   if (warp == kMmaWarp) tc05::tmem_alloc(&S.tmem, kTmemCols);
   pdl_wait();
   pdl_trigger();
-  const bool cached = A.B <= kPrefCache;
-  if (cached)
-    for (int i = tid; i <= A.B; i += kThreads) S.pref[i] = __ldcg(A.pref + i);
   tc05::fence_before();
   __syncthreads();
   tc05::fence_after();
-  auto pref = [&](int b) { return cached ? S.pref[b] : __ldcg(A.pref + b); };
   const uint32_t tmem = S.tmem;
   volatile int* abort = &S.abort;
-  const long long F = pref(A.B) * A.h_kv;
   const int w = blockIdx.x;
-  const long long f0 = F * w / A.W, f1 = F * (w + 1) / A.W;
-
+  // the CTA's n-th piece, as every warp but the finder's takes it; false after the last
+  auto next_piece = [&](uint32_t n, Piece& p) {
+    const uint32_t i = n % kPieces;
+    if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(&S.piece_full[i], n / kPieces & 1, abort)))
+      return false;
+    p = S.piece[i];
+    __syncwarp();
+    if (lane == 0) tc05::bar_arrive(&S.piece_empty[i]);
+    return p.t1 > p.t0;
+  };
   if (warp < kDeqWarp)
     tc05::reg_inc<kRegSoftmax>();
   else if (warp < kTmaWarp)
@@ -348,24 +379,28 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
     const int g = warp >> 2, row = 32 * (warp & 3) + lane;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t tS = tmem + lanes + kColS + 128u * g, tO = tmem + lanes + kColO + 128u * g;
-    uint32_t step = 0, ns = 0, no = 0;  // ring entries, S and O phases seen
+    uint32_t nk = 0, ns = 0, no = 0;  // key tiles of the CTA; S and O phases seen
     bool dead = false;
     auto wait = [&](uint64_t* bar, uint32_t phase) {
       if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
       tc05::fence_after();
       return !dead;
     };
-    for (long long f = f0; f < f1 && !dead;) {
-      const Piece p = locate_piece(A, pref, f, f1);
-      f += p.t1 - p.t0;
-      const int nint = max(0, min(p.t1, p.I) - p.t0), nother = p.t1 - p.t0 - nint;
-      const uint32_t base = step;
-      step += p.t1 - p.t0 + (nint > 0);
+    auto ready = [&]() {  // the warp's rows of P are in tensor memory
+      tc05::fence_before();
+      __syncwarp();
+      if (lane == 0) tc05::bar_arrive(&S.p_ready[g]);
+    };
+    Piece p;
+    for (uint32_t n = 0; !dead && next_piece(n, p); ++n) {
+      const int nint = p.int_tiles(), nother = p.t1 - p.t0 - nint;
+      const uint32_t base = nk;
+      nk += p.t1 - p.t0;
       const int i0 = p.qb * kQTok + 32 * g;  // the tile's first token
-      if (i0 >= p.s.n_new) continue;
+      if (i0 >= p.n_new) continue;
       const int i = i0 + (row >> 2), j = row & 3;
-      const bool valid = i < p.s.n_new;
-      const size_t at = ((size_t)p.s.c0 + i) * 4 * A.h_kv + 4 * p.h + j;
+      const bool valid = i < p.n_new;
+      const size_t at = ((size_t)p.c0 + i) * 4 * A.h_kv + 4 * p.h + j;
       float scale = kLogit, off = 0.f, m = -1e30f, l = 0.f;
       if (p.I > 0 && valid) {
         const float2 x = __ldcg(A.qinfo + at);
@@ -375,11 +410,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
       bool fresh = true;
       for (int t = 0; t < nint; ++t) {
         if (!wait(&S.s_full[g], ns++)) break;
-        const uint4 mask = *reinterpret_cast<const uint4*>(S.mask[(base + t) % kRing]);
-        softmax_tile<false>(tS, tO, scale, 0.f, mask, kTile, fresh, m, l);
+        const uint4 mask = *reinterpret_cast<const uint4*>(S.mask[(base + t) % 4]);
+        softmax_tile<false>(tS, tO, scale, 0.f, mask, p.n_int - kTile * (p.t0 + t), fresh, m, l);
         fresh = false;
-        tc05::fence_before();
-        tc05::bar_arrive(&S.p_ready[g]);
+        ready();
       }
       if (dead) break;
       if (nint > 0) {
@@ -402,21 +436,17 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
           m += __log2f(l) - 6.f;
           l = 64.f;
         }
-        tc05::fence_before();
-        tc05::bar_arrive(&S.p_ready[g]);
+        ready();
       }
       const float sub = p.I > 0 ? off : 0.f;
       for (int t = 0; t < nother; ++t) {
         if (!wait(&S.s_full[g], ns++)) break;
-        const uint4 mask = *reinterpret_cast<const uint4*>(
-            S.mask[(base + nint + (nint > 0) + t) % kRing]);
-        // own tiles: causal
-        const int own = p.t0 + nint + t - p.I - p.Wt;
-        const int lim = own < 0 ? kTile : i + 1 - kTile * own;
-        softmax_tile<true>(tS, tO, kLogit, sub, mask, lim, fresh, m, l);
+        // window rows as far as they are filled; own tiles causally
+        const int tile = p.t0 + nint + t - p.I;
+        const int lim = tile < p.Wt ? p.n_win - kTile * tile : i + 1 - kTile * (tile - p.Wt);
+        softmax_tile<true>(tS, tO, kLogit, sub, make_uint4(~0u, ~0u, ~0u, ~0u), lim, fresh, m, l);
         fresh = false;
-        tc05::fence_before();
-        tc05::bar_arrive(&S.p_ready[g]);
+        ready();
       }
       if (dead || !wait(&S.o_full[g], no++)) break;
       if (p.t1 - p.t0 == p.total) {
@@ -428,13 +458,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
           tc05::tmem_wait_ld();
           if (valid)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint32_t y[4];
+            for (int e = 0; e < 2; ++e) {
+              uint32_t y[8];
 #pragma unroll
-              for (int z = 0; z < 4; ++z)
-                y[z] = pack16<true>(__uint_as_float(o[8 * e + 2 * z]) * inv,
-                                    __uint_as_float(o[8 * e + 2 * z + 1]) * inv);
-              reinterpret_cast<uint4*>(A.out + at * kD + 32 * c)[e] = make_uint4(y[0], y[1], y[2], y[3]);
+              for (int z = 0; z < 8; ++z)
+                y[z] = pack16<true>(__uint_as_float(o[16 * e + 2 * z]) * inv,
+                                    __uint_as_float(o[16 * e + 2 * z + 1]) * inv);
+              store32(A.out + at * kD + 32 * c + 16 * e, y, A.out32);
             }
         }
       } else {
@@ -464,7 +494,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
     // tiles, which TMA brings, it clears the values that do not count (0 times
     // what lies there need not be 0)
     const int key = tid - 32 * kDeqWarp;
-    uint32_t step = 0, tma[kRing] = {0, 0};
+    uint32_t nk = 0, nv = 0, tma[kRing] = {0, 0};
     bool dead = false;
     auto wait = [&](uint64_t* bar, uint32_t phase) {
       if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
@@ -475,11 +505,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
     // only what it copied itself), their pages looked up three tiles ahead.
     auto request = [&](const Piece& p, int t) {
       const int n = t * kTile + key;
-      return n < p.s.n_int && t < p.t1
+      return n < p.n_int && t < p.t1
                  ? __ldcg(A.bt + (size_t)p.b * A.max_pages + (A.sink + n) / kPage) : -1;
     };
     auto copy = [&](const Piece& p, int t, int page) {
-      bool ok = t * kTile + key < p.s.n_int && t < p.t1;
+      bool ok = t * kTile + key < p.n_int && t < p.t1;
       if (ok && (page < 0 || page >= A.num_pages)) {
         atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
         ok = false;
@@ -505,10 +535,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
       cp_async_commit();
       return ok;
     };
-    for (long long f = f0; f < f1 && !dead;) {
-      const Piece p = locate_piece(A, pref, f, f1);
-      f += p.t1 - p.t0;
-      const int nint = max(0, min(p.t1, p.I) - p.t0), nother = p.t1 - p.t0 - nint;
+    Piece p;
+    for (uint32_t n = 0; !dead && next_piece(n, p); ++n) {
+      const int nint = p.int_tiles(), nother = p.t1 - p.t0 - nint;
       bool okn[2] = {false, false};
       int page = -1;
       if (nint > 0) {
@@ -517,8 +546,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
         okn[0] = copy(p, p.t0, e0);
         okn[1] = copy(p, p.t0 + 1, e1);
       }
-      for (int t = 0; t < nint && !dead; ++t, ++step) {
-        const int st = step % kRing, tile = p.t0 + t;
+      for (int t = 0; t < nint && !dead; ++t, ++nk, ++nv) {
+        const int tile = p.t0 + t;
         cp_async_wait<1>();
         const bool ok = okn[0];
         uint4 kc[2] = {}, vc[2] = {}, km = {}, vm = {};
@@ -530,9 +559,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
         okn[0] = okn[1];
         okn[1] = copy(p, tile + 2, page);
         page = request(p, tile + 3);
-        if (step >= kRing && !wait(&S.kv_empty[st], step / kRing - 1)) break;
-        const uint32_t bits = __ballot_sync(0xffffffffu, ok);
-        if (lane == 0) S.mask[st][key >> 5] = bits;
         auto put = [&](uint8_t* dst, const uint4 (&c)[2], const uint4& mm) {
           const SlotMeta sm = slot_meta(mm.x, mm.y, mm.z, mm.w);
           const uint32_t word[8] = {c[0].x, c[0].y, c[0].z, c[0].w, c[1].x, c[1].y, c[1].z, c[1].w};
@@ -546,23 +572,27 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
             *reinterpret_cast<uint4*>(r + (((c0 + 1) ^ (key & 7)) << 4)) = make_uint4(x[4], x[5], x[6], x[7]);
           }
         };
-        put(S.ring[st][0], kc, km);
-        put(S.ring[st][1], vc, vm);
+        if (nk >= kRing && !wait(&S.k_empty[nk % kRing], nk / kRing - 1)) break;
+        const uint32_t bits = __ballot_sync(0xffffffffu, ok || tile * kTile + key >= p.n_int);
+        if (lane == 0) S.mask[nk % 4][key >> 5] = bits;
+        put(S.k[nk % kRing], kc, km);
         tc05::fence_proxy_async();
-        tc05::bar_arrive(&S.kv_full[st]);
+        tc05::bar_arrive(&S.k_full[nk % kRing]);
+        if (nv >= kRing && !wait(&S.v_empty[nv % kRing], nv / kRing - 1)) break;
+        put(S.v[nv % kRing], vc, vm);
+        tc05::fence_proxy_async();
+        tc05::bar_arrive(&S.v_full[nv % kRing]);
       }
       if (dead) break;
-      for (int t = nint > 0 ? -1 : 0; t < nother; ++t, ++step) {  // -1: R_v^T
-        const int st = step % kRing;
-        if (!wait(&S.kv_tma[st], tma[st]++)) break;
-        if (t >= 0) {
-          const int tile = p.t0 + nint + t - p.I;
-          const int n = tile < p.Wt ? p.s.n_win - kTile * tile : p.s.n_new - kTile * (tile - p.Wt);
-          const bool ok = key < n;
-          const uint32_t bits = __ballot_sync(0xffffffffu, ok);
-          if (lane == 0) S.mask[st][key >> 5] = bits;
-          if (!ok) {
-            uint8_t* r = S.ring[st][1] + key * 128;
+      nk += nother;
+      for (int t = nint > 0 ? -1 : 0; t < nother; ++t, ++nv) {  // -1: R_v^T
+        const int st = nv % kRing;
+        if (!wait(&S.v_tma[st], tma[st]++)) break;
+        const int tile = p.t0 + nint + t - p.I;
+        const int n = tile < p.Wt ? p.n_win - kTile * tile : p.n_new - kTile * (tile - p.Wt);
+        if (t >= 0 && n < kTile) {
+          if (key >= n) {
+            uint8_t* r = S.v[st] + key * 128;
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
               *reinterpret_cast<uint4*>(r + 16 * c) = make_uint4(0u, 0u, 0u, 0u);
@@ -571,152 +601,182 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
           }
           tc05::fence_proxy_async();
         }
-        tc05::bar_arrive(&S.kv_full[st]);
+        tc05::bar_arrive(&S.v_full[st]);
       }
     }
     cp_async_wait<0>();
-  } else if (warp == kTmaWarp) {
+  } else if (warp == kTmaWarp || warp == kTmaWarp + 1) {
     // ------------------------------------------------------------ TMA
+    // one warp for the queries and keys, one for the values and R_v^T.  Every
+    // phase of a tile's `empty` is waited for, those of dequantized tiles too:
+    // a wait tells a phase from the next, not from the next but one.
+    const bool values = warp != kTmaWarp;
+    uint64_t* const empty = values ? S.v_empty : S.k_empty;
+    uint64_t* const full = values ? S.v_tma : S.k_tma;
     uint32_t step = 0, nq = 0, pending[kRing] = {0, 0};
-    if (lane == 0) {
-      bool dead = false;
-      auto load_q = [&](const CUtensorMap* map, const Piece& p) {
-        if (nq > 0 && !tc05::bar_wait_spin(&S.q_empty, (nq - 1) & 1, abort)) {
-          dead = true;
-          return;
-        }
-        const int tiles = p.s.n_new - p.qb * kQTok > 32 ? 2 : 1;
+    bool dead = false;
+    auto wait = [&](uint64_t* bar, uint32_t phase) {
+      if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
+      return !dead;
+    };
+    auto load_q = [&](const CUtensorMap* map, const Piece& p) {
+      if (values || dead || (nq > 0 && !wait(&S.q_empty, nq - 1))) return;
+      if (lane == 0) {
+        const int tiles = p.q_tiles();
         tc05::bar_arrive_expect_tx(&S.q_full, tiles * kOperand);
         for (int g = 0; g < tiles; ++g)
           for (int c = 0; c < 2; ++c)
             tc05::tma_load_3d(S.q[g] + c * kHalf, map, 64 * c, 4 * p.h,
-                              p.s.c0 + p.qb * kQTok + 32 * g, &S.q_full);
-        ++nq;
-      };
-      for (long long f = f0; f < f1 && !dead;) {
-        const Piece p = locate_piece(A, pref, f, f1);
-        f += p.t1 - p.t0;
-        const int nint = max(0, min(p.t1, p.I) - p.t0), nother = p.t1 - p.t0 - nint;
-        if (nint > 0) {
-          load_q(&tm_qrot, p);
-          // every phase of kv_empty is waited for, those of the other warps'
-          // tiles too: a wait for a phase tells it from the next but one only
-          for (int t = 0; t < nint && !dead; ++t, ++step)
-            if (step >= kRing &&
-                !tc05::bar_wait_spin(&S.kv_empty[step % kRing], (step / kRing - 1) & 1, abort))
-              dead = true;
-        }
-        for (int t = nint > 0 ? -1 : 0; t < nother && !dead; ++t, ++step) {
-          const int st = step % kRing;
-          if (t == 0) load_q(&tm_q, p);
-          if (dead || (step >= kRing && !tc05::bar_wait_spin(&S.kv_empty[st], (step / kRing - 1) & 1, abort))) {
-            dead = true;
-            break;
-          }
-          if (t < 0) {  // 64 R_v^T, fp16
-            tc05::bar_arrive_expect_tx(&S.kv_tma[st], kOperand);
-            tc05::bulk_g2s(S.ring[st][0], A.Rv_back + (size_t)p.h * kRT5Halves, kOperand, &S.kv_tma[st]);
-          } else {
-            const int tile = p.t0 + nint + t - p.I;
-            tc05::bar_arrive_expect_tx(&S.kv_tma[st], 2 * kOperand);
-            for (int kind = 0; kind < 2; ++kind)
-              for (int c = 0; c < 2; ++c) {
-                uint8_t* dst = S.ring[st][kind] + c * kHalf;
-                if (tile < p.Wt)
-                  tc05::tma_load_3d(dst, &tm_win, 64 * c, 0,
-                                    ((p.s.slot * A.h_kv + p.h) * 2 + kind) * (A.sink + A.recent) +
-                                        kTile * tile, &S.kv_tma[st]);
-                else
-                  tc05::tma_load_3d(dst, kind ? &tm_v : &tm_k, 64 * c, p.h,
-                                    p.s.c0 + kTile * (tile - p.Wt), &S.kv_tma[st]);
-              }
+                              p.c0 + p.qb * kQTok + 32 * g, &S.q_full);
+      }
+      ++nq;
+    };
+    auto free_slot = [&]() {
+      return !dead && (step < kRing || wait(&empty[step % kRing], step / kRing - 1));
+    };
+    Piece p;
+    for (uint32_t n = 0; !dead && next_piece(n, p); ++n) {
+      const int nint = p.int_tiles(), nother = p.t1 - p.t0 - nint;
+      if (nint > 0) {
+        load_q(&tm_qrot, p);
+        for (int t = 0; t < nint && free_slot(); ++t) ++step;
+        if (values && free_slot()) {  // 64 R_v^T, fp16
+          const int st = step++ % kRing;
+          if (lane == 0) {
+            tc05::bar_arrive_expect_tx(&full[st], kOperand);
+            tc05::bulk_g2s(S.v[st], A.Rv_back + (size_t)p.h * kRT5Halves, kOperand, &full[st]);
           }
           ++pending[st];
         }
       }
-      // copies in flight land before the CTA exits (after an abort nobody else
-      // waits for them)
-      for (int s = 0; s < kRing; ++s)
-        if (pending[s]) tc05::bar_wait_drain(&S.kv_tma[s], (pending[s] - 1) & 1);
-      if (nq) tc05::bar_wait_drain(&S.q_full, (nq - 1) & 1);
+      for (int t = 0; t < nother && free_slot(); ++t) {
+        const int st = step++ % kRing, tile = p.t0 + nint + t - p.I;
+        if (lane == 0) {
+          tc05::bar_arrive_expect_tx(&full[st], kOperand);
+          for (int c = 0; c < 2; ++c) {
+            uint8_t* dst = (values ? S.v[st] : S.k[st]) + c * kHalf;
+            if (tile < p.Wt)
+              tc05::tma_load_3d(dst, &tm_win, 64 * c, 0,
+                                ((p.slot * A.h_kv + p.h) * 2 + values) * (A.sink + A.recent) +
+                                    kTile * tile, &full[st]);
+            else
+              tc05::tma_load_3d(dst, values ? &tm_v : &tm_k, 64 * c, p.h,
+                                p.c0 + kTile * (tile - p.Wt), &full[st]);
+          }
+        }
+        __syncwarp();
+        ++pending[st];
+        if (t == 0) load_q(&tm_q, p);
+      }
     }
+    // copies in flight land before the CTA exits (after an abort nobody else
+    // waits for them)
+    for (int s = 0; s < kRing; ++s)
+      if (pending[s]) tc05::bar_wait_drain(&full[s], (pending[s] - 1) & 1);
+    if (nq) tc05::bar_wait_drain(&S.q_full, (nq - 1) & 1);
     __syncwarp();
+  } else if (warp == kPlanWarp) {
+    // ---------------------------------------------------------- pieces
+    const long long F = __ldcg(A.pref + A.B) * A.h_kv;
+    long long f = F * w / A.W, f_seg;
+    const long long f1 = F * (w + 1) / A.W;
+    bool more = true;
+    for (uint32_t n = 0; more; ++n) {
+      const uint32_t i = n % kPieces;
+      Piece p;
+      p.t0 = p.t1 = 0;
+      while (f < f1 && p.t1 == p.t0) f = locate_piece(A, f, f1, p, &f_seg);
+      more = p.t1 > p.t0;
+      if (n >= kPieces && !__all_sync(0xffffffffu, tc05::bar_wait_spin(&S.piece_empty[i],
+                                                                       (n / kPieces - 1) & 1, abort)))
+        break;
+      if (lane == 0) {
+        S.piece[i] = p;
+        tc05::bar_arrive(&S.piece_full[i]);
+      }
+      __syncwarp();
+    }
   } else {
     // ------------------------------------------------------------ MMA
-    if (warp == kMmaWarp && lane == 0) {
+    if (warp == kMmaWarp) {
       constexpr uint32_t kId = tc05::idesc_f16(128, 128);
-      const uint32_t sq = tc05::smem_addr(S.q[0]), sr = tc05::smem_addr(S.ring[0][0]);
-      uint32_t step = 0, nq = 0, np[2] = {0, 0};
+      const uint32_t sq = tc05::smem_addr(S.q[0]), sk = tc05::smem_addr(S.k[0]),
+                     sv = tc05::smem_addr(S.v[0]);
+      uint32_t nk = 0, nv = 0, nq = 0, np[2] = {0, 0}, kd[kRing] = {0, 0}, kt[kRing] = {0, 0};
       bool dead = false, used = false;
       auto wait = [&](uint64_t* bar, uint32_t phase) {
-        if (!tc05::bar_wait_spin(bar, phase & 1, abort)) dead = true;
+        if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
         tc05::fence_after();
         return !dead;
       };
-      auto qk = [&](int g, uint32_t st, uint32_t type) {
-        const uint32_t a = sq + g * kOperand, b = sr + st * 2 * kOperand;
+      auto wait_k = [&](int phase) {  // keys of tile nk, dequantized or by TMA
+        const uint32_t st = nk % kRing;
+        return phase ? wait(&S.k_tma[st], kt[st]++) : wait(&S.k_full[st], kd[st]++);
+      };
+      auto qk = [&](int g, uint32_t type) {
+        const uint32_t a = sq + g * kOperand, b = sk + nk % kRing * kOperand;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
           const uint32_t o = (ks >> 2) * kHalf + (ks & 3) * 32;
-          tc05::mma_ss(tmem + kColS + 128u * g, tc05::smem_desc_sw128(a + o, 16),
+          tc05::mma_ss_warp(tmem + kColS + 128u * g, tc05::smem_desc_sw128(a + o, 16),
                        tc05::smem_desc_sw128(b + o, 16), kId | type, ks != 0);
         }
-        tc05::mma_commit(&S.s_full[g]);
+        tc05::mma_commit_warp(&S.s_full[g]);
       };
-      auto pv = [&](int g, uint32_t st, uint32_t type, bool add) {
-        const uint32_t b = sr + (st * 2 + 1) * kOperand;
+      auto pv = [&](int g, uint32_t type, bool add) {
+        const uint32_t b = sv + nv % kRing * kOperand;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks)
-          tc05::mma_ts(tmem + kColO + 128u * g, tmem + kColS + 128u * g + 8u * ks,
+          tc05::mma_ts_warp(tmem + kColO + 128u * g, tmem + kColS + 128u * g + 8u * ks,
                        tc05::smem_desc_sw128(b + ks * 2048, kHalf),
                        kId | type | tc05::kIdescMajorMnB, add || ks != 0);
       };
-      for (long long f = f0; f < f1 && !dead;) {
-        const Piece p = locate_piece(A, pref, f, f1);
-        f += p.t1 - p.t0;
-        const int nint = max(0, min(p.t1, p.I) - p.t0), nother = p.t1 - p.t0 - nint;
-        const int G = p.s.n_new - p.qb * kQTok > 32 ? 2 : 1;
+      Piece p;
+      for (uint32_t n = 0; !dead && next_piece(n, p); ++n) {
+        const int nint = p.int_tiles(), nother = p.t1 - p.t0 - nint;
+        const int G = p.q_tiles();
         bool add = false;
         for (int phase = 0; phase < 2 && !dead; ++phase) {
           const int n = phase ? nother : nint;
           const uint32_t type = phase ? tc05::kIdescBf16 : 0u;
           if (n == 0) continue;
           used = true;
-          if (!wait(&S.q_full, nq++)) break;
-          if (!wait(&S.kv_full[step % kRing], step / kRing)) break;
-          for (int g = 0; g < G; ++g) qk(g, step % kRing, type);
-          if (n == 1) tc05::mma_commit(&S.q_empty);
-          for (int t = 0; t < n && !dead; ++t, ++step) {
+          if (!wait(&S.q_full, nq++) || !wait_k(phase)) break;
+          for (int g = 0; g < G; ++g) qk(g, type);
+          tc05::mma_commit_warp(&S.k_empty[nk++ % kRing]);
+          if (n == 1) tc05::mma_commit_warp(&S.q_empty);
+          for (int t = 0; t < n && !dead; ++t, ++nv) {
             for (int g = 0; g < G; ++g) {
+              if (g == 0 && !wait(&S.v_full[nv % kRing], nv / kRing)) break;
               if (!wait(&S.p_ready[g], np[g]++)) break;
-              pv(g, step % kRing, type, add);
-              if (t == n - 1) tc05::mma_commit(&S.o_full[g]);
-              if (g == G - 1) tc05::mma_commit(&S.kv_empty[step % kRing]);
+              pv(g, type, add);
+              if (t == n - 1) tc05::mma_commit_warp(&S.o_full[g]);
+              if (g == G - 1) tc05::mma_commit_warp(&S.v_empty[nv % kRing]);
               if (t + 1 < n) {
-                if (g == 0 && !wait(&S.kv_full[(step + 1) % kRing], (step + 1) / kRing)) break;
-                qk(g, (step + 1) % kRing, type);
+                if (g == 0 && !wait_k(phase)) break;
+                qk(g, type);
               }
             }
-            if (t + 2 == n) tc05::mma_commit(&S.q_empty);
+            if (t + 1 < n) tc05::mma_commit_warp(&S.k_empty[nk++ % kRing]);
+            if (t + 2 == n) tc05::mma_commit_warp(&S.q_empty);
             add = true;
           }
           if (dead || phase) continue;
-          if (!wait(&S.kv_full[step % kRing], step / kRing)) break;
+          if (!wait(&S.v_full[nv % kRing], nv / kRing)) break;
           for (int g = 0; g < G; ++g) {
             if (!wait(&S.p_ready[g], np[g]++)) break;
-            const uint32_t b = sr + (step % kRing) * 2 * kOperand;
+            const uint32_t b = sv + nv % kRing * kOperand;
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks)
-              tc05::mma_ts(tmem + kColO + 128u * g, tmem + kColS + 128u * g + 8u * ks,
+              tc05::mma_ts_warp(tmem + kColO + 128u * g, tmem + kColS + 128u * g + 8u * ks,
                            tc05::smem_desc(b + ks * 256, 128, 2048), kId, ks != 0);
-            if (nother == 0) tc05::mma_commit(&S.o_full[g]);
+            if (nother == 0) tc05::mma_commit_warp(&S.o_full[g]);
           }
-          tc05::mma_commit(&S.kv_empty[step % kRing]);
-          ++step;
+          tc05::mma_commit_warp(&S.v_empty[nv++ % kRing]);
         }
       }
       if (used) {  // the tensor core is done with tensor memory before it is freed
-        tc05::mma_commit(&S.drained);
+        tc05::mma_commit_warp(&S.drained);
         tc05::bar_wait_drain(&S.drained, 0);
       }
     }
@@ -741,17 +801,18 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
 __global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
   pdl_wait();
   pdl_trigger();
-  auto pref = [&](int b) { return __ldcg(A.pref + b); };
-  const long long F = pref(A.B) * A.h_kv;
+  const long long F = __ldcg(A.pref + A.B) * A.h_kv;
   const int w = blockIdx.x, tid = threadIdx.x;
   const long long f0 = F * w / A.W, f1 = F * (w + 1) / A.W;
   if (f0 == f1 || f1 == F) return;
-  const Piece p = locate_piece(A, pref, f1, f1 + 1);
-  if (p.t0 == 0 || p.f_seg < f0) return;
+  Piece p;
+  long long f_seg;
+  locate_piece(A, f1, f1 + 1, p, &f_seg);
+  const long long first = f_seg + kBegin, end = first + p.total;  // units of its tiles
+  if (f1 <= first || first < f0) return;
   const int r = 8 * blockIdx.y + (tid & 7), cg = tid >> 3;
   const int i = p.qb * kQTok + r / 4;
-  if (r >= A.rows || i >= p.s.n_new) return;
-  const long long end = p.f_seg + p.total;
+  if (r >= A.rows || i >= p.n_new) return;
   float M = -INFINITY, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int x = w; x < A.W; ++x) {
@@ -768,7 +829,7 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
     o = make_float4(o.x * u + y.x * v, o.y * u + y.y * v, o.z * u + y.z * v, o.w * u + y.w * v);
   }
   const float inv = L > 0.f ? 1.f / L : 0.f;
-  const size_t at = ((size_t)p.s.c0 + i) * 4 * A.h_kv + 4 * p.h + r % 4;
+  const size_t at = ((size_t)p.c0 + i) * 4 * A.h_kv + 4 * p.h + r % 4;
   *reinterpret_cast<uint2*>(A.out + at * kD + 4 * cg) =
       make_uint2(pack16<true>(o.x * inv, o.y * inv), pack16<true>(o.z * inv, o.w * inv));
 }
@@ -835,7 +896,7 @@ extern "C" optr_status optr_chunk_attention_win(
                     pool, num_pages, w, p->cfg.sink, p->cfg.recent, h_kv, p->cfg.group == 4 * kG,
                     p->Rk_frag, p->Rv_back, p->mu, (__nv_bfloat16*)out, p->err,
                     (long long*)(ws + l.pref), (__half*)(ws + l.qrot), (float2*)(ws + l.qinfo),
-                    (float*)(ws + l.part), l.rows, l.W};
+                    (float*)(ws + l.part), l.rows, l.W, aligned(out, 32)};
   cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(chunk_kernel), sizeof(Smem));
   if (e != cudaSuccess) return OPTR_ERR_CUDA;
   CUtensorMap mq, mr, mk, mv, mw;

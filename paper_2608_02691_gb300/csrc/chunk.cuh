@@ -24,12 +24,13 @@ struct ChunkArgs {
   __nv_bfloat16* out;
   unsigned* err;
   // workspace
-  long long* pref;       // [B + 1] tiles of the sequences before b, one head
+  long long* pref;       // [B + 1] cost of the sequences before b, one head
   __half* qrot;          // [n_tok][h_q][128] rotated queries, scaled, order of dequant.cuh
   float2* qinfo;         // [n_tok][h_q] logit scale of a rotated query; <q, mu>
   float* part;           // partial results, ChunkPart
   int rows;              // rows of a partial
   int W;                 // CTAs of the attention kernel
+  bool out32;            // out is 32-byte aligned
 };
 
 constexpr int kQTok = 64;     // tokens of a query block: two tiles of 32 x 4 heads
@@ -69,53 +70,65 @@ __device__ __forceinline__ SeqWork seq_work(const ChunkArgs& A, int b) {
 
 __device__ __forceinline__ int tiles_of(int keys) { return (keys + kTile - 1) / kTile; }
 
-// Tiles of the first m query blocks of a sequence (one head), `past` cached
-// tiles each: block qb sees own tiles 0 .. qb / 2.
-__device__ __forceinline__ long long block_tiles(long long m, int past) {
-  return m * past + (m + 1) * (m + 1) / 4;
+// Cost of the first m query blocks of a sequence (one head), in tiles, `past`
+// cached tiles each: block qb sees own tiles 0 .. qb / 2, and kBegin tiles' time
+// goes into its start and end.
+constexpr int kBegin = 2;
+__device__ __forceinline__ long long block_cost(long long m, int past) {
+  return m * (past + kBegin) + (m + 1) * (m + 1) / 4;
 }
 
 // A run of tiles of one (sequence, KV head, query block): tiles t0 .. t1-1 of
 // its `total`, INT2 tiles first, then the windows', then the chunk's own.
 struct Piece {
-  SeqWork s;
   int b, h, qb;
-  int t0, t1, total;
+  int c0, n_new, n_int, n_win, slot;
   int I, Wt;         // INT2 and window tiles of the segment
-  long long f_seg;   // flat index of the segment's first tile
+  int t0, t1, total;
+  __device__ __forceinline__ int int_tiles() const { return max(0, min(t1, I) - t0); }
+  // query tiles that have rows
+  __device__ __forceinline__ int q_tiles() const { return n_new - qb * kQTok > kQTok / 2 ? 2 : 1; }
 };
 
-// The flat index space orders tiles as (sequence, KV head, query block, tile);
-// CTA w takes [w F / W, (w + 1) F / W).  The piece that starts at f.
-template <typename Pref>
-__device__ __forceinline__ Piece locate_piece(const ChunkArgs& A, Pref pref, long long f,
-                                              long long f1) {
-  Piece p;
+// The flat index space orders units of cost as (sequence, KV head, query block,
+// unit); CTA w takes [w F / W, (w + 1) F / W).  Of a block's kBegin + tiles units
+// the first kBegin stand for no tile.  Called by a whole warp: the piece that
+// starts at f < F of a range that ends at f1, in all lanes; *f_seg receives the
+// flat index of the segment's first unit, the return value is the next piece's
+// start.  The piece has no tile (t1 = t0) where the range ends within kBegin.
+__device__ __forceinline__ long long locate_piece(const ChunkArgs& A, long long f, long long f1,
+                                                  Piece& p, long long* f_seg) {
+  const int lane = threadIdx.x & 31;
+  // the last sequence b with pref[b] h_kv <= f, 32 probes at a time
   int lo = 0, hi = A.B;
   while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (pref(mid) * A.h_kv <= f) lo = mid; else hi = mid;
+    const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+    const bool le = at < hi && __ldcg(A.pref + at) * A.h_kv <= f;
+    lo += (__popc(__ballot_sync(0xffffffffu, le)) - 1) * step;
+    hi = min(hi, lo + step);
   }
-  p.b = lo;
-  const long long base = pref(lo), cost = pref(lo + 1) - base;
+  const long long base = __ldcg(A.pref + lo), cost = __ldcg(A.pref + lo + 1) - base;
+  const SeqWork s = seq_work(A, lo);
   long long r = f - base * A.h_kv;
+  p.b = lo;
   p.h = (int)(r / cost);
   r -= p.h * cost;
-  p.s = seq_work(A, lo);
-  p.I = tiles_of(p.s.n_int);
-  p.Wt = tiles_of(p.s.n_win);
-  int q0 = 0, q1 = (p.s.n_new + kQTok - 1) / kQTok;
+  p.c0 = s.c0, p.n_new = s.n_new, p.n_int = s.n_int, p.n_win = s.n_win, p.slot = s.slot;
+  p.I = tiles_of(s.n_int);
+  p.Wt = tiles_of(s.n_win);
+  int q0 = 0, q1 = (s.n_new + kQTok - 1) / kQTok;
   while (q1 - q0 > 1) {
     const int mid = (q0 + q1) >> 1;
-    if (block_tiles(mid, p.I + p.Wt) <= r) q0 = mid; else q1 = mid;
+    if (block_cost(mid, p.I + p.Wt) <= r) q0 = mid; else q1 = mid;
   }
   p.qb = q0;
-  const long long t0 = r - block_tiles(q0, p.I + p.Wt);
-  p.t0 = (int)t0;
   p.total = p.I + p.Wt + q0 / 2 + 1;
-  p.t1 = (int)min((long long)p.total, t0 + (f1 - f));
-  p.f_seg = f - t0;
-  return p;
+  const long long u0 = r - block_cost(q0, p.I + p.Wt);
+  const long long u1 = min((long long)p.total + kBegin, u0 + (f1 - f));
+  p.t0 = (int)max(0ll, u0 - kBegin);
+  p.t1 = (int)max(0ll, u1 - kBegin);
+  *f_seg = f - u0;
+  return f + (u1 - u0);
 }
 
 // A partial: O [32 channel groups][rows][4], then m [rows] and l [rows].
