@@ -1,9 +1,8 @@
 // Attention of a chunk of new tokens over the paged INT2 cache
 // (include/optr.h, "optr_chunk_attention").
 //
-// Three launches.  chunk_prologue_kernel rotates the queries and lays out the
-// work; chunk_kernel attends; chunk_combine_kernel joins the segments that more
-// than one CTA worked on.
+// Two launches: chunk_kernel attends, chunk_combine_kernel joins the segments
+// that more than one CTA worked on.
 //
 // Work.  A query block is 64 new tokens of one sequence with the 4 query heads
 // of one KV head: 256 rows, two tensor-core tiles of 32 tokens x 4 heads.  It
@@ -32,154 +31,6 @@
 
 namespace optr {
 namespace {
-
-// ------------------------------------------------------------ prologue
-
-constexpr int kProThreads = 256;
-
-__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0,
-                                         uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 "
-      "{%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-__device__ __forceinline__ float bf_lo(uint32_t x) { return __uint_as_float(x << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
-
-// The plan (one CTA): the cost of one head of the sequences before b, for all b.
-__device__ void chunk_plan(const ChunkArgs& A) {
-  __shared__ long long warp_sum[kProThreads / 32];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  long long carry = 0;
-  if (tid == 0) A.pref[0] = 0;
-  for (int b0 = 0; b0 < A.B; b0 += kProThreads) {
-    const int b = b0 + tid;
-    long long x = 0;
-    if (b < A.B) {
-      const SeqWork s = seq_work(A, b);
-      unsigned bad = s.bad;
-      if (!bad && A.win.win && (s.slot < 0 || s.slot >= A.win.n_slots)) bad = OPTR_DEVERR_WIN_SLOT;
-      if (bad) atomicOr(A.err, bad);
-      if (s.n_new > 0)
-        x = block_cost((s.n_new + kQTok - 1) / kQTok, tiles_of(s.n_int) + tiles_of(s.n_win));
-    }
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    if (lane == 31) warp_sum[warp] = x;
-    __syncthreads();
-    for (int w = 0; w < kProThreads / 32; ++w) {
-      if (w < warp) x += warp_sum[w];
-    }
-    x += carry;
-    if (b < A.B) A.pref[b + 1] = x;
-    for (int w = 0; w < kProThreads / 32; ++w) carry += warp_sum[w];
-    __syncthreads();
-  }
-}
-
-// CTA 0 plans; the others rotate the queries of `per` tokens (a multiple of 4)
-// and one KV head: warp w makes 16 of the 128 columns, 16 rows (4 tokens) at a
-// time, mma.sync on bf16 q and R_k as bf16 hi + lo.  q R_k is stored as fp16
-// over the power of two 2^E > sqrt(128) max |q| >= |q R_k| of its row.
-__global__ void __launch_bounds__(kProThreads) chunk_prologue_kernel(const ChunkArgs A, int per) {
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if (blockIdx.x == 0) {
-    pdl_wait();
-    pdl_trigger();
-    chunk_plan(A);
-    return;
-  }
-  const int h = (blockIdx.x - 1) % A.h_kv, h_q = 4 * A.h_kv;
-  const int t0 = (blockIdx.x - 1) / A.h_kv * per, t1 = min(A.n_tok, t0 + per);
-  uint4 bf[8][2];
-#pragma unroll
-  for (int ks = 0; ks < 8; ++ks)
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-      bf[ks][nt] = __ldg(A.Rk_frag + (((size_t)h * 8 + warp) * 16 + 2 * ks + nt) * 32 + lane);
-  pdl_wait();
-  pdl_trigger();
-  for (int t = t0; t < t1; t += 4) {
-    // tokens t .. t + 3: outside every sequence (zero rows), or of one that
-    // has INT2 positions
-    bool need = false;
-    if (lane < 4 && t + lane < t1) {
-      const int b = find_seq(A.cu, A.B, t + lane);
-      const SeqWork s = seq_work(A, b);
-      const bool in = !s.bad && s.c0 <= t + lane && t + lane < s.c0 + s.n_new;
-      need = in && s.n_int > 0;
-      if (!in && warp == 0) {
-        if (!s.bad) atomicOr(A.err, OPTR_DEVERR_CU_NEW);
-        uint4* o = reinterpret_cast<uint4*>(A.out + ((size_t)(t + lane) * h_q + 4 * h) * kD);
-        for (int i = 0; i < 4 * kD / 8; ++i) o[i] = make_uint4(0u, 0u, 0u, 0u);
-      }
-    }
-    if (!__any_sync(0xffffffffu, need)) continue;
-    // rows g and g + 8 of the tile: token row / 4, head row % 4
-    const int g = lane >> 2, c = 2 * (lane & 3);
-    const uint32_t* row[2];
-    bool ok[2];
-    size_t at[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = g + 8 * i;
-      ok[i] = t + r / 4 < t1;
-      at[i] = (size_t)(t + r / 4) * h_q + 4 * h + r % 4;
-      row[i] = reinterpret_cast<const uint32_t*>(A.q + at[i] * kD + c);
-    }
-    uint32_t a[8][4];
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        a[ks][j] = ok[j & 1] ? __ldcg(row[j & 1] + 8 * ks + 4 * (j >> 1)) : 0u;
-    float amax[2] = {0.f, 0.f}, qmu[2] = {0.f, 0.f};
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float x = bf_lo(a[ks][j]), y = bf_hi(a[ks][j]);
-        amax[j & 1] = fmaxf(amax[j & 1], fmaxf(fabsf(x), fabsf(y)));
-        if (warp == 0) {
-          const float2 m = __ldg(reinterpret_cast<const float2*>(A.mu + h * kD + 16 * ks +
-                                                                 8 * (j >> 1) + c));
-          qmu[j & 1] = fmaf(x, m.x, fmaf(y, m.y, qmu[j & 1]));
-        }
-      }
-    float d[2][4] = {};
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks)
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
-        mma_bf16(d[nt], a[ks], bf[ks][nt].x, bf[ks][nt].y);
-        mma_bf16(d[nt], a[ks], bf[ks][nt].z, bf[ks][nt].w);
-      }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-#pragma unroll
-      for (int o = 1; o < 4; o <<= 1) {
-        amax[i] = fmaxf(amax[i], __shfl_xor_sync(0xffffffffu, amax[i], o));
-        qmu[i] += __shfl_xor_sync(0xffffffffu, qmu[i], o);
-      }
-      // 2^E, E = exponent(amax) + 5 within float's range
-      const int E = min(max((int)(__float_as_uint(amax[i]) >> 23) - 127 + 5, -120), 120);
-      const float up = __uint_as_float((uint32_t)(127 + E) << 23);
-      const float down = __uint_as_float((uint32_t)(127 - E) << 23);
-      if (!ok[i]) continue;
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
-        *reinterpret_cast<__half2*>(A.qrot + at[i] * kD + 8 * (2 * warp + nt) + c) =
-            __floats2half2_rn(d[nt][2 * i] * down, d[nt][2 * i + 1] * down);
-      if (warp == 0 && (lane & 3) == 0) A.qinfo[at[i]] = make_float2(up * kLogit, qmu[i] * kLogit);
-    }
-  }
-}
 
 // ----------------------------------------------------------- attention
 
@@ -213,7 +64,7 @@ struct Smem {
   uint64_t k_full[kRing], k_tma[kRing], k_empty[kRing];
   uint64_t v_full[kRing], v_tma[kRing], v_empty[kRing];
   uint64_t piece_full[kPieces], piece_empty[kPieces];
-  uint64_t s_full[2], p_ready[2], o_full[2], q_full, q_empty, drained;
+  uint64_t s_full[2], p_ready[2], o_full[2], q_ready[2], q_full, q_empty, drained;
   uint32_t tmem;
   int abort;
 };
@@ -317,8 +168,42 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, float sca
   tc05::tmem_wait_st();
 }
 
+// One row of the rotated queries (128 columns of tensor memory at tS) as the
+// INT2 tiles' query operand: fp16 over a power of two >= its largest value, so
+// that no query leaves fp16's range.  The logit of an INT2 key is then
+// S scale - off, in the units of the other keys' <q, k>: -off carries <q, mu>,
+// which centering took from the keys.
+__device__ __forceinline__ void rotated_query(uint32_t tS, uint8_t* q, int row, const float* muR,
+                                              float& scale, float& off) {
+  uint32_t s[kD];
+  auto chunk = [&](int c) -> uint32_t (&)[32] { return reinterpret_cast<uint32_t(&)[32]>(s[32 * c]); };
+#pragma unroll
+  for (int c = 0; c < 4; ++c) tc05::tmem_ld32(tS + 32 * c, chunk(c));
+  tc05::tmem_wait_ld();
+  float top = 0.f, dot[2] = {0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < kD; ++k) {
+    top = fmaxf(top, fabsf(__uint_as_float(s[k])));
+    dot[k & 1] = fmaf(__uint_as_float(s[k]), __ldg(muR + row_channel(k)), dot[k & 1]);
+  }
+  const int E = min(max((int)(__float_as_uint(top) >> 23) - 126, -120), 120);
+  const float down = __uint_as_float((uint32_t)(127 - E) << 23);
+  scale = __uint_as_float((uint32_t)(127 + E) << 23) * kLogit;
+  off = -(dot[0] + dot[1]) * kLogit;
+#pragma unroll
+  for (int c = 0; c < 16; ++c) {
+    uint32_t y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      y[e] = pack16<false>(__uint_as_float(s[8 * c + 2 * e]) * down,
+                           __uint_as_float(s[8 * c + 2 * e + 1]) * down);
+    *reinterpret_cast<uint4*>(q + (c >> 3) * kHalf + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
+        make_uint4(y[0], y[1], y[2], y[3]);
+  }
+}
+
 __global__ void __launch_bounds__(kThreads, 1)
-chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_qrot,
+chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
              const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
              const __grid_constant__ CUtensorMap tm_win, const __grid_constant__ ChunkArgs A) {
   extern __shared__ __align__(1024) unsigned char dsm_[];
@@ -342,6 +227,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
       tc05::bar_init(&S.s_full[g], 1);
       tc05::bar_init(&S.p_ready[g], 4);
       tc05::bar_init(&S.o_full[g], 1);
+      tc05::bar_init(&S.q_ready[g], 4);
     }
     tc05::bar_init(&S.q_full, 1);
     tc05::bar_init(&S.q_empty, 1);
@@ -394,6 +280,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
     Piece p;
     for (uint32_t n = 0; !dead && next_piece(n, p); ++n) {
       const int nint = p.int_tiles(), nother = p.t1 - p.t0 - nint;
+      nk += nint > 0;
       const uint32_t base = nk;
       nk += p.t1 - p.t0;
       const int i0 = p.qb * kQTok + 32 * g;  // the tile's first token
@@ -401,17 +288,20 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
       const int i = i0 + (row >> 2), j = row & 3;
       const bool valid = i < p.n_new;
       const size_t at = ((size_t)p.c0 + i) * 4 * A.h_kv + 4 * p.h + j;
-      float scale = kLogit, off = 0.f, m = -1e30f, l = 0.f;
-      if (p.I > 0 && valid) {
-        const float2 x = __ldcg(A.qinfo + at);
-        scale = x.x;
-        off = x.y;
+      float scale = 0.f, off = 0.f, m = -1e30f, l = 0.f;
+      if (nint > 0) {
+        if (!wait(&S.s_full[g], ns++)) break;
+        rotated_query(tS, S.q[g], row, A.muR + p.h * kD, scale, off);
+        tc05::fence_before();
+        tc05::fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) tc05::bar_arrive(&S.q_ready[g]);
       }
       bool fresh = true;
       for (int t = 0; t < nint; ++t) {
         if (!wait(&S.s_full[g], ns++)) break;
         const uint4 mask = *reinterpret_cast<const uint4*>(S.mask[(base + t) % 4]);
-        softmax_tile<false>(tS, tO, scale, 0.f, mask, p.n_int - kTile * (p.t0 + t), fresh, m, l);
+        softmax_tile<false>(tS, tO, scale, off, mask, p.n_int - kTile * (p.t0 + t), fresh, m, l);
         fresh = false;
         ready();
       }
@@ -438,13 +328,12 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
         }
         ready();
       }
-      const float sub = p.I > 0 ? off : 0.f;
       for (int t = 0; t < nother; ++t) {
         if (!wait(&S.s_full[g], ns++)) break;
         // window rows as far as they are filled; own tiles causally
         const int tile = p.t0 + nint + t - p.I;
         const int lim = tile < p.Wt ? p.n_win - kTile * tile : i + 1 - kTile * (tile - p.Wt);
-        softmax_tile<true>(tS, tO, kLogit, sub, make_uint4(~0u, ~0u, ~0u, ~0u), lim, fresh, m, l);
+        softmax_tile<true>(tS, tO, kLogit, 0.f, make_uint4(~0u, ~0u, ~0u, ~0u), lim, fresh, m, l);
         fresh = false;
         ready();
       }
@@ -545,6 +434,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
         page = request(p, p.t0 + 2);
         okn[0] = copy(p, p.t0, e0);
         okn[1] = copy(p, p.t0 + 1, e1);
+        // R_k's parts: one entry of each ring, brought by TMA
+        if (!wait(&S.v_tma[nv % kRing], tma[nv % kRing]++)) break;
+        tc05::bar_arrive(&S.v_full[nv % kRing]);
+        ++nk, ++nv;
       }
       for (int t = 0; t < nint && !dead; ++t, ++nk, ++nv) {
         const int tile = p.t0 + t;
@@ -619,14 +512,14 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
       if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
       return !dead;
     };
-    auto load_q = [&](const CUtensorMap* map, const Piece& p) {
+    auto load_q = [&](const Piece& p) {
       if (values || dead || (nq > 0 && !wait(&S.q_empty, nq - 1))) return;
       if (lane == 0) {
         const int tiles = p.q_tiles();
         tc05::bar_arrive_expect_tx(&S.q_full, tiles * kOperand);
         for (int g = 0; g < tiles; ++g)
           for (int c = 0; c < 2; ++c)
-            tc05::tma_load_3d(S.q[g] + c * kHalf, map, 64 * c, 4 * p.h,
+            tc05::tma_load_3d(S.q[g] + c * kHalf, &tm_q, 64 * c, 4 * p.h,
                               p.c0 + p.qb * kQTok + 32 * g, &S.q_full);
       }
       ++nq;
@@ -634,20 +527,25 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
     auto free_slot = [&]() {
       return !dead && (step < kRing || wait(&empty[step % kRing], step / kRing - 1));
     };
+    auto bring = [&](const uint16_t* operand) {  // a 32 KB operand into the ring
+      if (!free_slot()) return;
+      const int st = step++ % kRing;
+      if (lane == 0) {
+        tc05::bar_arrive_expect_tx(&full[st], kOperand);
+        tc05::bulk_g2s(values ? S.v[st] : S.k[st], operand, kOperand, &full[st]);
+      }
+      __syncwarp();
+      ++pending[st];
+    };
     Piece p;
     for (uint32_t n = 0; !dead && next_piece(n, p); ++n) {
       const int nint = p.int_tiles(), nother = p.t1 - p.t0 - nint;
       if (nint > 0) {
-        load_q(&tm_qrot, p);
+        load_q(p);
+        // hi and lo of R_k
+        bring(A.Rk_query + (size_t)p.h * kRT5Halves + (values ? kD * kD : 0));
         for (int t = 0; t < nint && free_slot(); ++t) ++step;
-        if (values && free_slot()) {  // 64 R_v^T, fp16
-          const int st = step++ % kRing;
-          if (lane == 0) {
-            tc05::bar_arrive_expect_tx(&full[st], kOperand);
-            tc05::bulk_g2s(S.v[st], A.Rv_back + (size_t)p.h * kRT5Halves, kOperand, &full[st]);
-          }
-          ++pending[st];
-        }
+        if (values) bring(A.Rv_back + (size_t)p.h * kRT5Halves);  // hi of 64 R_v^T
       }
       for (int t = 0; t < nother && free_slot(); ++t) {
         const int st = step++ % kRing, tile = p.t0 + nint + t - p.I;
@@ -666,7 +564,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
         }
         __syncwarp();
         ++pending[st];
-        if (t == 0) load_q(&tm_q, p);
+        if (t == 0) load_q(p);
       }
     }
     // copies in flight land before the CTA exits (after an abort nobody else
@@ -677,16 +575,28 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
     __syncwarp();
   } else if (warp == kPlanWarp) {
     // ---------------------------------------------------------- pieces
-    const long long F = __ldcg(A.pref + A.B) * A.h_kv;
-    long long f = F * w / A.W, f_seg;
-    const long long f1 = F * (w + 1) / A.W;
+    if (w == 0) {  // what is wrong with the sequences, once
+      if (lane == 0 && (__ldcg(A.cu) != 0 || __ldcg(A.cu + A.B) != A.n_tok))
+        atomicOr(A.err, OPTR_DEVERR_CU_NEW);
+      for (int b = lane; b < A.B; b += 32) {
+        const SeqWork x = seq_work(A, b);
+        unsigned bad = x.bad;
+        if (!bad && A.win.win && (x.slot < 0 || x.slot >= A.win.n_slots)) bad = OPTR_DEVERR_WIN_SLOT;
+        if (bad) atomicOr(A.err, bad);
+      }
+    }
+    PieceFinder next;
+    next.start(A, w);
+    ChunkSeg seg{};
     bool more = true;
     for (uint32_t n = 0; more; ++n) {
       const uint32_t i = n % kPieces;
       Piece p;
       p.t0 = p.t1 = 0;
-      while (f < f1 && p.t1 == p.t0) f = locate_piece(A, f, f1, p, &f_seg);
+      while (next.f < next.f1 && p.t1 == p.t0) next.next(A, p);
       more = p.t1 > p.t0;
+      if (more && p.t0 == 0 && p.t1 < p.total)
+        seg = ChunkSeg{next.F, next.f_seg + kBegin + p.total, p.c0, p.n_new, p.h, p.qb, 1};
       if (n >= kPieces && !__all_sync(0xffffffffu, tc05::bar_wait_spin(&S.piece_empty[i],
                                                                        (n / kPieces - 1) & 1, abort)))
         break;
@@ -696,13 +606,14 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
       }
       __syncwarp();
     }
+    if (lane == 0) A.seg[w] = seg;
   } else {
     // ------------------------------------------------------------ MMA
     if (warp == kMmaWarp) {
       constexpr uint32_t kId = tc05::idesc_f16(128, 128);
       const uint32_t sq = tc05::smem_addr(S.q[0]), sk = tc05::smem_addr(S.k[0]),
                      sv = tc05::smem_addr(S.v[0]);
-      uint32_t nk = 0, nv = 0, nq = 0, np[2] = {0, 0}, kd[kRing] = {0, 0}, kt[kRing] = {0, 0};
+      uint32_t nk = 0, nv = 0, nq = 0, np[2] = {0, 0}, nr[2] = {0, 0}, kd[kRing] = {0, 0}, kt[kRing] = {0, 0};
       bool dead = false, used = false;
       auto wait = [&](uint64_t* bar, uint32_t phase) {
         if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
@@ -741,8 +652,32 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
           const uint32_t type = phase ? tc05::kIdescBf16 : 0u;
           if (n == 0) continue;
           used = true;
-          if (!wait(&S.q_full, nq++) || !wait_k(phase)) break;
-          for (int g = 0; g < G; ++g) qk(g, type);
+          if (!wait(&S.q_full, nq++)) break;
+          if (!phase) {  // q R_k, bf16 hi + lo, by way of S
+            if (!wait_k(1) || !wait(&S.v_full[nv % kRing], nv / kRing)) break;
+            for (int g = 0; g < G; ++g) {
+              const uint32_t a = sq + g * kOperand;
+#pragma unroll
+              for (int part = 0; part < 2; ++part) {
+                const uint32_t b = part ? sv + nv % kRing * kOperand : sk + nk % kRing * kOperand;
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                  tc05::mma_ss_warp(tmem + kColS + 128u * g,
+                                    tc05::smem_desc_sw128(a + (ks >> 2) * kHalf + (ks & 3) * 32, 16),
+                                    tc05::smem_desc(b + ks * 256, 128, 2048), kId | tc05::kIdescBf16,
+                                    (part | ks) != 0);
+              }
+              tc05::mma_commit_warp(&S.s_full[g]);
+            }
+            tc05::mma_commit_warp(&S.k_empty[nk++ % kRing]);
+            tc05::mma_commit_warp(&S.v_empty[nv++ % kRing]);
+          }
+          if (!wait_k(phase)) break;
+          for (int g = 0; g < G; ++g) {
+            if (!phase && !wait(&S.q_ready[g], nr[g]++)) break;
+            qk(g, type);
+          }
+          if (dead) break;
           tc05::mma_commit_warp(&S.k_empty[nk++ % kRing]);
           if (n == 1) tc05::mma_commit_warp(&S.q_empty);
           for (int t = 0; t < n && !dead; ++t, ++nv) {
@@ -795,41 +730,63 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ C
 // ------------------------------------------------------------- combine
 
 // Joins the partials of the segments that several CTAs of chunk_kernel worked
-// on.  CTA (w, y) takes the segment that spans the end of range w, if its first
-// tile lies in range w, and rows 8 y .. 8 y + 7 of it: thread = 4 channels of a
-// row.
+// on: CTA (w, y) rows 8 y .. 8 y + 7 of the one that CTA w began, thread = 4
+// channels of a row.  The CTAs also clear the rows of sequences that were left
+// out and those of none.
 __global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
+  const int w = blockIdx.x, tid = threadIdx.x;
   pdl_wait();
   pdl_trigger();
-  const long long F = __ldcg(A.pref + A.B) * A.h_kv;
-  const int w = blockIdx.x, tid = threadIdx.x;
-  const long long f0 = F * w / A.W, f1 = F * (w + 1) / A.W;
-  if (f0 == f1 || f1 == F) return;
-  Piece p;
-  long long f_seg;
-  locate_piece(A, f1, f1 + 1, p, &f_seg);
-  const long long first = f_seg + kBegin, end = first + p.total;  // units of its tiles
-  if (f1 <= first || first < f0) return;
+  auto clear = [&](int t0, int t1) {
+    uint4* o = reinterpret_cast<uint4*>(A.out);
+    const size_t n = (size_t)A.h_kv * 4 * kD / 8;
+    if (t1 <= t0) return;
+    for (size_t i = t0 * n + tid; i < t1 * n; i += 256) o[i] = make_uint4(0u, 0u, 0u, 0u);
+  };
+  const int id = w + blockIdx.y * gridDim.x, all = gridDim.x * gridDim.y;
+  for (int b = id; b <= A.B; b += all) {
+    const int c1 = b < A.B ? __ldcg(A.cu + b + 1) : __ldcg(A.cu);
+    if (b == A.B) {
+      clear(0, min(c1, A.n_tok));
+    } else {
+      if (b == A.B - 1) clear(max(c1, 0), A.n_tok);
+      if (seq_work(A, b).bad) clear(max(0, __ldcg(A.cu + b)), min(c1, A.n_tok));
+    }
+  }
+  const ChunkSeg seg = A.seg[w];
   const int r = 8 * blockIdx.y + (tid & 7), cg = tid >> 3;
-  const int i = p.qb * kQTok + r / 4;
-  if (r >= A.rows || i >= p.n_new) return;
+  const int i = seg.qb * kQTok + r / 4;
+  if (!seg.valid || r >= A.rows || i >= seg.n_new) return;
   float M = -INFINITY, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int x = w; x < A.W; ++x) {
-    const long long a = F * x / A.W, b = F * (x + 1) / A.W;
-    if (a >= end) break;
-    if (a == b) continue;
-    const float* part = part_of(A, x, x != w);
-    const float m = __ldcg(part + (size_t)A.rows * kD + r), l = __ldcg(part + (size_t)A.rows * (kD + 1) + r);
-    const float4 y = __ldcg(reinterpret_cast<const float4*>(part) + (size_t)cg * A.rows + r);
-    if (l == 0.f) continue;  // a part whose keys were all left out
-    const float mn = fmaxf(M, m), u = ex2(M - mn), v = ex2(m - mn);
-    M = mn;
-    L = L * u + l * v;
-    o = make_float4(o.x * u + y.x * v, o.y * u + y.y * v, o.z * u + y.z * v, o.w * u + y.w * v);
+  constexpr int kAhead = 4;  // partials requested at a time
+  for (int x0 = w; x0 < A.W && seg.F * x0 / A.W < seg.end; x0 += kAhead) {
+    float m[kAhead], l[kAhead];
+    float4 y[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int x = x0 + k;
+      const long long a = seg.F * x / A.W, b = seg.F * (x + 1) / A.W;
+      l[k] = 0.f;
+      if (x < A.W && a < seg.end && a < b) {
+        const float* part = part_of(A, x, x != w);
+        m[k] = __ldcg(part + (size_t)A.rows * kD + r);
+        l[k] = __ldcg(part + (size_t)A.rows * (kD + 1) + r);
+        y[k] = __ldcg(reinterpret_cast<const float4*>(part) + (size_t)cg * A.rows + r);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (l[k] == 0.f) continue;  // none, or one whose keys were all left out
+      const float mn = fmaxf(M, m[k]), u = ex2(M - mn), v = ex2(m[k] - mn);
+      M = mn;
+      L = L * u + l[k] * v;
+      o = make_float4(o.x * u + y[k].x * v, o.y * u + y[k].y * v, o.z * u + y[k].z * v,
+                      o.w * u + y[k].w * v);
+    }
   }
   const float inv = L > 0.f ? 1.f / L : 0.f;
-  const size_t at = ((size_t)p.c0 + i) * 4 * A.h_kv + 4 * p.h + r % 4;
+  const size_t at = ((size_t)seg.c0 + i) * 4 * A.h_kv + 4 * seg.h + r % 4;
   *reinterpret_cast<uint2*>(A.out + at * kD + 4 * cg) =
       make_uint2(pack16<true>(o.x * inv, o.y * inv), pack16<true>(o.z * inv, o.w * inv));
 }
@@ -838,19 +795,15 @@ size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 
 // Offsets of a call's workspace, bytes.
 struct ChunkLayout {
-  size_t pref, qrot, qinfo, part, total;
+  size_t part, total;
   int rows, W;
 };
 
-ChunkLayout chunk_layout(const optr_params* p, int n_tok, int B, int max_new) {
+ChunkLayout chunk_layout(const optr_params* p, int max_new) {
   ChunkLayout l;
-  const size_t rows = (size_t)n_tok * p->cfg.h_q;
   l.rows = max_new > 32 ? 256 : 128;
   l.W = p->num_sms;
-  l.pref = 0;
-  l.qrot = round_up(sizeof(long long) * ((size_t)B + 1));
-  l.qinfo = l.qrot + round_up(rows * kD * sizeof(__half));
-  l.part = l.qinfo + round_up(rows * sizeof(float2));
+  l.part = round_up(sizeof(ChunkSeg) * (size_t)l.W);
   l.total = l.part + round_up(2 * (size_t)l.W * part_floats(l.rows) * sizeof(float));
   return l;
 }
@@ -862,7 +815,7 @@ using namespace optr;
 
 extern "C" size_t optr_chunk_workspace_size(const optr_params* p, int n_tok, int B, int max_new) {
   if (!p || n_tok < 0 || B <= 0 || max_new <= 0) return 0;
-  return chunk_layout(p, n_tok, B, max_new).total;
+  return chunk_layout(p, max_new).total;
 }
 
 extern "C" optr_status optr_chunk_attention_win(
@@ -889,32 +842,24 @@ extern "C" optr_status optr_chunk_attention_win(
   const int h_kv = p->cfg.h_kv, win_rows = p->cfg.sink + p->cfg.recent;
   // token and window rows are counted with 32 bits
   if ((long long)n_slots * h_kv * 2 * win_rows >= (1LL << 31)) return OPTR_ERR_OUT_OF_RANGE;
-  const ChunkLayout l = chunk_layout(p, n_tok, B, max_new);
+  const ChunkLayout l = chunk_layout(p, max_new);
   if (!workspace || ws_bytes < l.total || !aligned(workspace, 256)) return OPTR_ERR_WORKSPACE;
   char* ws = static_cast<char*>(workspace);
-  const ChunkArgs A{(const __nv_bfloat16*)q, n_tok, cu_new, pos0, max_new, block_table, B, max_pages,
-                    pool, num_pages, w, p->cfg.sink, p->cfg.recent, h_kv, p->cfg.group == 4 * kG,
-                    p->Rk_frag, p->Rv_back, p->mu, (__nv_bfloat16*)out, p->err,
-                    (long long*)(ws + l.pref), (__half*)(ws + l.qrot), (float2*)(ws + l.qinfo),
-                    (float*)(ws + l.part), l.rows, l.W, aligned(out, 32)};
+  const ChunkArgs A{n_tok, cu_new, pos0, max_new, block_table, B, max_pages, pool, num_pages, w,
+                    p->cfg.sink, p->cfg.recent, h_kv, p->cfg.group == 4 * kG, p->Rk_query, p->Rv_back,
+                    p->muR, (__nv_bfloat16*)out, p->err, (ChunkSeg*)ws, (float*)(ws + l.part),
+                    l.rows, l.W, aligned(out, 32)};
   cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(chunk_kernel), sizeof(Smem));
   if (e != cudaSuccess) return OPTR_ERR_CUDA;
-  CUtensorMap mq, mr, mk, mv, mw;
+  CUtensorMap mq, mk, mv, mw;
   if (!token_rows_map(&mq, q, n_tok, 4 * h_kv, 32, 4) ||
-      !token_rows_map(&mr, A.qrot, n_tok, 4 * h_kv, 32, 4) ||
       !token_rows_map(&mk, k, n_tok, h_kv, kTile) || !token_rows_map(&mv, v, n_tok, h_kv, kTile) ||
       !(w.win ? token_rows_map(&mw, w.win, n_slots * h_kv * 2 * win_rows, 1, kTile)
               : token_rows_map(&mw, k, n_tok, h_kv, kTile)))
     return OPTR_ERR_CUDA;
-  // tokens per rotating CTA: about two CTAs per SM, at most 64 tokens each
-  const long long heads = (long long)n_tok * h_kv;
-  const int per = (int)std::min<long long>(64, std::max<long long>(4, heads / (2 * p->num_sms) / 4 * 4));
-  const long long rot = (n_tok + per - 1) / per * (long long)h_kv;
-  e = launch_pdl(chunk_prologue_kernel, dim3((unsigned)(rot + 1)), dim3(kProThreads), 0, stream, A, per);
+  e = launch_pdl(chunk_kernel, dim3(l.W), dim3(kThreads), sizeof(Smem), stream, mq, mk, mv, mw, A);
   if (e == cudaSuccess)
-    e = launch_pdl(chunk_kernel, dim3(l.W), dim3(kThreads), sizeof(Smem), stream, mq, mr, mk, mv, mw, A);
-  if (e == cudaSuccess)
-    e = launch_pdl(chunk_combine_kernel, dim3(l.W - 1, (std::min(l.rows, 4 * max_new) + 7) / 8),
+    e = launch_pdl(chunk_combine_kernel, dim3(l.W, (std::min(l.rows, 4 * max_new) + 7) / 8),
                    dim3(256), 0, stream, A);
   return cuda_status(e);
 }

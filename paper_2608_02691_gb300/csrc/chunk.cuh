@@ -8,7 +8,6 @@
 namespace optr {
 
 struct ChunkArgs {
-  const __nv_bfloat16* q;
   int n_tok;
   const int32_t *cu, *pos0;
   int max_new;
@@ -18,19 +17,24 @@ struct ChunkArgs {
   int num_pages;
   WinArgs win;
   int sink, recent, h_kv, compact;
-  const uint4* Rk_frag;
-  const uint16_t* Rv_back;
-  const float* mu;
+  const uint16_t *Rk_query, *Rv_back;
+  const float* muR;
   __nv_bfloat16* out;
   unsigned* err;
   // workspace
-  long long* pref;       // [B + 1] cost of the sequences before b, one head
-  __half* qrot;          // [n_tok][h_q][128] rotated queries, scaled, order of dequant.cuh
-  float2* qinfo;         // [n_tok][h_q] logit scale of a rotated query; <q, mu>
-  float* part;           // partial results, ChunkPart
+  struct ChunkSeg* seg;  // [W] segments begun by a CTA and ended by another
+  float* part;           // partial results
   int rows;              // rows of a partial
   int W;                 // CTAs of the attention kernel
   bool out32;            // out is 32-byte aligned
+};
+
+// A segment that CTA w begins and another one ends: its pieces are those of the
+// CTAs from w on whose ranges begin before `end`.
+struct ChunkSeg {
+  long long F, end;
+  int c0, n_new, h, qb;
+  int valid;
 };
 
 constexpr int kQTok = 64;     // tokens of a query block: two tiles of 32 x 4 heads
@@ -90,46 +94,89 @@ struct Piece {
   __device__ __forceinline__ int q_tiles() const { return n_new - qb * kQTok > kQTok / 2 ? 2 : 1; }
 };
 
+__device__ __forceinline__ long long seq_cost(const SeqWork& s) {
+  return s.n_new > 0 ? block_cost((s.n_new + kQTok - 1) / kQTok, tiles_of(s.n_int) + tiles_of(s.n_win))
+                     : 0;
+}
+
 // The flat index space orders units of cost as (sequence, KV head, query block,
 // unit); CTA w takes [w F / W, (w + 1) F / W).  Of a block's kBegin + tiles units
-// the first kBegin stand for no tile.  Called by a whole warp: the piece that
-// starts at f < F of a range that ends at f1, in all lanes; *f_seg receives the
-// flat index of the segment's first unit, the return value is the next piece's
-// start.  The piece has no tile (t1 = t0) where the range ends within kBegin.
-__device__ __forceinline__ long long locate_piece(const ChunkArgs& A, long long f, long long f1,
-                                                  Piece& p, long long* f_seg) {
-  const int lane = threadIdx.x & 31;
-  // the last sequence b with pref[b] h_kv <= f, 32 probes at a time
-  int lo = 0, hi = A.B;
-  while (hi - lo > 1) {
-    const int step = (hi - lo + 31) / 32, at = lo + lane * step;
-    const bool le = at < hi && __ldcg(A.pref + at) * A.h_kv <= f;
-    lo += (__popc(__ballot_sync(0xffffffffu, le)) - 1) * step;
-    hi = min(hi, lo + step);
+// the first kBegin stand for no tile.  One warp goes through a CTA's range: lane
+// i holds sequence b0 + i.
+struct PieceFinder {
+  long long f, f1, F;    // the next unit, the range's end, all units
+  long long f_seg;       // first unit of the last piece's segment
+  int b0;                // the 32 sequences held, and what comes before them
+  long long base, incl;  // (cost of one head); incl: up to and with the lane's
+  SeqWork s;
+
+  __device__ __forceinline__ void hold(const ChunkArgs& A, int first) {
+    const int lane = threadIdx.x & 31;
+    b0 = first;
+    s.n_new = 0;
+    if (b0 + lane < A.B) s = seq_work(A, b0 + lane);
+    incl = seq_cost(s);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
   }
-  const long long base = __ldcg(A.pref + lo), cost = __ldcg(A.pref + lo + 1) - base;
-  const SeqWork s = seq_work(A, lo);
-  long long r = f - base * A.h_kv;
-  p.b = lo;
-  p.h = (int)(r / cost);
-  r -= p.h * cost;
-  p.c0 = s.c0, p.n_new = s.n_new, p.n_int = s.n_int, p.n_win = s.n_win, p.slot = s.slot;
-  p.I = tiles_of(s.n_int);
-  p.Wt = tiles_of(s.n_win);
-  int q0 = 0, q1 = (s.n_new + kQTok - 1) / kQTok;
-  while (q1 - q0 > 1) {
-    const int mid = (q0 + q1) >> 1;
-    if (block_cost(mid, p.I + p.Wt) <= r) q0 = mid; else q1 = mid;
+
+  __device__ __forceinline__ void start(const ChunkArgs& A, int w) {
+    const int lane = threadIdx.x & 31;
+    long long sum = 0;
+#pragma unroll 4
+    for (int b = lane; b < A.B; b += 32) sum += seq_cost(seq_work(A, b));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    F = sum * A.h_kv;
+    f = F * w / A.W;
+    f1 = F * (w + 1) / A.W;
+    base = 0;
+    hold(A, 0);
   }
-  p.qb = q0;
-  p.total = p.I + p.Wt + q0 / 2 + 1;
-  const long long u0 = r - block_cost(q0, p.I + p.Wt);
-  const long long u1 = min((long long)p.total + kBegin, u0 + (f1 - f));
-  p.t0 = (int)max(0ll, u0 - kBegin);
-  p.t1 = (int)max(0ll, u1 - kBegin);
-  *f_seg = f - u0;
-  return f + (u1 - u0);
-}
+
+  // The piece at f (< f1), in all lanes; it has no tile (t1 = t0) where the
+  // range ends within kBegin.
+  __device__ __forceinline__ void next(const ChunkArgs& A, Piece& p) {
+    unsigned over;  // lanes whose sequence ends after f
+    while (!(over = __ballot_sync(0xffffffffu, (base + incl) * A.h_kv > f))) {
+      if (b0 >= A.B) {  // (only where the tables change under the call)
+        f = f1;
+        p.t0 = p.t1 = 0;
+        return;
+      }
+      base += __shfl_sync(0xffffffffu, incl, 31);
+      hold(A, b0 + 32);
+    }
+    const int l = __ffs(over) - 1;
+    auto of = [&](int x) { return __shfl_sync(0xffffffffu, x, l); };
+    const long long c = __shfl_sync(0xffffffffu, seq_cost(s), l);
+    const long long before = base + __shfl_sync(0xffffffffu, incl, l) - c;
+    p.b = b0 + l;
+    p.c0 = of(s.c0), p.n_new = of(s.n_new), p.n_int = of(s.n_int), p.n_win = of(s.n_win);
+    p.slot = of(s.slot);
+    p.I = tiles_of(p.n_int);
+    p.Wt = tiles_of(p.n_win);
+    long long r = f - before * A.h_kv;
+    p.h = (int)(r / c);
+    r -= p.h * c;
+    int q0 = 0, q1 = (p.n_new + kQTok - 1) / kQTok;
+    while (q1 - q0 > 1) {
+      const int mid = (q0 + q1) >> 1;
+      if (block_cost(mid, p.I + p.Wt) <= r) q0 = mid; else q1 = mid;
+    }
+    p.qb = q0;
+    p.total = p.I + p.Wt + q0 / 2 + 1;
+    const long long u0 = r - block_cost(q0, p.I + p.Wt);
+    const long long u1 = min((long long)p.total + kBegin, u0 + (f1 - f));
+    p.t0 = (int)max(0ll, u0 - kBegin);
+    p.t1 = (int)max(0ll, u1 - kBegin);
+    f_seg = f - u0;
+    f += u1 - u0;
+  }
+};
 
 // A partial: O [32 channel groups][rows][4], then m [rows] and l [rows].
 // CTA w has two: of a segment begun by an earlier CTA, and of one that a later

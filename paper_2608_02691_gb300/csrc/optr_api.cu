@@ -306,7 +306,7 @@ void optr_params_destroy(optr_params* p) {
   cudaFree(p->Rv_t5);
   cudaFree(p->Rk_back);
   cudaFree(p->Rv_back);
-  cudaFree(p->Rk_frag);
+  cudaFree(p->Rk_query);
   cudaFree(p->err);
   free(p);
 }
