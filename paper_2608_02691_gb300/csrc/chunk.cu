@@ -103,60 +103,59 @@ __device__ __forceinline__ void store32(void* p, const uint32_t (&y)[8], bool wh
 template <bool kBf16>
 __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, float scale, float off,
                                              uint4 mask, int lim, bool fresh, float& m, float& l) {
-  const uint32_t word[4] = {mask.x, mask.y, mask.z, mask.w};
   const bool whole = __all_sync(0xffffffffu, lim >= kTile) &&
                      (mask.x & mask.y & mask.z & mask.w) == 0xffffffffu;
-  auto keep = [&](int c) {  // the columns of chunk c that count
-    const int n = lim - 32 * c;
-    return word[c] & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u);
-  };
-  uint32_t s[kTile];
-  auto chunk = [&](int c) -> uint32_t (&)[32] { return reinterpret_cast<uint32_t(&)[32]>(s[32 * c]); };
-#pragma unroll
-  for (int c = 0; c < 4; ++c) tc05::tmem_ld32(tS + 32 * c, chunk(c));
-  tc05::tmem_wait_ld();
-  if (!whole) {
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const uint32_t k = keep(c);
+  // chunk c of the row, the columns that do not count at -infinity
+  auto load = [&](int c, uint32_t (&s)[32]) {
+    tc05::tmem_ld32(tS + 32 * c, s);
+    tc05::tmem_wait_ld();
+    if (!whole) {
+      const int n = lim - 32 * c;
+      const uint32_t word = c == 0 ? mask.x : c == 1 ? mask.y : c == 2 ? mask.z : mask.w;
+      const uint32_t k = word & (n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u);
 #pragma unroll
       for (int j = 0; j < 32; ++j)
-        if (!(k >> j & 1)) s[32 * c + j] = 0xff800000u;
+        if (!(k >> j & 1)) s[j] = 0xff800000u;
     }
-  }
+  };
   float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+  for (int c = 0; c < 4; ++c) {
+    uint32_t s[32];
+    load(c, s);
 #pragma unroll
-  for (int j = 0; j < kTile; j += 8)
+    for (int j = 0; j < 32; j += 8)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      x[i] = fmaxf(x[i], fmaxf(__uint_as_float(s[j + i]), __uint_as_float(s[j + 4 + i])));
-  const float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-  const float t = fmaf(top, scale, -off);
+      for (int i = 0; i < 4; ++i)
+        x[i] = fmaxf(x[i], fmaxf(__uint_as_float(s[j + i]), __uint_as_float(s[j + 4 + i])));
+  }
+  const float t = fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), scale, -off);
   if (fresh) {
     m = fmaxf(m, t);
   } else if (__any_sync(0xffffffffu, t > m + kSlack)) {
     const float mn = t > m + kSlack ? t : m, al = ex2(m - mn);
     m = mn;
     l *= al;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      uint32_t o[16];
-      tc05::tmem_ld16(tO + 16 * c, o);
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+      uint32_t o[32];
+      tc05::tmem_ld32(tO + 32 * c, o);
       tc05::tmem_wait_ld();
 #pragma unroll
-      for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * al);
-      tc05::tmem_st16(tO + 16 * c, o);
+      for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * al);
+      tc05::tmem_st32(tO + 32 * c, o);
     }
   }
   const float2 scale2 = make_float2(scale, scale), sub2 = make_float2(-(off + m), -(off + m));
   float2 sum[2] = {};
-#pragma unroll
+#pragma unroll 1
   for (int c = 0; c < 4; ++c) {
-    uint32_t p[16];
+    uint32_t s[32], p[16];
+    load(c, s);
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-      const float2 y = fma2(make_float2(__uint_as_float(s[32 * c + 2 * j]),
-                                        __uint_as_float(s[32 * c + 2 * j + 1])), scale2, sub2);
+      const float2 y = fma2(make_float2(__uint_as_float(s[2 * j]), __uint_as_float(s[2 * j + 1])),
+                            scale2, sub2);
       const float2 e = make_float2(ex2(y.x), ex2(y.y));
       sum[j & 1] = add2(sum[j & 1], e);
       p[j] = pack16<kBf16>(e.x, e.y);
@@ -175,30 +174,38 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, float sca
 // which centering took from the keys.
 __device__ __forceinline__ void rotated_query(uint32_t tS, uint8_t* q, int row, const float* muR,
                                               float& scale, float& off) {
-  uint32_t s[kD];
-  auto chunk = [&](int c) -> uint32_t (&)[32] { return reinterpret_cast<uint32_t(&)[32]>(s[32 * c]); };
+  float top = 0.f, dot = 0.f;
+#pragma unroll 1
+  for (int c = 0; c < 4; ++c) {
+    uint32_t s[32];
+    tc05::tmem_ld32(tS + 32 * c, s);
+    tc05::tmem_wait_ld();
 #pragma unroll
-  for (int c = 0; c < 4; ++c) tc05::tmem_ld32(tS + 32 * c, chunk(c));
-  tc05::tmem_wait_ld();
-  float top = 0.f, dot[2] = {0.f, 0.f};
-#pragma unroll
-  for (int k = 0; k < kD; ++k) {
-    top = fmaxf(top, fabsf(__uint_as_float(s[k])));
-    dot[k & 1] = fmaf(__uint_as_float(s[k]), __ldg(muR + row_channel(k)), dot[k & 1]);
+    for (int k = 0; k < 32; ++k) {
+      top = fmaxf(top, fabsf(__uint_as_float(s[k])));
+      dot = fmaf(__uint_as_float(s[k]), __ldg(muR + row_channel(k) + 8 * c), dot);
+    }
   }
   const int E = min(max((int)(__float_as_uint(top) >> 23) - 126, -120), 120);
   const float down = __uint_as_float((uint32_t)(127 - E) << 23);
   scale = __uint_as_float((uint32_t)(127 + E) << 23) * kLogit;
-  off = -(dot[0] + dot[1]) * kLogit;
+  off = -dot * kLogit;
+#pragma unroll 1
+  for (int c = 0; c < 4; ++c) {
+    uint32_t s[32];
+    tc05::tmem_ld32(tS + 32 * c, s);
+    tc05::tmem_wait_ld();
 #pragma unroll
-  for (int c = 0; c < 16; ++c) {
-    uint32_t y[4];
+    for (int i = 0; i < 4; ++i) {
+      uint32_t y[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      y[e] = pack16<false>(__uint_as_float(s[8 * c + 2 * e]) * down,
-                           __uint_as_float(s[8 * c + 2 * e + 1]) * down);
-    *reinterpret_cast<uint4*>(q + (c >> 3) * kHalf + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
-        make_uint4(y[0], y[1], y[2], y[3]);
+      for (int e = 0; e < 4; ++e)
+        y[e] = pack16<false>(__uint_as_float(s[8 * i + 2 * e]) * down,
+                             __uint_as_float(s[8 * i + 2 * e + 1]) * down);
+      const int piece = 4 * (c & 1) + i;  // of the channel half c / 2
+      *reinterpret_cast<uint4*>(q + (c >> 1) * kHalf + row * 128 + ((piece ^ (row & 7)) << 4)) =
+          make_uint4(y[0], y[1], y[2], y[3]);
+    }
   }
 }
 
@@ -311,7 +318,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
         // R_v^T takes P's place
         if (!wait(&S.o_full[g], no++)) break;
         const float inv = l > 0.f ? 1.f / l : 0.f;
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t o[32], a[16];
           tc05::tmem_ld32(tO + 32 * c, o);
@@ -340,7 +347,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
       if (dead || !wait(&S.o_full[g], no++)) break;
       if (p.t1 - p.t0 == p.total) {
         const float inv = l > 0.f ? 1.f / l : 0.f;
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t o[32];
           tc05::tmem_ld32(tO + 32 * c, o);
@@ -359,7 +366,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
       } else {
         float* part = part_of(A, w, p.t0 > 0);
         const int r = 128 * g + row;
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t o[32];
           tc05::tmem_ld32(tO + 32 * c, o);
@@ -443,38 +450,40 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
         const int tile = p.t0 + t;
         cp_async_wait<1>();
         const bool ok = okn[0];
-        uint4 kc[2] = {}, vc[2] = {}, km = {}, vm = {};
-        if (ok) {
-          const uint4* d = &S.raw[tile & 1][0][key];
-          kc[0] = d[0], kc[1] = d[128], vc[0] = d[256], vc[1] = d[384], km = d[512], vm = d[640];
-          if (A.compact) km.y = km.z = km.w = km.x, vm.y = vm.z = vm.w = vm.x;
+        const uint32_t bits = __ballot_sync(0xffffffffu, ok || tile * kTile + key >= p.n_int);
+#pragma unroll 1
+        for (int kind = 0; kind < 2; ++kind) {
+          const uint32_t e = kind ? nv : nk;
+          if (e >= kRing && !wait(kind ? &S.v_empty[e % kRing] : &S.k_empty[e % kRing], e / kRing - 1))
+            break;
+          if (!kind && lane == 0) S.mask[nk % 4][key >> 5] = bits;
+          const uint4* raw = &S.raw[tile & 1][2 * kind][key];
+          uint8_t* dst = (kind ? S.v[e % kRing] : S.k[e % kRing]) + key * 128;
+          uint4 mm = raw[(4 - kind) * 128];
+          if (A.compact) mm.y = mm.z = mm.w = mm.x;
+          if (!ok) mm = make_uint4(0u, 0u, 0u, 0u);  // a row of zeros, whatever was copied
+          const SlotMeta sm = slot_meta(mm.x, mm.y, mm.z, mm.w);
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            const uint4 c = raw[half * 128];
+            const uint32_t word[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t x[8];
+              dequant_word(word[i], sm, x);
+              *reinterpret_cast<uint4*>(dst + half * kHalf + (((2 * i) ^ (key & 7)) << 4)) =
+                  make_uint4(x[0], x[1], x[2], x[3]);
+              *reinterpret_cast<uint4*>(dst + half * kHalf + (((2 * i + 1) ^ (key & 7)) << 4)) =
+                  make_uint4(x[4], x[5], x[6], x[7]);
+            }
+          }
+          tc05::fence_proxy_async();
+          tc05::bar_arrive(kind ? &S.v_full[e % kRing] : &S.k_full[e % kRing]);
         }
+        if (dead) break;
         okn[0] = okn[1];
         okn[1] = copy(p, tile + 2, page);
         page = request(p, tile + 3);
-        auto put = [&](uint8_t* dst, const uint4 (&c)[2], const uint4& mm) {
-          const SlotMeta sm = slot_meta(mm.x, mm.y, mm.z, mm.w);
-          const uint32_t word[8] = {c[0].x, c[0].y, c[0].z, c[0].w, c[1].x, c[1].y, c[1].z, c[1].w};
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            uint32_t x[8];
-            dequant_word(word[i], sm, x);
-            uint8_t* r = dst + (i >> 2) * kHalf + key * 128;
-            const int c0 = 2 * (i & 3);
-            *reinterpret_cast<uint4*>(r + ((c0 ^ (key & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
-            *reinterpret_cast<uint4*>(r + (((c0 + 1) ^ (key & 7)) << 4)) = make_uint4(x[4], x[5], x[6], x[7]);
-          }
-        };
-        if (nk >= kRing && !wait(&S.k_empty[nk % kRing], nk / kRing - 1)) break;
-        const uint32_t bits = __ballot_sync(0xffffffffu, ok || tile * kTile + key >= p.n_int);
-        if (lane == 0) S.mask[nk % 4][key >> 5] = bits;
-        put(S.k[nk % kRing], kc, km);
-        tc05::fence_proxy_async();
-        tc05::bar_arrive(&S.k_full[nk % kRing]);
-        if (nv >= kRing && !wait(&S.v_empty[nv % kRing], nv / kRing - 1)) break;
-        put(S.v[nv % kRing], vc, vm);
-        tc05::fence_proxy_async();
-        tc05::bar_arrive(&S.v_full[nv % kRing]);
       }
       if (dead) break;
       nk += nother;
