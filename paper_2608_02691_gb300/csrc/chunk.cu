@@ -463,7 +463,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
           if (A.compact) mm.y = mm.z = mm.w = mm.x;
           if (!ok) mm = make_uint4(0u, 0u, 0u, 0u);  // a row of zeros, whatever was copied
           const SlotMeta sm = slot_meta(mm.x, mm.y, mm.z, mm.w);
-#pragma unroll 1
+#pragma unroll
           for (int half = 0; half < 2; ++half) {
             const uint4 c = raw[half * 128];
             const uint32_t word[4] = {c.x, c.y, c.z, c.w};
@@ -584,16 +584,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
     __syncwarp();
   } else if (warp == kPlanWarp) {
     // ---------------------------------------------------------- pieces
-    if (w == 0) {  // what is wrong with the sequences, once
-      if (lane == 0 && (__ldcg(A.cu) != 0 || __ldcg(A.cu + A.B) != A.n_tok))
-        atomicOr(A.err, OPTR_DEVERR_CU_NEW);
-      for (int b = lane; b < A.B; b += 32) {
-        const SeqWork x = seq_work(A, b);
-        unsigned bad = x.bad;
-        if (!bad && A.win.win && (x.slot < 0 || x.slot >= A.win.n_slots)) bad = OPTR_DEVERR_WIN_SLOT;
-        if (bad) atomicOr(A.err, bad);
-      }
-    }
+    if (w == 0) report_sequences(A);
     PieceFinder next;
     next.start(A, w);
     ChunkSeg seg{};
@@ -742,6 +733,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
 // on: CTA (w, y) rows 8 y .. 8 y + 7 of the one that CTA w began, thread = 4
 // channels of a row.  The CTAs also clear the rows of sequences that were left
 // out and those of none.
+template <bool kSmall>
 __global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
   const int w = blockIdx.x, tid = threadIdx.x;
   pdl_wait();
@@ -763,7 +755,7 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
     }
   }
   const ChunkSeg seg = A.seg[w];
-  const int r = 8 * blockIdx.y + (tid & 7), cg = tid >> 3;
+  const int r = 8 * blockIdx.y + (kSmall ? tid >> 5 : tid & 7), cg = kSmall ? tid & 31 : tid >> 3;
   const int i = seg.qb * kQTok + r / 4;
   if (!seg.valid || r >= A.rows || i >= seg.n_new) return;
   float M = -INFINITY, L = 0.f;
@@ -781,7 +773,8 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
         const float* part = part_of(A, x, x != w);
         m[k] = __ldcg(part + (size_t)A.rows * kD + r);
         l[k] = __ldcg(part + (size_t)A.rows * (kD + 1) + r);
-        y[k] = __ldcg(reinterpret_cast<const float4*>(part) + (size_t)cg * A.rows + r);
+        y[k] = __ldcg(reinterpret_cast<const float4*>(part) +
+                      (kSmall ? (size_t)r * (kD / 4) + cg : (size_t)cg * A.rows + r));
       }
     }
 #pragma unroll
@@ -806,12 +799,15 @@ size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 struct ChunkLayout {
   size_t part, total;
   int rows, W;
+  bool small;
 };
 
 ChunkLayout chunk_layout(const optr_params* p, int max_new) {
   ChunkLayout l;
-  l.rows = max_new > 32 ? 256 : 128;
-  l.W = p->num_sms;
+  l.rows = chunk_small_rows(max_new);
+  l.small = l.rows > 0;
+  if (!l.small) l.rows = max_new > 32 ? 256 : 128;
+  l.W = p->num_sms * (l.small ? chunk_small_groups(l.rows) : 1);
   l.part = round_up(sizeof(ChunkSeg) * (size_t)l.W);
   l.total = l.part + round_up(2 * (size_t)l.W * part_floats(l.rows) * sizeof(float));
   return l;
@@ -861,15 +857,20 @@ extern "C" optr_status optr_chunk_attention_win(
   cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(chunk_kernel), sizeof(Smem));
   if (e != cudaSuccess) return OPTR_ERR_CUDA;
   CUtensorMap mq, mk, mv, mw;
-  if (!token_rows_map(&mq, q, n_tok, 4 * h_kv, 32, 4) ||
+  if ((!l.small && !token_rows_map(&mq, q, n_tok, 4 * h_kv, 32, 4)) ||
       !token_rows_map(&mk, k, n_tok, h_kv, kTile) || !token_rows_map(&mv, v, n_tok, h_kv, kTile) ||
       !(w.win ? token_rows_map(&mw, w.win, n_slots * h_kv * 2 * win_rows, 1, kTile)
               : token_rows_map(&mw, k, n_tok, h_kv, kTile)))
     return OPTR_ERR_CUDA;
+  const dim3 joins(l.W, (std::min(l.rows, 4 * max_new) + 7) / 8);
+  if (l.small) {
+    e = launch_chunk_small(p, A, (const __nv_bfloat16*)q, mk, mv, mw, stream);
+    if (e == cudaSuccess) e = launch_pdl(chunk_combine_kernel<true>, joins, dim3(256), 0, stream, A);
+    return cuda_status(e);
+  }
   e = launch_pdl(chunk_kernel, dim3(l.W), dim3(kThreads), sizeof(Smem), stream, mq, mk, mv, mw, A);
   if (e == cudaSuccess)
-    e = launch_pdl(chunk_combine_kernel, dim3(l.W, (std::min(l.rows, 4 * max_new) + 7) / 8),
-                   dim3(256), 0, stream, A);
+    e = launch_pdl(chunk_combine_kernel<false>, joins, dim3(256), 0, stream, A);
   return cuda_status(e);
 }
 

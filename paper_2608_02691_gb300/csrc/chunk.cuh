@@ -2,6 +2,8 @@
 // kernels (chunk.cu).
 #pragma once
 
+#include <cudaTypedefs.h>
+
 #include "decode_common.cuh"
 #include "optr_internal.cuh"
 
@@ -25,7 +27,7 @@ struct ChunkArgs {
   struct ChunkSeg* seg;  // [W] segments begun by a CTA and ended by another
   float* part;           // partial results
   int rows;              // rows of a partial
-  int W;                 // CTAs of the attention kernel
+  int W;                 // workers: CTAs of chunk_kernel, warpgroups of chunk_small_kernel
   bool out32;            // out is 32-byte aligned
 };
 
@@ -178,12 +180,34 @@ struct PieceFinder {
   }
 };
 
-// A partial: O [32 channel groups][rows][4], then m [rows] and l [rows].
-// CTA w has two: of a segment begun by an earlier CTA, and of one that a later
+// Flags what is wrong with the sequences; one warp of a call's.
+__device__ __forceinline__ void report_sequences(const ChunkArgs& A) {
+  const int lane = threadIdx.x & 31;
+  if (lane == 0 && (__ldcg(A.cu) != 0 || __ldcg(A.cu + A.B) != A.n_tok))
+    atomicOr(A.err, OPTR_DEVERR_CU_NEW);
+  for (int b = lane; b < A.B; b += 32) {
+    const SeqWork x = seq_work(A, b);
+    unsigned bad = x.bad;
+    if (!bad && A.win.win && (x.slot < 0 || x.slot >= A.win.n_slots)) bad = OPTR_DEVERR_WIN_SLOT;
+    if (bad) atomicOr(A.err, bad);
+  }
+}
+
+// A partial: O, [32 channel groups][rows][4] from chunk_kernel and [rows][128]
+// from chunk_small_kernel (as their threads hold it), then m [rows] and l [rows].
+// Worker w (a CTA, or a warpgroup of chunk_small_kernel) has two: of a segment begun by an earlier CTA, and of one that a later
 // CTA ends.
 __host__ __device__ constexpr size_t part_floats(int rows) { return (size_t)rows * (kD + 2); }
 __device__ __forceinline__ float* part_of(const ChunkArgs& A, int w, bool begun) {
   return A.part + (2 * (size_t)w + (begun ? 1 : 0)) * part_floats(A.rows);
 }
+
+// chunk_small.cu: rows of its query operand for up to max_new tokens (0: too
+// many), its warpgroups per CTA with so many rows, and the launch.
+int chunk_small_rows(int max_new);
+int chunk_small_groups(int rows);
+cudaError_t launch_chunk_small(const optr_params* p, const ChunkArgs& A, const __nv_bfloat16* q,
+                               const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mw,
+                               cudaStream_t s);
 
 }  // namespace optr

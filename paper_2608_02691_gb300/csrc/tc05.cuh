@@ -39,7 +39,7 @@ __device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t saddr, uint32_t lbo
 }
 
 constexpr uint32_t kIdescBf16 = (1u << 7) | (1u << 10);  // A and B bf16
-constexpr uint32_t kIdescMajorMnB = 1u << 16;
+constexpr uint32_t kIdescMajorMnA = 1u << 15, kIdescMajorMnB = 1u << 16;
 
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N) {
   return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
