@@ -596,7 +596,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
       while (next.f < next.f1 && p.t1 == p.t0) next.next(A, p);
       more = p.t1 > p.t0;
       if (more && p.t0 == 0 && p.t1 < p.total)
-        seg = ChunkSeg{next.F, next.f_seg + kBegin + p.total, p.c0, p.n_new, p.h, p.qb, 1};
+        seg = ChunkSeg{next.F, next.f_seg + kBegin + p.total, p.c0, p.n_new, p.h, p.qb, next.W, 1};
       if (n >= kPieces && !__all_sync(0xffffffffu, tc05::bar_wait_spin(&S.piece_empty[i],
                                                                        (n / kPieces - 1) & 1, abort)))
         break;
@@ -729,15 +729,21 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
 
 // ------------------------------------------------------------- combine
 
-// Joins the partials of the segments that several CTAs of chunk_kernel worked
-// on: CTA (w, y) rows 8 y .. 8 y + 7 of the one that CTA w began, thread = 4
-// channels of a row.  The CTAs also clear the rows of sequences that were left
-// out and those of none.
+// Joins the partials of the segments that several workers had a part in: CTA
+// (w, y) rows kRows y .. of the one that worker w began.  A thread has 4 channels
+// of a row and every kSplit-th part: a prefill's segments are of two or three
+// parts and many rows (kSplit 1), those of a few tokens over a long context of
+// many parts and few rows (kSplit 4).  The CTAs also clear the rows of sequences
+// that were left out and those of none.
 template <bool kSmall>
 __global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
+  constexpr int kSplit = kSmall ? 4 : 1, kRows = 8 / kSplit;
+  __shared__ float4 so[kSplit][kRows][32];
+  __shared__ float2 sml[kSplit][kRows];
   const int w = blockIdx.x, tid = threadIdx.x;
   pdl_wait();
   pdl_trigger();
+  const ChunkSeg seg = A.seg[w];
   auto clear = [&](int t0, int t1) {
     uint4* o = reinterpret_cast<uint4*>(A.out);
     const size_t n = (size_t)A.h_kv * 4 * kD / 8;
@@ -754,22 +760,31 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
       if (seq_work(A, b).bad) clear(max(0, __ldcg(A.cu + b)), min(c1, A.n_tok));
     }
   }
-  const ChunkSeg seg = A.seg[w];
-  const int r = 8 * blockIdx.y + (kSmall ? tid >> 5 : tid & 7), cg = kSmall ? tid & 31 : tid >> 3;
+  // rows along the threads as the partials have them, or channels
+  const int split = kSmall ? tid >> 6 : 0;
+  const int row = kSmall ? tid >> 5 & (kRows - 1) : tid & 7, cg = kSmall ? tid & 31 : tid >> 3;
+  const int r = kRows * blockIdx.y + row;
   const int i = seg.qb * kQTok + r / 4;
-  if (!seg.valid || r >= A.rows || i >= seg.n_new) return;
+  if (!seg.valid || seg.qb * kQTok + kRows * (int)blockIdx.y / 4 >= seg.n_new) return;
+  const bool in = r < A.rows && i < seg.n_new;
   float M = -INFINITY, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto join = [&](float m, float l, float4 y) {
+    if (l == 0.f) return;  // no part, or one whose keys were all left out
+    const float mn = fmaxf(M, m), u = ex2(M - mn), v = ex2(m - mn);
+    M = mn;
+    L = L * u + l * v;
+    o = make_float4(o.x * u + y.x * v, o.y * u + y.y * v, o.z * u + y.z * v, o.w * u + y.w * v);
+  };
   constexpr int kAhead = 4;  // partials requested at a time
-  for (int x0 = w; x0 < A.W && seg.F * x0 / A.W < seg.end; x0 += kAhead) {
+  for (int x0 = w + split; x0 < seg.W && seg.F * x0 / seg.W < seg.end; x0 += kAhead * kSplit) {
     float m[kAhead], l[kAhead];
     float4 y[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const int x = x0 + k;
-      const long long a = seg.F * x / A.W, b = seg.F * (x + 1) / A.W;
+      const int x = x0 + k * kSplit;
       l[k] = 0.f;
-      if (x < A.W && a < seg.end && a < b) {
+      if (in && x < seg.W && seg.F * x / seg.W < seg.end) {
         const float* part = part_of(A, x, x != w);
         m[k] = __ldcg(part + (size_t)A.rows * kD + r);
         l[k] = __ldcg(part + (size_t)A.rows * (kD + 1) + r);
@@ -778,15 +793,16 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
       }
     }
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      if (l[k] == 0.f) continue;  // none, or one whose keys were all left out
-      const float mn = fmaxf(M, m[k]), u = ex2(M - mn), v = ex2(m[k] - mn);
-      M = mn;
-      L = L * u + l[k] * v;
-      o = make_float4(o.x * u + y[k].x * v, o.y * u + y[k].y * v, o.z * u + y[k].z * v,
-                      o.w * u + y[k].w * v);
-    }
+    for (int k = 0; k < kAhead; ++k) join(m[k], l[k], y[k]);
   }
+  if (kSplit > 1) {
+    so[split][row][cg] = o;
+    if (cg == 0) sml[split][row] = make_float2(M, L);
+    __syncthreads();
+    if (split != 0) return;
+    for (int k = 1; k < kSplit; ++k) join(sml[k][row].x, sml[k][row].y, so[k][row][cg]);
+  }
+  if (!in) return;
   const float inv = L > 0.f ? 1.f / L : 0.f;
   const size_t at = ((size_t)seg.c0 + i) * 4 * A.h_kv + 4 * seg.h + r % 4;
   *reinterpret_cast<uint2*>(A.out + at * kD + 4 * cg) =
@@ -862,7 +878,8 @@ extern "C" optr_status optr_chunk_attention_win(
       !(w.win ? token_rows_map(&mw, w.win, n_slots * h_kv * 2 * win_rows, 1, kTile)
               : token_rows_map(&mw, k, n_tok, h_kv, kTile)))
     return OPTR_ERR_CUDA;
-  const dim3 joins(l.W, (std::min(l.rows, 4 * max_new) + 7) / 8);
+  const int per = l.small ? 2 : 8;  // rows of a joining CTA
+  const dim3 joins(l.W, (std::min(l.rows, 4 * max_new) + per - 1) / per);
   if (l.small) {
     e = launch_chunk_small(p, A, (const __nv_bfloat16*)q, mk, mv, mw, stream);
     if (e == cudaSuccess) e = launch_pdl(chunk_combine_kernel<true>, joins, dim3(256), 0, stream, A);

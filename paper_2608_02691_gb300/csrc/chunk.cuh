@@ -36,6 +36,7 @@ struct ChunkArgs {
 struct ChunkSeg {
   long long F, end;
   int c0, n_new, h, qb;
+  int W;              // workers that the line is cut for
   int valid;
 };
 
@@ -80,6 +81,7 @@ __device__ __forceinline__ int tiles_of(int keys) { return (keys + kTile - 1) / 
 // cached tiles each: block qb sees own tiles 0 .. qb / 2, and kBegin tiles' time
 // goes into its start and end.
 constexpr int kBegin = 2;
+constexpr int kLeast = 4;  // units that are worth a range of their own
 __device__ __forceinline__ long long block_cost(long long m, int past) {
   return m * (past + kBegin) + (m + 1) * (m + 1) / 4;
 }
@@ -102,11 +104,12 @@ __device__ __forceinline__ long long seq_cost(const SeqWork& s) {
 }
 
 // The flat index space orders units of cost as (sequence, KV head, query block,
-// unit); CTA w takes [w F / W, (w + 1) F / W).  Of a block's kBegin + tiles units
+// unit); worker w takes [w F / W, (w + 1) F / W).  Of a block's kBegin + tiles units
 // the first kBegin stand for no tile.  One warp goes through a CTA's range: lane
 // i holds sequence b0 + i.
 struct PieceFinder {
   long long f, f1, F;    // the next unit, the range's end, all units
+  int W;                 // ranges: A.W, or fewer so that each has kLeast units
   long long f_seg;       // first unit of the last piece's segment
   int b0;                // the 32 sequences held, and what comes before them
   long long base, incl;  // (cost of one head); incl: up to and with the lane's
@@ -133,8 +136,9 @@ struct PieceFinder {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     F = sum * A.h_kv;
-    f = F * w / A.W;
-    f1 = F * (w + 1) / A.W;
+    W = (int)min((long long)A.W, max(1ll, F / kLeast));
+    f = w < W ? F * w / W : F;
+    f1 = w < W ? F * (w + 1) / W : F;
     base = 0;
     hold(A, 0);
   }

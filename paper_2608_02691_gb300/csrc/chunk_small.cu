@@ -16,10 +16,9 @@
 // Thread = key of the tile.  Its record is in registers a tile ahead.  The key goes
 // into tensor memory as a row of the A operand, the value into a row of shared
 // memory (V^T is that tile read along its other dimension).  The thread then holds
-// its key's logits with all rows: probabilities go into shared memory transposed, a
-// row's maximum is kept for the warpgroup and only looked at again when some
-// thread's logit passes it by 2^8, its sum is kept per thread and added up at the
-// end.
+// its key's logits with all rows: probabilities go into shared memory transposed, where
+// the rows' sums are taken; a row's maximum is kept for the warpgroup and only
+// looked at again when some thread's logit passes it by 2^8.
 #include "append_common.cuh"
 #include "chunk.cuh"
 #include "dequant.cuh"
@@ -87,8 +86,13 @@ __device__ __forceinline__ uint32_t at16(int row, int i) {
   return (i >> 6) * (N * 128) + row * 128 + ((((i >> 3) & 7) ^ (row & 7)) << 4) + (i & 7) * 2;
 }
 
-__device__ __forceinline__ uint16_t half_bits(float x, bool bf16) {
-  return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : __half_as_ushort(__float2half_rn(x));
+__device__ __forceinline__ uint32_t pack16(float a, float b, bool bf16) {  // a in the low half
+  uint32_t r;
+  if (bf16)
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  else
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
 }
 
 // A key's record of one kind, as read: codes and {scale, min} words.
@@ -130,7 +134,7 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
   const uint32_t tK = base, tS = base + 64, tO = base + 64 + N;
   volatile int* abort = &S.abort;
-  const int w = blockIdx.x * kGroupsN + g;
+  const int w = g * gridDim.x + blockIdx.x;  // (few workers have work: of different SMs)
 
   if (w == 0 && quarter == 0) report_sequences(A);
   PieceFinder next;  // the group's first warp's
@@ -144,13 +148,15 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   };
   const uint32_t sv = tc05::smem_addr(G.v), sq = tc05::smem_addr(G.q), sp = tc05::smem_addr(G.p);
 
+  constexpr int kPerRow = N == 16 ? 8 : N == 32 ? 4 : 2;  // threads per row's sum
+  const int lrow = key / kPerRow, lpart = key % kPerRow;
   while (true) {
     if (quarter == 0) {
       Piece x;
       x.t0 = x.t1 = 0;
       while (next.f < next.f1 && x.t1 == x.t0) next.next(A, x);
       if (x.t1 > 0 && x.t0 == 0 && x.t1 < x.total)
-        seg = ChunkSeg{next.F, next.f_seg + kBegin + x.total, x.c0, x.n_new, x.h, x.qb, 1};
+        seg = ChunkSeg{next.F, next.f_seg + kBegin + x.total, x.c0, x.n_new, x.h, x.qb, next.W, 1};
       if (lane == 0) G.piece = x;
     }
     group_sync(g);
@@ -160,9 +166,7 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const int nint = p.int_tiles();
     const int rows = 4 * p.n_new, nc = (rows + 15) / 16;  // rows, in chunks of 16
     const uint32_t id = tc05::idesc_f16(128, 16 * nc);
-    float l[N];
-#pragma unroll
-    for (int c = 0; c < N; ++c) l[c] = 0.f;
+    float l = 0.f;      // sum of row `lrow`'s probabilities over the thread's share of the keys
     bool fresh = true;  // nothing in O yet
     bool first = true;  // no maximum yet
 
@@ -225,7 +229,7 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       group_sync(g);
       if (quarter == 0) {
         tc05::fence_after();
-#pragma unroll 1
+#pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
           const uint64_t db = tc05::smem_desc_sw128(b + (ks >> 2) * (N * 128) + (ks & 3) * 32, 16);
           const uint32_t acc = add || ks != 0;
@@ -242,103 +246,108 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         tc05::mma_commit_warp(bar);
       }
     };
-    // l summed over the threads, into G.l
-    auto sum_rows = [&]() {
+    // Adds the tile's probabilities, as they stand in shared memory, to l.
+    auto add_rows = [&](bool bf16) {
+      if (lrow >= 16 * nc) return;
 #pragma unroll
-      for (int c = 0; c < N; ++c)
-        if (c < 16 * nc) {
-          float x = l[c];
+      for (int i = 0; i < 16 / kPerRow; ++i) {
+        const int k = 8 * (lpart + kPerRow * i);
+        const uint4 x = *reinterpret_cast<const uint4*>(G.p + at16<N>(lrow, k));
+        const uint32_t word[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-          for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-          if (lane == 0) G.quarter[quarter][c] = x;
-        }
-      group_sync(g);
-      for (int c = key; c < 16 * nc; c += 128)
-        G.l[c] = (G.quarter[0][c] + G.quarter[1][c]) + (G.quarter[2][c] + G.quarter[3][c]);
-      group_sync(g);
-    };
-    // The tile's logits become probabilities; bit c / 4 of `seen` says whether
-    // the thread's key counts for the rows of new token c / 4.
-    auto softmax = [&](uint32_t seen, bool bf16) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int c0 = 0; c0 < N; c0 += 16)
-        if (c0 < 16 * nc) {
-          uint32_t s[16];
-          tc05::tmem_ld16(tS + lanes + c0, s);
-          tc05::tmem_wait_ld();
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float2 x = G.ms[c0 + j];
-            const float y = fmaf(__uint_as_float(s[j]), x.x, x.y);
-            if (seen >> ((c0 + j) >> 2) & 1) top = fmaxf(top, y);
-          }
-        }
-      // (a warp whose wait ran out leads the group out with it)
-      if (group_any(g, first || top > kSlack || dead)) {
-        if (group_any(g, dead)) {
-          dead = true;
-          return;
-        }
-#pragma unroll
-        for (int c0 = 0; c0 < N; c0 += 16)
-          if (c0 < 16 * nc) {
-            uint32_t s[16];
-            tc05::tmem_ld16(tS + lanes + c0, s);
-            tc05::tmem_wait_ld();
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const float2 x = G.ms[c0 + j];
-              const float y = seen >> ((c0 + j) >> 2) & 1
-                                  ? fmaf(__uint_as_float(s[j]), x.x, x.y) : -INFINITY;
-              const float z = warp_max(y);
-              if (lane == j) G.quarter[quarter][c0 + j] = z;
-            }
-          }
-        group_sync(g);
-        for (int c = key; c < 16 * nc; c += 128) {
-          const float z = fmaxf(fmaxf(G.quarter[0][c], G.quarter[1][c]), fmaxf(G.quarter[2][c], G.quarter[3][c]));
-          const float d = (first && z > -INFINITY) || z > kSlack ? z : 0.f;  // the maximum's growth
-          G.m[c] += d;
-          G.d[c] = d;
-          G.ms[c].y -= d;
-        }
-        group_sync(g);
-        const bool was_first = first;  // then l and O are zero
-        first = first && fmaxf(fmaxf(G.quarter[0][0], G.quarter[1][0]),
-                               fmaxf(G.quarter[2][0], G.quarter[3][0])) == -INFINITY;
-        if (!was_first) {
-#pragma unroll
-          for (int c0 = 0; c0 < N; c0 += 16)
-            if (c0 < 16 * nc) {
-              uint32_t o[16];
-              tc05::tmem_ld16(tO + lanes + c0, o);
-              tc05::tmem_wait_ld();
-#pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                const float al = ex2(-G.d[c0 + j]);
-                l[c0 + j] *= al;
-                o[j] = __float_as_uint(__uint_as_float(o[j]) * al);
-              }
-              tc05::tmem_st16(tO + lanes + c0, o);
-            }
-          tc05::tmem_wait_st();
+        for (int e = 0; e < 4; ++e) {
+          const float2 y = bf16 ? make_float2(__uint_as_float(word[e] << 16),
+                                              __uint_as_float(word[e] & 0xffff0000u))
+                                : __half22float2(*reinterpret_cast<const __half2*>(&word[e]));
+          l += y.x + y.y;
         }
       }
+    };
+    // l summed over a row's threads, into G.l
+    auto sum_rows = [&]() {
+      float x = l;
 #pragma unroll
-      for (int c0 = 0; c0 < N; c0 += 16)
-        if (c0 < 16 * nc) {
-          uint32_t s[16];
-          tc05::tmem_ld16(tS + lanes + c0, s);
+      for (int o = 1; o < kPerRow; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+      if (lpart == 0 && lrow < N) G.l[lrow] = x;
+      group_sync(g);
+    };
+    // The tile's probabilities, from its logits, under the maxima as they are;
+    // returns the largest logit over its row's maximum.  Bit c / 4 of `seen`
+    // says whether the thread's key counts for the rows of new token c / 4.
+    auto probabilities = [&](uint32_t seen, bool bf16) {
+      float top = -INFINITY;
+#pragma unroll 1
+      for (int c0 = 0; c0 < 16 * nc; c0 += 16) {
+        uint32_t s[16];
+        tc05::tmem_ld16(tS + lanes + c0, s);
+        tc05::tmem_wait_ld();
+        const uint32_t bits = seen >> (c0 >> 2);
+        uint8_t* row = G.p + c0 * 128;
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) {
+          const float4 x = *reinterpret_cast<const float4*>(&G.ms[c0 + j]);
+          const bool in = bits >> (j >> 2) & 1;
+          const float y0 = in ? fmaf(__uint_as_float(s[j]), x.x, x.y) : -INFINITY;
+          const float y1 = in ? fmaf(__uint_as_float(s[j + 1]), x.z, x.w) : -INFINITY;
+          top = fmaxf(top, fmaxf(y0, y1));
+          const uint32_t e = pack16(ex2(y0), ex2(y1), bf16);
+          *reinterpret_cast<uint16_t*>(row + at16<N>(j, key)) = (uint16_t)e;
+          *reinterpret_cast<uint16_t*>(row + at16<N>(j + 1, key)) = (uint16_t)(e >> 16);
+        }
+      }
+      return top;
+    };
+    auto softmax = [&](uint32_t seen, bool bf16) {
+      const float top = probabilities(seen, bf16);
+      // (a warp whose wait ran out leads the group out with it)
+      if (!group_any(g, first || top > kSlack || dead)) return;
+      if (group_any(g, dead)) {
+        dead = true;
+        return;
+      }
+      // maxima anew
+#pragma unroll 1
+      for (int c0 = 0; c0 < 16 * nc; c0 += 16) {
+        uint32_t s[16];
+        tc05::tmem_ld16(tS + lanes + c0, s);
+        tc05::tmem_wait_ld();
+        float z = 0.f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float2 x = G.ms[c0 + j];
+          const float y = seen >> ((c0 + j) >> 2) & 1 ? fmaf(__uint_as_float(s[j]), x.x, x.y) : -INFINITY;
+          const float t = warp_max(y);
+          if (lane == j) z = t;
+        }
+        if (lane < 16) G.quarter[quarter][c0 + lane] = z;
+      }
+      group_sync(g);
+      for (int c = key; c < 16 * nc; c += 128) {
+        const float z = fmaxf(fmaxf(G.quarter[0][c], G.quarter[1][c]),
+                              fmaxf(G.quarter[2][c], G.quarter[3][c]));
+        const float d = (first && z > -INFINITY) || z > kSlack ? z : 0.f;  // the maximum's growth
+        G.m[c] += d;
+        G.d[c] = d;
+        G.ms[c].y -= d;
+      }
+      group_sync(g);
+      const bool was_first = first;  // then l and O are zero
+      first = first && fmaxf(fmaxf(G.quarter[0][0], G.quarter[1][0]),
+                             fmaxf(G.quarter[2][0], G.quarter[3][0])) == -INFINITY;
+      if (!was_first) {
+        if (lrow < 16 * nc) l *= ex2(-G.d[lrow]);
+#pragma unroll 1
+        for (int c0 = 0; c0 < 16 * nc; c0 += 16) {
+          uint32_t o[16];
+          tc05::tmem_ld16(tO + lanes + c0, o);
           tc05::tmem_wait_ld();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float2 x = G.ms[c0 + j];
-            const float e = seen >> ((c0 + j) >> 2) & 1 ? ex2(fmaf(__uint_as_float(s[j]), x.x, x.y)) : 0.f;
-            l[c0 + j] += e;
-            *reinterpret_cast<uint16_t*>(G.p + at16<N>(c0 + j, key)) = half_bits(e, bf16);
-          }
+          for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * ex2(-G.d[c0 + j]));
+          tc05::tmem_st16(tO + lanes + c0, o);
         }
+        tc05::tmem_wait_st();
+      }
+      probabilities(seen, bf16);
     };
 
     if (nint > 0) {
@@ -349,17 +358,19 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       product(kOperandSmem, tS, sq, 0u, false, &S.s_done[g]);
       wait(&S.s_done[g], ns++);
       if (group_any(g, dead)) break;
+#pragma unroll 1
+      for (int c0 = 0; c0 < 16 * nc; c0 += 16) {
+        uint32_t s[16];
+        tc05::tmem_ld16(tS + lanes + c0, s);
+        tc05::tmem_wait_ld();
 #pragma unroll
-      for (int c0 = 0; c0 < N; c0 += 16)
-        if (c0 < 16 * nc) {
-          uint32_t s[16];
-          tc05::tmem_ld16(tS + lanes + c0, s);
-          tc05::tmem_wait_ld();
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            *reinterpret_cast<uint16_t*>(G.q + at16<N>(c0 + j, key)) =
-                half_bits(__uint_as_float(s[j]) * (1.f / 64.f), false);
+        for (int j = 0; j < 16; j += 2) {
+          const uint32_t e = pack16(__uint_as_float(s[j]) * (1.f / 64.f),
+                                    __uint_as_float(s[j + 1]) * (1.f / 64.f), false);
+          *reinterpret_cast<uint16_t*>(G.q + c0 * 128 + at16<N>(j, key)) = (uint16_t)e;
+          *reinterpret_cast<uint16_t*>(G.q + c0 * 128 + at16<N>(j + 1, key)) = (uint16_t)(e >> 16);
         }
+      }
       for (int c = key; c < 16 * nc; c += 128) {
         G.m[c] = 0.f;
         G.ms[c] = make_float2(G.scale[c], -G.off[c]);
@@ -402,9 +413,10 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       for (int t = p.t0; t < p.t0 + nint; ++t) {
         const bool okn = counts(t + 1, page);
         const SlotMeta km = slot_meta(rk.m.x, rk.m.y, rk.m.z, rk.m.w);
-#pragma unroll
+#pragma unroll 1
         for (int half = 0; half < 2; ++half) {
-          const uint32_t word[4] = {rk.c[half].x, rk.c[half].y, rk.c[half].z, rk.c[half].w};
+          const uint4 c = half ? rk.c[1] : rk.c[0];
+          const uint32_t word[4] = {c.x, c.y, c.z, c.w};
           uint32_t x[32];
 #pragma unroll
           for (int i = 0; i < 4; ++i) dequant_word(word[i], km, reinterpret_cast<uint32_t(&)[8]>(x[8 * i]));
@@ -416,9 +428,10 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         // the last tile's values and probabilities are done with
         if (!fresh) wait(&S.o_done[g], no++);
         const SlotMeta vm = slot_meta(rv.m.x, rv.m.y, rv.m.z, rv.m.w);
-#pragma unroll
+#pragma unroll 1
         for (int half = 0; half < 2; ++half) {
-          const uint32_t word[4] = {rv.c[half].x, rv.c[half].y, rv.c[half].z, rv.c[half].w};
+          const uint4 c = half ? rv.c[1] : rv.c[0];
+          const uint32_t word[4] = {c.x, c.y, c.z, c.w};
           uint8_t* dst = G.v + half * (kBuf / 2) + key * 128;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -435,6 +448,7 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         softmax(ok ? 0xffffu : 0u, false);
         if (dead) break;
         product(kValues, tO, sp, 0u, !fresh, &S.o_done[g]);
+        add_rows(false);
         fresh = false;
         ok = okn;
       }
@@ -444,20 +458,22 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       if (group_any(g, dead)) break;
       bring(A.Rv_back + (size_t)p.h * kRT5Halves);
       sum_rows();
+#pragma unroll 1
+      for (int c0 = 0; c0 < 16 * nc; c0 += 16) {
+        uint32_t o[16];
+        tc05::tmem_ld16(tO + lanes + c0, o);
+        tc05::tmem_wait_ld();
 #pragma unroll
-      for (int c0 = 0; c0 < N; c0 += 16)
-        if (c0 < 16 * nc) {
-          uint32_t o[16];
-          tc05::tmem_ld16(tO + lanes + c0, o);
-          tc05::tmem_wait_ld();
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float L = G.l[c0 + j], inv = L > 0.f ? 1.f / L : 0.f;
-            *reinterpret_cast<uint16_t*>(G.p + at16<N>(c0 + j, key)) =
-                half_bits(__uint_as_float(o[j]) * inv, false);
-            l[c0 + j] = key == 0 && L > 0.f ? 64.f : 0.f;  // O is now 64 of weight 2^m l / 64
-          }
+        for (int j = 0; j < 16; j += 2) {
+          const float L0 = G.l[c0 + j], L1 = G.l[c0 + j + 1];
+          const uint32_t e = pack16(L0 > 0.f ? __fdividef(__uint_as_float(o[j]), L0) : 0.f,
+                                    L1 > 0.f ? __fdividef(__uint_as_float(o[j + 1]), L1) : 0.f, false);
+          *reinterpret_cast<uint16_t*>(G.p + c0 * 128 + at16<N>(j, key)) = (uint16_t)e;
+          *reinterpret_cast<uint16_t*>(G.p + c0 * 128 + at16<N>(j + 1, key)) = (uint16_t)(e >> 16);
         }
+      }
+      if (lrow < N)  // O is now 64 of weight 2^m l / 64
+        l = lpart == 0 && G.l[lrow] > 0.f ? 64.f : 0.f;
       for (int c = key; c < 16 * nc; c += 128)
         if (G.l[c] > 0.f) G.m[c] += __log2f(G.l[c]) - 6.f;
       wait(&S.t_done[g], nt++);
@@ -494,6 +510,7 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         }
       }
       product(kValues, tO, sp, tc05::kIdescBf16, !fresh, &S.o_done[g]);
+      add_rows(true);
       fresh = false;
     }
     if (dead) break;
@@ -503,25 +520,23 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     sum_rows();
     const bool whole = p.t1 - p.t0 == p.total;
     float* part = part_of(A, w, p.t0 > 0);
+#pragma unroll 1
+    for (int c0 = 0; c0 < 16 * nc; c0 += 16) {
+      uint32_t o[16];
+      tc05::tmem_ld16(tO + lanes + c0, o);
+      tc05::tmem_wait_ld();
 #pragma unroll
-    for (int c0 = 0; c0 < N; c0 += 16)
-      if (c0 < 16 * nc) {
-        uint32_t o[16];
-        tc05::tmem_ld16(tO + lanes + c0, o);
-        tc05::tmem_wait_ld();
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int r = c0 + j;
-          if (r < rows) {
-            const float x = __uint_as_float(o[j]), L = G.l[r];
-            if (whole)
-              A.out[(((size_t)p.c0 + r / 4) * 4 * A.h_kv + 4 * p.h + r % 4) * kD + key] =
-                  __float2bfloat16_rn(L > 0.f ? x / L : 0.f);
-            else
-              part[(size_t)r * kD + key] = x;
-          }
-        }
+      for (int j = 0; j < 16; ++j) {
+        const int r = c0 + j;
+        if (r >= rows) continue;
+        const float x = __uint_as_float(o[j]), L = G.l[r];
+        if (whole)
+          A.out[(((size_t)p.c0 + r / 4) * 4 * A.h_kv + 4 * p.h + r % 4) * kD + key] =
+              __float2bfloat16_rn(L > 0.f ? __fdividef(x, L) : 0.f);
+        else
+          part[(size_t)r * kD + key] = x;
       }
+    }
     if (!whole)
       for (int r = key; r < rows; r += 128) {
         part[(size_t)A.rows * kD + r] = G.m[r];
