@@ -63,6 +63,7 @@ struct Smem {
   // rows that do not count are cleared
   uint64_t k_full[kRing], k_tma[kRing], k_empty[kRing];
   uint64_t v_full[kRing], v_tma[kRing], v_empty[kRing];
+  uint64_t k_grant[kRing], v_grant[kRing];  // a slot is the dequantizing warps'
   uint64_t piece_full[kPieces], piece_empty[kPieces];
   uint64_t s_full[2], p_ready[2], o_full[2], q_ready[2], q_full, q_empty, drained;
   uint32_t tmem;
@@ -225,6 +226,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
       tc05::bar_init(&S.v_full[s], 128);
       tc05::bar_init(&S.v_tma[s], 1);
       tc05::bar_init(&S.v_empty[s], 1);
+      tc05::bar_init(&S.k_grant[s], 1);
+      tc05::bar_init(&S.v_grant[s], 1);
     }
     for (int i = 0; i < kPieces; ++i) {
       tc05::bar_init(&S.piece_full[i], 1);
@@ -390,7 +393,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
     // tiles, which TMA brings, it clears the values that do not count (0 times
     // what lies there need not be 0)
     const int key = tid - 32 * kDeqWarp;
-    uint32_t nk = 0, nv = 0, tma[kRing] = {0, 0};
+    uint32_t nk = 0, nv = 0, tma[kRing] = {0, 0}, grants[2][kRing] = {};
     bool dead = false;
     auto wait = [&](uint64_t* bar, uint32_t phase) {
       if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
@@ -454,7 +457,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
 #pragma unroll 1
         for (int kind = 0; kind < 2; ++kind) {
           const uint32_t e = kind ? nv : nk;
-          if (e >= kRing && !wait(kind ? &S.v_empty[e % kRing] : &S.k_empty[e % kRing], e / kRing - 1))
+          if (!wait(kind ? &S.v_grant[e % kRing] : &S.k_grant[e % kRing], grants[kind][e % kRing]++))
             break;
           if (!kind && lane == 0) S.mask[nk % 4][key >> 5] = bits;
           const uint4* raw = &S.raw[tile & 1][2 * kind][key];
@@ -509,9 +512,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
     cp_async_wait<0>();
   } else if (warp == kTmaWarp || warp == kTmaWarp + 1) {
     // ------------------------------------------------------------ TMA
-    // one warp for the queries and keys, one for the values and R_v^T.  Every
-    // phase of a tile's `empty` is waited for, those of dequantized tiles too:
-    // a wait tells a phase from the next, not from the next but one.
+    // One warp for the queries, keys and R_k, one for the values and R_v^T.  They
+    // alone wait for the ring's slots, every phase in turn, and grant the
+    // dequantizing warps theirs: a wait tells a phase from the next but not from
+    // the next but one, and whoever waited for some of the phases only could miss
+    // two.
     const bool values = warp != kTmaWarp;
     uint64_t* const empty = values ? S.v_empty : S.k_empty;
     uint64_t* const full = values ? S.v_tma : S.k_tma;
@@ -553,7 +558,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
         load_q(p);
         // hi and lo of R_k
         bring(A.Rk_query + (size_t)p.h * kRT5Halves + (values ? kD * kD : 0));
-        for (int t = 0; t < nint && free_slot(); ++t) ++step;
+        for (int t = 0; t < nint && free_slot(); ++t, ++step) {
+          if (lane == 0) tc05::bar_arrive(values ? &S.v_grant[step % kRing] : &S.k_grant[step % kRing]);
+          __syncwarp();
+        }
         if (values) bring(A.Rv_back + (size_t)p.h * kRT5Halves);  // hi of 64 R_v^T
       }
       for (int t = 0; t < nother && free_slot(); ++t) {
@@ -584,29 +592,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
     __syncwarp();
   } else if (warp == kPlanWarp) {
     // ---------------------------------------------------------- pieces
-    if (w == 0) report_sequences(A);
-    PieceFinder next;
-    next.start(A, w);
-    ChunkSeg seg{};
-    bool more = true;
-    for (uint32_t n = 0; more; ++n) {
-      const uint32_t i = n % kPieces;
-      Piece p;
-      p.t0 = p.t1 = 0;
-      while (next.f < next.f1 && p.t1 == p.t0) next.next(A, p);
-      more = p.t1 > p.t0;
-      if (more && p.t0 == 0 && p.t1 < p.total)
-        seg = ChunkSeg{next.F, next.f_seg + kBegin + p.total, p.c0, p.n_new, p.h, p.qb, next.W, 1};
-      if (n >= kPieces && !__all_sync(0xffffffffu, tc05::bar_wait_spin(&S.piece_empty[i],
-                                                                       (n / kPieces - 1) & 1, abort)))
-        break;
-      if (lane == 0) {
-        S.piece[i] = p;
-        tc05::bar_arrive(&S.piece_full[i]);
-      }
-      __syncwarp();
-    }
-    if (lane == 0) A.seg[w] = seg;
+    find_pieces<kPieces>(A, w, S.piece, S.piece_full, S.piece_empty, abort);
   } else {
     // ------------------------------------------------------------ MMA
     if (warp == kMmaWarp) {
@@ -729,8 +715,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
 
 // ------------------------------------------------------------- combine
 
-// Joins the partials of the segments that several workers had a part in: CTA
-// (w, y) rows kRows y .. of the one that worker w began.  A thread has 4 channels
+// Joins the partials of the segments that several CTAs had a part in: CTA
+// (w, y) rows kRows y .. of the one that CTA w began.  A thread has 4 channels
 // of a row and every kSplit-th part: a prefill's segments are of two or three
 // parts and many rows (kSplit 1), those of a few tokens over a long context of
 // many parts and few rows (kSplit 4).  The CTAs also clear the rows of sequences
@@ -823,7 +809,7 @@ ChunkLayout chunk_layout(const optr_params* p, int max_new) {
   l.rows = chunk_small_rows(max_new);
   l.small = l.rows > 0;
   if (!l.small) l.rows = max_new > 32 ? 256 : 128;
-  l.W = p->num_sms * (l.small ? chunk_small_groups(l.rows) : 1);
+  l.W = p->num_sms;
   l.part = round_up(sizeof(ChunkSeg) * (size_t)l.W);
   l.total = l.part + round_up(2 * (size_t)l.W * part_floats(l.rows) * sizeof(float));
   return l;

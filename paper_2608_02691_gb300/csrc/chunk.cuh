@@ -6,6 +6,7 @@
 
 #include "decode_common.cuh"
 #include "optr_internal.cuh"
+#include "tc05.cuh"
 
 namespace optr {
 
@@ -27,7 +28,7 @@ struct ChunkArgs {
   struct ChunkSeg* seg;  // [W] segments begun by a CTA and ended by another
   float* part;           // partial results
   int rows;              // rows of a partial
-  int W;                 // workers: CTAs of chunk_kernel, warpgroups of chunk_small_kernel
+  int W;                 // CTAs
   bool out32;            // out is 32-byte aligned
 };
 
@@ -36,7 +37,7 @@ struct ChunkArgs {
 struct ChunkSeg {
   long long F, end;
   int c0, n_new, h, qb;
-  int W;              // workers that the line is cut for
+  int W;              // ranges that the line is cut into
   int valid;
 };
 
@@ -104,7 +105,7 @@ __device__ __forceinline__ long long seq_cost(const SeqWork& s) {
 }
 
 // The flat index space orders units of cost as (sequence, KV head, query block,
-// unit); worker w takes [w F / W, (w + 1) F / W).  Of a block's kBegin + tiles units
+// unit); CTA w takes [w F / W, (w + 1) F / W).  Of a block's kBegin + tiles units
 // the first kBegin stand for no tile.  One warp goes through a CTA's range: lane
 // i holds sequence b0 + i.
 struct PieceFinder {
@@ -199,17 +200,47 @@ __device__ __forceinline__ void report_sequences(const ChunkArgs& A) {
 
 // A partial: O, [32 channel groups][rows][4] from chunk_kernel and [rows][128]
 // from chunk_small_kernel (as their threads hold it), then m [rows] and l [rows].
-// Worker w (a CTA, or a warpgroup of chunk_small_kernel) has two: of a segment begun by an earlier CTA, and of one that a later
+// CTA w has two: of a segment begun by an earlier CTA, and of one that a later
 // CTA ends.
 __host__ __device__ constexpr size_t part_floats(int rows) { return (size_t)rows * (kD + 2); }
 __device__ __forceinline__ float* part_of(const ChunkArgs& A, int w, bool begun) {
   return A.part + (2 * (size_t)w + (begun ? 1 : 0)) * part_floats(A.rows);
 }
 
+// A CTA's warp that finds its pieces for the others, kAhead ahead: a piece
+// without tiles ends them.
+template <int kAhead>
+__device__ __forceinline__ void find_pieces(const ChunkArgs& A, int w, Piece* piece, uint64_t* full,
+                                            uint64_t* empty, volatile int* abort) {
+  const int lane = threadIdx.x & 31;
+  if (w == 0) report_sequences(A);
+  PieceFinder next;
+  next.start(A, w);
+  ChunkSeg seg{};
+  bool more = true;
+  for (uint32_t n = 0; more; ++n) {
+    const uint32_t i = n % kAhead;
+    Piece p;
+    p.t0 = p.t1 = 0;
+    while (next.f < next.f1 && p.t1 == p.t0) next.next(A, p);
+    more = p.t1 > p.t0;
+    if (more && p.t0 == 0 && p.t1 < p.total)
+      seg = ChunkSeg{next.F, next.f_seg + kBegin + p.total, p.c0, p.n_new, p.h, p.qb, next.W, 1};
+    if (n >= kAhead &&
+        !__all_sync(0xffffffffu, tc05::bar_wait_spin(&empty[i], (n / kAhead - 1) & 1, abort)))
+      break;
+    if (lane == 0) {
+      piece[i] = p;
+      tc05::bar_arrive(&full[i]);
+    }
+    __syncwarp();
+  }
+  if (lane == 0) A.seg[w] = seg;
+}
+
 // chunk_small.cu: rows of its query operand for up to max_new tokens (0: too
-// many), its warpgroups per CTA with so many rows, and the launch.
+// many), and the launch.
 int chunk_small_rows(int max_new);
-int chunk_small_groups(int rows);
 cudaError_t launch_chunk_small(const optr_params* p, const ChunkArgs& A, const __nv_bfloat16* q,
                                const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mw,
                                cudaStream_t s);
