@@ -31,6 +31,7 @@ constexpr uint32_t kOperand = 2 * kHalf;
 constexpr float kSlack = 8.f;
 constexpr int kRing = 2;
 constexpr int kPieces = 3;  // pieces found ahead
+constexpr int kRaw = 4;     // tiles of records
 // Warpgroups: two of softmax, two of keys and values, one of two TMA warps, the
 // MMA warp and the one that finds the CTA's pieces.
 constexpr int kDeqWarp = 8, kTmaWarp = 16, kMmaWarp = 18, kPlanWarp = 19;
@@ -40,21 +41,20 @@ static_assert(2 * kRegSoftmax + 2 * kRegDeq + kRegIssue <= 5 * kRegLaunch, "regi
 
 template <int N>
 struct Smem {
-  uint8_t k[kRing][kOperand];
+  uint8_t k[kRing][kOperand];    // keys by TMA, R_k (dequantized keys: tensor memory)
   uint8_t v[kRing][kOperand];
   uint8_t q[N * kD * 2];         // queries [row][channel or place], two halves of 64
   // probabilities [row][key] by softmax group; O [row][place] for its rotation;
   // at a piece's end both together are the second group's O, float [row][channel]
   uint8_t p[2][N * kTile * 2];
-  // INT2 records of the tiles: [group][buffer][keys, values][page] codes, {scale, min}
-  uint8_t raw[2][2][2][8][768];
+  uint8_t raw[kRaw][8][kChunk];  // records of the tiles' pages, as in the pool
   uint32_t mask[4][4];           // INT2 tiles: keys whose page is in range (as in chunk.cu)
   alignas(16) float mul[2][N], add[2][N];  // logit over the maximum = S mul + add
   float quarter[2][4][N];        // of a group's four warps
   float m[2][N], l[2][N], d[2][N], off[N], scale[N];
   Piece piece[kPieces];
   uint64_t piece_full[kPieces], piece_empty[kPieces];
-  uint64_t raw_full[2][2], raw_empty[2][2];
+  uint64_t raw_full[kRaw], raw_empty[kRaw];
   uint64_t k_full[kRing], k_tma[kRing], k_empty[kRing];
   uint64_t v_full[kRing], v_tma[kRing], v_empty[kRing];
   uint64_t k_grant[2][kRing], v_grant[2][kRing];  // a slot is the dequantizing group's
@@ -118,7 +118,8 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
                    const __grid_constant__ CUtensorMap tm_win, const __nv_bfloat16* __restrict__ q_in,
                    const float* __restrict__ mu, const uint16_t* __restrict__ Rk_row,
                    const __grid_constant__ ChunkArgs A) {
-  constexpr uint32_t kCols = N == 16 ? 64 : N == 32 ? 128 : 256;  // S[2], O[2]
+  constexpr uint32_t kColK = 4 * N;                 // after S[2], O[2]: keys by slot, 64 each
+  constexpr uint32_t kCols = N <= 32 ? 256 : 512;
   extern __shared__ __align__(1024) unsigned char dsm_[];
   Smem<N>& S = *reinterpret_cast<Smem<N>*>(dsm_);
   const int tid = threadIdx.x, lane = tid & 31;
@@ -136,15 +137,15 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         tc05::bar_init(&S.v_grant[g][s], 1);
       }
     }
+    for (int i = 0; i < kRaw; ++i) {
+      tc05::bar_init(&S.raw_full[i], 1);
+      tc05::bar_init(&S.raw_empty[i], 4);
+    }
     for (int i = 0; i < kPieces; ++i) {
       tc05::bar_init(&S.piece_full[i], 1);
       tc05::bar_init(&S.piece_empty[i], kPlanWarp);
     }
     for (int g = 0; g < 2; ++g) {
-      tc05::bar_init(&S.raw_full[g][0], 1);
-      tc05::bar_init(&S.raw_full[g][1], 1);
-      tc05::bar_init(&S.raw_empty[g][0], 4);
-      tc05::bar_init(&S.raw_empty[g][1], 4);
       tc05::bar_init(&S.s_full[g], 1);
       tc05::bar_init(&S.p_ready[g], 4);
       tc05::bar_init(&S.o_full[g], 1);
@@ -529,9 +530,9 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     // warps grant them; of the tiles that TMA brings, the group of the slot clears
     // the values that do not count.
     const int g = (warp - kDeqWarp) >> 2, quarter = warp & 3, key = tid & 127;
-    uint32_t nk = 0, nv = 0, nt = 0, mine = 0, fetched = 0, tma = 0;
+    const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
+    uint32_t nk = 0, nv = 0, nt = 0, tma = 0;
     const int ms = meta_stride(A.compact);
-    const uint32_t meta = 16 * ms;
     uint32_t gk[kRing] = {0, 0}, gv[kRing] = {0, 0};  // grants seen
     Piece p;
     for (uint32_t n = 0; next_piece(n, p); ++n) {
@@ -539,86 +540,79 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       nk += nint > 0;  // R_k
       // the group's first INT2 tile of the piece
       const int t0 = (int)((nt ^ g) & 1);
-      // A tile's records into a raw buffer, both kinds; lanes 0 .. 7 of the
-      // group's first warp have a page each, lanes 8 .. 15 its values
-      auto fetch = [&](int t) {
-        if (t >= nint || quarter != 0) return;
-        const uint32_t buf = fetched & 1;
-        if (fetched >= 2 && !wait(&S.raw_empty[g][buf], fetched / 2 - 1)) return;
-        ++fetched;
-        int page = -1;
-        const int i = lane & 7, pos = (p.t0 + t) * kTile + 16 * i;
-        if (lane < 16 && pos < p.n_int)
-          page = __ldcg(A.bt + (size_t)p.b * A.max_pages + (A.sink + pos) / kPage);
-        const bool in = page >= 0 && page < A.num_pages;
-        const uint32_t copies = __popc(__ballot_sync(0xffffffffu, in));
-        if (lane == 0) tc05::bar_arrive_expect_tx(&S.raw_full[g][buf], copies * (512 + meta));
-        __syncwarp();
-        if (in) {
-          const int kind = lane >> 3;
-          const uint8_t* x = A.pool + ((size_t)page * A.h_kv + p.h) * chunk_bytes(A.compact);
-          uint8_t* to = S.raw[g][buf][kind][i];
-          tc05::bulk_g2s(to, x + (kind ? OPTR_V_CODES_OFFSET : OPTR_K_CODES_OFFSET), 512,
-                         &S.raw_full[g][buf]);
-          tc05::bulk_g2s(to + 512, x + (kind ? vmeta_offset(A.compact) : OPTR_K_META_OFFSET), meta,
-                         &S.raw_full[g][buf]);
-        }
-        __syncwarp();
-      };
       auto request = [&](int t) {
         const int pos = (p.t0 + t) * kTile + key;
         return t < nint && pos < p.n_int
                    ? __ldcg(A.bt + (size_t)p.b * A.max_pages + (A.sink + pos) / kPage) : -1;
       };
-      fetch(t0);
-      fetch(t0 + 2);
       int page = request(t0);
       for (int t = 0; t < nint; ++t, ++nk, ++nv, ++nt) {
         if (t % 2 != t0) continue;
-        if (!wait(&S.k_grant[g][nk % kRing], gk[nk % kRing]++)) break;
-        const uint32_t buf = mine & 1;
+        const uint32_t slot = nt % kRaw;
         const bool inside = (p.t0 + t) * kTile + key < p.n_int;
         const bool ok = inside && page >= 0 && page < A.num_pages;
         if (inside && !ok) atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
         page = request(t + 2);
         const uint32_t bits = __ballot_sync(0xffffffffu, ok || !inside);
-        if (lane == 0) S.mask[nk % 4][quarter] = bits;
-        if (!wait(&S.raw_full[g][buf], mine >> 1)) break;
-        ++mine;
-#pragma unroll 1
-        for (int kind = 0; kind < 2; ++kind) {
-          if (kind && !wait(&S.v_grant[g][nv % kRing], gv[nv % kRing]++)) break;
-          const uint8_t* raw = S.raw[g][buf][kind][key / kPage];
-          uint4 mm = make_uint4(0u, 0u, 0u, 0u);  // a row of zeros where the key does not count
+        if (!wait(&S.raw_full[slot], nt / kRaw)) break;
+        const uint8_t* raw = S.raw[slot][key / kPage];
+        // the codes of one kind, the halves read in an order that keeps eight
+        // lanes' pieces, 32 B apart, in different banks; and the metadata
+        auto codes = [&](int kind, uint4 (&c)[2]) {
+          const uint8_t* x = raw + (kind ? OPTR_V_CODES_OFFSET : OPTR_K_CODES_OFFSET) + 32 * (key % kPage);
+          const int first = key >> 2 & 1;
+          const uint4 a = *reinterpret_cast<const uint4*>(x + 16 * first);
+          const uint4 b = *reinterpret_cast<const uint4*>(x + 16 * (1 - first));
+          c[0] = first ? b : a;
+          c[1] = first ? a : b;
+        };
+        auto pairs = [&](int kind) {  // zero where the key does not count: a row of zeros
+          const uint8_t* x = raw + (kind ? vmeta_offset(A.compact) : OPTR_K_META_OFFSET) + ms * (key % kPage);
+          uint4 mm = make_uint4(0u, 0u, 0u, 0u);
           if (ok) {
-            const uint8_t* x = raw + 512 + ms * (key % kPage);
             if (A.compact)
               mm.x = mm.y = mm.z = mm.w = *reinterpret_cast<const uint32_t*>(x);
             else
               mm = *reinterpret_cast<const uint4*>(x);
           }
-          const SlotMeta sm = slot_meta(mm.x, mm.y, mm.z, mm.w);
-          uint8_t* dst = (kind ? S.v[nv % kRing] : S.k[nk % kRing]) + key * 128;
+          return slot_meta(mm.x, mm.y, mm.z, mm.w);
+        };
+        if (!wait(&S.k_grant[g][nk % kRing], gk[nk % kRing]++)) break;
+        if (lane == 0) S.mask[nk % 4][quarter] = bits;
+        uint4 c[2];
+        codes(0, c);
+        const SlotMeta km = pairs(0);
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const uint4 c = *reinterpret_cast<const uint4*>(raw + 32 * (key % kPage) + 16 * half);
-            const uint32_t word[4] = {c.x, c.y, c.z, c.w};
+        for (int half = 0; half < 2; ++half) {
+          const uint32_t word[4] = {c[half].x, c[half].y, c[half].z, c[half].w};
+          uint32_t x[32];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t x[8];
-              dequant_word(word[i], sm, x);
-              *reinterpret_cast<uint4*>(dst + half * kHalf + (((2 * i) ^ (key & 7)) << 4)) =
-                  make_uint4(x[0], x[1], x[2], x[3]);
-              *reinterpret_cast<uint4*>(dst + half * kHalf + (((2 * i + 1) ^ (key & 7)) << 4)) =
-                  make_uint4(x[4], x[5], x[6], x[7]);
-            }
-          }
-          tc05::fence_proxy_async();
-          tc05::bar_arrive(kind ? &S.v_full[nv % kRing] : &S.k_full[nk % kRing]);
+          for (int i = 0; i < 4; ++i) dequant_word(word[i], km, reinterpret_cast<uint32_t(&)[8]>(x[8 * i]));
+          tc05::tmem_st32(tmem + lanes + kColK + 64 * (nk % kRing) + 32 * half, x);
         }
-        if (dead) break;
-        arrive(&S.raw_empty[g][buf]);
-        fetch(t + 4);
+        tc05::tmem_wait_st();
+        tc05::fence_before();
+        tc05::bar_arrive(&S.k_full[nk % kRing]);
+        if (!wait(&S.v_grant[g][nv % kRing], gv[nv % kRing]++)) break;
+        codes(1, c);
+        const SlotMeta vm = pairs(1);
+        uint8_t* dst = S.v[nv % kRing] + key * 128;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const uint32_t word[4] = {c[half].x, c[half].y, c[half].z, c[half].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t x[8];
+            dequant_word(word[i], vm, x);
+            *reinterpret_cast<uint4*>(dst + half * kHalf + (((2 * i) ^ (key & 7)) << 4)) =
+                make_uint4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<uint4*>(dst + half * kHalf + (((2 * i + 1) ^ (key & 7)) << 4)) =
+                make_uint4(x[4], x[5], x[6], x[7]);
+          }
+        }
+        tc05::fence_proxy_async();
+        tc05::bar_arrive(&S.v_full[nv % kRing]);
+        arrive(&S.raw_empty[slot]);
       }
       if (dead) break;
       nk += nother;
@@ -642,21 +636,16 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         tc05::bar_arrive(&S.v_full[st]);
       }
     }
-    // copies in flight land before the CTA exits
-    for (uint32_t b = 0; b < 2; ++b) {
-      const uint32_t uses = (fetched + 1 - b) / 2;
-      if (uses > 0) tc05::bar_wait_drain(&S.raw_full[g][b], (uses - 1) & 1);
-    }
   } else if (warp == kTmaWarp || warp == kTmaWarp + 1) {
     // ------------------------------------------------------------ TMA
-    // One warp for the keys and R_k, one for the values and R_v^T.  They alone wait
+    // One warp for the records, keys and R_k, one for the values and R_v^T.  They alone wait
     // for the ring's slots, every phase in turn, and grant the dequantizing groups
     // theirs: a wait tells a phase from the next but not from the next but one,
     // and whoever waited for some of the phases only could miss two.
     const bool values = warp != kTmaWarp;
     uint64_t* const empty = values ? S.v_empty : S.k_empty;
     uint64_t* const full = values ? S.v_tma : S.k_tma;
-    uint32_t step = 0, nt = 0, pending[kRing] = {0, 0};
+    uint32_t step = 0, nt = 0, fetched = 0, pending[kRing] = {0, 0};
     auto free_slot = [&]() {
       return !dead && (step < kRing || wait(&empty[step % kRing], step / kRing - 1));
     };
@@ -675,8 +664,43 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const int nint = p.int_tiles(), nother = p.t1 - p.t0 - nint;
       if (nint > 0) {
         if (!values) bring(Rk_row + (size_t)p.h * kD * kD);
-        for (int t = 0; t < nint && free_slot(); ++t, ++step, ++nt)
-          arrive(values ? &S.v_grant[nt & 1][step % kRing] : &S.k_grant[nt & 1][step % kRing]);
+        // INT2 tiles: records two tiles ahead, the pages' entries three
+        auto request = [&](int t) {
+          const int pos = (p.t0 + t) * kTile + 16 * lane;
+          return t < nint && lane < 8 && pos < p.n_int
+                     ? __ldcg(A.bt + (size_t)p.b * A.max_pages + (A.sink + pos) / kPage) : -1;
+        };
+        auto fetch = [&](int t, int page) {
+          if (t >= nint || dead) return;
+          const uint32_t i = nt + t, slot = i % kRaw, bytes = chunk_bytes(A.compact);
+          if (i >= kRaw && !wait(&S.raw_empty[slot], i / kRaw - 1)) return;
+          const bool in = page >= 0 && page < A.num_pages;
+          const uint32_t copies = __popc(__ballot_sync(0xffffffffu, in));
+          if (lane == 0) tc05::bar_arrive_expect_tx(&S.raw_full[slot], copies * bytes);
+          __syncwarp();
+          if (in)
+            tc05::bulk_g2s(S.raw[slot][lane], A.pool + ((size_t)page * A.h_kv + p.h) * bytes, bytes,
+                           &S.raw_full[slot]);
+          __syncwarp();
+          fetched = i + 1;
+        };
+        int page = -1;
+        if (!values) {
+          const int e0 = request(0), e1 = request(1);
+          page = request(2);
+          fetch(0, e0);
+          fetch(1, e1);
+        }
+        for (int t = 0; t < nint; ++t, ++step) {
+          if (!values) {
+            fetch(t + 2, page);
+            page = request(t + 3);
+          }
+          if (!free_slot()) break;
+          const uint32_t g = (nt + t) & 1;
+          arrive(values ? &S.v_grant[g][step % kRing] : &S.k_grant[g][step % kRing]);
+        }
+        nt += nint;
         if (values) bring(A.Rv_back + (size_t)p.h * kRT5Halves);  // hi of 64 R_v^T
       }
       for (int t = 0; t < nother && free_slot(); ++t) {
@@ -698,8 +722,11 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         ++pending[st];
       }
     }
-    for (int s = 0; s < kRing; ++s)  // copies in flight land before the CTA exits
+    // copies in flight land before the CTA exits
+    for (int s = 0; s < kRing; ++s)
       if (pending[s]) tc05::bar_wait_drain(&full[s], (pending[s] - 1) & 1);
+    for (uint32_t i = fetched > kRaw ? fetched - kRaw : 0; i < fetched; ++i)
+      tc05::bar_wait_drain(&S.raw_full[i % kRaw], i / kRaw & 1);
     __syncwarp();
   } else if (warp == kPlanWarp) {
     // ---------------------------------------------------------- pieces
@@ -724,12 +751,18 @@ chunk_small_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       used = true;
       bool add[2] = {false, false};
       auto qk = [&](int s, uint32_t type) {
-        const uint32_t a = sk + nk % kRing * kOperand;
+        const uint32_t a = sk + nk % kRing * kOperand, t = tmem + kColK + nk % kRing * 64;
+        if (type) {
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-          tc05::mma_ss_warp(tmem + s * N,
-                            tc05::smem_desc_sw128(a + (ks >> 2) * kHalf + (ks & 3) * 32, 16),
-                            rows_desc(sq, ks), id | type, ks != 0);
+          for (int ks = 0; ks < 8; ++ks)
+            tc05::mma_ss_warp(tmem + s * N,
+                              tc05::smem_desc_sw128(a + (ks >> 2) * kHalf + (ks & 3) * 32, 16),
+                              rows_desc(sq, ks), id | type, ks != 0);
+        } else {
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks)
+            tc05::mma_ts_warp(tmem + s * N, t + 8 * ks, rows_desc(sq, ks), id, ks != 0);
+        }
         tc05::mma_commit_warp(&S.s_full[s]);
         tc05::mma_commit_warp(&S.k_empty[nk++ % kRing]);
       };
