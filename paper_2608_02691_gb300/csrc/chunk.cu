@@ -34,13 +34,13 @@ namespace {
 
 // ----------------------------------------------------------- attention
 
-// Warpgroups: two of softmax, one of keys and values, one of two TMA
-// warps, the MMA warp and the one that finds the CTA's pieces.  Registers a thread after the split (65536 in all, as launched):
-// a softmax thread holds a whole row of 128 logits.
-constexpr int kDeqWarp = 8, kTmaWarp = 12, kMmaWarp = 14, kPlanWarp = 15;
-constexpr int kThreads = 512;
-constexpr int kRegSoftmax = 192, kRegDeq = 72, kRegIssue = 56;
-static_assert(2 * kRegSoftmax + kRegDeq + kRegIssue == 4 * 128, "registers of the launch");
+// Warpgroups: two of softmax, two of keys and values, one of two TMA warps, the
+// MMA warp and the one that finds the CTA's pieces.  Registers a thread after the
+// split, of the launch's 640 x 96.
+constexpr int kDeqWarp = 8, kTmaWarp = 16, kMmaWarp = 18, kPlanWarp = 19;
+constexpr int kThreads = 640;
+constexpr int kRegLaunch = 96, kRegSoftmax = 128, kRegDeq = 72, kRegIssue = 72;
+static_assert(2 * kRegSoftmax + 2 * kRegDeq + kRegIssue <= 5 * kRegLaunch, "registers of the launch");
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 0, kColO = 256;  // S[g] (and P[g]) at 128 g, O[g] at 256 + 128 g
 constexpr int kRing = 2;
@@ -53,17 +53,22 @@ struct Smem {
   uint8_t q[2][kOperand];            // the query operand, by tile
   uint8_t k[kRing][kOperand];        // keys by tile
   uint8_t v[kRing][kOperand];        // values by tile; R_v^T
-  uint4 raw[2][6][128];              // INT2 records as read: codes and metadata, by key
+  uint8_t raw[2][8][kChunk];         // records of a tile's pages, as in the pool
   // INT2 tiles: keys whose page is in range.  Read between the tile's logits
   // and its probabilities: by when K of tile t + 4 may be written, the logits of
   // t + 2 are done, so the probabilities of t + 1.
   alignas(16) uint32_t mask[4][4];
+  // what the first softmax group tells the second of a query tile that they
+  // share, and the second the first of its part of the output
+  float scale[128], off[128];
+  float2 ml[128];
   Piece piece[kPieces];
   // dequantized, brought by TMA, free again; v_full also after v_tma, once the
   // rows that do not count are cleared
   uint64_t k_full[kRing], k_tma[kRing], k_empty[kRing];
   uint64_t v_full[kRing], v_tma[kRing], v_empty[kRing];
-  uint64_t k_grant[kRing], v_grant[kRing];  // a slot is the dequantizing warps'
+  uint64_t k_grant[2][kRing], v_grant[2][kRing];  // a slot is the dequantizing group's
+  uint64_t raw_full[2], raw_empty[2], second_ready, joined;
   uint64_t piece_full[kPieces], piece_empty[kPieces];
   uint64_t s_full[2], p_ready[2], o_full[2], q_ready[2], q_full, q_empty, drained;
   uint32_t tmem;
@@ -226,8 +231,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
       tc05::bar_init(&S.v_full[s], 128);
       tc05::bar_init(&S.v_tma[s], 1);
       tc05::bar_init(&S.v_empty[s], 1);
-      tc05::bar_init(&S.k_grant[s], 1);
-      tc05::bar_init(&S.v_grant[s], 1);
+      for (int g = 0; g < 2; ++g) {
+        tc05::bar_init(&S.k_grant[g][s], 1);
+        tc05::bar_init(&S.v_grant[g][s], 1);
+      }
     }
     for (int i = 0; i < kPieces; ++i) {
       tc05::bar_init(&S.piece_full[i], 1);
@@ -238,7 +245,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
       tc05::bar_init(&S.p_ready[g], 4);
       tc05::bar_init(&S.o_full[g], 1);
       tc05::bar_init(&S.q_ready[g], 4);
+      tc05::bar_init(&S.raw_full[g], 1);
+      tc05::bar_init(&S.raw_empty[g], 4);
     }
+    tc05::bar_init(&S.second_ready, 4);
+    tc05::bar_init(&S.joined, 4);
     tc05::bar_init(&S.q_full, 1);
     tc05::bar_init(&S.q_empty, 1);
     tc05::bar_init(&S.drained, 1);
@@ -251,17 +262,25 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
   tc05::fence_before();
   __syncthreads();
   tc05::fence_after();
-  const uint32_t tmem = S.tmem;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, S.tmem, 0);
   volatile int* abort = &S.abort;
   const int w = blockIdx.x;
+  bool dead = false;
+  auto wait = [&](uint64_t* bar, uint32_t phase) {
+    if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
+    tc05::fence_after();
+    return !dead;
+  };
+  auto arrive = [&](uint64_t* bar) {  // the warp
+    __syncwarp();
+    if (lane == 0) tc05::bar_arrive(bar);
+  };
   // the CTA's n-th piece, as every warp but the finder's takes it; false after the last
   auto next_piece = [&](uint32_t n, Piece& p) {
     const uint32_t i = n % kPieces;
-    if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(&S.piece_full[i], n / kPieces & 1, abort)))
-      return false;
+    if (dead || !wait(&S.piece_full[i], n / kPieces)) return false;
     p = S.piece[i];
-    __syncwarp();
-    if (lane == 0) tc05::bar_arrive(&S.piece_empty[i]);
+    arrive(&S.piece_empty[i]);
     return p.t1 > p.t0;
   };
   if (warp < kDeqWarp)
@@ -275,48 +294,51 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
     const int g = warp >> 2, row = 32 * (warp & 3) + lane;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t tS = tmem + lanes + kColS + 128u * g, tO = tmem + lanes + kColO + 128u * g;
-    uint32_t nk = 0, ns = 0, no = 0;  // key tiles of the CTA; S and O phases seen
-    bool dead = false;
-    auto wait = [&](uint64_t* bar, uint32_t phase) {
-      if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
-      tc05::fence_after();
-      return !dead;
-    };
+    uint32_t nk = 0, ns = 0, no = 0, nj = 0;  // key tiles of the CTA; S, O and joining phases
     auto ready = [&]() {  // the warp's rows of P are in tensor memory
       tc05::fence_before();
-      __syncwarp();
-      if (lane == 0) tc05::bar_arrive(&S.p_ready[g]);
+      arrive(&S.p_ready[g]);
     };
     Piece p;
-    for (uint32_t n = 0; !dead && next_piece(n, p); ++n) {
-      const int nint = p.int_tiles(), nother = p.t1 - p.t0 - nint;
-      nk += nint > 0;
-      const uint32_t base = nk;
-      nk += p.t1 - p.t0;
-      const int i0 = p.qb * kQTok + 32 * g;  // the tile's first token
-      if (i0 >= p.n_new) continue;
-      const int i = i0 + (row >> 2), j = row & 3;
+    for (uint32_t n = 0; next_piece(n, p); ++n) {
+      const int all_tiles = p.t1 - p.t0, nint = p.int_tiles();
+      const uint32_t base = nk + (nint > 0);
+      nk = base + all_tiles;
+      // The groups have a query tile each, or alternate key tiles of the one
+      const bool pair = p.q_tiles() == 2;
+      const int stride = pair ? 1 : 2, from = pair ? 0 : g;
+      const int ints = pair ? nint : (nint + 1 - g) / 2;
+      const int tiles = pair ? all_tiles : (all_tiles + 1 - g) / 2;
+      const int i = p.qb * kQTok + (pair ? 32 * g : 0) + (row >> 2), j = row & 3;
       const bool valid = i < p.n_new;
       const size_t at = ((size_t)p.c0 + i) * 4 * A.h_kv + 4 * p.h + j;
       float scale = 0.f, off = 0.f, m = -1e30f, l = 0.f;
-      if (nint > 0) {
+      if (nint > 0 && (pair || g == 0)) {
         if (!wait(&S.s_full[g], ns++)) break;
         rotated_query(tS, S.q[g], row, A.muR + p.h * kD, scale, off);
+        if (!pair) {
+          S.scale[row] = scale;
+          S.off[row] = off;
+        }
         tc05::fence_before();
         tc05::fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) tc05::bar_arrive(&S.q_ready[g]);
+        arrive(&S.q_ready[g]);
       }
       bool fresh = true;
-      for (int t = 0; t < nint; ++t) {
+      for (int k = 0; k < ints; ++k) {
+        const int t = from + stride * k;
         if (!wait(&S.s_full[g], ns++)) break;
+        if (fresh && !pair) {  // (the first group wrote them before these logits)
+          scale = S.scale[row];
+          off = S.off[row];
+        }
         const uint4 mask = *reinterpret_cast<const uint4*>(S.mask[(base + t) % 4]);
         softmax_tile<false>(tS, tO, scale, off, mask, p.n_int - kTile * (p.t0 + t), fresh, m, l);
         fresh = false;
         ready();
       }
       if (dead) break;
-      if (nint > 0) {
+      if (ints > 0) {
         // O / l into the model's basis: the A operand of the product with 64
         // R_v^T takes P's place
         if (!wait(&S.o_full[g], no++)) break;
@@ -338,23 +360,55 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
         }
         ready();
       }
-      for (int t = 0; t < nother; ++t) {
+      for (int k = ints; k < tiles; ++k) {
         if (!wait(&S.s_full[g], ns++)) break;
         // window rows as far as they are filled; own tiles causally
-        const int tile = p.t0 + nint + t - p.I;
+        const int tile = p.t0 + from + stride * k - p.I;
         const int lim = tile < p.Wt ? p.n_win - kTile * tile : i + 1 - kTile * (tile - p.Wt);
         softmax_tile<true>(tS, tO, kLogit, 0.f, make_uint4(~0u, ~0u, ~0u, ~0u), lim, fresh, m, l);
         fresh = false;
         ready();
       }
-      if (dead || !wait(&S.o_full[g], no++)) break;
-      if (p.t1 - p.t0 == p.total) {
+      if (dead || (tiles > 0 && !wait(&S.o_full[g], no++))) break;
+      // The groups' parts of one query tile meet: the second's output is in the
+      // same lanes of tensor memory
+      float u = 1.f, v = 0.f;
+      const bool join = !pair && all_tiles > 1;
+      if (join && g == 1) {
+        S.ml[row] = make_float2(m, l);
+        tc05::fence_before();
+        arrive(&S.second_ready);
+        if (!wait(&S.joined, nj++)) break;
+        continue;
+      }
+      if (!pair && g == 1) continue;
+      if (join) {
+        if (!wait(&S.second_ready, nj++)) break;
+        const float2 o = S.ml[row];
+        const float mn = fmaxf(m, o.x);
+        u = ex2(m - mn);
+        v = ex2(o.x - mn);
+        l = l * u + o.y * v;
+        m = mn;
+      }
+      auto output = [&](int c, uint32_t (&o)[32]) {
+        tc05::tmem_ld32(tO + 32 * c, o);
+        tc05::tmem_wait_ld();
+        if (join) {
+          uint32_t x[32];
+          tc05::tmem_ld32(tO + 128 + 32 * c, x);
+          tc05::tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            o[e] = __float_as_uint(__uint_as_float(o[e]) * u + __uint_as_float(x[e]) * v);
+        }
+      };
+      if (all_tiles == p.total) {
         const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t o[32];
-          tc05::tmem_ld32(tO + 32 * c, o);
-          tc05::tmem_wait_ld();
+          output(c, o);
           if (valid)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -372,8 +426,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           uint32_t o[32];
-          tc05::tmem_ld32(tO + 32 * c, o);
-          tc05::tmem_wait_ld();
+          output(c, o);
           if (valid)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -386,90 +439,76 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
         }
       }
       tc05::fence_before();
+      if (join) arrive(&S.joined);
     }
   } else if (warp < kTmaWarp) {
     // --------------------------------------------------- keys and values
-    // thread = key: dequantizes its key and value of an INT2 tile; of the other
-    // tiles, which TMA brings, it clears the values that do not count (0 times
-    // what lies there need not be 0)
-    const int key = tid - 32 * kDeqWarp;
-    uint32_t nk = 0, nv = 0, tma[kRing] = {0, 0}, grants[2][kRing] = {};
-    bool dead = false;
-    auto wait = [&](uint64_t* bar, uint32_t phase) {
-      if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
-      return !dead;
-    };
+    // The groups take alternate INT2 tiles, thread = key, in slots that the TMA
+    // warps grant them; of the tiles that TMA brings, the group of the slot clears
+    // the values that do not count (0 times what lies there need not be 0).
+    const int g = (warp - kDeqWarp) >> 2, quarter = warp & 3, key = tid & 127;
     const int ms = meta_stride(A.compact);
-    // Records are copied into shared memory two tiles ahead (each thread reads
-    // only what it copied itself), their pages looked up three tiles ahead.
-    auto request = [&](const Piece& p, int t) {
-      const int n = t * kTile + key;
-      return n < p.n_int && t < p.t1
-                 ? __ldcg(A.bt + (size_t)p.b * A.max_pages + (A.sink + n) / kPage) : -1;
-    };
-    auto copy = [&](const Piece& p, int t, int page) {
-      bool ok = t * kTile + key < p.n_int && t < p.t1;
-      if (ok && (page < 0 || page >= A.num_pages)) {
-        atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
-        ok = false;
-      }
-      if (ok) {
-        const uint8_t* rec = A.pool + ((size_t)page * A.h_kv + p.h) * chunk_bytes(A.compact);
-        const int slot = (t * kTile + key) % kPage;  // (sink is a multiple of 16)
-        uint4* d = &S.raw[t & 1][0][key];
-        for (int i = 0; i < 2; ++i) {
-          cp_async16_zfill(d + i * 128, rec + OPTR_K_CODES_OFFSET + 32 * slot + 16 * i, true);
-          cp_async16_zfill(d + (2 + i) * 128, rec + OPTR_V_CODES_OFFSET + 32 * slot + 16 * i, true);
-        }
-        const uint8_t* mk = rec + OPTR_K_META_OFFSET + ms * slot;
-        const uint8_t* mv = rec + vmeta_offset(A.compact) + ms * slot;
-        if (A.compact) {
-          cp_async4(d + 4 * 128, mk);
-          cp_async4(d + 5 * 128, mv);
-        } else {
-          cp_async16_zfill(d + 4 * 128, mk, true);
-          cp_async16_zfill(d + 5 * 128, mv, true);
-        }
-      }
-      cp_async_commit();
-      return ok;
-    };
+    uint32_t nk = 0, nv = 0, nt = 0, raws = 0, tma = 0, grants[2][kRing] = {};
     Piece p;
-    for (uint32_t n = 0; !dead && next_piece(n, p); ++n) {
+    for (uint32_t n = 0; next_piece(n, p); ++n) {
       const int nint = p.int_tiles(), nother = p.t1 - p.t0 - nint;
-      bool okn[2] = {false, false};
-      int page = -1;
-      if (nint > 0) {
-        const int e0 = request(p, p.t0), e1 = request(p, p.t0 + 1);
-        page = request(p, p.t0 + 2);
-        okn[0] = copy(p, p.t0, e0);
-        okn[1] = copy(p, p.t0 + 1, e1);
-        // R_k's parts: one entry of each ring, brought by TMA
-        if (!wait(&S.v_tma[nv % kRing], tma[nv % kRing]++)) break;
-        tc05::bar_arrive(&S.v_full[nv % kRing]);
+      if (nint > 0) {  // R_k's parts: one entry of each ring, brought by TMA
+        if (nv % kRing == g) {
+          if (!wait(&S.v_tma[g], tma++)) break;
+          tc05::bar_arrive(&S.v_full[g]);
+        }
         ++nk, ++nv;
       }
-      for (int t = 0; t < nint && !dead; ++t, ++nk, ++nv) {
-        const int tile = p.t0 + t;
-        cp_async_wait<1>();
-        const bool ok = okn[0];
-        const uint32_t bits = __ballot_sync(0xffffffffu, ok || tile * kTile + key >= p.n_int);
+      auto request = [&](int t) {
+        const int pos = (p.t0 + t) * kTile + key;
+        return t < nint && pos < p.n_int
+                   ? __ldcg(A.bt + (size_t)p.b * A.max_pages + (A.sink + pos) / kPage) : -1;
+      };
+      const int t0 = (int)((nt ^ g) & 1);  // the group's first tile of the piece
+      int page = request(t0);
+      for (int t = 0; t < nint; ++t, ++nk, ++nv, ++nt) {
+        if (t % 2 != t0) continue;
+        const bool inside = (p.t0 + t) * kTile + key < p.n_int;
+        const bool ok = inside && page >= 0 && page < A.num_pages;
+        if (inside && !ok) atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
+        page = request(t + 2);
+        const uint32_t bits = __ballot_sync(0xffffffffu, ok || !inside);
+        if (!wait(&S.raw_full[g], raws++)) break;
+        // Codes and metadata of both kinds, so that the buffer is free at once.  The
+        // halves are read in an order that keeps eight lanes' pieces, 32 B apart,
+        // in different banks.
+        const uint8_t* raw = S.raw[g][key / kPage];
+        const int slot = key % kPage, second = key >> 2 & 1;
+        uint4 c[2][2], mm[2];
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind) {
+          const uint8_t* x = raw + (kind ? OPTR_V_CODES_OFFSET : OPTR_K_CODES_OFFSET) + 32 * slot;
+          const uint4 a = *reinterpret_cast<const uint4*>(x + 16 * second);
+          const uint4 b = *reinterpret_cast<const uint4*>(x + 16 * (1 - second));
+          c[kind][0] = second ? b : a;
+          c[kind][1] = second ? a : b;
+          const uint8_t* y = raw + (kind ? vmeta_offset(A.compact) : OPTR_K_META_OFFSET) + ms * slot;
+          mm[kind] = make_uint4(0u, 0u, 0u, 0u);  // a row of zeros where the key does not count
+          if (ok) {
+            if (A.compact)
+              mm[kind].x = mm[kind].y = mm[kind].z = mm[kind].w = *reinterpret_cast<const uint32_t*>(y);
+            else
+              mm[kind] = *reinterpret_cast<const uint4*>(y);
+          }
+        }
+        arrive(&S.raw_empty[g]);
 #pragma unroll 1
         for (int kind = 0; kind < 2; ++kind) {
-          const uint32_t e = kind ? nv : nk;
-          if (!wait(kind ? &S.v_grant[e % kRing] : &S.k_grant[e % kRing], grants[kind][e % kRing]++))
-            break;
-          if (!kind && lane == 0) S.mask[nk % 4][key >> 5] = bits;
-          const uint4* raw = &S.raw[tile & 1][2 * kind][key];
-          uint8_t* dst = (kind ? S.v[e % kRing] : S.k[e % kRing]) + key * 128;
-          uint4 mm = raw[(4 - kind) * 128];
-          if (A.compact) mm.y = mm.z = mm.w = mm.x;
-          if (!ok) mm = make_uint4(0u, 0u, 0u, 0u);  // a row of zeros, whatever was copied
-          const SlotMeta sm = slot_meta(mm.x, mm.y, mm.z, mm.w);
+          const uint32_t st = (kind ? nv : nk) % kRing;
+          if (!wait(kind ? &S.v_grant[g][st] : &S.k_grant[g][st], grants[kind][st]++)) break;
+          if (!kind && lane == 0) S.mask[nk % 4][quarter] = bits;
+          uint8_t* dst = (kind ? S.v[st] : S.k[st]) + key * 128;
+          const uint4 m = kind ? mm[1] : mm[0];
+          const SlotMeta sm = slot_meta(m.x, m.y, m.z, m.w);
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            const uint4 c = raw[half * 128];
-            const uint32_t word[4] = {c.x, c.y, c.z, c.w};
+            const uint4 y = kind ? c[1][half] : c[0][half];
+            const uint32_t word[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               uint32_t x[8];
@@ -481,22 +520,20 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
             }
           }
           tc05::fence_proxy_async();
-          tc05::bar_arrive(kind ? &S.v_full[e % kRing] : &S.k_full[e % kRing]);
+          tc05::bar_arrive(kind ? &S.v_full[st] : &S.k_full[st]);
         }
         if (dead) break;
-        okn[0] = okn[1];
-        okn[1] = copy(p, tile + 2, page);
-        page = request(p, tile + 3);
       }
       if (dead) break;
       nk += nother;
       for (int t = nint > 0 ? -1 : 0; t < nother; ++t, ++nv) {  // -1: R_v^T
         const int st = nv % kRing;
-        if (!wait(&S.v_tma[st], tma[st]++)) break;
+        if (st != g) continue;
+        if (!wait(&S.v_tma[st], tma++)) break;
         const int tile = p.t0 + nint + t - p.I;
-        const int n = tile < p.Wt ? p.n_win - kTile * tile : p.n_new - kTile * (tile - p.Wt);
-        if (t >= 0 && n < kTile) {
-          if (key >= n) {
+        const int count = tile < p.Wt ? p.n_win - kTile * tile : p.n_new - kTile * (tile - p.Wt);
+        if (t >= 0 && count < kTile) {
+          if (key >= count) {
             uint8_t* r = S.v[st] + key * 128;
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
@@ -509,23 +546,17 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
         tc05::bar_arrive(&S.v_full[st]);
       }
     }
-    cp_async_wait<0>();
   } else if (warp == kTmaWarp || warp == kTmaWarp + 1) {
     // ------------------------------------------------------------ TMA
-    // One warp for the queries, keys and R_k, one for the values and R_v^T.  They
-    // alone wait for the ring's slots, every phase in turn, and grant the
-    // dequantizing warps theirs: a wait tells a phase from the next but not from
-    // the next but one, and whoever waited for some of the phases only could miss
-    // two.
+    // One warp for the queries, records, keys and R_k, one for the values and
+    // R_v^T.  They alone wait for the ring's slots, every phase in turn, and grant
+    // the dequantizing groups theirs: a wait tells a phase from the next but not
+    // from the next but one, and whoever waited for some of the phases only could
+    // miss two.
     const bool values = warp != kTmaWarp;
     uint64_t* const empty = values ? S.v_empty : S.k_empty;
     uint64_t* const full = values ? S.v_tma : S.k_tma;
-    uint32_t step = 0, nq = 0, pending[kRing] = {0, 0};
-    bool dead = false;
-    auto wait = [&](uint64_t* bar, uint32_t phase) {
-      if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
-      return !dead;
-    };
+    uint32_t step = 0, nq = 0, nt = 0, fetched = 0, pending[kRing] = {0, 0};
     auto load_q = [&](const Piece& p) {
       if (values || dead || (nq > 0 && !wait(&S.q_empty, nq - 1))) return;
       if (lane == 0) {
@@ -552,16 +583,48 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
       ++pending[st];
     };
     Piece p;
-    for (uint32_t n = 0; !dead && next_piece(n, p); ++n) {
+    for (uint32_t n = 0; next_piece(n, p); ++n) {
       const int nint = p.int_tiles(), nother = p.t1 - p.t0 - nint;
       if (nint > 0) {
         load_q(p);
         // hi and lo of R_k
         bring(A.Rk_query + (size_t)p.h * kRT5Halves + (values ? kD * kD : 0));
-        for (int t = 0; t < nint && free_slot(); ++t, ++step) {
-          if (lane == 0) tc05::bar_arrive(values ? &S.v_grant[step % kRing] : &S.k_grant[step % kRing]);
+        // INT2 tiles: records two tiles ahead, the pages' entries three; lane = page
+        auto request = [&](int t) {
+          const int pos = (p.t0 + t) * kTile + kPage * lane;
+          return t < nint && lane < 8 && pos < p.n_int
+                     ? __ldcg(A.bt + (size_t)p.b * A.max_pages + (A.sink + pos) / kPage) : -1;
+        };
+        auto fetch = [&](int t, int page) {
+          if (t >= nint || dead) return;
+          const uint32_t x = nt + t, g = x & 1, bytes = chunk_bytes(A.compact);
+          if (x >= 2 && !wait(&S.raw_empty[g], x / 2 - 1)) return;
+          const bool in = page >= 0 && page < A.num_pages;
+          const uint32_t copies = __popc(__ballot_sync(0xffffffffu, in));
+          if (lane == 0) tc05::bar_arrive_expect_tx(&S.raw_full[g], copies * bytes);
           __syncwarp();
+          if (in)
+            tc05::bulk_g2s(S.raw[g][lane], A.pool + ((size_t)page * A.h_kv + p.h) * bytes, bytes,
+                           &S.raw_full[g]);
+          __syncwarp();
+          fetched = x + 1;
+        };
+        int page = -1;
+        if (!values) {
+          const int e0 = request(0), e1 = request(1);
+          page = request(2);
+          fetch(0, e0);
+          fetch(1, e1);
         }
+        for (int t = 0; t < nint && free_slot(); ++t, ++step) {
+          const uint32_t g = (nt + t) & 1;
+          arrive(values ? &S.v_grant[g][step % kRing] : &S.k_grant[g][step % kRing]);
+          if (!values) {
+            fetch(t + 2, page);
+            page = request(t + 3);
+          }
+        }
+        nt += nint;
         if (values) bring(A.Rv_back + (size_t)p.h * kRT5Halves);  // hi of 64 R_v^T
       }
       for (int t = 0; t < nother && free_slot(); ++t) {
@@ -589,117 +652,122 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
     for (int s = 0; s < kRing; ++s)
       if (pending[s]) tc05::bar_wait_drain(&full[s], (pending[s] - 1) & 1);
     if (nq) tc05::bar_wait_drain(&S.q_full, (nq - 1) & 1);
+    for (uint32_t x = fetched > 2 ? fetched - 2 : 0; x < fetched; ++x)
+      tc05::bar_wait_drain(&S.raw_full[x & 1], x / 2 & 1);
     __syncwarp();
   } else if (warp == kPlanWarp) {
     // ---------------------------------------------------------- pieces
     find_pieces<kPieces>(A, w, S.piece, S.piece_full, S.piece_empty, abort);
   } else {
     // ------------------------------------------------------------ MMA
-    if (warp == kMmaWarp) {
-      constexpr uint32_t kId = tc05::idesc_f16(128, 128);
-      const uint32_t sq = tc05::smem_addr(S.q[0]), sk = tc05::smem_addr(S.k[0]),
-                     sv = tc05::smem_addr(S.v[0]);
-      uint32_t nk = 0, nv = 0, nq = 0, np[2] = {0, 0}, nr[2] = {0, 0}, kd[kRing] = {0, 0}, kt[kRing] = {0, 0};
-      bool dead = false, used = false;
-      auto wait = [&](uint64_t* bar, uint32_t phase) {
-        if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
-        tc05::fence_after();
-        return !dead;
-      };
-      auto wait_k = [&](int phase) {  // keys of tile nk, dequantized or by TMA
-        const uint32_t st = nk % kRing;
-        return phase ? wait(&S.k_tma[st], kt[st]++) : wait(&S.k_full[st], kd[st]++);
-      };
-      auto qk = [&](int g, uint32_t type) {
-        const uint32_t a = sq + g * kOperand, b = sk + nk % kRing * kOperand;
+    constexpr uint32_t kId = tc05::idesc_f16(128, 128);
+    const uint32_t sq = tc05::smem_addr(S.q[0]), sk = tc05::smem_addr(S.k[0]),
+                   sv = tc05::smem_addr(S.v[0]);
+    uint32_t nk = 0, nv = 0, nq = 0, np[2] = {0, 0}, nr[2] = {0, 0}, kd[kRing] = {0, 0}, kt[kRing] = {0, 0};
+    bool used = false;
+    auto wait_k = [&](int phase) {  // keys of tile nk, dequantized or by TMA
+      const uint32_t st = nk % kRing;
+      return phase ? wait(&S.k_tma[st], kt[st]++) : wait(&S.k_full[st], kd[st]++);
+    };
+    // S[g] = query tile t times key tile nk
+    auto qk = [&](int t, int g, uint32_t type) {
+      const uint32_t a = sq + t * kOperand, b = sk + nk % kRing * kOperand;
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-          const uint32_t o = (ks >> 2) * kHalf + (ks & 3) * 32;
-          tc05::mma_ss_warp(tmem + kColS + 128u * g, tc05::smem_desc_sw128(a + o, 16),
-                       tc05::smem_desc_sw128(b + o, 16), kId | type, ks != 0);
-        }
-        tc05::mma_commit_warp(&S.s_full[g]);
-      };
-      auto pv = [&](int g, uint32_t type, bool add) {
-        const uint32_t b = sv + nv % kRing * kOperand;
+      for (int ks = 0; ks < 8; ++ks) {
+        const uint32_t o = (ks >> 2) * kHalf + (ks & 3) * 32;
+        tc05::mma_ss_warp(tmem + kColS + 128u * g, tc05::smem_desc_sw128(a + o, 16),
+                          tc05::smem_desc_sw128(b + o, 16), kId | type, ks != 0);
+      }
+      tc05::mma_commit_warp(&S.s_full[g]);
+    };
+    Piece p;
+    for (uint32_t n = 0; next_piece(n, p); ++n) {
+      const int all_tiles = p.t1 - p.t0, nint = p.int_tiles();
+      // Tile u is for both groups (each its query tile), or for group u % 2; the
+      // logits of the next one of a group follow its product with the values.
+      const bool pair = p.q_tiles() == 2;
+      const int ahead = pair ? 1 : 2;
+      auto first_of = [&](int u) { return pair ? 0 : u & 1; };
+      auto last_of = [&](int u) { return pair ? 1 : u & 1; };
+      bool add[2] = {false, false};
+      used = true;
+      for (int phase = 0; phase < 2 && !dead; ++phase) {
+        const int u0 = phase ? nint : 0, u1 = phase ? all_tiles : nint;
+        if (u0 == u1) continue;
+        const uint32_t type = phase ? tc05::kIdescBf16 : 0u;
+        if (!wait(&S.q_full, nq++)) break;
+        if (!phase) {  // q R_k, bf16 hi + lo, by way of S
+          if (!wait_k(1) || !wait(&S.v_full[nv % kRing], nv / kRing)) break;
+          for (int g = 0; g < (pair ? 2 : 1); ++g) {
+            const uint32_t a = sq + g * kOperand;
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-          tc05::mma_ts_warp(tmem + kColO + 128u * g, tmem + kColS + 128u * g + 8u * ks,
-                       tc05::smem_desc_sw128(b + ks * 2048, kHalf),
-                       kId | type | tc05::kIdescMajorMnB, add || ks != 0);
-      };
-      Piece p;
-      for (uint32_t n = 0; !dead && next_piece(n, p); ++n) {
-        const int nint = p.int_tiles(), nother = p.t1 - p.t0 - nint;
-        const int G = p.q_tiles();
-        bool add = false;
-        for (int phase = 0; phase < 2 && !dead; ++phase) {
-          const int n = phase ? nother : nint;
-          const uint32_t type = phase ? tc05::kIdescBf16 : 0u;
-          if (n == 0) continue;
-          used = true;
-          if (!wait(&S.q_full, nq++)) break;
-          if (!phase) {  // q R_k, bf16 hi + lo, by way of S
-            if (!wait_k(1) || !wait(&S.v_full[nv % kRing], nv / kRing)) break;
-            for (int g = 0; g < G; ++g) {
-              const uint32_t a = sq + g * kOperand;
+            for (int part = 0; part < 2; ++part) {
+              const uint32_t b = part ? sv + nv % kRing * kOperand : sk + nk % kRing * kOperand;
 #pragma unroll
-              for (int part = 0; part < 2; ++part) {
-                const uint32_t b = part ? sv + nv % kRing * kOperand : sk + nk % kRing * kOperand;
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-                  tc05::mma_ss_warp(tmem + kColS + 128u * g,
-                                    tc05::smem_desc_sw128(a + (ks >> 2) * kHalf + (ks & 3) * 32, 16),
-                                    tc05::smem_desc(b + ks * 256, 128, 2048), kId | tc05::kIdescBf16,
-                                    (part | ks) != 0);
-              }
-              tc05::mma_commit_warp(&S.s_full[g]);
+              for (int ks = 0; ks < 8; ++ks)
+                tc05::mma_ss_warp(tmem + kColS + 128u * g,
+                                  tc05::smem_desc_sw128(a + (ks >> 2) * kHalf + (ks & 3) * 32, 16),
+                                  tc05::smem_desc(b + ks * 256, 128, 2048), kId | tc05::kIdescBf16,
+                                  (part | ks) != 0);
             }
-            tc05::mma_commit_warp(&S.k_empty[nk++ % kRing]);
-            tc05::mma_commit_warp(&S.v_empty[nv++ % kRing]);
+            tc05::mma_commit_warp(&S.s_full[g]);
           }
-          if (!wait_k(phase)) break;
-          for (int g = 0; g < G; ++g) {
-            if (!phase && !wait(&S.q_ready[g], nr[g]++)) break;
-            qk(g, type);
-          }
-          if (dead) break;
           tc05::mma_commit_warp(&S.k_empty[nk++ % kRing]);
-          if (n == 1) tc05::mma_commit_warp(&S.q_empty);
-          for (int t = 0; t < n && !dead; ++t, ++nv) {
-            for (int g = 0; g < G; ++g) {
-              if (g == 0 && !wait(&S.v_full[nv % kRing], nv / kRing)) break;
-              if (!wait(&S.p_ready[g], np[g]++)) break;
-              pv(g, type, add);
-              if (t == n - 1) tc05::mma_commit_warp(&S.o_full[g]);
-              if (g == G - 1) tc05::mma_commit_warp(&S.v_empty[nv % kRing]);
-              if (t + 1 < n) {
-                if (g == 0 && !wait_k(phase)) break;
-                qk(g, type);
-              }
-            }
-            if (t + 1 < n) tc05::mma_commit_warp(&S.k_empty[nk++ % kRing]);
-            if (t + 2 == n) tc05::mma_commit_warp(&S.q_empty);
-            add = true;
+          tc05::mma_commit_warp(&S.v_empty[nv++ % kRing]);
+        }
+        for (int u = u0; u < min(u0 + ahead, u1); ++u) {
+          if (!wait_k(phase)) break;
+          for (int g = first_of(u); g <= last_of(u); ++g) {
+            const int t = pair ? g : 0;
+            if (!phase && u == u0 && !wait(&S.q_ready[t], nr[t]++)) break;
+            qk(t, g, type);
           }
-          if (dead || phase) continue;
+          tc05::mma_commit_warp(&S.k_empty[nk++ % kRing]);
+        }
+        if (u1 - u0 <= ahead) tc05::mma_commit_warp(&S.q_empty);
+        for (int u = u0; u < u1 && !dead; ++u) {
           if (!wait(&S.v_full[nv % kRing], nv / kRing)) break;
-          for (int g = 0; g < G; ++g) {
+          const uint32_t b = sv + nv % kRing * kOperand;
+          const bool more = u + ahead < u1;
+          for (int g = first_of(u); g <= last_of(u); ++g) {
             if (!wait(&S.p_ready[g], np[g]++)) break;
-            const uint32_t b = sv + nv % kRing * kOperand;
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks)
               tc05::mma_ts_warp(tmem + kColO + 128u * g, tmem + kColS + 128u * g + 8u * ks,
-                           tc05::smem_desc(b + ks * 256, 128, 2048), kId, ks != 0);
-            if (nother == 0) tc05::mma_commit_warp(&S.o_full[g]);
+                                tc05::smem_desc_sw128(b + ks * 2048, kHalf),
+                                kId | type | tc05::kIdescMajorMnB, add[g] || ks != 0);
+            add[g] = true;
+            if (!more) tc05::mma_commit_warp(&S.o_full[g]);
+            if (g == last_of(u)) tc05::mma_commit_warp(&S.v_empty[nv % kRing]);
+            if (more) {
+              if (g == first_of(u) && !wait_k(phase)) break;
+              qk(pair ? g : 0, g, type);
+            }
           }
-          tc05::mma_commit_warp(&S.v_empty[nv++ % kRing]);
+          ++nv;
+          if (more) tc05::mma_commit_warp(&S.k_empty[nk++ % kRing]);
+          if (u + ahead + 1 == u1) tc05::mma_commit_warp(&S.q_empty);
         }
+        if (dead || phase) continue;
+        // O R_v^T of the groups that have INT2 tiles
+        if (!wait(&S.v_full[nv % kRing], nv / kRing)) break;
+        for (int g = 0; g < (pair ? 2 : min(nint, 2)); ++g) {
+          if (!wait(&S.p_ready[g], np[g]++)) break;
+          const uint32_t b = sv + nv % kRing * kOperand;
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks)
+            tc05::mma_ts_warp(tmem + kColO + 128u * g, tmem + kColS + 128u * g + 8u * ks,
+                              tc05::smem_desc(b + ks * 256, 128, 2048), kId, ks != 0);
+          // the group has no tile after these
+          if (pair ? nint == all_tiles : (all_tiles + 1 - g) / 2 == (nint + 1 - g) / 2)
+            tc05::mma_commit_warp(&S.o_full[g]);
+        }
+        tc05::mma_commit_warp(&S.v_empty[nv++ % kRing]);
       }
-      if (used) {  // the tensor core is done with tensor memory before it is freed
-        tc05::mma_commit_warp(&S.drained);
-        tc05::bar_wait_drain(&S.drained, 0);
-      }
+    }
+    if (used) {  // the tensor core is done with tensor memory before it is freed
+      tc05::mma_commit_warp(&S.drained);
+      tc05::bar_wait_drain(&S.drained, 0);
     }
     __syncwarp();
   }
@@ -721,9 +789,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
 // parts and many rows (kSplit 1), those of a few tokens over a long context of
 // many parts and few rows (kSplit 4).  The CTAs also clear the rows of sequences
 // that were left out and those of none.
-template <bool kSmall>
+template <bool kFew>
 __global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
-  constexpr int kSplit = kSmall ? 4 : 1, kRows = 8 / kSplit;
+  constexpr int kSplit = kFew ? 4 : 1, kRows = 8 / kSplit;
   __shared__ float4 so[kSplit][kRows][32];
   __shared__ float2 sml[kSplit][kRows];
   const int w = blockIdx.x, tid = threadIdx.x;
@@ -746,9 +814,7 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
       if (seq_work(A, b).bad) clear(max(0, __ldcg(A.cu + b)), min(c1, A.n_tok));
     }
   }
-  // rows along the threads as the partials have them, or channels
-  const int split = kSmall ? tid >> 6 : 0;
-  const int row = kSmall ? tid >> 5 & (kRows - 1) : tid & 7, cg = kSmall ? tid & 31 : tid >> 3;
+  const int row = tid % kRows, split = tid / kRows % kSplit, cg = tid / (kRows * kSplit);
   const int r = kRows * blockIdx.y + row;
   const int i = seg.qb * kQTok + r / 4;
   if (!seg.valid || seg.qb * kQTok + kRows * (int)blockIdx.y / 4 >= seg.n_new) return;
@@ -774,8 +840,7 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
         const float* part = part_of(A, x, x != w);
         m[k] = __ldcg(part + (size_t)A.rows * kD + r);
         l[k] = __ldcg(part + (size_t)A.rows * (kD + 1) + r);
-        y[k] = __ldcg(reinterpret_cast<const float4*>(part) +
-                      (kSmall ? (size_t)r * (kD / 4) + cg : (size_t)cg * A.rows + r));
+        y[k] = __ldcg(reinterpret_cast<const float4*>(part) + (size_t)cg * A.rows + r);
       }
     }
 #pragma unroll
@@ -801,14 +866,11 @@ size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 struct ChunkLayout {
   size_t part, total;
   int rows, W;
-  bool small;
 };
 
 ChunkLayout chunk_layout(const optr_params* p, int max_new) {
   ChunkLayout l;
-  l.rows = chunk_small_rows(max_new);
-  l.small = l.rows > 0;
-  if (!l.small) l.rows = max_new > 32 ? 256 : 128;
+  l.rows = max_new > kQTok / 2 ? 256 : 128;
   l.W = p->num_sms;
   l.part = round_up(sizeof(ChunkSeg) * (size_t)l.W);
   l.total = l.part + round_up(2 * (size_t)l.W * part_floats(l.rows) * sizeof(float));
@@ -859,21 +921,18 @@ extern "C" optr_status optr_chunk_attention_win(
   cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(chunk_kernel), sizeof(Smem));
   if (e != cudaSuccess) return OPTR_ERR_CUDA;
   CUtensorMap mq, mk, mv, mw;
-  if ((!l.small && !token_rows_map(&mq, q, n_tok, 4 * h_kv, 32, 4)) ||
+  if (!token_rows_map(&mq, q, n_tok, 4 * h_kv, 32, 4) ||
       !token_rows_map(&mk, k, n_tok, h_kv, kTile) || !token_rows_map(&mv, v, n_tok, h_kv, kTile) ||
       !(w.win ? token_rows_map(&mw, w.win, n_slots * h_kv * 2 * win_rows, 1, kTile)
               : token_rows_map(&mw, k, n_tok, h_kv, kTile)))
     return OPTR_ERR_CUDA;
-  const int per = l.small ? 2 : 8;  // rows of a joining CTA
+  const bool few = max_new <= 16;
+  const int per = few ? 2 : 8;  // rows of a joining CTA
   const dim3 joins(l.W, (std::min(l.rows, 4 * max_new) + per - 1) / per);
-  if (l.small) {
-    e = launch_chunk_small(p, A, (const __nv_bfloat16*)q, mk, mv, mw, stream);
-    if (e == cudaSuccess) e = launch_pdl(chunk_combine_kernel<true>, joins, dim3(256), 0, stream, A);
-    return cuda_status(e);
-  }
   e = launch_pdl(chunk_kernel, dim3(l.W), dim3(kThreads), sizeof(Smem), stream, mq, mk, mv, mw, A);
   if (e == cudaSuccess)
-    e = launch_pdl(chunk_combine_kernel<false>, joins, dim3(256), 0, stream, A);
+    e = launch_pdl(few ? chunk_combine_kernel<true> : chunk_combine_kernel<false>, joins, dim3(256), 0,
+                   stream, A);
   return cuda_status(e);
 }
 

@@ -95,7 +95,7 @@ struct Piece {
   int I, Wt;         // INT2 and window tiles of the segment
   int t0, t1, total;
   __device__ __forceinline__ int int_tiles() const { return max(0, min(t1, I) - t0); }
-  // query tiles that have rows
+  // query tiles that have rows: 2, or 1 that both softmax groups work on
   __device__ __forceinline__ int q_tiles() const { return n_new - qb * kQTok > kQTok / 2 ? 2 : 1; }
 };
 
@@ -198,8 +198,7 @@ __device__ __forceinline__ void report_sequences(const ChunkArgs& A) {
   }
 }
 
-// A partial: O, [32 channel groups][rows][4] from chunk_kernel and [rows][128]
-// from chunk_small_kernel (as their threads hold it), then m [rows] and l [rows].
+// A partial: O [32 channel groups][rows][4], then m [rows] and l [rows].
 // CTA w has two: of a segment begun by an earlier CTA, and of one that a later
 // CTA ends.
 __host__ __device__ constexpr size_t part_floats(int rows) { return (size_t)rows * (kD + 2); }
@@ -237,12 +236,5 @@ __device__ __forceinline__ void find_pieces(const ChunkArgs& A, int w, Piece* pi
   }
   if (lane == 0) A.seg[w] = seg;
 }
-
-// chunk_small.cu: rows of its query operand for up to max_new tokens (0: too
-// many), and the launch.
-int chunk_small_rows(int max_new);
-cudaError_t launch_chunk_small(const optr_params* p, const ChunkArgs& A, const __nv_bfloat16* q,
-                               const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mw,
-                               cudaStream_t s);
 
 }  // namespace optr

@@ -38,9 +38,7 @@ __global__ void tc05_operands_kernel(const float* R_k, const float* R_v, uint16_
 
 // R_k as bf16 hi + lo (17 bits of it) in the same layout, columns in the order
 // of dequantized rows: queries are rotated as they come, in bf16.
-// And the fp16 hi part of 64 R_k alone, for queries that are few (their rounding
-// to fp16, as far as it is one, and this one's are alike).
-__global__ void query_operand_kernel(const float* R_k, uint16_t* out, uint16_t* row) {
+__global__ void query_operand_kernel(const float* R_k, uint16_t* out) {
   const int h = blockIdx.x;
   for (int i = threadIdx.x; i < kD * kD; i += blockDim.x) {
     const int n = i / kD, k = i % kD;
@@ -48,7 +46,6 @@ __global__ void query_operand_kernel(const float* R_k, uint16_t* out, uint16_t* 
     const __nv_bfloat16 hi = __float2bfloat16_rn(x);
     uint16_t* o = out + (size_t)h * kRT5Halves + tc05_offset(n, k);
     o[0] = __bfloat16_as_ushort(hi);
-    row[(size_t)h * kD * kD + tc05_offset(n, k)] = __half_as_ushort(__float2half_rn(x * 64.0f));
     o[kD * kD] = __bfloat16_as_ushort(__float2bfloat16_rn(x - __bfloat162float(hi)));
   }
 }
@@ -61,11 +58,10 @@ cudaError_t build_operands(optr_params* p) {
   cudaError_t e = cudaSuccess;
   for (uint16_t** x : {&p->Rk_t5, &p->Rv_t5, &p->Rk_back, &p->Rv_back, &p->Rk_query})
     if (e == cudaSuccess) e = cudaMalloc(x, bytes);
-  if (e == cudaSuccess) e = cudaMalloc(&p->Rk_row, bytes / 2);
   if (e != cudaSuccess) return e;
   tc05_operands_kernel<<<dim3(H, 2), 256>>>(p->R_k, p->R_v, p->Rk_t5, p->Rv_t5, p->Rk_back,
                                             p->Rv_back);
-  query_operand_kernel<<<H, 256>>>(p->R_k, p->Rk_query, p->Rk_row);
+  query_operand_kernel<<<H, 256>>>(p->R_k, p->Rk_query);
   e = cudaGetLastError();
   return e == cudaSuccess ? cudaStreamSynchronize(nullptr) : e;
 }

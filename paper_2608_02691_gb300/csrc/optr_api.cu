@@ -307,7 +307,6 @@ void optr_params_destroy(optr_params* p) {
   cudaFree(p->Rk_back);
   cudaFree(p->Rv_back);
   cudaFree(p->Rk_query);
-  cudaFree(p->Rk_row);
   cudaFree(p->err);
   free(p);
 }

@@ -55,7 +55,6 @@ struct optr_params {
   uint16_t* Rk_back;   // the same of R_k^T and R_v^T, for dequantized rows
   uint16_t* Rv_back;   // (inner index in the order of dequant.cuh)
   uint16_t* Rk_query;  // R_k in bf16 parts, for queries (operands.cu)
-  uint16_t* Rk_row;    // the same in fp16
   unsigned* err;       // device error word
   // device address of the fixed scratch array of
   // optr_decode_attention_noalloc on this params' device (noalloc.cu),
