@@ -505,9 +505,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
           uint8_t* dst = (kind ? S.v[st] : S.k[st]) + key * 128;
           const uint4 m = kind ? mm[1] : mm[0];
           const SlotMeta sm = slot_meta(m.x, m.y, m.z, m.w);
-#pragma unroll
+#pragma unroll 1
           for (int half = 0; half < 2; ++half) {
-            const uint4 y = kind ? c[1][half] : c[0][half];
+            const uint4 y = kind ? (half ? c[1][1] : c[1][0]) : (half ? c[0][1] : c[0][0]);
             const uint32_t word[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -672,12 +672,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
     // S[g] = query tile t times key tile nk
     auto qk = [&](int t, int g, uint32_t type) {
       const uint32_t a = sq + t * kOperand, b = sk + nk % kRing * kOperand;
-#pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        const uint32_t o = (ks >> 2) * kHalf + (ks & 3) * 32;
-        tc05::mma_ss_warp(tmem + kColS + 128u * g, tc05::smem_desc_sw128(a + o, 16),
-                          tc05::smem_desc_sw128(b + o, 16), kId | type, ks != 0);
-      }
+      tc05::mma128_ss<2, 2, true, true>(tmem + kColS + 128u * g, tc05::smem_desc_sw128(a, 16),
+                                        tc05::smem_desc_sw128(b, 16), kId | type, 0);
       tc05::mma_commit_warp(&S.s_full[g]);
     };
     Piece p;
@@ -700,15 +696,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
           if (!wait_k(1) || !wait(&S.v_full[nv % kRing], nv / kRing)) break;
           for (int g = 0; g < (pair ? 2 : 1); ++g) {
             const uint32_t a = sq + g * kOperand;
-#pragma unroll
             for (int part = 0; part < 2; ++part) {
               const uint32_t b = part ? sv + nv % kRing * kOperand : sk + nk % kRing * kOperand;
-#pragma unroll
-              for (int ks = 0; ks < 8; ++ks)
-                tc05::mma_ss_warp(tmem + kColS + 128u * g,
-                                  tc05::smem_desc_sw128(a + (ks >> 2) * kHalf + (ks & 3) * 32, 16),
-                                  tc05::smem_desc(b + ks * 256, 128, 2048), kId | tc05::kIdescBf16,
-                                  (part | ks) != 0);
+              tc05::mma128_ss<2, 16, true, false>(tmem + kColS + 128u * g, tc05::smem_desc_sw128(a, 16),
+                                                  tc05::smem_desc(b, 128, 2048),
+                                                  kId | tc05::kIdescBf16, part);
             }
             tc05::mma_commit_warp(&S.s_full[g]);
           }
@@ -731,11 +723,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
           const bool more = u + ahead < u1;
           for (int g = first_of(u); g <= last_of(u); ++g) {
             if (!wait(&S.p_ready[g], np[g]++)) break;
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-              tc05::mma_ts_warp(tmem + kColO + 128u * g, tmem + kColS + 128u * g + 8u * ks,
-                                tc05::smem_desc_sw128(b + ks * 2048, kHalf),
-                                kId | type | tc05::kIdescMajorMnB, add[g] || ks != 0);
+            tc05::mma128_ts<128>(tmem + kColO + 128u * g, tmem + kColS + 128u * g,
+                                 tc05::smem_desc_sw128(b, kHalf), kId | type | tc05::kIdescMajorMnB,
+                                 add[g]);
             add[g] = true;
             if (!more) tc05::mma_commit_warp(&S.o_full[g]);
             if (g == last_of(u)) tc05::mma_commit_warp(&S.v_empty[nv % kRing]);
@@ -754,10 +744,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
         for (int g = 0; g < (pair ? 2 : min(nint, 2)); ++g) {
           if (!wait(&S.p_ready[g], np[g]++)) break;
           const uint32_t b = sv + nv % kRing * kOperand;
-#pragma unroll
-          for (int ks = 0; ks < 8; ++ks)
-            tc05::mma_ts_warp(tmem + kColO + 128u * g, tmem + kColS + 128u * g + 8u * ks,
-                              tc05::smem_desc(b + ks * 256, 128, 2048), kId, ks != 0);
+          tc05::mma128_ts<16>(tmem + kColO + 128u * g, tmem + kColS + 128u * g,
+                              tc05::smem_desc(b, 128, 2048), kId, 0);
           // the group has no tile after these
           if (pair ? nint == all_tiles : (all_tiles + 1 - g) / 2 == (nint + 1 - g) / 2)
             tc05::mma_commit_warp(&S.o_full[g]);

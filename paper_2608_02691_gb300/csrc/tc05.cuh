@@ -207,15 +207,6 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b,
       ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// The same with A in shared memory.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t accumulate) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-}
-
 // Arrive on bar once every tcgen05.mma issued so far by this thread is done.
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
   asm volatile(
@@ -223,25 +214,67 @@ __device__ __forceinline__ void mma_commit(uint64_t* bar) {
       ::"r"(smem_addr(bar)) : "memory");
 }
 
-// The same, called by a whole converged warp, one elected thread of which
-// issues.  Where the code around them is converged and its waits are voted on,
-// the operands stay in uniform registers: issued by `if (lane == 0)`, each MMA
-// first moves its six operands there, about 120 cycles against the 64 that a
-// 128 x 128 x 16 takes.
-__device__ __forceinline__ void mma_ss_warp(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
-                                            uint32_t accumulate) {
+// D (+)= A B^T over 128 of the inner dimension: eight MMAs, issued by one elected
+// thread of a whole converged warp.  One block of code for all eight, so that only
+// the bases have to be brought into uniform registers and the steps are added
+// there: one by one, from operands that the compiler cannot prove uniform, each
+// MMA took about 120 cycles to issue, against the 64 that a 128 x 128 x 16 takes.
+// kA, kB: how far apart the steps lie, in units of 16 bytes (descriptors) or
+// columns (A in tensor memory); kWrap: 64 of the inner dimension fill 128-byte rows,
+// and the other 64 lie 16 KB on (K-major, 128-byte swizzle, 128 rows).
+template <int kA, int kB, bool kWrapA, bool kWrapB>
+__device__ __forceinline__ void mma128_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
+                                          uint32_t accumulate) {
+  constexpr int kHalfOff = 1024 - 4 * 2;  // 16 KB instead of four steps of 32 B
+  constexpr int wa = kWrapA ? kHalfOff : 0, wb = kWrapB ? kHalfOff : 0;
   asm volatile(
-      "{\n .reg .pred p, e;\n setp.ne.b32 p, %4, 0;\n elect.sync _|e, 0xffffffff;\n"
-      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+      "{\n .reg .pred p, t, e;\n .reg .b64 x<8>, y<8>;\n"
+      " setp.ne.b32 p, %4, 0;\n setp.eq.u32 t, 0, 0;\n elect.sync _|e, 0xffffffff;\n"
+      " add.s64 x1, %1, %5;\n add.s64 y1, %2, %12;\n"
+      " add.s64 x2, %1, %6;\n add.s64 y2, %2, %13;\n"
+      " add.s64 x3, %1, %7;\n add.s64 y3, %2, %14;\n"
+      " add.s64 x4, %1, %8;\n add.s64 y4, %2, %15;\n"
+      " add.s64 x5, %1, %9;\n add.s64 y5, %2, %16;\n"
+      " add.s64 x6, %1, %10;\n add.s64 y6, %2, %17;\n"
+      " add.s64 x7, %1, %11;\n add.s64 y7, %2, %18;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], x1, y1, %3, t;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], x2, y2, %3, t;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], x3, y3, %3, t;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], x4, y4, %3, t;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], x5, y5, %3, t;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], x6, y6, %3, t;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], x7, y7, %3, t;\n}\n"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "n"(kA), "n"(2 * kA), "n"(3 * kA),
+        "n"(4 * kA + wa), "n"(5 * kA + wa), "n"(6 * kA + wa), "n"(7 * kA + wa), "n"(kB), "n"(2 * kB),
+        "n"(3 * kB), "n"(4 * kB + wb), "n"(5 * kB + wb), "n"(6 * kB + wb), "n"(7 * kB + wb)
+      : "memory");
 }
 
-__device__ __forceinline__ void mma_ts_warp(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
-                                            uint32_t accumulate) {
+template <int kB>
+__device__ __forceinline__ void mma128_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
+                                          uint32_t accumulate) {
   asm volatile(
-      "{\n .reg .pred p, e;\n setp.ne.b32 p, %4, 0;\n elect.sync _|e, 0xffffffff;\n"
-      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+      "{\n .reg .pred p, t, e;\n .reg .b32 x<8>;\n .reg .b64 y<8>;\n"
+      " setp.ne.b32 p, %4, 0;\n setp.eq.u32 t, 0, 0;\n elect.sync _|e, 0xffffffff;\n"
+      " add.u32 x1, %1, 8;\n add.s64 y1, %2, %5;\n"
+      " add.u32 x2, %1, 16;\n add.s64 y2, %2, %6;\n"
+      " add.u32 x3, %1, 24;\n add.s64 y3, %2, %7;\n"
+      " add.u32 x4, %1, 32;\n add.s64 y4, %2, %8;\n"
+      " add.u32 x5, %1, 40;\n add.s64 y5, %2, %9;\n"
+      " add.u32 x6, %1, 48;\n add.s64 y6, %2, %10;\n"
+      " add.u32 x7, %1, 56;\n add.s64 y7, %2, %11;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [x1], y1, %3, t;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [x2], y2, %3, t;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [x3], y3, %3, t;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [x4], y4, %3, t;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [x5], y5, %3, t;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [x6], y6, %3, t;\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [x7], y7, %3, t;\n}\n"
+      ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "n"(kB), "n"(2 * kB), "n"(3 * kB),
+        "n"(4 * kB), "n"(5 * kB), "n"(6 * kB), "n"(7 * kB)
+      : "memory");
 }
 
 __device__ __forceinline__ void mma_commit_warp(uint64_t* bar) {
