@@ -311,11 +311,14 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
       const int tiles = pair ? all_tiles : (all_tiles + 1 - g) / 2;
       const int i = p.qb * kQTok + (pair ? 32 * g : 0) + (row >> 2), j = row & 3;
       const bool valid = i < p.n_new;
+      // A warp without a row only keeps the others' phases: what its rows of S, P
+      // and O hold stays in them.
+      const bool rows = __any_sync(0xffffffffu, valid);
       const size_t at = ((size_t)p.c0 + i) * 4 * A.h_kv + 4 * p.h + j;
       float scale = 0.f, off = 0.f, m = -1e30f, l = 0.f;
       if (nint > 0 && (pair || g == 0)) {
         if (!wait(&S.s_full[g], ns++)) break;
-        rotated_query(tS, S.q[g], row, A.muR + p.h * kD, scale, off);
+        if (rows) rotated_query(tS, S.q[g], row, A.muR + p.h * kD, scale, off);
         if (!pair) {
           S.scale[row] = scale;
           S.off[row] = off;
@@ -333,7 +336,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
           off = S.off[row];
         }
         const uint4 mask = *reinterpret_cast<const uint4*>(S.mask[(base + t) % 4]);
-        softmax_tile<false>(tS, tO, scale, off, mask, p.n_int - kTile * (p.t0 + t), fresh, m, l);
+        if (rows)
+          softmax_tile<false>(tS, tO, scale, off, mask, p.n_int - kTile * (p.t0 + t), fresh, m,
+                              l);
         fresh = false;
         ready();
       }
@@ -344,7 +349,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
         if (!wait(&S.o_full[g], no++)) break;
         const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 4 && rows; ++c) {
           uint32_t o[32], a[16];
           tc05::tmem_ld32(tO + 32 * c, o);
           tc05::tmem_wait_ld();
@@ -365,7 +370,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
         // window rows as far as they are filled; own tiles causally
         const int tile = p.t0 + from + stride * k - p.I;
         const int lim = tile < p.Wt ? p.n_win - kTile * tile : i + 1 - kTile * (tile - p.Wt);
-        softmax_tile<true>(tS, tO, kLogit, 0.f, make_uint4(~0u, ~0u, ~0u, ~0u), lim, fresh, m, l);
+        if (rows)
+          softmax_tile<true>(tS, tO, kLogit, 0.f, make_uint4(~0u, ~0u, ~0u, ~0u), lim, fresh, m, l);
         fresh = false;
         ready();
       }
@@ -406,7 +412,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
       if (all_tiles == p.total) {
         const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 4 && rows; ++c) {
           uint32_t o[32];
           output(c, o);
           if (valid)
@@ -424,7 +430,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
         float* part = part_of(A, w, p.t0 > 0);
         const int r = 128 * g + row;
 #pragma unroll 1
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 4 && rows; ++c) {
           uint32_t o[32];
           output(c, o);
           if (valid)
