@@ -12,7 +12,7 @@
 //   8 converter warps  two groups of 4 take alternate tiles, a thread per row:
 //                   table entry requested two of its tiles ahead, record one
 //                   tile ahead, then 128 values into tensor memory (A operand);
-//   MMA warp        one thread issues a tile's 16 tcgen05.mma;
+//   MMA warp        issues a tile's 16 tcgen05.mma;
 //   8 epilogue warps  two groups likewise: accumulator rows back, mu, bf16,
 //                   into a swizzled shared-memory tile that two TMA copies
 //                   store.
@@ -86,7 +86,8 @@ kv_read_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
   extern __shared__ __align__(1024) unsigned char dsm_[];
   Smem& S = *reinterpret_cast<Smem*>(dsm_);
   const int h = blockIdx.y, kind = blockIdx.z;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int tiles = (n_tok + kRows - 1) / kRows;
   const int my_tiles =
       tiles > (int)blockIdx.x ? (tiles - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0;
@@ -122,7 +123,7 @@ kv_read_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
   tc05::fence_before();
   __syncthreads();
   tc05::fence_after();
-  const uint32_t tmem = S.tmem;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, S.tmem, 0);
   volatile int* abort = &S.abort;
 
   if (warp < kConvWarps) {
@@ -203,31 +204,24 @@ kv_read_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
   } else if (warp == kMmaWarp) {
     // --------------------------------------------------------------- MMA
     int last = -1;
-    if (lane == 0) {
-      const uint32_t b0 = tc05::smem_addr(&S.b[0][0]);
-      for (int i = 0; i < my_tiles; ++i) {
-        const int g = i & 1, k = i >> 1;
-        if (!tc05::bar_wait(&S.aready[g], k & 1, abort)) break;
-        if (k > 0 && !tc05::bar_wait(&S.dfree[g], (k - 1) & 1, abort)) break;
-        tc05::fence_after();
-        const uint32_t d = tmem + kColD + 128u * g, a = tmem + kColA + 64u * g;
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-#pragma unroll
-          for (int term = 0; term < 2; ++term)
-            tc05::mma_ts(d, a + 8u * ks,
-                         tc05::smem_desc(b0 + term * kD * kD * 2 + ks * 256, 128, 2048),
-                         tc05::idesc_f16(128, 128), (ks | term) != 0);
-        tc05::mma_commit(&S.dready[g]);
-        tc05::mma_commit(&S.adone[g]);
-        last = i;
-      }
-      if (last >= 0) {  // the tensor core is done with tensor memory before it is freed
-        tc05::bar_wait_drain(&S.dready[last & 1], (last >> 1) & 1);
-        tc05::bar_wait_drain(&S.adone[last & 1], (last >> 1) & 1);
-      }
+    const uint32_t b0 = tc05::smem_addr(&S.b[0][0]);
+    for (int i = 0; i < my_tiles; ++i) {
+      const int g = i & 1, k = i >> 1;
+      if (!__all_sync(0xffffffffu, tc05::bar_wait(&S.aready[g], k & 1, abort))) break;
+      if (k > 0 && !__all_sync(0xffffffffu, tc05::bar_wait(&S.dfree[g], (k - 1) & 1, abort))) break;
+      tc05::fence_after();
+      const uint32_t d = tmem + kColD + 128u * g, a = tmem + kColA + 64u * g;
+      for (int term = 0; term < 2; ++term)
+        tc05::mma128_ts<16>(d, a, tc05::smem_desc(b0 + term * kD * kD * 2, 128, 2048),
+                            tc05::idesc_f16(128, 128), term);
+      tc05::mma_commit_warp(&S.dready[g]);
+      tc05::mma_commit_warp(&S.adone[g]);
+      last = i;
     }
-    __syncwarp();
+    if (last >= 0) {  // the tensor core is done with tensor memory before it is freed
+      tc05::bar_wait_drain(&S.dready[last & 1], (last >> 1) & 1);
+      tc05::bar_wait_drain(&S.adone[last & 1], (last >> 1) & 1);
+    }
   } else {
     // ---------------------------------------------------------- epilogue
     const int g = (warp - kEpiWarp) >> 2, q = warp & 3, row = 32 * q + lane;

@@ -23,7 +23,6 @@ namespace optr {
 namespace {
 
 constexpr int kVerifyThreads = 512;
-constexpr int kVerifyUnroll = 8;
 
 __device__ __forceinline__ float prob(float x) { return x; }
 __device__ __forceinline__ float prob(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -64,13 +63,38 @@ __device__ __forceinline__ unsigned long long cluster_load(const unsigned long l
   return v;
 }
 
-template <typename T>
+// kVec consecutive probabilities or noise values, as float.
+template <int kVec>
+__device__ __forceinline__ void load_vec(const float* p, float (&x)[kVec]) {
+  if constexpr (kVec == 1) {
+    x[0] = *p;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; i += 4) {
+      const float4 y = *reinterpret_cast<const float4*>(p + i);
+      x[i] = y.x, x[i + 1] = y.y, x[i + 2] = y.z, x[i + 3] = y.w;
+    }
+  }
+}
+template <int kVec>
+__device__ __forceinline__ void load_vec(const __nv_bfloat16* p, float (&x)[kVec]) {
+  if constexpr (kVec == 1) {
+    x[0] = __bfloat162float(*p);
+  } else {
+    const uint2 y = *reinterpret_cast<const uint2*>(p);
+    x[0] = __uint_as_float(y.x << 16), x[1] = __uint_as_float(y.x & 0xffff0000u);
+    x[2] = __uint_as_float(y.y << 16), x[3] = __uint_as_float(y.y & 0xffff0000u);
+  }
+}
+
+template <typename T, int kVec>
 __global__ void __launch_bounds__(kVerifyThreads)
 verify_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
               const int32_t* __restrict__ drafts, const float* __restrict__ u,
               const float* __restrict__ noise, const int32_t* __restrict__ cu, int n_draft,
               int V, int cs, int32_t* __restrict__ accepted, int32_t* __restrict__ tokens,
               unsigned* err) {
+  constexpr int kUnroll = kVec == 1 ? 8 : 4;
   __shared__ int head[2];
   __shared__ unsigned long long wbest[kVerifyThreads / 32];
   __shared__ unsigned long long best[2];  // this CTA's, by pass
@@ -87,6 +111,9 @@ verify_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
     return;
   }
   const int n = c1 - c0;
+  const float* e = noise + (size_t)b * V;
+  const int n_vec = V / kVec;
+  const int lo = (int)((long long)n_vec * rank / cs), hi = (int)((long long)n_vec * (rank + 1) / cs);
   // first rejected draft: one lane per draft, 32 at a time
   if (warp == 0) {
     int a = n, bad = -1;
@@ -121,40 +148,39 @@ verify_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
   const T* p = tp + ((size_t)c0 + b + a) * V;
   const T* q = dp && a < n ? dp + ((size_t)c0 + a) * V : nullptr;
   const int cut = !dp && a < n ? head[1] : -1;  // a draft without probabilities: q is 1 there
-  const float* e = noise + (size_t)b * V;
-  const int lo = (int)((long long)V * rank / cs), hi = (int)((long long)V * (rank + 1) / cs);
   // pass 0: the residual.  Where it is zero everywhere (p <= q throughout, to
   // rounding) pass 1 draws from p.
   unsigned long long all = 0;
   for (int pass = 0; pass < 2; ++pass) {
     float top = -1.f;
     int at = 0;
-    for (int v0 = lo + tid; v0 < hi; v0 += kVerifyThreads * kVerifyUnroll) {
-      float r[kVerifyUnroll], z[kVerifyUnroll];
+    const bool less = q && pass == 0;
+    for (int v0 = lo + tid; v0 < hi; v0 += kVerifyThreads * kUnroll) {
+      float r[kUnroll][kVec], z[kUnroll][kVec], y[kUnroll][kVec];
 #pragma unroll
-      for (int j = 0; j < kVerifyUnroll; ++j) {
-        const int v = v0 + j * kVerifyThreads;
-        r[j] = v < hi ? prob(p[v]) : -1.f;
-        z[j] = v < hi ? e[v] : 1.f;
-      }
-      if (q && pass == 0) {
-#pragma unroll
-        for (int j = 0; j < kVerifyUnroll; ++j) {
-          const int v = v0 + j * kVerifyThreads;
-          if (v < hi) r[j] = fmaxf(__fsub_rn(r[j], prob(q[v])), 0.f);
-        }
+      for (int j = 0; j < kUnroll; ++j) {
+        const size_t v = (size_t)min(v0 + j * kVerifyThreads, hi - 1) * kVec;
+        load_vec(p + v, r[j]);
+        load_vec(e + v, z[j]);
+        if (less) load_vec(q + v, y[j]);
       }
 #pragma unroll
-      for (int j = 0; j < kVerifyUnroll; ++j) {
+      for (int j = 0; j < kUnroll; ++j) {
         const int v = v0 + j * kVerifyThreads;
-        if (pass == 0 && v == cut) r[j] = 0.f;
-        // r / z > top needs r >= top z up to rounding: most candidates fall
-        // here, without a division
-        if (r[j] >= 0.f && r[j] >= top * z[j] * 0.99999f) {
-          const float w = __fdiv_rn(r[j], z[j]);
-          if (w > top) {
-            top = w;
-            at = v;
+        if (v >= hi) break;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          float x = r[j][i];
+          if (less) x = fmaxf(__fsub_rn(x, y[j][i]), 0.f);
+          if (pass == 0 && v * kVec + i == cut) x = 0.f;
+          // x / z > top needs x >= top z up to rounding: most candidates fall
+          // here, without a division
+          if (x >= 0.f && x >= top * z[j][i] * 0.99999f) {
+            const float w = __fdiv_rn(x, z[j][i]);
+            if (w > top) {
+              top = w;
+              at = v * kVec + i;
+            }
           }
         }
       }
@@ -191,12 +217,17 @@ cudaError_t launch_verify(const optr_params* p, const void* tp, const void* dp,
                           const int32_t* drafts, const float* u, const float* noise,
                           const int32_t* cu, int n_draft, int B, int V, int32_t* accepted,
                           int32_t* tokens, cudaStream_t s) {
-  // CTAs per sequence: about two per SM in all, at least a round of loads each
+  // four values an access where the vocabulary and the rows' alignment admit it
+  const bool wide = V % 4 == 0 && aligned(tp, 4 * sizeof(T)) && aligned(dp, 4 * sizeof(T)) &&
+                    aligned(noise, 16);
+  // CTAs per sequence: about kPerSm per SM in all, a round of loads each at least
+  constexpr int kPerSm = 2;
   int cs = 8;
-  while (cs > 1 && ((long long)B * cs > 2LL * p->num_sms ||
-                    (long long)cs * kVerifyThreads * kVerifyUnroll > 2LL * V))
+  while (cs > 1 && ((long long)B * cs > (long long)kPerSm * p->num_sms ||
+                    (long long)cs * kVerifyThreads * 8 > 2LL * V))
     cs >>= 1;
-  return launch_pdl_cluster(verify_kernel<T>, dim3((unsigned)B * cs), dim3(kVerifyThreads), cs, 0, s,
+  auto fn = wide ? verify_kernel<T, 4> : verify_kernel<T, 1>;
+  return launch_pdl_cluster(fn, dim3((unsigned)B * cs), dim3(kVerifyThreads), cs, 0, s,
                             (const T*)tp, (const T*)dp, drafts, u, noise, cu, n_draft, V, cs,
                             accepted, tokens, p->err);
 }
