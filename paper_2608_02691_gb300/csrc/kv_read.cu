@@ -35,11 +35,14 @@ constexpr int kThreads = (kMmaWarp + 1) * 32;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColD = 0, kColA = 256;  // D[g] at 128 g, A[g] at 256 + 64 g
 constexpr uint32_t kTileBytes = kRows * kD * 2;
+constexpr int kAhead = 4;  // tiles whose records a converter group has in flight
 
 struct Smem {
   uint16_t b[2][kD * kD];
   // output rows, bf16: [channel half][row][128 B], TMA 128-byte swizzle
   uint8_t stage[2][kTileBytes];
+  // records as read, of the group's next tiles: codes (2 x 16 B), {scale, min} words
+  uint4 raw[2][kAhead][3][kRows];
   alignas(16) float add[kD];  // mu (keys) or 0 (values)
   int cu[kCuCache + 1];
   int p0[kCuCache];
@@ -69,11 +72,6 @@ __device__ __forceinline__ void tma_store_3d(const void* tmap, int c0, int c1, i
                  "r"(tc05::smem_addr(src))
                : "memory");
 }
-
-// A row's record as read: codes and {scale, min} words.
-struct RawRow {
-  uint4 c0, c1, m;
-};
 
 template <bool kG128>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -131,17 +129,24 @@ kv_read_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
     const int g = warp >> 2, q = warp & 3, row = 32 * q + lane;
     const uint32_t tA = tmem + ((uint32_t)(32 * q) << 16) + kColA + 64u * g;
     auto cu = [&](int b) { return cached ? S.cu[b] : __ldcg(cu_read + b); };
-    // the record's page is requested a tile before the record itself
-    int page = -1, slot = 0;
+    // A tile's page entry is requested one tile of the group before its
+    // records are. The group's tokens only rise, so the sequence is searched
+    // once and then followed.
+    int lo = 0, page = 0, slot = 0;  // page is left as loaded: a test here would wait for it
+    bool have = false, found = false;
     auto request = [&](int i) {
-      page = -1;
+      have = false;
       const int tok = ((int)blockIdx.x + i * (int)gridDim.x) * kRows + row;
       if (i >= my_tiles || tok >= n_tok) return;
-      int lo = 0, hi = B;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (cu(mid) <= tok) lo = mid; else hi = mid;
+      if (!found) {
+        found = true;
+        int hi = B;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (cu(mid) <= tok) lo = mid; else hi = mid;
+        }
       }
+      while (lo + 1 < B && cu(lo + 1) <= tok) ++lo;
       const int c0 = cu(lo);
       if (!(c0 <= tok && tok < cu(lo + 1))) {
         atomicOr(err, OPTR_DEVERR_CU_NEW);
@@ -152,42 +157,49 @@ kv_read_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
         atomicOr(err, OPTR_DEVERR_POSITION);
         return;
       }
-      slot = (int)(pos % kPage);
-      page = __ldcg(bt + (size_t)lo * max_pages + pos / kPage);
-      if (page < 0) page = num_pages;  // flagged where it is used
+      have = true;
+      slot = (int)pos % kPage;
+      page = __ldcg(bt + (size_t)lo * max_pages + (int)pos / kPage);
     };
-    auto fetch = [&](RawRow& r) {
-      r.c0 = r.c1 = r.m = make_uint4(0u, 0u, 0u, 0u);
-      if (page < 0) return;
-      if (page >= num_pages) {
-        atomicOr(err, OPTR_DEVERR_PAGE_ID);
-        return;
-      }
-      const uint8_t* rec = pool + ((size_t)page * h_kv + h) * chunk_bytes(kG128);
-      const uint4* c = reinterpret_cast<const uint4*>(
-          rec + (kind ? OPTR_V_CODES_OFFSET : OPTR_K_CODES_OFFSET) + slot * 32);
+    uint32_t words = 0;  // G = 128: which of its 16 bytes of {scale, min} a tile's row has
+    // Copies into shared memory keep their loads in flight without registers;
+    // a thread reads back what it copied itself, so its own wait is enough.
+    auto fetch = [&](int at) {
+      uint4(*raw)[kRows] = S.raw[g][at];
+      const bool ok = have && (unsigned)page < (unsigned)num_pages;
+      if (have && !ok) atomicOr(err, OPTR_DEVERR_PAGE_ID);
+      const uint8_t* rec = pool + (ok ? ((size_t)page * h_kv + h) * chunk_bytes(kG128) : 0);
+      const int s = ok ? slot : 0;
+      const uint8_t* c = rec + (kind ? OPTR_V_CODES_OFFSET : OPTR_K_CODES_OFFSET) + s * 32;
       const uint8_t* m = rec + (kind ? vmeta_offset(kG128) : OPTR_K_META_OFFSET) +
-                         slot * meta_stride(kG128);
-      r.c0 = __ldcg(c);
-      r.c1 = __ldcg(c + 1);
-      if (kG128)
-        r.m.x = __ldcg(reinterpret_cast<const uint32_t*>(m));
-      else
-        r.m = __ldcg(reinterpret_cast<const uint4*>(m));
+                         (kG128 ? s & ~3 : s) * meta_stride(kG128);  // 16 bytes at least
+      cp_async16_zfill(&raw[0][row], c, ok);
+      cp_async16_zfill(&raw[1][row], c + 16, ok);
+      cp_async16_zfill(&raw[2][row], m, ok);
+      cp_async_commit();
+      words = words << 2 | (uint32_t)(s & 3);
     };
-    RawRow next;
     request(g);
-    fetch(next);
-    request(g + 2);
+    for (int k = 0; k < kAhead - 1; ++k) {
+      fetch(k);
+      request(g + 2 * (k + 1));
+    }
+#pragma unroll 1
     for (int i = g, k = 0; i < my_tiles; i += 2, ++k) {
-      const RawRow cur = next;
-      fetch(next);
-      request(i + 4);
+      fetch((k + kAhead - 1) % kAhead);
+      request(i + 2 * kAhead);
+      cp_async_wait<kAhead - 1>();
+      const uint4(*raw)[kRows] = S.raw[g][k % kAhead];
+      const uint4 c0 = raw[0][row], c1 = raw[1][row];
+      uint4 mw;
+      if (kG128)
+        mw.x = mw.y = mw.z = mw.w =
+            reinterpret_cast<const uint32_t*>(&raw[2][row])[words >> (2 * (kAhead - 1)) & 3u];
+      else
+        mw = raw[2][row];
+      const SlotMeta m = slot_meta(mw.x, mw.y, mw.z, mw.w);
+      const uint32_t word[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
       if (k > 0 && !__all_sync(0xffffffffu, tc05::bar_wait(&S.adone[g], (k - 1) & 1, abort))) break;
-      const SlotMeta m = kG128 ? slot_meta(cur.m.x, cur.m.x, cur.m.x, cur.m.x)
-                               : slot_meta(cur.m.x, cur.m.y, cur.m.z, cur.m.w);
-      const uint32_t word[8] = {cur.c0.x, cur.c0.y, cur.c0.z, cur.c0.w,
-                                cur.c1.x, cur.c1.y, cur.c1.z, cur.c1.w};
       tc05::fence_after();
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
@@ -201,6 +213,7 @@ kv_read_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       tc05::fence_before();
       tc05::bar_arrive(&S.aready[g]);
     }
+    cp_async_wait<0>();
   } else if (warp == kMmaWarp) {
     // --------------------------------------------------------------- MMA
     int last = -1;
