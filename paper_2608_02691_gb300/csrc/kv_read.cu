@@ -21,6 +21,7 @@
 #include "append_common.cuh"
 #include "decode_common.cuh"
 #include "dequant.cuh"
+#include "f32x2.cuh"
 #include "tc05.cuh"
 #include "tmap.cuh"
 
@@ -239,48 +240,61 @@ kv_read_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
     // ---------------------------------------------------------- epilogue
     const int g = (warp - kEpiWarp) >> 2, q = warp & 3, row = 32 * q + lane;
     const uint32_t tD = tmem + ((uint32_t)(32 * q) << 16) + kColD + 128u * g;
-    uint8_t* out = S.stage[g];
     const bool leader = q == 0 && lane == 0;
     const CUtensorMap* tmap = kind ? &tmap_v : &tmap_k;
-    for (int i = g, k = 0; i < my_tiles; i += 2, ++k) {
+    bool left = false;
+    for (int i = g, k = 0; i < my_tiles && !left; i += 2, ++k) {
       const bool ok = __all_sync(0xffffffffu, tc05::bar_wait(&S.dready[g], k & 1, abort));
-      // the group's previous copies have read the stage
-      if (leader) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-      group_sync(1 + g);
-      if (ok) {
-        tc05::fence_after();
+      tc05::fence_after();
+      // a channel half at a time: the other half's copy may still be reading
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t d[32];
-          tc05::tmem_ld32(tD + 32u * c, d);
-          tc05::tmem_wait_ld();
+      for (int half = 0; half < 2; ++half) {
+        uint8_t* out = S.stage[g] + half * (kTileBytes / 2);
+        if (leader) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+        group_sync(1 + g);
+        if (ok) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int ch = 32 * c + 8 * j + 2 * e;
-              const float2 add = *reinterpret_cast<const float2*>(&S.add[ch]);
-              const __nv_bfloat162 z = __floats2bfloat162_rn(
-                  fmaf(__uint_as_float(d[8 * j + 2 * e]), 1.f / 64.f, add.x),
-                  fmaf(__uint_as_float(d[8 * j + 2 * e + 1]), 1.f / 64.f, add.y));
-              y[e] = *reinterpret_cast<const uint32_t*>(&z);
+          for (int c = 0; c < 2; ++c) {
+            uint32_t d[32];
+            tc05::tmem_ld32(tD + 64u * half + 32u * c, d);
+            tc05::tmem_wait_ld();
+            if (half == 1 && c == 1) {
+              tc05::fence_before();
+              tc05::bar_arrive(&S.dfree[g]);
             }
-            const int chunk = 4 * (c & 1) + j;  // of the channel half c / 2
-            *reinterpret_cast<uint4*>(out + (c >> 1) * (kTileBytes / 2) + row * 128 +
-                                      ((chunk ^ (row & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              uint32_t y[4];
+#pragma unroll
+              for (int e = 0; e < 4; e += 2) {
+                const float4 add =
+                    *reinterpret_cast<const float4*>(&S.add[64 * half + 32 * c + 8 * j + 2 * e]);
+                const uint32_t* x = &d[8 * j + 2 * e];
+                const float2 inv = make_float2(1.f / 64.f, 1.f / 64.f);
+                const float2 lo = fma2(make_float2(__uint_as_float(x[0]), __uint_as_float(x[1])),
+                                       inv, make_float2(add.x, add.y));
+                const float2 hi = fma2(make_float2(__uint_as_float(x[2]), __uint_as_float(x[3])),
+                                       inv, make_float2(add.z, add.w));
+                const __nv_bfloat162 zl = __floats2bfloat162_rn(lo.x, lo.y);
+                const __nv_bfloat162 zh = __floats2bfloat162_rn(hi.x, hi.y);
+                y[e] = *reinterpret_cast<const uint32_t*>(&zl);
+                y[e + 1] = *reinterpret_cast<const uint32_t*>(&zh);
+              }
+              *reinterpret_cast<uint4*>(out + row * 128 + (((4 * c + j) ^ (row & 7)) << 4)) =
+                  make_uint4(y[0], y[1], y[2], y[3]);
+            }
           }
+          tc05::fence_proxy_async();
         }
-        tc05::fence_before();
-        tc05::bar_arrive(&S.dfree[g]);
-        tc05::fence_proxy_async();
-      }
-      if (group_any(1 + g, !ok)) break;  // the group leaves together
-      if (leader) {
-        const int tok0 = ((int)blockIdx.x + i * (int)gridDim.x) * kRows;
-        tma_store_3d(tmap, 0, h, tok0, out);
-        tma_store_3d(tmap, 64, h, tok0, out + kTileBytes / 2);
-        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        if (group_any(1 + g, !ok)) {  // the group leaves together
+          left = true;
+          break;
+        }
+        if (leader) {
+          const int tok0 = ((int)blockIdx.x + i * (int)gridDim.x) * kRows;
+          tma_store_3d(tmap, 64 * half, h, tok0, out);
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
       }
     }
     if (leader) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
