@@ -28,9 +28,10 @@ __device__ __forceinline__ float prob(float x) { return x; }
 __device__ __forceinline__ float prob(__nv_bfloat16 x) { return __bfloat162float(x); }
 
 // A candidate as one number: the larger value first, then the lower token
-// (values are not negative, so their bits order as they do).
+// (values are not negative, so their bits order as they do; the sum makes -0 a
+// zero like any other).
 __device__ __forceinline__ unsigned long long candidate(float value, int token) {
-  return ((unsigned long long)__float_as_uint(value) << 32) | (0xFFFFFFFFu - (unsigned)token);
+  return ((unsigned long long)__float_as_uint(__fadd_rn(value, 0.f)) << 32) | (0xFFFFFFFFu - (unsigned)token);
 }
 
 __device__ __forceinline__ unsigned long long warp_max(unsigned long long x) {
