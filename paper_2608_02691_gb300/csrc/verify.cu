@@ -156,7 +156,8 @@ verify_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
     float top = -1.f;
     int at = 0;
     const bool less = q && pass == 0;
-    for (int v0 = lo + tid; v0 < hi; v0 += kVerifyThreads * kUnroll) {
+    for (int base = lo; base < hi; base += kVerifyThreads * kUnroll) {
+      const int v0 = base + tid;
       float r[kUnroll][kVec], z[kUnroll][kVec], y[kUnroll][kVec];
 #pragma unroll
       for (int j = 0; j < kUnroll; ++j) {
@@ -165,22 +166,35 @@ verify_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
         load_vec(e + v, z[j]);
         if (less) load_vec(q + v, y[j]);
       }
+      // approximate quotients choose whom to divide: those that may reach the
+      // warp's largest so far
+      float m = fmaxf(top, 0.f);
 #pragma unroll
       for (int j = 0; j < kUnroll; ++j) {
         const int v = v0 + j * kVerifyThreads;
-        if (v >= hi) break;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
           float x = r[j][i];
           if (less) x = fmaxf(__fsub_rn(x, y[j][i]), 0.f);
           if (pass == 0 && v * kVec + i == cut) x = 0.f;
-          // x / z > top needs x >= top z up to rounding: most candidates fall
-          // here, without a division
-          if (x >= 0.f && x >= top * z[j][i] * 0.99999f) {
-            const float w = __fdiv_rn(x, z[j][i]);
+          r[j][i] = v < hi ? x : -1.f;
+          y[j][i] = __fdividef(r[j][i], z[j][i]);
+          m = fmaxf(m, y[j][i]);
+        }
+      }
+      m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
+      // outside kFar the approximation may be off by more than 2 ulp: divide all there
+      constexpr float kFar = 1e30f;
+      const float least = m < 1.f / kFar ? 0.f : fminf(m, kFar) * 0.99999f;
+#pragma unroll
+      for (int j = 0; j < kUnroll; ++j) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          if (!(y[j][i] < least) || !(z[j][i] < kFar)) {
+            const float w = r[j][i] >= 0.f ? __fdiv_rn(r[j][i], z[j][i]) : -1.f;
             if (w > top) {
               top = w;
-              at = v * kVec + i;
+              at = (v0 + j * kVerifyThreads) * kVec + i;
             }
           }
         }
