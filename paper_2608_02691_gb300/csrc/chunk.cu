@@ -11,7 +11,15 @@
 // (sequence, KV head, query block) segments are put into one line that is cut
 // into equal ranges, one per SM: a long context of one sequence, a ragged batch
 // and a causal prompt (whose blocks see between one tile and all) fill the GPU
-// alike, and a CTA leaves at most two partial results.
+// alike, and a CTA leaves at most two partial results.  A block of 32 tokens or
+// fewer is one query tile, whose key tiles the two softmax groups take in turn.
+//
+// Bound.  Chunk tokens (bf16): the tensor cores; an 8192-token prompt of 32 heads
+// takes 405 us, 1.36 PFLOP/s.  INT2 tiles: shared memory and the chain of a tile.
+// A 128-key tile is 64 KB of fp16 operands written (two warpgroups, from the
+// records' 12 KB) and 96 KB read per query tile by its two products, 1.4 us for
+// one query tile and 2.0 us for two; 2048 tokens over 32768 take 880 us, 16 x 5 over
+// 8192 78 us and 8 over 131072 75 us, the records alone at 1.3 TB/s.
 //
 // A row's softmax runs over the tiles with a running maximum m and sum l
 // (float32, log2 domain); O and m, l of different ranges merge exactly.
@@ -920,7 +928,10 @@ extern "C" optr_status optr_chunk_attention_win(
       !(w.win ? token_rows_map(&mw, w.win, n_slots * h_kv * 2 * win_rows, 1, kTile)
               : token_rows_map(&mw, k, n_tok, h_kv, kTile)))
     return OPTR_ERR_CUDA;
-  const bool few = max_new <= 16;
+  // few rows of many parts: 8 or more for each (sequence, KV head).  8 drafts over
+  // 131072 tokens: 74.8 us, 76.0 without the split; 16 x 5 over 8192, where the
+  // rule says no: 78.6, 81.6 with it.
+  const bool few = max_new <= 16 && (long long)B * h_kv * 8 <= l.W;
   const int per = few ? 2 : 8;  // rows of a joining CTA
   const dim3 joins(l.W, (std::min(l.rows, 4 * max_new) + per - 1) / per);
   e = launch_pdl(chunk_kernel, dim3(l.W), dim3(kThreads), sizeof(Smem), stream, mq, mk, mv, mw, A);

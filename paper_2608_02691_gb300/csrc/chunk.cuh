@@ -2,8 +2,6 @@
 // kernels (chunk.cu).
 #pragma once
 
-#include <cudaTypedefs.h>
-
 #include "decode_common.cuh"
 #include "optr_internal.cuh"
 #include "tc05.cuh"
@@ -79,12 +77,14 @@ __device__ __forceinline__ SeqWork seq_work(const ChunkArgs& A, int b) {
 __device__ __forceinline__ int tiles_of(int keys) { return (keys + kTile - 1) / kTile; }
 
 // Cost of the first m query blocks of a sequence (one head), in tiles, `past`
-// cached tiles each: block qb sees own tiles 0 .. qb / 2, and kBegin tiles' time
-// goes into its start and end.
-constexpr int kBegin = 2;
-constexpr int kLeast = 4;  // units that are worth a range of their own
-__device__ __forceinline__ long long block_cost(long long m, int past) {
-  return m * (past + kBegin) + (m + 1) * (m + 1) / 4;
+// cached tiles each: block qb sees own tiles 0 .. qb / 2, and begin_cost tiles'
+// time goes into its start and end, more where INT2 tiles have the queries rotated
+// and the output rotated back.  Measured: a ragged batch of 64 sequences takes 134 us,
+// 156 with 2 for all; an 8192-token prompt 405 us, 418 with 5 for all.
+constexpr int kBegin = 2, kBeginInt2 = 6;
+__device__ __forceinline__ int begin_cost(int n_int) { return n_int > 0 ? kBeginInt2 : kBegin; }
+__device__ __forceinline__ long long block_cost(long long m, int past, int begin) {
+  return m * (past + begin) + (m + 1) * (m + 1) / 4;
 }
 
 // A run of tiles of one (sequence, KV head, query block): tiles t0 .. t1-1 of
@@ -100,17 +100,19 @@ struct Piece {
 };
 
 __device__ __forceinline__ long long seq_cost(const SeqWork& s) {
-  return s.n_new > 0 ? block_cost((s.n_new + kQTok - 1) / kQTok, tiles_of(s.n_int) + tiles_of(s.n_win))
+  return s.n_new > 0 ? block_cost((s.n_new + kQTok - 1) / kQTok, tiles_of(s.n_int) + tiles_of(s.n_win),
+                                  begin_cost(s.n_int))
                      : 0;
 }
 
 // The flat index space orders units of cost as (sequence, KV head, query block,
-// unit); CTA w takes [w F / W, (w + 1) F / W).  Of a block's kBegin + tiles units
-// the first kBegin stand for no tile.  One warp goes through a CTA's range: lane
+// unit); CTA w takes [w F / W, (w + 1) F / W).  Of a block's begin_cost + tiles
+// units the first begin_cost stand for no tile.  One warp goes through a CTA's range: lane
 // i holds sequence b0 + i.
 struct PieceFinder {
   long long f, f1, F;    // the next unit, the range's end, all units
-  int W;                 // ranges: A.W, or fewer so that each has kLeast units
+  int W;                 // ranges: A.W, or fewer so that each has a unit (one token over 1024:
+                         // 14.3 us, 19.2 with four units at least)
   long long f_seg;       // first unit of the last piece's segment
   int b0;                // the 32 sequences held, and what comes before them
   long long base, incl;  // (cost of one head); incl: up to and with the lane's
@@ -137,7 +139,7 @@ struct PieceFinder {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     F = sum * A.h_kv;
-    W = (int)min((long long)A.W, max(1ll, F / kLeast));
+    W = (int)min((long long)A.W, max(1ll, F));
     f = w < W ? F * w / W : F;
     f1 = w < W ? F * (w + 1) / W : F;
     base = 0;
@@ -145,7 +147,7 @@ struct PieceFinder {
   }
 
   // The piece at f (< f1), in all lanes; it has no tile (t1 = t0) where the
-  // range ends within kBegin.
+  // range ends within begin_cost.
   __device__ __forceinline__ void next(const ChunkArgs& A, Piece& p) {
     unsigned over;  // lanes whose sequence ends after f
     while (!(over = __ballot_sync(0xffffffffu, (base + incl) * A.h_kv > f))) {
@@ -169,17 +171,18 @@ struct PieceFinder {
     long long r = f - before * A.h_kv;
     p.h = (int)(r / c);
     r -= p.h * c;
+    const int begin = begin_cost(p.n_int);
     int q0 = 0, q1 = (p.n_new + kQTok - 1) / kQTok;
     while (q1 - q0 > 1) {
       const int mid = (q0 + q1) >> 1;
-      if (block_cost(mid, p.I + p.Wt) <= r) q0 = mid; else q1 = mid;
+      if (block_cost(mid, p.I + p.Wt, begin) <= r) q0 = mid; else q1 = mid;
     }
     p.qb = q0;
     p.total = p.I + p.Wt + q0 / 2 + 1;
-    const long long u0 = r - block_cost(q0, p.I + p.Wt);
-    const long long u1 = min((long long)p.total + kBegin, u0 + (f1 - f));
-    p.t0 = (int)max(0ll, u0 - kBegin);
-    p.t1 = (int)max(0ll, u1 - kBegin);
+    const long long u0 = r - block_cost(q0, p.I + p.Wt, begin);
+    const long long u1 = min((long long)p.total + begin, u0 + (f1 - f));
+    p.t0 = (int)max(0ll, u0 - begin);
+    p.t1 = (int)max(0ll, u1 - begin);
     f_seg = f - u0;
     f += u1 - u0;
   }
@@ -224,7 +227,7 @@ __device__ __forceinline__ void find_pieces(const ChunkArgs& A, int w, Piece* pi
     while (next.f < next.f1 && p.t1 == p.t0) next.next(A, p);
     more = p.t1 > p.t0;
     if (more && p.t0 == 0 && p.t1 < p.total)
-      seg = ChunkSeg{next.F, next.f_seg + kBegin + p.total, p.c0, p.n_new, p.h, p.qb, next.W, 1};
+      seg = ChunkSeg{next.F, next.f_seg + begin_cost(p.n_int) + p.total, p.c0, p.n_new, p.h, p.qb, next.W, 1};
     if (n >= kAhead &&
         !__all_sync(0xffffffffu, tc05::bar_wait_spin(&empty[i], (n / kAhead - 1) & 1, abort)))
       break;
