@@ -17,7 +17,9 @@
 //                   into a swizzled shared-memory tile that two TMA copies
 //                   store.
 // Bound by memory: 96 B (G = 32) or 72 B read and 512 B written per token and
-// KV head.
+// KV head.  16 x 8192 tokens of 8 KV heads take 126 us, 5.0 TB/s, 74% of a copy's
+// rate; 144 with the records a tile ahead in registers, 129 with whole tiles
+// stored at a time.  777 tokens take 7.4 us, all latency.
 #include "append_common.cuh"
 #include "decode_common.cuh"
 #include "dequant.cuh"
