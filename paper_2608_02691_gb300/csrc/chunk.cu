@@ -15,7 +15,7 @@
 // fewer is one query tile, whose key tiles the two softmax groups take in turn.
 //
 // Bound.  Chunk tokens (bf16): the tensor cores; an 8192-token prompt of 32 heads
-// takes 405 us, 1.36 PFLOP/s.  INT2 tiles: shared memory and the chain of a tile.
+// takes 405 us, 1.36 PFLOP/s.  INT2 tiles: the chain of a tile, no one part of it.
 // A 128-key tile is 64 KB of fp16 operands written (two warpgroups, from the
 // records' 12 KB) and 96 KB read per query tile by its two products, 1.4 us for
 // one query tile and 2.0 us for two; 2048 tokens over 32768 take 880 us, 16 x 5 over
