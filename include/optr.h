@@ -439,7 +439,7 @@ optr_status optr_decode_step_win(const optr_params* p, const void* q,
  * tokens are written (optr_kv_append_win turns the window ring over), and write
  * only those that stay: rejected drafts then leave no trace.  With R_v = NULL
  * at create, v and out are in the folded basis.
- *   q, out      device bf16 [n_tok][h_q][D].
+ *   q, out      device bf16 [n_tok][h_q][D]; out overlaps none of the inputs.
  *   k, v        device bf16 [n_tok][h_kv][D].
  *   n_tok       host; new tokens of all sequences (0 is a no-op).
  *   cu_new      device int32 [B+1], as in optr_kv_append.
@@ -507,8 +507,8 @@ optr_status optr_kv_read(const optr_params* p, int n_tok,
  * while u_i q_i(x_i) < p_i(x_i) (one float32 product); a of them are.  The next
  * token is the first maximum over the vocabulary of r(v) / e(v) in float32,
  *      r = max(p_a - q_a, 0)  (a < n)     or  r = p_n  (a = n),
- * and r = p_a where that residual is zero everywhere: a draw from r / sum r
- * when the numbers e of the sequence are independent and exponential.
+ * and r = p_a where the residual's quotients are zero everywhere: a draw from
+ * r / sum r when the numbers e of the sequence are independent and exponential.
  *   target_probs device [n_draft + B][vocab], float32 or bf16 (probs_dtype).
  *   draft_probs  device [n_draft][vocab] of the same type, or NULL: drafted
  *                without probabilities (q_i is 1 at x_i and 0 elsewhere).
