@@ -100,7 +100,7 @@ verify_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
               const float* __restrict__ noise, const int32_t* __restrict__ cu, int n_draft,
               int V, int cs, int32_t* __restrict__ accepted, int32_t* __restrict__ tokens,
               unsigned* err) {
-  constexpr int kUnroll = kVec == 1 ? 4 : 1;
+  constexpr int kUnroll = kVec == 1 ? 4 : 1;  // accesses of a batch (wide, 2: 14.4 us for 10.3)
   __shared__ int head[2];
   __shared__ unsigned long long wbest[kVerifyThreads / 32];
   __shared__ unsigned long long best[2];  // this CTA's, by pass
