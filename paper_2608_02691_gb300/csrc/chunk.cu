@@ -56,6 +56,9 @@ constexpr uint32_t kHalf = kTile * 128;      // 64 channels of 128 rows
 constexpr uint32_t kOperand = 2 * kHalf;     // 128 x 128 of 16 bits
 constexpr int kPieces = 3;       // pieces found ahead
 constexpr float kSlack = 8.f;  // a row's maximum may grow by 2^8 before O is rescaled
+// The largest weight stands at 2^kLift, with the slack at 2^15 at most, inside fp16:
+// weights count down to 2^-32 of it, and a million keys below that weigh 2^-12.
+constexpr float kLift = 7.f;
 
 struct Smem {
   uint8_t q[2][kOperand];            // the query operand, by tile
@@ -113,7 +116,8 @@ __device__ __forceinline__ void store32(void* p, const uint32_t (&y)[8], bool wh
 
 // One row of a logit tile: S (128 columns of tensor memory at tS) becomes P =
 // 2^(S scale - off - m) in 16 bits over its first 64 columns; m, l and O are
-// brought along.  Bits of `mask` and the first `lim` columns count.
+// brought along.  Bits of `mask` and the first `lim` columns count.  l sums the weights
+// before they are rounded (by up to 2^-11 each in fp16, 2^-8 in bf16, to either side).
 template <bool kBf16>
 __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, float scale, float off,
                                              uint4 mask, int lim, bool fresh, float& m, float& l) {
@@ -143,7 +147,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, float sca
       for (int i = 0; i < 4; ++i)
         x[i] = fmaxf(x[i], fmaxf(__uint_as_float(s[j + i]), __uint_as_float(s[j + 4 + i])));
   }
-  const float t = fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), scale, -off);
+  const float t = fmaf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), scale, -off) - kLift;
   if (fresh) {
     m = fmaxf(m, t);
   } else if (__any_sync(0xffffffffu, t > m + kSlack)) {
