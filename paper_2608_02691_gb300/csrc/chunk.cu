@@ -357,23 +357,37 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
       if (dead) break;
       if (ints > 0) {
         // O / l into the model's basis: the A operand of the product with 64
-        // R_v^T takes P's place
+        // R_v^T takes P's place, in fp16; where a row lies too low in fp16's range
+        // (a mean over many keys, or small values) over a power of two 2^E > its largest
         if (!wait(&S.o_full[g], no++)) break;
         const float inv = l > 0.f ? 1.f / l : 0.f;
+        float down = inv;
+        int E = 0;
 #pragma unroll 1
-        for (int c = 0; c < 4 && rows; ++c) {
-          uint32_t o[32], a[16];
-          tc05::tmem_ld32(tO + 32 * c, o);
-          tc05::tmem_wait_ld();
+        for (int pass = 0; pass < 2 && rows; ++pass) {
+          __half2 x = __float2half2_rn(0.f);
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            uint32_t o[32], a[16];
+            tc05::tmem_ld32(tO + 32 * c, o);
+            tc05::tmem_wait_ld();
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            a[e] = pack16<false>(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
-          tc05::tmem_st16(tS + 16 * c, a);
+            for (int e = 0; e < 16; ++e) {
+              a[e] = pack16<false>(__uint_as_float(o[2 * e]) * down, __uint_as_float(o[2 * e + 1]) * down);
+              x = __hmax2(x, __habs2(*reinterpret_cast<const __half2*>(&a[e])));
+            }
+            tc05::tmem_st16(tS + 16 * c, a);
+          }
+          tc05::tmem_wait_st();
+          const float top = fmaxf(__low2float(x), __high2float(x));
+          // from 2^-10 on fp16's steps of 2^-24 are at most 2^-14 of the row's largest
+          if (pass == 1 || !__any_sync(0xffffffffu, valid && top < 0x1p-10f)) break;
+          E = max((int)(__float_as_uint(top) >> 23) - 126, -24);
+          down = inv * __uint_as_float((uint32_t)(127 - E) << 23);
         }
-        tc05::tmem_wait_st();
-        if (l > 0.f) {  // O is now 64 of weight 2^m l / 64
-          m += __log2f(l) - 6.f;
-          l = 64.f;
+        if (l > 0.f) {  // O is now 2^(6 - E) of weight 2^m l / 2^(6 - E)
+          m += __log2f(l) - (float)(6 - E);
+          l = __uint_as_float((uint32_t)(133 - E) << 23);
         }
         ready();
       }
