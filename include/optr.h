@@ -160,7 +160,8 @@ typedef enum {
 #define OPTR_DEVERR_POSITION 2u  /* append position >= max_pages * 16 or <0 */
 #define OPTR_DEVERR_SEQ_LEN 4u   /* seq_lens[b] < 0 or > max_pages * 16     */
 #define OPTR_DEVERR_CU_NEW 8u    /* cu_new not non-decreasing within n_tok  */
-#define OPTR_DEVERR_FP16_RANGE 16u /* tensor-core append: |k| or |v| >= 65504 */
+#define OPTR_DEVERR_FP16_RANGE 16u /* tensor-core append: |k| or |v| >= 65504;
+                                      chunk attention, read-back: a cached value past fp16 */
 #define OPTR_DEVERR_TIMEOUT 32u  /* internal: a kernel's bounded wait gave up */
 #define OPTR_DEVERR_WIN_SLOT 64u /* window slot of a sequence < 0 or >= n_slots */
 #define OPTR_DEVERR_CALIB_RANGE 128u /* calibration: generator norm past exp's scaling range */
@@ -454,7 +455,10 @@ optr_status optr_decode_step_win(const optr_params* p, const void* q,
  * sequence with pos0 out of range (OPTR_DEVERR_SEQ_LEN), more than max_new
  * tokens or inconsistent cu_new (OPTR_DEVERR_CU_NEW) gets zero rows; keys of an
  * out-of-range page (OPTR_DEVERR_PAGE_ID) or window slot
- * (OPTR_DEVERR_WIN_SLOT) are left out.  Nothing is allocated or synchronised.
+ * (OPTR_DEVERR_WIN_SLOT) are left out.  An INT2 group with an end (min or
+ * 3 scale + min) past fp16's range, which a rotated range of 65504 or more can
+ * have, sets OPTR_DEVERR_FP16_RANGE and leaves the rows that attend to it
+ * unspecified.  Nothing is allocated or synchronised.
  */
 size_t optr_chunk_workspace_size(const optr_params* p, int n_tok, int B, int max_new);
 
@@ -490,7 +494,9 @@ optr_status optr_chunk_attention_win(const optr_params* p, const void* q,
  *   k, v        device bf16 [n_tok][h_kv][D], written.
  *   n_tok       host; rows (0 is a no-op).  The rest as in optr_kv_append.
  * A row whose position, page or cu_read entry is out of range is flagged
- * (OPTR_DEVERR_*) and reads as the row of an all-zero record.
+ * (OPTR_DEVERR_*) and reads as the row of an all-zero record.  One with a group
+ * end (min or 3 scale + min) past fp16's range sets OPTR_DEVERR_FP16_RANGE and is
+ * unspecified.
  */
 optr_status optr_kv_read(const optr_params* p, int n_tok,
                          const int32_t* cu_read, const int32_t* pos0,

@@ -481,6 +481,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
     const int g = (warp - kDeqWarp) >> 2, quarter = warp & 3, key = tid & 127;
     const int ms = meta_stride(A.compact);
     uint32_t nk = 0, nv = 0, nt = 0, raws = 0, tma = 0, grants[2][kRing] = {};
+    uint32_t past = 0;  // whether a key or value left fp16's range
     Piece p;
     for (uint32_t n = 0; next_piece(n, p); ++n) {
       const int nint = p.int_tiles(), nother = p.t1 - p.t0 - nint;
@@ -537,6 +538,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
           uint8_t* dst = (kind ? S.v[st] : S.k[st]) + key * 128;
           const uint4 m = kind ? mm[1] : mm[0];
           const SlotMeta sm = slot_meta(m.x, m.y, m.z, m.w);
+          note_range(sm, past);
 #pragma unroll 1
           for (int half = 0; half < 2; ++half) {
             const uint4 y = kind ? (half ? c[1][1] : c[1][0]) : (half ? c[0][1] : c[0][0]);
@@ -578,6 +580,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
         tc05::bar_arrive(&S.v_full[st]);
       }
     }
+    if (any_past_range(past)) atomicOr(A.err, OPTR_DEVERR_FP16_RANGE);
   } else if (warp == kTmaWarp || warp == kTmaWarp + 1) {
     // ------------------------------------------------------------ TMA
     // One warp for the queries, records, keys and R_k, one for the values and

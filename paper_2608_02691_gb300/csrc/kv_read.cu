@@ -182,6 +182,7 @@ kv_read_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       cp_async_commit();
       words = words << 2 | (uint32_t)(s & 3);
     };
+    uint32_t past = 0;  // whether a value left fp16's range
     request(g);
     for (int k = 0; k < kAhead - 1; ++k) {
       fetch(k);
@@ -201,6 +202,7 @@ kv_read_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       else
         mw = raw[2][row];
       const SlotMeta m = slot_meta(mw.x, mw.y, mw.z, mw.w);
+      note_range(m, past);
       const uint32_t word[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
       if (k > 0 && !__all_sync(0xffffffffu, tc05::bar_wait(&S.adone[g], (k - 1) & 1, abort))) break;
       tc05::fence_after();
@@ -217,6 +219,7 @@ kv_read_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
       tc05::bar_arrive(&S.aready[g]);
     }
     cp_async_wait<0>();
+    if (any_past_range(past)) atomicOr(err, OPTR_DEVERR_FP16_RANGE);
   } else if (warp == kMmaWarp) {
     // --------------------------------------------------------------- MMA
     int last = -1;
