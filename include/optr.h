@@ -526,10 +526,10 @@ optr_status optr_kv_read(const optr_params* p, int n_tok,
  *   tokens       device int32 [n_draft + B], rows as target_probs': the
  *                accepted drafts, the next token, then -1.
  * Probabilities are finite and not negative; a row need not sum to exactly 1.
- * A draft out of 0 .. vocab-1 is rejected and sets OPTR_DEVERR_TOKEN; a
- * sequence whose cu_draft is out of range gets accepted = -1 and sets
- * OPTR_DEVERR_CU_NEW (p serves the device error word only).  Nothing is
- * allocated or synchronised.
+ * A draft out of 0 .. vocab-1 sets OPTR_DEVERR_TOKEN wherever it stands in its
+ * sequence, and is rejected where it is reached; a sequence whose cu_draft is
+ * out of range gets accepted = -1, no tokens, and sets OPTR_DEVERR_CU_NEW (p
+ * serves the device error word only).  Nothing is allocated or synchronised.
  */
 #define OPTR_PROBS_F32 0
 #define OPTR_PROBS_BF16 1

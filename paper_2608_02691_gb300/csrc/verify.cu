@@ -122,7 +122,7 @@ verify_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
   const int lo = (int)((long long)n_vec * rank / cs), hi = (int)((long long)n_vec * (rank + 1) / cs);
   // first rejected draft: one lane per draft, 32 at a time
   if (warp == 0) {
-    int a = n, bad = -1;
+    int a = n, x_a = -1;
     for (int i0 = 0; i0 < n; i0 += 32) {
       const int i = i0 + lane;
       bool rej = false;
@@ -139,14 +139,19 @@ verify_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
       const unsigned m = __ballot_sync(0xffffffffu, rej);
       if (m) {
         a = i0 + __ffs(m) - 1;
-        bad = __shfl_sync(0xffffffffu, x, __ffs(m) - 1);
+        x_a = __shfl_sync(0xffffffffu, x, __ffs(m) - 1);
         break;
       }
     }
     if (lane == 0) {
       head[0] = a;
-      head[1] = bad;
-      if (a < n && (bad < 0 || bad >= V) && rank == 0) atomicOr(err, OPTR_DEVERR_TOKEN);
+      head[1] = x_a;
+    }
+  } else if (warp == 1 && rank == 0) {
+    // drafts out of range, also those that no acceptance reaches
+    for (int i = lane; i < n; i += 32) {
+      const int x = __ldcg(drafts + c0 + i);
+      if (x < 0 || x >= V) atomicOr(err, OPTR_DEVERR_TOKEN);
     }
   }
   __syncthreads();
