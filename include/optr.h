@@ -521,15 +521,18 @@ optr_status optr_kv_read(const optr_params* p, int n_tok,
  *   drafts       device int32 [n_draft].
  *   uniform      device float32 [n_draft]: u, in [0, 1).
  *   noise        device float32 [B][vocab]: e, positive.
- *   cu_draft     device int32 [B+1], cu_draft[B] = n_draft.
+ *   cu_draft     device int32 [B+1], cu_draft[0] = 0, non-decreasing,
+ *                cu_draft[B] = n_draft.
  *   accepted     device int32 [B]: a.
  *   tokens       device int32 [n_draft + B], rows as target_probs': the
  *                accepted drafts, the next token, then -1.
  * Probabilities are finite and not negative; a row need not sum to exactly 1.
  * A draft out of 0 .. vocab-1 sets OPTR_DEVERR_TOKEN wherever it stands in its
  * sequence, and is rejected where it is reached; a sequence whose cu_draft is
- * out of range gets accepted = -1, no tokens, and sets OPTR_DEVERR_CU_NEW (p
- * serves the device error word only).  Nothing is allocated or synchronised.
+ * out of range gets accepted = -1, no tokens, and sets OPTR_DEVERR_CU_NEW.  So
+ * do offsets that do not begin at 0 or end at n_draft; rows of tokens that
+ * belong to no sequence are not written.  (p serves the device error word
+ * only.)  Nothing is allocated or synchronised.
  */
 #define OPTR_PROBS_F32 0
 #define OPTR_PROBS_BF16 1

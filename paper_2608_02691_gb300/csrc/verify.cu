@@ -108,6 +108,9 @@ verify_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_wait();
   pdl_trigger();
+  // drafts before the first sequence's or after the last one's
+  if (blockIdx.x == 0 && tid == 64 && (__ldcg(cu) != 0 || __ldcg(cu + gridDim.x / cs) != n_draft))
+    atomicOr(err, OPTR_DEVERR_CU_NEW);
   const int c0 = __ldcg(cu + b), c1 = __ldcg(cu + b + 1);
   if (c0 < 0 || c1 < c0 || c1 > n_draft) {  // the same for the whole cluster
     if (rank == 0 && tid == 0) {

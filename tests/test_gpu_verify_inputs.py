@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2608_02691_gb300 import optr
-from test_gpu_verify import Case, p  # noqa: F401
+from test_gpu_verify import Case, i32, p  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -22,3 +22,19 @@ def test_bad_tokens_after_a_rejection_are_flagged(p, first, at, bad, probs):  # 
     c.x[3 + at] = bad
     assert c.run(p) == want
     assert optr.optr_device_error(p) == optr.OPTR_DEVERR_TOKEN
+
+
+@pytest.mark.parametrize("cu,rows", [([2, 5, 9], (2, 11)), ([0, 5, 7], (0, 9)), ([1, 1, 1], (1, 3))])
+def test_offsets_that_leave_drafts_out_are_flagged(p, cu, rows):  # noqa: F811
+    """Offsets that do not begin at 0 or end at n_draft: each sequence has its
+    drafts all the same, rows of none stay as they were."""
+    c = Case([5, 4], 700, seed=21)
+    c.u.zero_()
+    acc, tok = c.run(p, cu=i32(cu))
+    assert optr.optr_device_error(p) == optr.OPTR_DEVERR_CU_NEW
+    lo, hi = rows
+    assert tok[:lo] == [99] * lo and tok[hi:] == [99] * (11 - hi)
+    assert all(0 <= t < 700 or t == -1 for t in tok[lo:hi])
+    c.lens = [b - a for a, b in zip(cu, cu[1:])]
+    c.tp, c.dp, c.x, c.u = c.tp[lo:hi], c.dp[cu[0]:cu[-1]], c.x[cu[0]:cu[-1]], c.u[cu[0]:cu[-1]]
+    assert (acc, tok[lo:hi]) == c.plain()
