@@ -69,15 +69,16 @@ __device__ __forceinline__ unsigned long long cluster_load(const unsigned long l
   return v;
 }
 
-// kVec consecutive probabilities or noise values, as float.
+// kVec consecutive probabilities or noise values, as float (the kernel may have
+// started while their producer ran: not through the non-coherent path).
 template <int kVec>
 __device__ __forceinline__ void load_vec(const float* p, float (&x)[kVec]) {
   if constexpr (kVec == 1) {
-    x[0] = *p;
+    x[0] = __ldcg(p);
   } else {
 #pragma unroll
     for (int i = 0; i < kVec; i += 4) {
-      const float4 y = *reinterpret_cast<const float4*>(p + i);
+      const float4 y = __ldcg(reinterpret_cast<const float4*>(p + i));
       x[i] = y.x, x[i + 1] = y.y, x[i + 2] = y.z, x[i + 3] = y.w;
     }
   }
@@ -85,9 +86,9 @@ __device__ __forceinline__ void load_vec(const float* p, float (&x)[kVec]) {
 template <int kVec>
 __device__ __forceinline__ void load_vec(const __nv_bfloat16* p, float (&x)[kVec]) {
   if constexpr (kVec == 1) {
-    x[0] = __bfloat162float(*p);
+    x[0] = __bfloat162float(__ldcg(p));
   } else {
-    const uint2 y = *reinterpret_cast<const uint2*>(p);
+    const uint2 y = __ldcg(reinterpret_cast<const uint2*>(p));
     x[0] = __uint_as_float(y.x << 16), x[1] = __uint_as_float(y.x & 0xffff0000u);
     x[2] = __uint_as_float(y.y << 16), x[3] = __uint_as_float(y.y & 0xffff0000u);
   }
@@ -134,8 +135,8 @@ verify_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
         x = __ldcg(drafts + c0 + i);
         rej = true;
         if (x >= 0 && x < V) {
-          const float p = prob(tp[((size_t)c0 + b + i) * V + x]);
-          const float q = dp ? prob(dp[((size_t)c0 + i) * V + x]) : 1.f;
+          const float p = prob(__ldcg(tp + ((size_t)c0 + b + i) * V + x));
+          const float q = dp ? prob(__ldcg(dp + ((size_t)c0 + i) * V + x)) : 1.f;
           rej = !(__fmul_rn(__ldcg(u + c0 + i), q) < p);
         }
       }
