@@ -820,7 +820,9 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const ChunkArgs A) {
   const int w = blockIdx.x, tid = threadIdx.x;
   pdl_wait();
   pdl_trigger();
-  const ChunkSeg seg = A.seg[w];
+  const ChunkSeg* from = A.seg + w;
+  const ChunkSeg seg{__ldcg(&from->F),  __ldcg(&from->end), __ldcg(&from->c0), __ldcg(&from->n_new),
+                     __ldcg(&from->h), __ldcg(&from->qb),  __ldcg(&from->W),  __ldcg(&from->valid)};
   auto clear = [&](int t0, int t1) {
     uint4* o = reinterpret_cast<uint4*>(A.out);
     const size_t n = (size_t)A.h_kv * 4 * kD / 8;

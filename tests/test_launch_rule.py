@@ -22,3 +22,14 @@ def test_verification_reads_its_inputs_past_the_caches():
     for body in loads:
         assert body.count("__ldcg(") == 2
         assert not re.search(r"[(=]\s*\*\s*(p\b|reinterpret_cast)", body)
+
+
+def test_the_join_reads_what_the_attention_wrote_past_the_caches():
+    src = source("chunk.cu")
+    join = src[src.index("chunk_combine_kernel(const ChunkArgs A)"):]
+    join = join[:join.index("\n}\n")]
+    assert "__ldcg(" in join
+    for name in ("A.seg", "A.part", "A.cu", "A.pos0", "part", "from"):
+        assert not re.search(rf"(?<![\w.&]){re.escape(name)}\s*\[", join), name
+        assert not re.search(rf"[(=?:,]\s*\*\s*{re.escape(name)}\b", join), name
+    assert not re.search(r"(?<!&)\bfrom->", join)
