@@ -38,3 +38,27 @@ def test_offsets_that_leave_drafts_out_are_flagged(p, cu, rows):  # noqa: F811
     c.lens = [b - a for a, b in zip(cu, cu[1:])]
     c.tp, c.dp, c.x, c.u = c.tp[lo:hi], c.dp[cu[0]:cu[-1]], c.x[cu[0]:cu[-1]], c.u[cu[0]:cu[-1]]
     assert (acc, tok[lo:hi]) == c.plain()
+
+
+@pytest.mark.parametrize("vocab", [4096, 4001])
+def test_a_subnormal_noise_value_hides_no_larger_quotient(p, vocab):  # noqa: F811
+    c = Case([0], vocab, seed=22)
+    c.tp.fill_(1e-6)
+    c.e.fill_(1.0)
+    c.tp[0, 40], c.e[0, 40] = 1e-10, 1e-39  # 1e29, where 1 / 1e-39 is past float32
+    c.tp[0, 41], c.e[0, 41] = 0.5, 1e-30    # 5e29
+    assert c.run(p) == c.plain() == ([0], [41])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [5, 128, 1000, 4096, 50257])
+@pytest.mark.parametrize("low", [-40.0, -37.0, 20.0])
+def test_noise_over_the_whole_range(p, vocab, low, dtype):  # noqa: F811
+    c = Case([2, 0, 3], vocab, dtype, seed=23)
+    g = torch.Generator(device="cuda").manual_seed(24)
+    draw = lambda *s: torch.rand(*s, device="cuda", generator=g)
+    c.tp = (c.tp.float() * 10 ** (-30 * draw(8, vocab))).to(dtype)
+    for seed in range(4):
+        c.e = (10 ** (low + (38.4 - low) * draw(3, vocab).double())).float().clamp(1e-40, 3e38)
+        c.u = draw(5)
+        assert c.run(p) == c.plain()
