@@ -450,7 +450,13 @@ optr_status optr_decode_step_win(const optr_params* p, const void* q,
  *               (read only).
  *   workspace   device, optr_chunk_workspace_size bytes, 256-byte aligned,
  *               scratch as in optr_decode_attention.
- * Softmax, sums and accumulators are float32; out is rounded once to bf16.
+ * Softmax, sums and accumulators are float32.  Each of these is rounded once to
+ * 16 bits: the rotated query (fp16 over a power of two per row, from R_k to 17
+ * bits), cached INT2 keys and values (fp16), the weights (fp16 at INT2 positions,
+ * bf16 at the others), the mean of the INT2 values before R_v^T (fp16, over a
+ * power of two per row where it is small), R_v^T itself (fp16) and out (bf16).
+ * Together they are 0.0017 to 0.0021 of the output in norm, of which out's own
+ * rounding alone is 0.0016 to 0.0017; the decode's float32 output is good to 2e-5.
  * Inputs must be finite; a sequence's rows depend on no other sequence's.  A
  * sequence with pos0 out of range (OPTR_DEVERR_SEQ_LEN), more than max_new
  * tokens or inconsistent cu_new (OPTR_DEVERR_CU_NEW) gets zero rows; keys of an

@@ -15,11 +15,13 @@
 // fewer is one query tile, whose key tiles the two softmax groups take in turn.
 //
 // Bound.  Chunk tokens (bf16): the tensor cores; an 8192-token prompt of 32 heads
-// takes 405 us, 1.36 PFLOP/s.  INT2 tiles: the chain of a tile, no one part of it.
+// takes 408 us, 1.35 PFLOP/s.  INT2 tiles: the chain of a tile, no one part of it.
 // A 128-key tile is 64 KB of fp16 operands written (two warpgroups, from the
 // records' 12 KB) and 96 KB read per query tile by its two products, 1.4 us for
-// one query tile and 2.0 us for two; 2048 tokens over 32768 take 880 us, 16 x 5 over
-// 8192 78 us and 8 over 131072 75 us, the records alone at 1.3 TB/s.
+// one query tile and 2.0 us for two; 2048 tokens over 32768 take 885 us, 16 x 5 over
+// 8192 80 us and 8 over 131072 77 us, the records alone at 1.3 TB/s.  Of up to 8 new
+// tokens all rows lie in one quarter of the query tile, so one warp of each softmax
+// group has them all.
 //
 // A row's softmax runs over the tiles with a running maximum m and sum l
 // (float32, log2 domain); O and m, l of different ranges merge exactly.
@@ -28,6 +30,12 @@
 // scaled by a power of two per row; q itself in bf16, and the constant <q, mu>
 // taken off).  Values: O is normalised and multiplied by R_v^T once, after the
 // last INT2 tile, and the other tiles go on from there.
+//
+// Both operands of a product have one type: fp16 where the keys and values are
+// dequantized (their codes, scales and minima are fp16, and 11 bits of the query,
+// the weights and the normalised O lose less than 8), bf16 where they are given so.
+// Of R_v^T the fp16 part alone is taken: its lo part would cost a product more at
+// a segment's end for 2^-12 of an element, under the output's 2^-9.
 #include "append_common.cuh"
 #include "chunk.cuh"
 #include "dequant.cuh"
@@ -117,7 +125,7 @@ __device__ __forceinline__ void store32(void* p, const uint32_t (&y)[8], bool wh
 // One row of a logit tile: S (128 columns of tensor memory at tS) becomes P =
 // 2^(S scale - off - m) in 16 bits over its first 64 columns; m, l and O are
 // brought along.  Bits of `mask` and the first `lim` columns count.  l sums the weights
-// before they are rounded (by up to 2^-11 each in fp16, 2^-8 in bf16, to either side).
+// before they are rounded (each by up to 2^-11 of it in fp16, 2^-8 in bf16, to either side).
 template <bool kBf16>
 __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, float scale, float off,
                                              uint4 mask, int lim, bool fresh, float& m, float& l) {
@@ -952,8 +960,8 @@ extern "C" optr_status optr_chunk_attention_win(
               : token_rows_map(&mw, k, n_tok, h_kv, kTile)))
     return OPTR_ERR_CUDA;
   // few rows of many parts: 8 or more for each (sequence, KV head).  8 drafts over
-  // 131072 tokens: 74.8 us, 76.0 without the split; 16 x 5 over 8192, where the
-  // rule says no: 78.6, 81.6 with it.
+  // 131072 tokens: 76.8 us, 77.8 without the split; 16 x 5 over 8192, where the
+  // rule says no: 80.0, 82.3 with it.
   const bool few = max_new <= 16 && (long long)B * h_kv * 8 <= l.W;
   const int per = few ? 2 : 8;  // rows of a joining CTA
   const dim3 joins(l.W, (std::min(l.rows, 4 * max_new) + per - 1) / per);

@@ -79,8 +79,8 @@ __device__ __forceinline__ int tiles_of(int keys) { return (keys + kTile - 1) / 
 // Cost of the first m query blocks of a sequence (one head), in tiles, `past`
 // cached tiles each: block qb sees own tiles 0 .. qb / 2, and begin_cost tiles'
 // time goes into its start and end, more where INT2 tiles have the queries rotated
-// and the output rotated back.  Measured: a ragged batch of 64 sequences takes 134 us,
-// 156 with 2 for all; an 8192-token prompt 405 us, 418 with 5 for all.
+// and the output rotated back.  Measured: a ragged batch of 64 sequences takes 139 us,
+// 160 with 2 for all; an 8192-token prompt 406 us, 415 with 5 where nothing is cached.
 constexpr int kBegin = 2, kBeginInt2 = 6;
 __device__ __forceinline__ int begin_cost(int n_int) { return n_int > 0 ? kBeginInt2 : kBegin; }
 __device__ __forceinline__ long long block_cost(long long m, int past, int begin) {
@@ -112,7 +112,7 @@ __device__ __forceinline__ long long seq_cost(const SeqWork& s) {
 struct PieceFinder {
   long long f, f1, F;    // the next unit, the range's end, all units
   int W;                 // ranges: A.W, or fewer so that each has a unit (one token over 1024:
-                         // 14.3 us, 19.2 with four units at least)
+                         // 14.7 us, 19.4 with four units at least)
   long long f_seg;       // first unit of the last piece's segment
   int b0;                // the 32 sequences held, and what comes before them
   long long base, incl;  // (cost of one head); incl: up to and with the lane's

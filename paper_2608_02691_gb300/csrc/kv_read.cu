@@ -10,16 +10,17 @@
 //
 // One CTA per SM works on one (KV head, kind) and loops over its tiles:
 //   8 converter warps  two groups of 4 take alternate tiles, a thread per row:
-//                   table entry requested two of its tiles ahead, record one
-//                   tile ahead, then 128 values into tensor memory (A operand);
+//                   table entry requested four of the group's tiles ahead,
+//                   record copied to shared memory three ahead, then 128 values
+//                   into tensor memory (A operand);
 //   MMA warp        issues a tile's 16 tcgen05.mma;
 //   8 epilogue warps  two groups likewise: accumulator rows back, mu, bf16,
 //                   into a swizzled shared-memory tile that two TMA copies
 //                   store.
 // Bound by memory: 96 B (G = 32) or 72 B read and 512 B written per token and
-// KV head.  16 x 8192 tokens of 8 KV heads take 126 us, 5.0 TB/s, 74% of a copy's
-// rate; 144 with the records a tile ahead in registers, 129 with whole tiles
-// stored at a time.  777 tokens take 7.4 us, all latency.
+// KV head.  16 x 8192 tokens of 8 KV heads take 127 us (124 to 129 from box to box),
+// 5.0 TB/s, 74% of a copy's rate; 144 with the records a tile ahead in registers, 3
+// more with whole tiles stored at a time.  777 tokens take 7.5 to 8.7 us, all latency.
 #include "append_common.cuh"
 #include "decode_common.cuh"
 #include "dequant.cuh"

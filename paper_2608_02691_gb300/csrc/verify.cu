@@ -16,9 +16,9 @@
 // vocabulary, and the CTAs' maxima meet in shared memory across the cluster.
 // The maximum does not depend on the order in which slices meet, and the
 // lowest token wins a tie.  A thread divides only where an approximate quotient
-// comes near its warp's largest: dividing everywhere took 16.8 us where this
-// takes 10.3 (16 sequences of 4 drafts, 131072 tokens, float32), and batches
-// loaded while others are looked at 29.6 us instead of 32.8 (128 ragged
+// comes near its warp's largest: dividing everywhere takes 16.9 us where this
+// takes 10.0 (16 sequences of 4 drafts, 131072 tokens, float32), and batches
+// loaded while others are looked at took it from 32.5 us to 29.2 (128 ragged
 // sequences, 100003 tokens; its bytes take 19 at the copy rate).  Bound by
 // memory for a serving batch, by the chain of loads (offsets, draft, its
 // probabilities, rows: 7 us in all) for one sequence.
@@ -101,7 +101,7 @@ verify_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
               const float* __restrict__ noise, const int32_t* __restrict__ cu, int n_draft,
               int V, int cs, int32_t* __restrict__ accepted, int32_t* __restrict__ tokens,
               unsigned* err) {
-  constexpr int kUnroll = kVec == 1 ? 4 : 1;  // accesses of a batch (wide, 2: 14.4 us for 10.3)
+  constexpr int kUnroll = kVec == 1 ? 4 : 1;  // accesses of a batch (wide, 2: 13.6 us for 10.0)
   __shared__ int head[2];
   __shared__ unsigned long long wbest[kVerifyThreads / 32];
   __shared__ unsigned long long best[2];  // this CTA's, by pass
@@ -202,7 +202,9 @@ verify_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
         }
       }
       m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
-      // outside kFar the approximation may be off by more than 2 ulp: divide all there
+      // The approximation is within 2 ulp; divisors past kFar may lie outside its range:
+      // divide all there.  (Its documented range begins at 2^-126.  Below, it was within
+      // 2 ulp too for every subnormal divisor, each with 256 dividends.)
       constexpr float kFar = 1e30f;
       const float least = m < 1.f / kFar ? 0.f : fminf(m, kFar) * 0.99999f;
 #pragma unroll
@@ -260,11 +262,11 @@ cudaError_t launch_verify(const optr_params* p, const void* tp, const void* dp,
                           const int32_t* cu, int n_draft, int B, int V, int32_t* accepted,
                           int32_t* tokens, cudaStream_t s) {
   // four values an access where the vocabulary and the rows' alignment admit it
-  // (16 sequences, 131072 tokens: 10.3 us, 11.9 with one value an access)
+  // (16 sequences, 131072 tokens: 10.0 us, 11.4 with one value an access)
   const bool wide = V % 4 == 0 && aligned(tp, 4 * sizeof(T)) && aligned(dp, 4 * sizeof(T)) &&
                     aligned(noise, 16);
   // CTAs per sequence: about kPerSm per SM in all, a round of loads each at least
-  // (128 ragged sequences: 29.1 us with 2 an SM, 38.0 with 1; with 4, more than fit, 39)
+  // (128 ragged sequences: 29.0 us with 2 an SM, 37.8 with 1; with 4, more than fit, 34)
   constexpr int kPerSm = 2;
   int cs = 8;
   while (cs > 1 && ((long long)B * cs > (long long)kPerSm * p->num_sms ||
