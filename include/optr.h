@@ -459,7 +459,8 @@ optr_status optr_decode_step_win(const optr_params* p, const void* q,
  * rounding alone is 0.0016 to 0.0017; the decode's float32 output is good to 2e-5.
  * Inputs must be finite; a sequence's rows depend on no other sequence's.  A
  * sequence with pos0 out of range (OPTR_DEVERR_SEQ_LEN), more than max_new
- * tokens or inconsistent cu_new (OPTR_DEVERR_CU_NEW) gets zero rows; keys of an
+ * tokens or inconsistent cu_new (OPTR_DEVERR_CU_NEW) gets zero rows, and so do
+ * rows of no sequence; those of sequences in order stay theirs.  Keys of an
  * out-of-range page (OPTR_DEVERR_PAGE_ID) or window slot
  * (OPTR_DEVERR_WIN_SLOT) are left out.  An INT2 group with an end (min or
  * 3 scale + min) past fp16's range, which a rotated range of 65504 or more can
