@@ -456,7 +456,7 @@ optr_status optr_decode_step_win(const optr_params* p, const void* q,
  * bf16 at the others), the mean of the INT2 values before R_v^T (fp16, over a
  * power of two per row where it is small), R_v^T itself (fp16) and out (bf16).
  * Together they are 0.0017 to 0.0021 of the output in norm, of which out's own
- * rounding alone is 0.0016 to 0.0017; the decode's float32 output is good to 2e-5.
+ * rounding alone is 0.0015 to 0.0017; the decode's float32 output is good to 2e-5.
  * Inputs must be finite; a sequence's rows depend on no other sequence's.  A
  * sequence with pos0 out of range (OPTR_DEVERR_SEQ_LEN), more than max_new
  * tokens or inconsistent cu_new (OPTR_DEVERR_CU_NEW) gets zero rows, and so do
