@@ -301,7 +301,7 @@ def _prepare_score(c, seed):
     if own:
         from paper_2608_02691_gb300 import optr
         s["p"] = _params(c, rot)
-        s["ws"] = optr.new_score_workspace(s["p"], n, c["B"], s["max_new"])
+        s["ws"] = optr.new_score_workspace(s["p"], n, c["B"], s["max_new"], table.shape[1])
     return s
 
 
