@@ -166,6 +166,7 @@ typedef enum {
 #define OPTR_DEVERR_WIN_SLOT 64u /* window slot of a sequence < 0 or >= n_slots */
 #define OPTR_DEVERR_CALIB_RANGE 128u /* calibration: generator norm past exp's scaling range */
 #define OPTR_DEVERR_TOKEN 256u   /* draft token < 0 or >= vocab */
+#define OPTR_DEVERR_TREE 512u    /* a tree row's parent is not one of the rows before it */
 
 /* Kernel variants (for measurement; 0 picks the library default). */
 #define OPTR_VARIANT_DEFAULT 0
@@ -490,6 +491,41 @@ optr_status optr_chunk_attention_win(const optr_params* p, const void* q,
                                      size_t ws_bytes, cudaStream_t stream);
 
 /*
+ * Attention of trees of drafted tokens over the paged cache: optr_chunk_attention
+ * whose rows see, of their own sequence's rows, themselves and their ancestors
+ * only.  Row i of sequence b (t = cu_tree[b] + i) has the parent
+ * parent[t], a row of the same sequence that comes before it (0 .. i-1), or -1:
+ * it then sees the cached tokens and itself.  (A row's position, for the rotary
+ * embedding of q and k, is pos0[b] plus its depth and the caller's business.)
+ *   parent      device int32 [n_tok].
+ *   max_new     host; at most OPTR_TREE_MAX_ROWS (else OPTR_ERR_OUT_OF_RANGE).
+ * Everything else, the workspace's size and the roundings as for
+ * optr_chunk_attention; parent[t] = i - 1 gives its result.  A parent out of
+ * range sets OPTR_DEVERR_TREE and counts as -1.
+ */
+#define OPTR_TREE_MAX_ROWS 1024
+optr_status optr_tree_attention(const optr_params* p, const void* q,
+                                const void* k, const void* v, int n_tok,
+                                const int32_t* parent, const int32_t* cu_tree,
+                                const int32_t* pos0, int max_new,
+                                const int32_t* block_table, int B,
+                                int max_pages, const uint8_t* pool,
+                                int num_pages, void* out, void* workspace,
+                                size_t ws_bytes, cudaStream_t stream);
+
+optr_status optr_tree_attention_win(const optr_params* p, const void* q,
+                                    const void* k, const void* v, int n_tok,
+                                    const int32_t* parent,
+                                    const int32_t* cu_tree,
+                                    const int32_t* pos0, int max_new,
+                                    const int32_t* block_table, int B,
+                                    int max_pages, const uint8_t* pool,
+                                    int num_pages, const void* win,
+                                    const int32_t* win_slot, int n_slots,
+                                    void* out, void* workspace,
+                                    size_t ws_bytes, cudaStream_t stream);
+
+/*
  * Read the cache back: the INT2 records of positions pos0[b] ..
  * pos0[b] + cu_read[b+1] - cu_read[b] - 1 of each sequence as rows
  * cu_read[b] .. cu_read[b+1]-1 of k and v in the model's basis,
@@ -550,6 +586,52 @@ optr_status optr_verify_drafts(const optr_params* p, const void* target_probs,
                                int n_draft, int B, int vocab,
                                int32_t* accepted, int32_t* tokens,
                                cudaStream_t stream);
+
+/*
+ * Verification of a tree of drafted tokens against the target's probabilities,
+ * from given random numbers.  Sequence b has the rows t = cu_tree[b] ..
+ * cu_tree[b+1]-1 of optr_tree_attention: row 0 is the text's last token (its
+ * parent is -1), every other row i holds the draft tokens[t], a child of row
+ * parent[t] (0 .. i-1); p_r and q_r are the target's and the draft's
+ * probabilities after row r.  From row r = 0 on, with w = p_r and S = 1 the
+ * children c of r are tried in the order of their rows; x is c's token:
+ *      u_c q_r(x) S < w(x)   c is accepted, and the walk goes on at r = c;
+ *      otherwise             w = max(w - S q_r, 0), S = sum over the vocabulary of w
+ * and where no child is accepted the next token is the first maximum over the
+ * vocabulary of w(v) / e(v) (of p_r(v) / e(v) where those are zero everywhere).
+ * When a row's children were drawn independently from q_r (the same token may
+ * come twice), each token of the text has the target's distribution.  Without
+ * draft probabilities q_r is 1 at each child's token: the product is u_c S, and
+ * a rejected child takes w(x) off S and leaves w(x) = 0.  The arithmetic is float32,
+ * one rounding an operation; S is summed in float32 over some hundred probabilities
+ * at most, and those sums in float64.
+ *   target_probs device [n_tok][vocab], float32 or bf16 (probs_dtype).
+ *   draft_probs  device [n_tok][vocab] of the same type (read where a row has
+ *                children), or NULL: drafted without probabilities.
+ *   tokens       device int32 [n_tok] (of row 0 not read).
+ *   parent       device int32 [n_tok].
+ *   uniform      device float32 [n_tok]: u, in [0, 1) (of row 0 not read).
+ *   noise        device float32 [B][vocab]: e, positive.
+ *   cu_tree      device int32 [B+1], as cu_new of optr_kv_append; no sequence has more
+ *                than OPTR_TREE_MAX_ROWS rows.
+ *   accepted     device int32 [B]: accepted drafts, a.
+ *   path         device int32 [n_tok]: cu_tree[b] + i is the row (of all rows) at depth
+ *                i of the way, i = 0 .. a (the rows whose keys and values stay), then -1.
+ *   next         device int32 [n_tok]: the accepted tokens, the next token, then -1.
+ * Probabilities are finite and not negative.  A draft out of 0 .. vocab-1 sets
+ * OPTR_DEVERR_TOKEN and is rejected where it is reached (w and S stay); a parent out
+ * of range sets OPTR_DEVERR_TREE, and its row is never reached.  A sequence
+ * without rows gets accepted = -1; so does one whose cu_tree is out of range or that
+ * has too many rows, which sets OPTR_DEVERR_CU_NEW, and neither writes rows.  (p
+ * serves the device error word only.)  Nothing is allocated or synchronised.
+ */
+optr_status optr_verify_tree(const optr_params* p, const void* target_probs,
+                             const void* draft_probs, int probs_dtype,
+                             const int32_t* tokens, const int32_t* parent,
+                             const float* uniform, const float* noise,
+                             const int32_t* cu_tree, int n_tok, int B, int vocab,
+                             int32_t* accepted, int32_t* path, int32_t* next,
+                             cudaStream_t stream);
 
 /* Static description of a status code. */
 const char* optr_strerror(optr_status s);

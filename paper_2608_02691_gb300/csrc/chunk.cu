@@ -1,5 +1,6 @@
 // Attention of a chunk of new tokens over the paged INT2 cache
-// (include/optr.h, "optr_chunk_attention").
+// (include/optr.h, "optr_chunk_attention"), and of a tree of drafted tokens
+// ("optr_tree_attention"), which differs in what a row sees of the chunk.
 //
 // Two launches: chunk_kernel attends, chunk_combine_kernel joins the segments
 // that more than one CTA worked on.
@@ -36,6 +37,11 @@
 // the weights and the normalised O lose less than 8), bf16 where they are given so.
 // Of R_v^T the fp16 part alone is taken: its lo part would cost a product more at
 // a segment's end for 2^-12 of an element, under the output's 2^-9.
+//
+// Trees.  A row's parent comes before it, so its ancestors lie in the same own tiles
+// that a causal row sees, and the tiles and their work stay as they are.  The warp
+// that finds the pieces brings the parents into shared memory, and each row walks from
+// itself up to mark its ancestors in a tile: a step is a shared-memory load.
 #include "append_common.cuh"
 #include "chunk.cuh"
 #include "dequant.cuh"
@@ -63,6 +69,7 @@ constexpr int kRing = 2;
 constexpr uint32_t kHalf = kTile * 128;      // 64 channels of 128 rows
 constexpr uint32_t kOperand = 2 * kHalf;     // 128 x 128 of 16 bits
 constexpr int kPieces = 3;       // pieces found ahead
+constexpr int kTrees = 2;        // pieces whose parents are in shared memory
 constexpr float kSlack = 8.f;  // a row's maximum may grow by 2^8 before O is rescaled
 // The largest weight stands at 2^kLift, with the slack at 2^15 at most, inside fp16:
 // weights count down to 2^-32 of it, and a million keys below that weigh 2^-12.
@@ -92,6 +99,12 @@ struct Smem {
   uint64_t s_full[2], p_ready[2], o_full[2], q_ready[2], q_full, q_empty, drained;
   uint32_t tmem;
   int abort;
+};
+
+// What the trees' attention has beside.
+struct TreeSmem {
+  int16_t parent[kTrees][OPTR_TREE_MAX_ROWS];
+  uint64_t full[kTrees], empty[kTrees];
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -235,12 +248,25 @@ __device__ __forceinline__ void rotated_query(uint32_t tS, uint8_t* q, int row, 
   }
 }
 
+// The ancestors of row i, itself among them, that lie in rows lo .. lo + 127.
+__device__ __forceinline__ uint4 ancestors(const int16_t* parent, int i, int lo) {
+  uint32_t m[4] = {0u, 0u, 0u, 0u};
+  for (; i >= lo; i = parent[i]) {
+    const int at = i - lo;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) m[c] |= at >> 5 == c ? 1u << (at & 31) : 0u;
+  }
+  return make_uint4(m[0], m[1], m[2], m[3]);
+}
+
+template <bool kTree>
 __global__ void __launch_bounds__(kThreads, 1)
 chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
              const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
              const __grid_constant__ CUtensorMap tm_win, const __grid_constant__ ChunkArgs A) {
   extern __shared__ __align__(1024) unsigned char dsm_[];
   Smem& S = *reinterpret_cast<Smem*>(dsm_);
+  TreeSmem& T = *reinterpret_cast<TreeSmem*>(dsm_ + sizeof(Smem));  // (trees only)
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);  // uniform, as the compiler sees it
   if (tid == 0) {
@@ -268,6 +294,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
       tc05::bar_init(&S.raw_full[g], 1);
       tc05::bar_init(&S.raw_empty[g], 4);
     }
+    if constexpr (kTree)
+      for (int i = 0; i < kTrees; ++i) {
+        tc05::bar_init(&T.full[i], 1);
+        tc05::bar_init(&T.empty[i], kDeqWarp);
+      }
     tc05::bar_init(&S.second_ready, 4);
     tc05::bar_init(&S.joined, 4);
     tc05::bar_init(&S.q_full, 1);
@@ -399,16 +430,23 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
         }
         ready();
       }
+      // (every piece's phase in turn, also where it has no own tile)
+      if (kTree && !wait(&T.full[n % kTrees], n / kTrees)) break;
       for (int k = ints; k < tiles; ++k) {
         if (!wait(&S.s_full[g], ns++)) break;
-        // window rows as far as they are filled; own tiles causally
+        // window rows as far as they are filled; own tiles causally, or up the tree
         const int tile = p.t0 + from + stride * k - p.I;
-        const int lim = tile < p.Wt ? p.n_win - kTile * tile : i + 1 - kTile * (tile - p.Wt);
-        if (rows)
-          softmax_tile<true>(tS, tO, kLogit, 0.f, make_uint4(~0u, ~0u, ~0u, ~0u), lim, fresh, m, l);
+        int lim = tile < p.Wt ? p.n_win - kTile * tile : i + 1 - kTile * (tile - p.Wt);
+        uint4 mask = make_uint4(~0u, ~0u, ~0u, ~0u);
+        if (kTree && tile >= p.Wt) {
+          lim = kTile;
+          mask = ancestors(T.parent[n % kTrees], valid ? i : -1, kTile * (tile - p.Wt));
+        }
+        if (rows) softmax_tile<true>(tS, tO, kLogit, 0.f, mask, lim, fresh, m, l);
         fresh = false;
         ready();
       }
+      if (kTree) arrive(&T.empty[n % kTrees]);
       if (dead || (tiles > 0 && !wait(&S.o_full[g], no++))) break;
       // The groups' parts of one query tile meet: the second's output is in the
       // same lanes of tensor memory
@@ -700,7 +738,25 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm_q,
     __syncwarp();
   } else if (warp == kPlanWarp) {
     // ---------------------------------------------------------- pieces
-    find_pieces<kPieces>(A, w, S.piece, S.piece_full, S.piece_empty, abort);
+    find_pieces<kPieces>(A, w, S.piece, S.piece_full, S.piece_empty, abort,
+                         [&](uint32_t n, const Piece& p) {
+      if constexpr (kTree) {
+        const uint32_t i = n % kTrees;
+        if (n >= kTrees && !wait(&T.empty[i], n / kTrees - 1)) return false;
+        // the rows that the piece's queries may descend from, where it has own tiles
+        const int rows = p.t1 > p.I + p.Wt ? min(p.n_new, kQTok * (p.qb + 1)) : 0;
+        for (int j = lane; j < rows; j += 32) {
+          int x = __ldcg(A.parent + p.c0 + j);
+          if (x < -1 || x >= j) {
+            atomicOr(A.err, OPTR_DEVERR_TREE);
+            x = -1;
+          }
+          T.parent[i][j] = (int16_t)x;
+        }
+        arrive(&T.full[i]);
+      }
+      return true;
+    });
   } else {
     // ------------------------------------------------------------ MMA
     constexpr uint32_t kId = tc05::idesc_f16(128, 128);
@@ -940,9 +996,12 @@ extern "C" size_t optr_chunk_workspace_size(const optr_params* p, int n_tok, int
   return chunk_layout(p, max_new).total;
 }
 
-extern "C" optr_status optr_chunk_attention_win(
+namespace {
+
+// Both attentions; parent is null where the chunk is causal.
+optr_status attend(
     const optr_params* p, const void* q, const void* k, const void* v, int n_tok,
-    const int32_t* cu_new, const int32_t* pos0, int max_new, const int32_t* block_table, int B,
+    const int32_t* parent, const int32_t* cu_new, const int32_t* pos0, int max_new, const int32_t* block_table, int B,
     int max_pages, const uint8_t* pool, int num_pages, const void* win, const int32_t* win_slot,
     int n_slots, void* out, void* workspace, size_t ws_bytes, cudaStream_t stream) {
   if (!p || n_tok < 0 || B <= 0 || max_pages <= 0 || num_pages <= 0 || max_new <= 0)
@@ -970,8 +1029,10 @@ extern "C" optr_status optr_chunk_attention_win(
   const ChunkArgs A{n_tok, cu_new, pos0, max_new, block_table, B, max_pages, pool, num_pages, w,
                     p->cfg.sink, p->cfg.recent, h_kv, p->cfg.group == 4 * kG, p->Rk_query, p->Rv_back,
                     p->muR, (__nv_bfloat16*)out, p->err, (ChunkSeg*)ws, (float*)(ws + l.part),
-                    l.rows, l.W, aligned(out, 32)};
-  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(chunk_kernel), sizeof(Smem));
+                    l.rows, l.W, aligned(out, 32), parent};
+  auto fn = parent ? chunk_kernel<true> : chunk_kernel<false>;
+  const size_t smem = sizeof(Smem) + (parent ? sizeof(TreeSmem) : 0);
+  cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), smem);
   if (e != cudaSuccess) return OPTR_ERR_CUDA;
   CUtensorMap mq, mk, mv, mw;
   if (!token_rows_map(&mq, q, n_tok, 4 * h_kv, 32, 4) ||
@@ -985,11 +1046,22 @@ extern "C" optr_status optr_chunk_attention_win(
   const bool few = max_new <= 16 && (long long)B * h_kv * 8 <= l.W;
   const int per = few ? 2 : 8;  // rows of a joining CTA
   const dim3 joins(l.W, (std::min(l.rows, 4 * max_new) + per - 1) / per);
-  e = launch_pdl(chunk_kernel, dim3(l.W), dim3(kThreads), sizeof(Smem), stream, mq, mk, mv, mw, A);
+  e = launch_pdl(fn, dim3(l.W), dim3(kThreads), smem, stream, mq, mk, mv, mw, A);
   if (e == cudaSuccess)
     e = launch_pdl(few ? chunk_combine_kernel<true> : chunk_combine_kernel<false>, joins, dim3(256), 0,
                    stream, A);
   return cuda_status(e);
+}
+
+}  // namespace
+
+extern "C" optr_status optr_chunk_attention_win(
+    const optr_params* p, const void* q, const void* k, const void* v, int n_tok,
+    const int32_t* cu_new, const int32_t* pos0, int max_new, const int32_t* block_table, int B,
+    int max_pages, const uint8_t* pool, int num_pages, const void* win, const int32_t* win_slot,
+    int n_slots, void* out, void* workspace, size_t ws_bytes, cudaStream_t stream) {
+  return attend(p, q, k, v, n_tok, nullptr, cu_new, pos0, max_new, block_table, B, max_pages, pool,
+                num_pages, win, win_slot, n_slots, out, workspace, ws_bytes, stream);
 }
 
 extern "C" optr_status optr_chunk_attention(const optr_params* p, const void* q, const void* k,
@@ -1002,4 +1074,28 @@ extern "C" optr_status optr_chunk_attention(const optr_params* p, const void* q,
   return optr_chunk_attention_win(p, q, k, v, n_tok, cu_new, pos0, max_new, block_table, B, max_pages,
                                   pool, num_pages, nullptr, nullptr, 0, out, workspace, ws_bytes,
                                   stream);
+}
+
+extern "C" optr_status optr_tree_attention_win(
+    const optr_params* p, const void* q, const void* k, const void* v, int n_tok,
+    const int32_t* parent, const int32_t* cu_tree, const int32_t* pos0, int max_new,
+    const int32_t* block_table, int B, int max_pages, const uint8_t* pool, int num_pages,
+    const void* win, const int32_t* win_slot, int n_slots, void* out, void* workspace,
+    size_t ws_bytes, cudaStream_t stream) {
+  if (!p || (n_tok > 0 && !parent)) return OPTR_ERR_INVALID_ARG;
+  if (max_new > OPTR_TREE_MAX_ROWS) return OPTR_ERR_OUT_OF_RANGE;
+  return attend(p, q, k, v, n_tok, parent, cu_tree, pos0, max_new, block_table, B, max_pages, pool,
+                num_pages, win, win_slot, n_slots, out, workspace, ws_bytes, stream);
+}
+
+extern "C" optr_status optr_tree_attention(const optr_params* p, const void* q, const void* k,
+                                           const void* v, int n_tok, const int32_t* parent,
+                                           const int32_t* cu_tree, const int32_t* pos0, int max_new,
+                                           const int32_t* block_table, int B, int max_pages,
+                                           const uint8_t* pool, int num_pages, void* out,
+                                           void* workspace, size_t ws_bytes, cudaStream_t stream) {
+  if (p && (p->cfg.sink > 0 || p->cfg.recent > 0)) return OPTR_ERR_INVALID_ARG;
+  return optr_tree_attention_win(p, q, k, v, n_tok, parent, cu_tree, pos0, max_new, block_table, B,
+                                 max_pages, pool, num_pages, nullptr, nullptr, 0, out, workspace,
+                                 ws_bytes, stream);
 }

@@ -28,6 +28,7 @@ struct ChunkArgs {
   int rows;              // rows of a partial
   int W;                 // CTAs
   bool out32;            // out is 32-byte aligned
+  const int32_t* parent; // trees: the rows' parents
 };
 
 // A segment that CTA w begins and another one ends: its pieces are those of the
@@ -210,10 +211,10 @@ __device__ __forceinline__ float* part_of(const ChunkArgs& A, int w, bool begun)
 }
 
 // A CTA's warp that finds its pieces for the others, kAhead ahead: a piece
-// without tiles ends them.
-template <int kAhead>
+// without tiles ends them.  then(n, p) follows the n-th one, and says whether to go on.
+template <int kAhead, typename Then>
 __device__ __forceinline__ void find_pieces(const ChunkArgs& A, int w, Piece* piece, uint64_t* full,
-                                            uint64_t* empty, volatile int* abort) {
+                                            uint64_t* empty, volatile int* abort, Then then) {
   const int lane = threadIdx.x & 31;
   if (w == 0) report_sequences(A);
   PieceFinder next;
@@ -236,6 +237,7 @@ __device__ __forceinline__ void find_pieces(const ChunkArgs& A, int w, Piece* pi
       tc05::bar_arrive(&full[i]);
     }
     __syncwarp();
+    if (more && !then(n, p)) break;
   }
   if (lane == 0) A.seg[w] = seg;
 }

@@ -1,0 +1,336 @@
+// Verification of a tree of drafted tokens against the target's probabilities
+// from given random numbers (include/optr.h, "optr_verify_tree").
+//
+// From the root on, at row r with the children c_1 < c_2 < .. whose tokens were
+// drawn independently from q_r: with w = p_r and S = 1, child c of token x is
+// accepted if u_c q_r(x) S < w(x), that is with probability min(1, (w(x) / S) / q_r(x));
+// if it is rejected, w becomes max(w - S q_r, 0) and S its sum, so that w / S is the
+// residual that the next child is measured against and, after the last one, the
+// next token is drawn from (as argmax w / e, see verify.cu).  By induction over the
+// children the token that is kept has the distribution p_r.  Without probabilities
+// q_r is 1 at each child's token: its w becomes 0, S loses w(x).
+//
+// A cluster of CTAs takes a sequence.  Every row's p, q, u at its own token are
+// loaded at once into shared memory; each CTA walks down the tree by itself (one
+// warp, in shared memory) until a sum S or the final draw needs the vocabulary.  Of
+// that each CTA has a slice; w is not stored but computed from p, q and the S so
+// far, and the CTAs' sums meet in shared memory across the cluster, in rank order
+// (equal calls give equal bits).
+#include "cluster.cuh"
+#include "optr_internal.cuh"
+
+namespace optr {
+namespace {
+
+constexpr int kTreeThreads = 512, kWarps = kTreeThreads / 32;
+constexpr int kRows = OPTR_TREE_MAX_ROWS;
+
+struct Node {
+  int parent, token;  // parent -2: never reached
+  float px, qx, u;    // of its token: target and draft probability at the parent's row
+};
+
+struct Walk {
+  int row;    // the last accepted row
+  int last;   // children up to this row were rejected
+  int n_cut;  // rejected children of `row`: their S (probabilities) or tokens in `cut`
+  int depth;  // accepted rows after the root
+  bool draw;  // no child is left
+};
+
+struct Smem {
+  Node node[kRows];
+  uint32_t cut[kRows];
+  int16_t path[kRows];
+  Walk walk;
+  double wsum[kWarps];
+  double sum[2];                    // this CTA's, by pass
+  unsigned long long wbest[kWarps];
+  unsigned long long best[2];
+};
+
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+// N consecutive values, past the caches that a kernel before may have left stale.
+template <int N>
+__device__ __forceinline__ void fetch(const float* p, float (&x)[N]) {
+  if constexpr (N == 4) {
+    const float4 y = __ldcg(reinterpret_cast<const float4*>(p));
+    x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;
+  } else {
+    x[0] = __ldcg(p);
+  }
+}
+template <int N>
+__device__ __forceinline__ void fetch(const __nv_bfloat16* p, float (&x)[N]) {
+  if constexpr (N == 4) {
+    const uint2 y = __ldcg(reinterpret_cast<const uint2*>(p));
+    x[0] = __uint_as_float(y.x << 16), x[1] = __uint_as_float(y.x & 0xffff0000u);
+    x[2] = __uint_as_float(y.y << 16), x[3] = __uint_as_float(y.y & 0xffff0000u);
+  } else {
+    x[0] = as_float(__ldcg(p));
+  }
+}
+
+// What a rejection by probabilities leaves.
+__device__ __forceinline__ float left(float w, float S, float q) {
+  return fmaxf(__fsub_rn(w, __fmul_rn(S, q)), 0.f);
+}
+
+// Larger value first, then the lower token (values are not negative, -0 is a zero).
+__device__ __forceinline__ unsigned long long ranked(float value, int token) {
+  return (unsigned long long)__float_as_uint(__fadd_rn(value, 0.f)) << 32 | (0xffffffffu - (unsigned)token);
+}
+
+// One warp: down from S.walk until a sum or the draw is needed.
+__device__ __forceinline__ void descend(Smem& S, int n, bool probs) {
+  const int lane = threadIdx.x & 31;
+  Walk w = S.walk;
+  float mass = 1.f;
+  if (w.n_cut > 0 && probs) mass = __uint_as_float(S.cut[w.n_cut]);
+  // w(x) of a child, from the masses of the rejected ones before it
+  for (;;) {
+    int child = n;
+    for (int i0 = (w.last + 1) & ~31; i0 < n && child == n; i0 += 32) {
+      const int i = i0 + lane;
+      const unsigned m = __ballot_sync(0xffffffffu, i > w.last && i < n && S.node[i].parent == w.row);
+      if (m) child = i0 + __ffs(m) - 1;
+    }
+    if (child == n) {
+      w.draw = true;
+      break;
+    }
+    const Node c = S.node[child];
+    float x = c.px;
+    bool known = true;  // whether S is
+    if (probs) {
+      for (int j = 0; j < w.n_cut; ++j) x = left(x, __uint_as_float(S.cut[j]), c.qx);
+      known = !(mass < 0.f);
+    } else {
+      for (int j = 0; j < w.n_cut; ++j)
+        if ((int)S.cut[j] == c.token) x = 0.f;
+    }
+    if (!known) break;  // (the mass of what is left comes first)
+    if (__fmul_rn(__fmul_rn(c.u, c.qx), mass) < x) {
+      w.row = w.last = child;
+      w.n_cut = 0;
+      mass = 1.f;
+      ++w.depth;
+      if (lane == 0) S.path[w.depth] = (int16_t)child;
+      continue;
+    }
+    w.last = child;
+    if (c.token < 0) continue;  // a draft out of range takes nothing from the target
+    if (lane == 0) S.cut[w.n_cut] = probs ? __float_as_uint(mass) : (uint32_t)c.token;
+    ++w.n_cut;
+    mass = probs ? -1.f : __fsub_rn(mass, x);
+    __syncwarp();
+  }
+  if (lane == 0) S.walk = w;
+}
+
+template <typename T, int kVec>
+__global__ void __launch_bounds__(kTreeThreads)
+verify_tree_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
+                   const int32_t* __restrict__ tokens, const int32_t* __restrict__ parent,
+                   const float* __restrict__ uniform, const float* __restrict__ noise,
+                   const int32_t* __restrict__ cu, int n_tok, int V, int cs,
+                   int32_t* __restrict__ accepted, int32_t* __restrict__ path,
+                   int32_t* __restrict__ next, unsigned* err) {
+  __shared__ Smem S;
+  const int b = blockIdx.x / cs, rank = cluster_rank_of();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  pdl_wait();
+  pdl_trigger();
+  if (blockIdx.x == 0 && tid == 64 && (__ldcg(cu) != 0 || __ldcg(cu + gridDim.x / cs) != n_tok))
+    atomicOr(err, OPTR_DEVERR_CU_NEW);
+  const int c0 = __ldcg(cu + b), c1 = __ldcg(cu + b + 1), n = c1 - c0;
+  const bool bad = c0 < 0 || c1 < c0 || c1 > n_tok || n > kRows;
+  if (bad || n == 0) {  // the same for the whole cluster
+    if (rank == 0 && tid == 0) {
+      accepted[b] = -1;
+      if (bad) atomicOr(err, OPTR_DEVERR_CU_NEW);
+    }
+    return;
+  }
+  for (int i = tid; i < n; i += kTreeThreads) {
+    Node x;
+    x.parent = __ldcg(parent + c0 + i);
+    x.token = __ldcg(tokens + c0 + i);
+    x.u = __ldcg(uniform + c0 + i);
+    x.px = x.qx = 0.f;
+    unsigned flag = 0;
+    if (i == 0 ? x.parent != -1 : x.parent < 0 || x.parent >= i) {
+      flag |= OPTR_DEVERR_TREE;
+      x.parent = -2;
+    }
+    if (i > 0) {
+      if (x.token < 0 || x.token >= V) {
+        flag |= OPTR_DEVERR_TOKEN;
+        x.token = -1;
+      } else if (x.parent >= 0) {
+        const size_t at = ((size_t)c0 + x.parent) * V + x.token;
+        x.px = as_float(__ldcg(tp + at));
+        x.qx = dp ? as_float(__ldcg(dp + at)) : 1.f;
+      }
+    }
+    S.node[i] = x;
+    if (flag && rank == 0) atomicOr(err, flag);
+  }
+  if (tid == 0) {
+    S.walk = Walk{0, 0, 0, 0, false};
+    S.path[0] = 0;
+  }
+  __syncthreads();
+  const int n_vec = V / kVec;
+  const int lo = (int)((long long)n_vec * rank / cs), hi = (int)((long long)n_vec * (rank + 1) / cs);
+  // Sums until the walk ends
+  Walk w;
+  for (int pass = 0;; ++pass) {
+    if (warp == 0) descend(S, n, dp != nullptr);
+    __syncthreads();
+    w = S.walk;
+    if (w.draw) break;
+    const T* p = tp + ((size_t)c0 + w.row) * V;
+    const T* q = dp + ((size_t)c0 + w.row) * V;
+    float sum = 0.f;
+#pragma unroll 4
+    for (int v = lo + tid; v < hi; v += kTreeThreads) {
+      float x[kVec], y[kVec];
+      fetch(p + (size_t)v * kVec, x);
+      fetch(q + (size_t)v * kVec, y);
+      for (int j = 0; j < w.n_cut; ++j) {
+        const float m = __uint_as_float(S.cut[j]);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) x[i] = left(x[i], m, y[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) sum += x[i];
+    }
+    double total = sum;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    if (lane == 0) S.wsum[warp] = total;
+    __syncthreads();
+    if (tid == 0) {
+      total = 0.;
+      for (int i = 0; i < kWarps; ++i) total += S.wsum[i];
+      S.sum[pass & 1] = total;
+    }
+    if (cs > 1) cluster_barrier(); else __syncthreads();
+    total = 0.;
+    for (int r = 0; r < cs; ++r)
+      total += cs > 1 ? __longlong_as_double((long long)cluster_ld64(&S.sum[pass & 1], r)) : S.sum[pass & 1];
+    // (the mass that the next child is measured against, where descend() looks for it)
+    if (tid == 0) S.cut[w.n_cut] = __float_as_uint((float)total);
+    __syncthreads();
+  }
+  // The next token: first maximum of w / e; of p / e where w is zero everywhere
+  const T* p = tp + ((size_t)c0 + w.row) * V;
+  const T* q = dp ? dp + ((size_t)c0 + w.row) * V : nullptr;
+  const float* e = noise + (size_t)b * V;
+  unsigned long long all = 0;
+  for (int pass = 0; pass < 2; ++pass) {
+    const int n_cut = pass == 0 ? w.n_cut : 0;
+    float top = -1.f;
+    int at = 0;
+#pragma unroll 2
+    for (int v = lo + tid; v < hi; v += kTreeThreads) {
+      float x[kVec], z[kVec], y[kVec];
+      fetch(p + (size_t)v * kVec, x);
+      fetch(e + (size_t)v * kVec, z);
+      if (q && n_cut > 0) fetch(q + (size_t)v * kVec, y);
+      for (int j = 0; j < n_cut; ++j) {
+        const uint32_t cut = S.cut[j];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          if (q)
+            x[i] = left(x[i], __uint_as_float(cut), y[i]);
+          else if ((int)cut == v * kVec + i)
+            x[i] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const float r = __fdiv_rn(x[i], z[i]);
+        if (r > top) {
+          top = r;
+          at = v * kVec + i;
+        }
+      }
+    }
+    unsigned long long c = top >= 0.f ? ranked(top, at) : 0ull;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const unsigned long long y = __shfl_xor_sync(0xffffffffu, c, o);
+      c = y > c ? y : c;
+    }
+    if (lane == 0) S.wbest[warp] = c;
+    __syncthreads();
+    if (tid == 0) {
+      for (int i = 1; i < kWarps; ++i) c = S.wbest[i] > c ? S.wbest[i] : c;
+      S.best[pass] = c;
+    }
+    if (cs > 1) cluster_barrier(); else __syncthreads();
+    all = S.best[pass];
+    if (cs > 1)
+      for (int r = 0; r < cs; ++r) {
+        const unsigned long long y = cluster_ld64(&S.best[pass], r);
+        all = y > all ? y : all;
+      }
+    if ((uint32_t)(all >> 32) != 0u) break;  // the same in the whole cluster
+  }
+  if (rank == 0) {
+    const int token = (int)(0xffffffffu - (unsigned)all);
+    if (tid == 0) accepted[b] = w.depth;
+    for (int i = tid; i < n; i += kTreeThreads) {
+      path[c0 + i] = i <= w.depth ? c0 + S.path[i] : -1;
+      next[c0 + i] = i < w.depth ? S.node[S.path[i + 1]].token : i == w.depth ? token : -1;
+    }
+  }
+  if (cs > 1) cluster_barrier();  // no CTA leaves while its shared memory may be read
+}
+
+template <typename T>
+cudaError_t launch_verify_tree(const optr_params* p, const void* tp, const void* dp,
+                               const int32_t* tokens, const int32_t* parent, const float* u,
+                               const float* noise, const int32_t* cu, int n_tok, int B, int V,
+                               int32_t* accepted, int32_t* path, int32_t* next, cudaStream_t s) {
+  // four values an access where the vocabulary and the rows' alignment admit it
+  const bool wide = V % 4 == 0 && aligned(tp, 4 * sizeof(T)) && aligned(dp, 4 * sizeof(T)) &&
+                    aligned(noise, 16);
+  // CTAs per sequence: about two per SM in all, a round of loads each at least
+  int cs = 8;
+  while (cs > 1 && ((long long)B * cs > 2LL * p->num_sms || (long long)cs * kTreeThreads * 8 > 2LL * V))
+    cs >>= 1;
+  auto fn = wide ? verify_tree_kernel<T, 4> : verify_tree_kernel<T, 1>;
+  return launch_pdl_cluster(fn, dim3((unsigned)B * cs), dim3(kTreeThreads), cs, 0, s, (const T*)tp,
+                            (const T*)dp, tokens, parent, u, noise, cu, n_tok, V, cs, accepted, path,
+                            next, p->err);
+}
+
+}  // namespace
+}  // namespace optr
+
+extern "C" optr_status optr_verify_tree(const optr_params* p, const void* target_probs,
+                                        const void* draft_probs, int probs_dtype,
+                                        const int32_t* tokens, const int32_t* parent,
+                                        const float* uniform, const float* noise,
+                                        const int32_t* cu_tree, int n_tok, int B, int vocab,
+                                        int32_t* accepted, int32_t* path, int32_t* next,
+                                        cudaStream_t stream) {
+  using namespace optr;
+  if (!p || n_tok < 0 || B <= 0 || vocab <= 0) return OPTR_ERR_INVALID_ARG;
+  if (!cu_tree || !accepted || !noise ||
+      (n_tok > 0 && (!target_probs || !tokens || !parent || !uniform || !path || !next)))
+    return OPTR_ERR_INVALID_ARG;
+  if (probs_dtype != OPTR_PROBS_F32 && probs_dtype != OPTR_PROBS_BF16) return OPTR_ERR_UNSUPPORTED;
+  const size_t size = probs_dtype == OPTR_PROBS_F32 ? 4 : 2;
+  if (!aligned(target_probs, size) || !aligned(draft_probs, size) || !aligned(noise, 4))
+    return OPTR_ERR_INVALID_ARG;
+  if (B > (1 << 24) || vocab > (1 << 30)) return OPTR_ERR_OUT_OF_RANGE;
+  auto fn = probs_dtype == OPTR_PROBS_F32 ? launch_verify_tree<float> : launch_verify_tree<__nv_bfloat16>;
+  return cuda_status(fn(p, target_probs, draft_probs, tokens, parent, uniform, noise, cu_tree, n_tok, B,
+                        vocab, accepted, path, next, stream));
+}

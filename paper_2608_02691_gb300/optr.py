@@ -35,6 +35,8 @@ OPTR_DEVERR_FP16_RANGE = 16
 OPTR_DEVERR_TIMEOUT = 32
 OPTR_DEVERR_WIN_SLOT = 64
 OPTR_DEVERR_TOKEN = 256
+OPTR_DEVERR_TREE = 512
+TREE_MAX_ROWS = 1024  # rows of a sequence's tree
 # types of probabilities (optr_verify_drafts)
 OPTR_PROBS_F32 = 0
 OPTR_PROBS_BF16 = 1
@@ -102,8 +104,13 @@ _SIG = {
                                   _V, ctypes.c_size_t, _V]),
     "optr_chunk_attention_win": (_I, [_V, _V, _V, _V, _I, _V, _V, _I, _V, _I, _I, _V, _I,
                                       _V, _V, _I, _V, _V, ctypes.c_size_t, _V]),
+    "optr_tree_attention": (_I, [_V, _V, _V, _V, _I, _V, _V, _V, _I, _V, _I, _I, _V, _I, _V,
+                                 _V, ctypes.c_size_t, _V]),
+    "optr_tree_attention_win": (_I, [_V, _V, _V, _V, _I, _V, _V, _V, _I, _V, _I, _I, _V, _I,
+                                     _V, _V, _I, _V, _V, ctypes.c_size_t, _V]),
     "optr_kv_read": (_I, [_V, _I, _V, _V, _V, _I, _I, _V, _I, _V, _V, _V]),
     "optr_verify_drafts": (_I, [_V, _V, _V, _I, _V, _V, _V, _V, _I, _I, _I, _V, _V, _V]),
+    "optr_verify_tree": (_I, [_V, _V, _V, _I, _V, _V, _V, _V, _V, _I, _I, _I, _V, _V, _V, _V]),
     "optr_profile_enable": (_I, [_V, _I]),
     "optr_profile_last": (_I, [_V, ctypes.POINTER(ctypes.c_float)]),
 }
@@ -454,6 +461,43 @@ def optr_chunk_attention_win(p: Params, q, k, v, cu_new, pos0, max_new: int, blo
         raise OptrError(st, "optr_chunk_attention_win")
 
 
+def _parents(parent, n):
+    if parent.numel() != n:
+        raise ValueError("parent must be [n_tok]")
+    return _dev(parent, torch.int32, "parent")
+
+
+def optr_tree_attention(p: Params, q, k, v, parent, cu_tree, pos0, max_new: int, block_table,
+                        pool, out, workspace, stream=None) -> None:
+    """optr_chunk_attention of trees: row i of a sequence sees its cached tokens, itself and its
+    ancestors (parent int32 [n_tok]: an earlier row of the sequence, or -1).  The same workspace;
+    max_new is TREE_MAX_ROWS at most."""
+    qp, kp, vp, n, cu, p0, bt, pl, op = _chunk_rows(p, q, k, v, cu_tree, pos0, block_table,
+                                                    pool, out)
+    B, max_pages = block_table.shape
+    st = lib().optr_tree_attention(p.handle, qp, kp, vp, n, _parents(parent, n), cu, p0, max_new, bt,
+                                   B, max_pages, pl, pool.shape[0], op,
+                                   _dev(workspace, torch.uint8, "workspace"), workspace.numel(),
+                                   _stream(stream))
+    if st:
+        raise OptrError(st, "optr_tree_attention")
+
+
+def optr_tree_attention_win(p: Params, q, k, v, parent, cu_tree, pos0, max_new: int, block_table,
+                            pool, win, win_slot, out, workspace, stream=None) -> None:
+    """optr_tree_attention with the cached tokens' BF16 windows read from win."""
+    qp, kp, vp, n, cu, p0, bt, pl, op = _chunk_rows(p, q, k, v, cu_tree, pos0, block_table,
+                                                    pool, out)
+    w, ws_, n_slots = _win_args(p, win, win_slot)
+    B, max_pages = block_table.shape
+    st = lib().optr_tree_attention_win(p.handle, qp, kp, vp, n, _parents(parent, n), cu, p0, max_new,
+                                       bt, B, max_pages, pl, pool.shape[0], w, ws_, n_slots, op,
+                                       _dev(workspace, torch.uint8, "workspace"),
+                                       workspace.numel(), _stream(stream))
+    if st:
+        raise OptrError(st, "optr_tree_attention_win")
+
+
 def optr_kv_read(p: Params, cu_read, pos0, block_table, pool, k, v, stream=None) -> None:
     """Cached rows back in the model's basis: k, v bf16 [n_tok][h_kv][128] (CUDA
     tensors, written), row cu_read[b] + i from position pos0[b] + i of sequence
@@ -497,6 +541,35 @@ def optr_verify_drafts(p: Params, target_probs, draft_probs, drafts, uniform, no
         n, B, vocab, _dev(accepted, i32, "accepted"), _dev(tokens, i32, "tokens"), _stream(stream))
     if st:
         raise OptrError(st, "optr_verify_drafts")
+
+
+def optr_verify_tree(p: Params, target_probs, draft_probs, tokens, parent, uniform, noise, cu_tree,
+                     accepted, path, next, stream=None) -> None:
+    """Verify trees of drafts (rows of optr_tree_attention: tokens and parent int32 [n_tok], row 0 of a
+    sequence its last token with parent -1) against target_probs [n_tok][vocab] (float32 or bf16) with
+    draft_probs [n_tok][vocab] (the same type, or None), uniform float32 [n_tok] and exponential noise
+    float32 [B][vocab].  Writes accepted int32 [B], and path and next int32 [n_tok]: the rows on the
+    accepted way, and the accepted tokens and the one after them, then -1."""
+    f32, i32 = torch.float32, torch.int32
+    n, B = tokens.numel(), cu_tree.numel() - 1
+    vocab = target_probs.shape[1] if target_probs.dim() == 2 else 0
+    if target_probs.shape[0] != n or tuple(noise.shape) != (B, vocab) or uniform.numel() != n \
+            or parent.numel() != n or (draft_probs is not None and draft_probs.shape != target_probs.shape) \
+            or accepted.numel() != B or path.numel() != n or next.numel() != n:
+        raise ValueError("target_probs, draft_probs must be [n_tok][vocab], noise [B][vocab], accepted [B], "
+                         "tokens, parent, uniform, path, next [n_tok]")
+    dtype = target_probs.dtype
+    if dtype not in (f32, torch.bfloat16):
+        raise ValueError("target_probs must be float32 or bfloat16")
+    st = lib().optr_verify_tree(
+        p.handle, _dev(target_probs, dtype, "target_probs"),
+        None if draft_probs is None else _dev(draft_probs, dtype, "draft_probs"),
+        OPTR_PROBS_F32 if dtype is f32 else OPTR_PROBS_BF16, _dev(tokens, i32, "tokens"),
+        _dev(parent, i32, "parent"), _dev(uniform, f32, "uniform"), _dev(noise, f32, "noise"),
+        _dev(cu_tree, i32, "cu_tree"), n, B, vocab, _dev(accepted, i32, "accepted"),
+        _dev(path, i32, "path"), _dev(next, i32, "next"), _stream(stream))
+    if st:
+        raise OptrError(st, "optr_verify_tree")
 
 
 def optr_device_error(p: Params) -> int:
