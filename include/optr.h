@@ -167,6 +167,7 @@ typedef enum {
 #define OPTR_DEVERR_CALIB_RANGE 128u /* calibration: generator norm past exp's scaling range */
 #define OPTR_DEVERR_TOKEN 256u   /* draft token < 0 or >= vocab */
 #define OPTR_DEVERR_TREE 512u    /* a tree row's parent is not one of the rows before it */
+#define OPTR_DEVERR_KEPT 1024u   /* kept positions that cannot be moved together in place */
 
 /* Kernel variants (for measurement; 0 picks the library default). */
 #define OPTR_VARIANT_DEFAULT 0
@@ -632,6 +633,63 @@ optr_status optr_verify_tree(const optr_params* p, const void* target_probs,
                              const int32_t* cu_tree, int n_tok, int B, int vocab,
                              int32_t* accepted, int32_t* path, int32_t* next,
                              cudaStream_t stream);
+
+/*
+ * Eviction, the choice: the positions that each KV head of a sequence of n = lens[b]
+ * cached tokens keeps, n' = min(n, max(keep[b], min(n, first + last))) of them:
+ * the first `first`, the last `last`, and of the others those of the largest scores
+ * (of equal ones the lowest positions; -0 is 0; NaN counts as the largest).
+ *   score    device float32 [B][h_kv][n_score], as optr_kv_score adds to.
+ *   lens     device int32 [B], 0 .. n_score.
+ *   keep     device int32 [B]: the cache's budget (a negative one counts as 0).
+ *   first, last  host, >= 0: with BF16 windows at least sink and recent, for
+ *            optr_kv_compact_win.
+ *   kept     device int32 [B][h_kv][n_most]: n' positions in rising order; what lies
+ *            behind them stays as it is.
+ *   n_kept   device int32 [B]: n'.
+ * A sequence with lens out of range, or n' > n_most, gets n_kept = -1, no positions,
+ * and sets OPTR_DEVERR_SEQ_LEN.  Nothing is allocated or synchronised.
+ */
+optr_status optr_evict_select(const optr_params* p, const float* score, int n_score,
+                              const int32_t* lens, const int32_t* keep, int B,
+                              int first, int last, int32_t* kept, int n_most,
+                              int32_t* n_kept, cudaStream_t stream);
+
+/*
+ * Eviction, the move: in each KV head h of sequence b the INT2 record of position
+ * kept[b][h][i] becomes that of position i, i = 0 .. n_kept[b]-1, in place; the cache
+ * then holds n_kept[b] tokens (pages behind them are the caller's again), and the next
+ * one is written at pos0 = n_kept[b].  Keys stay rotated by the positions that they had
+ * in the text: those of new queries and keys go on from there.  score moves along, and
+ * is 0 from n_kept[b] to lens[b]-1; NULL: there is none.
+ *   kept     device int32 [B][h_kv][n_most], rising, each in 0 .. lens[b]-1.
+ *   n_kept   device int32 [B], 0 .. min(lens[b], n_most).
+ *   lens     device int32 [B]: tokens before, 0 .. max_pages * 16 (and n_score).
+ *   block_table, pool  as in optr_kv_append; no page is in the tables of two
+ *            sequences that the call shortens (nor twice in one's).
+ * A sequence whose n_kept or lens is out of range is left as it is and sets
+ * OPTR_DEVERR_SEQ_LEN.  A position kept[..][i] that is not above the one before it, or
+ * not below lens[b], sets OPTR_DEVERR_KEPT, and record i stays what it is; so does one
+ * from or to a page out of range (OPTR_DEVERR_PAGE_ID).  Nothing is allocated or
+ * synchronised.
+ */
+optr_status optr_kv_compact(const optr_params* p, const int32_t* kept, int n_most,
+                            const int32_t* n_kept, const int32_t* lens,
+                            const int32_t* block_table, int B, int max_pages,
+                            uint8_t* pool, int num_pages, float* score, int n_score,
+                            cudaStream_t stream);
+
+/* The same with the BF16 windows of p: the first min(lens[b], sink) and the last
+ * min(lens[b], recent) positions have to be kept, and the ring's rows move to where the
+ * positions that they then have lie.  A head that does not keep them sets
+ * OPTR_DEVERR_KEPT and is left as it is; so is, with OPTR_DEVERR_WIN_SLOT, a sequence
+ * whose slot is out of range.  With sink = recent = 0 exactly the plain call. */
+optr_status optr_kv_compact_win(const optr_params* p, const int32_t* kept, int n_most,
+                                const int32_t* n_kept, const int32_t* lens,
+                                const int32_t* block_table, int B, int max_pages,
+                                uint8_t* pool, int num_pages, void* win,
+                                const int32_t* win_slot, int n_slots, float* score,
+                                int n_score, cudaStream_t stream);
 
 /* Static description of a status code. */
 const char* optr_strerror(optr_status s);

@@ -36,6 +36,7 @@ OPTR_DEVERR_TIMEOUT = 32
 OPTR_DEVERR_WIN_SLOT = 64
 OPTR_DEVERR_TOKEN = 256
 OPTR_DEVERR_TREE = 512
+OPTR_DEVERR_KEPT = 1024
 TREE_MAX_ROWS = 1024  # rows of a sequence's tree
 # types of probabilities (optr_verify_drafts)
 OPTR_PROBS_F32 = 0
@@ -111,6 +112,9 @@ _SIG = {
     "optr_kv_read": (_I, [_V, _I, _V, _V, _V, _I, _I, _V, _I, _V, _V, _V]),
     "optr_verify_drafts": (_I, [_V, _V, _V, _I, _V, _V, _V, _V, _I, _I, _I, _V, _V, _V]),
     "optr_verify_tree": (_I, [_V, _V, _V, _I, _V, _V, _V, _V, _V, _I, _I, _I, _V, _V, _V, _V]),
+    "optr_evict_select": (_I, [_V, _V, _I, _V, _V, _I, _I, _I, _V, _I, _V, _V]),
+    "optr_kv_compact": (_I, [_V, _V, _I, _V, _V, _V, _I, _I, _V, _I, _V, _I, _V]),
+    "optr_kv_compact_win": (_I, [_V, _V, _I, _V, _V, _V, _I, _I, _V, _I, _V, _V, _I, _V, _I, _V]),
     "optr_profile_enable": (_I, [_V, _I]),
     "optr_profile_last": (_I, [_V, ctypes.POINTER(ctypes.c_float)]),
 }
@@ -570,6 +574,62 @@ def optr_verify_tree(p: Params, target_probs, draft_probs, tokens, parent, unifo
         _dev(path, i32, "path"), _dev(next, i32, "next"), _stream(stream))
     if st:
         raise OptrError(st, "optr_verify_tree")
+
+
+def _score_rows(p, score, B):
+    """Pointer and row length of a score tensor (None: null)."""
+    if score is None:
+        return None, 0
+    if score.dim() != 3 or tuple(score.shape[:2]) != (B, p.h_kv):
+        raise ValueError("score must be [B][h_kv][positions]")
+    return _dev(score, torch.float32, "score"), score.shape[2]
+
+
+def optr_evict_select(p: Params, score, lens, keep, first: int, last: int, kept, n_kept,
+                      stream=None) -> None:
+    """The positions that stay: of each (sequence, KV head) the first and last ones and, up to keep[b]
+    in all, those of the largest score float32 [B][h_kv][positions].  lens, keep int32 [B].  Writes kept
+    int32 [B][h_kv][n_most] (rising; the rest stays as it is) and n_kept int32 [B]."""
+    i32 = torch.int32
+    B = lens.numel()
+    sp, n_score = _score_rows(p, score, B)
+    if kept.dim() != 3 or tuple(kept.shape[:2]) != (B, p.h_kv) or keep.numel() != B or n_kept.numel() != B:
+        raise ValueError("kept must be [B][h_kv][n_most], keep, n_kept [B]")
+    st = lib().optr_evict_select(p.handle, sp, n_score, _dev(lens, i32, "lens"), _dev(keep, i32, "keep"), B,
+                                 first, last, _dev(kept, i32, "kept"), kept.shape[2],
+                                 _dev(n_kept, i32, "n_kept"), _stream(stream))
+    if st:
+        raise OptrError(st, "optr_evict_select")
+
+
+def _compact_args(p, kept, n_kept, lens, block_table, pool):
+    i32 = torch.int32
+    B, max_pages = block_table.shape
+    if kept.dim() != 3 or tuple(kept.shape[:2]) != (B, p.h_kv) or n_kept.numel() != B or lens.numel() != B:
+        raise ValueError("kept must be [B][h_kv][n_most], n_kept, lens [B]")
+    return (_dev(kept, i32, "kept"), kept.shape[2], _dev(n_kept, i32, "n_kept"), _dev(lens, i32, "lens"),
+            _dev(block_table, i32, "block_table"), B, max_pages, _dev(pool, torch.uint8, "pool"),
+            pool.shape[0])
+
+
+def optr_kv_compact(p: Params, kept, n_kept, lens, block_table, pool, score=None, stream=None) -> None:
+    """Move the records of kept (as optr_evict_select writes it) together in place: sequence b then
+    holds n_kept[b] tokens instead of lens[b].  score moves along (None: there is none)."""
+    args = _compact_args(p, kept, n_kept, lens, block_table, pool)
+    st = lib().optr_kv_compact(p.handle, *args, *_score_rows(p, score, lens.numel()), _stream(stream))
+    if st:
+        raise OptrError(st, "optr_kv_compact")
+
+
+def optr_kv_compact_win(p: Params, kept, n_kept, lens, block_table, pool, win, win_slot, score=None,
+                        stream=None) -> None:
+    """optr_kv_compact with the BF16 windows' rings turned along; kept holds the first sink and the
+    last recent positions."""
+    args = _compact_args(p, kept, n_kept, lens, block_table, pool)
+    st = lib().optr_kv_compact_win(p.handle, *args, *_win_args(p, win, win_slot),
+                                   *_score_rows(p, score, lens.numel()), _stream(stream))
+    if st:
+        raise OptrError(st, "optr_kv_compact_win")
 
 
 def optr_device_error(p: Params) -> int:
