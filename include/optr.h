@@ -635,6 +635,47 @@ optr_status optr_verify_tree(const optr_params* p, const void* target_probs,
                              cudaStream_t stream);
 
 /*
+ * Attention weights of the new tokens, summed by position: what an eviction by
+ * accumulated attention keeps account of.  Sequence b's new tokens i = 0 .. m-1 (rows
+ * t = cu_new[b] + i of q) stand at positions pos0[b] + i of the cache, which holds them
+ * already (n = pos0[b] + m tokens); for each KV head h and cached position s
+ *      score[b][h][s] += sum over i and the query heads j of h of p_ij(s),
+ *      p_ij = softmax over s <= pos0[b] + i of l_ijs
+ * with l as in optr_decode_attention for a sequence of n tokens: INT2 positions from
+ * their records, BF16-window positions (of n tokens) from the store.  A decode step's
+ * tokens after optr_decode_step, the last tokens of a prompt after its cache write.
+ *   q           device bf16 [n_tok][h_q][D].
+ *   n_tok, cu_new, pos0, max_new  as in optr_chunk_attention.
+ *   score       device float32 [B][h_kv][n_score], added to at positions below n; it
+ *               starts as the caller's (zeros, or what is left of earlier sums).
+ *   workspace   device, optr_kv_score_workspace_size bytes, 256-byte aligned, scratch as
+ *               in optr_decode_attention.
+ * Logits are good to some 2^-20 of |q||k| / sqrt(128) (queries and keys of 22 bits,
+ * float32 sums); sums of a position are added in a fixed order.  Queries must be finite.  A
+ * sequence with pos0 < 0, or n past max_pages * 16 or n_score (OPTR_DEVERR_SEQ_LEN), more
+ * than max_new tokens or inconsistent cu_new (OPTR_DEVERR_CU_NEW) adds nothing.  Positions of
+ * an out-of-range page (OPTR_DEVERR_PAGE_ID) or window slot (OPTR_DEVERR_WIN_SLOT) are
+ * left out of the softmax.  Nothing is allocated or synchronised.
+ */
+size_t optr_kv_score_workspace_size(const optr_params* p, int n_tok, int B, int max_new,
+                                    int max_pages);
+
+optr_status optr_kv_score(const optr_params* p, const void* q, int n_tok,
+                          const int32_t* cu_new, const int32_t* pos0, int max_new,
+                          const int32_t* block_table, int B, int max_pages,
+                          const uint8_t* pool, int num_pages, float* score, int n_score,
+                          void* workspace, size_t ws_bytes, cudaStream_t stream);
+
+/* The same with the BF16 windows of p; with sink = recent = 0 exactly the plain call. */
+optr_status optr_kv_score_win(const optr_params* p, const void* q, int n_tok,
+                              const int32_t* cu_new, const int32_t* pos0, int max_new,
+                              const int32_t* block_table, int B, int max_pages,
+                              const uint8_t* pool, int num_pages, const void* win,
+                              const int32_t* win_slot, int n_slots, float* score,
+                              int n_score, void* workspace, size_t ws_bytes,
+                              cudaStream_t stream);
+
+/*
  * Eviction, the choice: the positions that each KV head of a sequence of n = lens[b]
  * cached tokens keeps, n' = min(n, max(keep[b], min(n, first + last))) of them:
  * the first `first`, the last `last`, and of the others those of the largest scores

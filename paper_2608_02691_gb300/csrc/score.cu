@@ -1,0 +1,799 @@
+// Attention weights of the new tokens, summed by position (include/optr.h,
+// "optr_kv_score"): score[s] += sum over tokens i and heads of softmax(l_i)(s).
+//
+// The sum over rows needs each row's normaliser first, and the logits are too many to
+// be kept (a row of 32768 floats for each of 64 tokens x 4 heads), so they are computed
+// twice: query_kernel rotates the queries, logit_kernel<false> finds each row's maximum
+// and sum by CTA, normaliser_kernel joins those, logit_kernel<true> computes the logits
+// again and adds exp2(l - lse) up.
+//
+// Layout.  A tile is 128 keys times the block's columns (64 tokens x 4 heads at most):
+// D[key][column] = K Q^T on the tensor core, K in tensor memory (written there by the
+// warps that dequantize: a lane has a key), Q in shared memory for a whole piece.  A
+// thread of the epilogue has one key: the sum over rows, which the second pass wants,
+// is a sum along its registers, and the sum over keys of the first pass is kept per
+// column in registers too and meets the other lanes' once a piece.
+//
+// Rounding.  The sums are float32, and a weight moves by what its logit does: rounding
+// queries or keys to 16 bits would move it by some 3e-4.  So both go in as fp16 hi + lo
+// parts (22 bits; queries over a power of two by row, keys over one by key), and a tile
+// takes the products hi hi + hi lo + lo hi.  A group of a slot has four values, so the
+// parts of 16 values are computed in float32 and the codes pick among them by byte
+// permutes.  Window keys and their queries are bf16 as they are, one product.
+#include "f32x2.cuh"
+#include "score.cuh"
+#include "tc05.cuh"
+
+#include <algorithm>
+
+namespace optr {
+namespace {
+
+// ------------------------------------------------------------- queries
+
+// Channel at place k of a key row: word w of a slot's codes has, by byte, the four
+// groups' channels 4 w .. 4 w + 3.
+__host__ __device__ constexpr int key_channel(int k) { return 32 * ((k >> 2) & 3) + 4 * (k >> 4) + (k & 3); }
+
+// Element (n, k) of an operand of n columns, K-major without swizzle: core matrices of
+// 8 columns x 8 of k (128 B), 128 B apart along k and 2048 B along n.
+__device__ __forceinline__ int operand_offset(int n, int k) {
+  return (n / 8) * 2048 + (k / 8) * 128 + (n % 8) * 16 + (k % 8) * 2;
+}
+
+constexpr int kRotThreads = 256;
+constexpr int kRotCols = 32;  // columns of a CTA: 8 tokens
+
+// CTA (x, seg): columns 32 x .. of the segment's block, rotated in float32.  Thread:
+// place k of the rows, 16 of the columns.
+__global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constant__ ScoreArgs A) {
+  __shared__ float q[kRotCols][kD];
+  __shared__ float top[4][kRotCols], dot[4][kRotCols];
+  const int seg = blockIdx.y, b = seg / A.h_kv, h = seg % A.h_kv, tid = threadIdx.x;
+  const int k = tid & 127, part = tid >> 7, lane = tid & 31, quarter = (tid >> 5) & 3;
+  pdl_wait();
+  pdl_trigger();
+  if (blockIdx.x == 0 && seg == 0 && A.t0 == 0 && tid < 32) report_sequences(A);
+  const ScoreSeq s = score_seq(A, b);
+  const int c0 = kRotCols * blockIdx.x, N = (4 * s.rows + 15) / 16 * 16;
+  if (c0 >= N || seq_tiles(s) == 0) return;
+  const bool win = A.win.win != nullptr;
+  uint8_t* out = qop_of(A, seg);
+  for (int i = tid; i < kRotCols * kD / 8; i += kRotThreads) {
+    const int c = i / (kD / 8), x = 8 * (i % (kD / 8)), tok = (c0 + c) / 4;
+    uint4 y = make_uint4(0u, 0u, 0u, 0u);
+    if (tok < s.rows)
+      y = __ldcg(reinterpret_cast<const uint4*>(
+          A.q + (((size_t)s.c0 + A.t0 + tok) * A.h_kv + h) * (4 * kD) + (c & 3) * kD + x));
+    const uint32_t word[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      q[c][x + 2 * e] = __uint_as_float(word[e] << 16);
+      q[c][x + 2 * e + 1] = __uint_as_float(word[e] & 0xffff0000u);
+    }
+    if (win && c0 + c < N)
+      *reinterpret_cast<uint4*>(out + (size_t)A.cols * 512 + operand_offset(c0 + c, x)) = y;
+  }
+  __syncthreads();
+  constexpr int kMine = kRotCols / 2;
+  float acc[kMine] = {};
+  const float* R = A.R_k + (size_t)h * kD * kD + key_channel(k);
+  for (int i0 = 0; i0 < kD; i0 += 16) {
+    float r[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = __ldg(R + (size_t)(i0 + i) * kD);
+#pragma unroll
+    for (int c = 0; c < kMine; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const float4 x = *reinterpret_cast<const float4*>(&q[kMine * part + c][i0 + i]);
+        acc[c] = fmaf(x.x, r[i], acc[c]);
+        acc[c] = fmaf(x.y, r[i + 1], acc[c]);
+        acc[c] = fmaf(x.z, r[i + 2], acc[c]);
+        acc[c] = fmaf(x.w, r[i + 3], acc[c]);
+      }
+  }
+  const float mu = __ldg(A.mu + (size_t)h * kD + k);
+#pragma unroll
+  for (int c = 0; c < kMine; ++c) {
+    float m = fabsf(acc[c]), d = q[kMine * part + c][k] * mu;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      d += __shfl_xor_sync(0xffffffffu, d, o);
+    }
+    if (lane == 0) {
+      top[quarter][kMine * part + c] = m;
+      dot[quarter][kMine * part + c] = d;
+    }
+  }
+  __syncthreads();
+  float* factor = reinterpret_cast<float*>(out + (size_t)A.cols * (win ? 768 : 512));
+#pragma unroll
+  for (int c = 0; c < kMine; ++c) {
+    const int n = kMine * part + c;
+    const float m = fmaxf(fmaxf(top[0][n], top[1][n]), fmaxf(top[2][n], top[3][n]));
+    // the row's largest at 2^13 .. 2^14, so that lo parts are normal fp16 down to 2^-17 of it
+    const int E = m > 0.f ? max(-100, min(100, 13 - ((int)(__float_as_uint(m) >> 23) - 127))) : 0;
+    const float x = acc[c] * __uint_as_float((uint32_t)(127 + E) << 23);
+    const __half hi = __float2half_rn(x), lo = __float2half_rn(x - __half2float(hi));
+    if (c0 + n >= N) break;
+    const int at = operand_offset(c0 + n, k);
+    *reinterpret_cast<__half*>(out + at) = hi;
+    *reinterpret_cast<__half*>(out + (size_t)A.cols * 256 + at) = lo;
+    if (k == 0) {
+      factor[c0 + n] = __uint_as_float((uint32_t)(127 - E) << 23) * kLogit;
+      factor[A.cols + c0 + n] = kLogit * ((dot[0][n] + dot[1][n]) + (dot[2][n] + dot[3][n]));
+    }
+  }
+}
+
+// -------------------------------------------------------------- logits
+
+// Warps: two epilogue groups of four, four that write keys, one each for the copies, the
+// products and the pieces.  Registers a thread after the split, of the launch's 512 x 128.
+constexpr int kKeyWarp = 8, kCopyWarp = 12, kMmaWarp = 13, kPlanWarp = 14;
+constexpr int kThreads = 512;
+constexpr int kRegLaunch = 128, kRegEpi = 208, kRegKey = 56, kRegIssue = 40;
+static_assert(2 * kRegEpi + kRegKey + kRegIssue <= 4 * kRegLaunch, "registers of the launch");
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kColD = 0, kColK = 256;  // D[d] at 128 d; keys' hi, lo [s] at 256 + 128 s
+constexpr int kRaw = 3;        // tiles of records on the way
+constexpr int kPieces = 3;     // pieces found ahead
+constexpr int kConsumers = 14; // warps that take the pieces
+constexpr float kSlack = 60.f; // a column's logits may pass its reference by 2^60
+constexpr int kHalfRec = 768;  // a page's key codes and pairs
+
+struct Smem {
+  uint8_t q[3][kBlockCols * 256];    // hi, lo, as given
+  uint8_t raw[kRaw][kKeys / kPage][kHalfRec];
+  alignas(16) float factor[kBlockCols], off[kBlockCols];
+  // minus the columns' references: pass 0 by warp, pass 1 the normalisers
+  alignas(16) float ref[8][kKeys];
+  float2 meet[8][kKeys];             // pass 0: the warps' parts of a piece
+  // a key's power of two, 0 where it does not count.  Read between the tile's logits
+  // and its D being free; written for tile t + 4 once the products of t + 2 are done,
+  // which waited for that.
+  float scale[4][kKeys];
+  ScorePiece piece[kPieces];
+  uint64_t raw_full[kRaw], raw_empty[kRaw], k_full[2], k_empty[2];
+  uint64_t d_full[2][2], d_empty[2];  // by D and the epilogue group that takes it
+  uint64_t piece_full[kPieces], piece_empty[kPieces], q_full, q_empty, drained;
+  uint32_t tmem;
+  int abort;
+};
+
+static_assert(sizeof(Smem) <= 232448, "shared memory of a CTA");
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_half(float a, float b) {  // a in the low half
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
+}
+__device__ __forceinline__ float2 unpack_half(uint32_t x) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&x));
+}
+
+// The 128 threads of an epilogue group.
+__device__ __forceinline__ void group_sync(int g) {
+  if (g == 0)
+    asm volatile("bar.sync 1, 128;" ::: "memory");
+  else
+    asm volatile("bar.sync 2, 128;" ::: "memory");
+}
+
+// Largest of x over the warp (x is not NaN).
+__device__ __forceinline__ float warp_largest(float x) {
+  const int i = __float_as_int(x);
+  const int y = __reduce_max_sync(0xffffffffu, i ^ ((i >> 31) & 0x7fffffff));
+  return __int_as_float(y ^ ((y >> 31) & 0x7fffffff));
+}
+
+template <bool kSum>
+__global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constant__ ScoreArgs A) {
+  extern __shared__ __align__(1024) unsigned char dsm_[];
+  Smem& S = *reinterpret_cast<Smem*>(dsm_);
+  const int tid = threadIdx.x, lane = tid & 31;
+  const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  if (tid == 0) {
+    for (int i = 0; i < kRaw; ++i) {
+      tc05::bar_init(&S.raw_full[i], 1);
+      tc05::bar_init(&S.raw_empty[i], 4);
+    }
+    for (int i = 0; i < 2; ++i) {
+      tc05::bar_init(&S.k_full[i], 4);
+      tc05::bar_init(&S.k_empty[i], 1);
+      tc05::bar_init(&S.d_empty[i], 4);
+      for (int e = 0; e < 2; ++e) tc05::bar_init(&S.d_full[i][e], 1);
+    }
+    for (int i = 0; i < kPieces; ++i) {
+      tc05::bar_init(&S.piece_full[i], 1);
+      tc05::bar_init(&S.piece_empty[i], kConsumers);
+    }
+    tc05::bar_init(&S.q_full, 1);
+    tc05::bar_init(&S.q_empty, 9);  // the products, and the epilogue's warps
+    tc05::bar_init(&S.drained, 1);
+    S.abort = 0;
+    tc05::bar_init_fence();
+  }
+  if (warp == kMmaWarp) tc05::tmem_alloc(&S.tmem, kTmemCols);
+  pdl_wait();
+  pdl_trigger();
+  tc05::fence_before();
+  __syncthreads();
+  tc05::fence_after();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, S.tmem, 0);
+  volatile int* abort = &S.abort;
+  const int w = blockIdx.x;
+  bool dead = false;
+  auto wait = [&](uint64_t* bar, uint32_t phase) {
+    if (!__all_sync(0xffffffffu, tc05::bar_wait_spin(bar, phase & 1, abort))) dead = true;
+    tc05::fence_after();
+    return !dead;
+  };
+  auto arrive = [&](uint64_t* bar) {  // the warp
+    __syncwarp();
+    if (lane == 0) tc05::bar_arrive(bar);
+  };
+  auto next_piece = [&](uint32_t n, ScorePiece& p) {
+    const uint32_t i = n % kPieces;
+    if (dead || !wait(&S.piece_full[i], n / kPieces)) return false;
+    p = S.piece[i];
+    arrive(&S.piece_empty[i]);
+    return p.t1 > p.t0;
+  };
+  const bool win = A.win.win != nullptr;
+  if (warp < kKeyWarp) {
+    // ------------------------------------------------------------ epilogue
+    // Columns beyond 128 have a D of their own.  Maxima and sums: group g takes its D
+    // (pair), or the tiles of its parity; weights: the tiles of its parity, both D.
+    tc05::reg_inc<kRegEpi>();
+    const int g = warp >> 2, key = 32 * (warp & 3) + lane;
+    const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
+    uint32_t nd[2] = {0, 0}, nk = 0;  // phases of d_full[.][g]; key tiles of the CTA
+    ScorePiece p;
+    for (uint32_t n = 0; next_piece(n, p); ++n) {
+      const int tiles = p.t1 - p.t0, cols = p.cols();
+      const bool pair = cols > kKeys;
+      if (!wait(&S.q_full, n)) break;
+      float* ref = kSum ? S.ref[0] : S.ref[warp];
+      const int cbase = !kSum && pair ? kKeys * g : 0;  // first column of the group's
+      float acc[kSum ? 1 : kKeys];
+      uint32_t set[kSum ? 1 : 4];
+      if constexpr (!kSum) {
+#pragma unroll
+        for (int c = 0; c < kKeys; ++c) acc[c] = 0.f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          // columns that are none need no reference
+          const int some = cols - cbase - 32 * c;
+          set[c] = some >= 32 ? 0u : some <= 0 ? ~0u : ~0u << some;
+          ref[32 * c + lane] = 0.f;
+        }
+        __syncwarp();
+      }
+      for (int t = 0; t < tiles; ++t) {
+        if ((kSum || !pair) && (t & 1) != g) continue;
+        const int tile = p.t0 + t;
+        const bool exact = tile >= p.I;  // a window tile
+        float scale = 0.f, sum = 0.f, old = 0.f;
+        int first = 0;                   // the first column that sees the key
+        float* at = nullptr;
+        bool begun = false;
+#pragma unroll 1
+        for (int d = kSum || !pair ? 0 : g; d < (pair && (kSum || g == 1) ? 2 : 1); ++d) {
+          const int D = pair ? d : t & 1;
+          if (!wait(&S.d_full[D][g], nd[D]++)) break;
+          if (!begun) {
+            begun = true;
+            scale = S.scale[(nk + t) % 4][key];
+            const int i = kKeys * (exact ? tile - p.I : tile) + key;
+            const int pos = exact ? win_pos(i, p.n, A.sink, A.recent) : A.sink + i;
+            if (scale != 0.f) {
+              const int tok = pos - p.pos0 - A.t0;
+              first = tok > 0 ? 4 * tok : 0;
+              if (kSum) {
+                at = A.score + (size_t)p.seg * A.n_score + pos;
+                old = __ldcg(at);
+              }
+            } else {
+              first = 1 << 20;
+            }
+          }
+          const uint32_t tD = tmem + lanes + kColD + 128u * D;
+          const int c_lo = kSum ? kKeys * d : cbase;    // the columns' place in the block
+          const int n_cols = min(kKeys, cols - c_lo);
+          const float2 scale2 = make_float2(scale, scale);
+#pragma unroll
+          for (int c = 0; c < kKeys / 16; ++c) {
+            if (16 * c >= n_cols) break;
+            uint32_t x[16];
+            tc05::tmem_ld16(tD + 16 * c, x);
+            tc05::tmem_wait_ld();
+            if (16 * (c + 1) >= n_cols) {
+              tc05::fence_before();
+              arrive(&S.d_empty[D]);
+            }
+            const float* r = kSum ? S.ref[0] + c_lo + 16 * c : ref + 16 * c;
+            float y[16];
+            if (exact) {
+#pragma unroll
+              for (int j = 0; j < 16; j += 4) {
+                const float4 o = *reinterpret_cast<const float4*>(&S.off[c_lo + 16 * c + j]);
+                const float4 m = *reinterpret_cast<const float4*>(r + j);
+                y[j] = fmaf(__uint_as_float(x[j]), kLogit, m.x - o.x);
+                y[j + 1] = fmaf(__uint_as_float(x[j + 1]), kLogit, m.y - o.y);
+                y[j + 2] = fmaf(__uint_as_float(x[j + 2]), kLogit, m.z - o.z);
+                y[j + 3] = fmaf(__uint_as_float(x[j + 3]), kLogit, m.w - o.w);
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 16; j += 4) {
+                const float4 f = *reinterpret_cast<const float4*>(&S.factor[c_lo + 16 * c + j]);
+                const float4 m = *reinterpret_cast<const float4*>(r + j);
+                const float2 f0 = mul2(make_float2(f.x, f.y), scale2), f1 = mul2(make_float2(f.z, f.w), scale2);
+                const float2 u = fma2(make_float2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), f0,
+                                      make_float2(m.x, m.y));
+                const float2 v = fma2(make_float2(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), f1,
+                                      make_float2(m.z, m.w));
+                y[j] = u.x, y[j + 1] = u.y, y[j + 2] = v.x, y[j + 3] = v.y;
+              }
+            }
+            if (__any_sync(0xffffffffu, first > c_lo + 16 * c)) {
+              const int k = first - c_lo - 16 * c;
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                if (j < k) y[j] = -INFINITY;
+            }
+            if constexpr (kSum) {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) sum += ex2(y[j]);
+            } else {
+              float top = y[0];
+#pragma unroll
+              for (int j = 1; j < 16; ++j) top = fmaxf(top, y[j]);
+              const uint32_t known = set[c / 2] >> (16 * (c & 1)) & 0xffffu;
+              if (__any_sync(0xffffffffu, known != 0xffffu || top > kSlack)) {
+                // columns without a reference, or with logits far above it: the warp's
+                // largest becomes it
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                  const float m = warp_largest(y[j]);
+                  const bool fresh = !(known >> j & 1);
+                  if (m > kSlack || (fresh && m > -INFINITY)) {
+                    acc[16 * c + j] = fresh ? 0.f : acc[16 * c + j] * ex2(-m);
+                    y[j] -= m;
+                    set[c / 2] |= 1u << (16 * (c & 1) + j);
+                    if (lane == 0) ref[16 * c + j] -= m;
+                  }
+                }
+                __syncwarp();
+              }
+#pragma unroll
+              for (int j = 0; j < 16; ++j) acc[16 * c + j] += ex2(y[j]);
+            }
+          }
+        }
+        if (dead) break;
+        if (kSum && scale != 0.f) *at = old + sum;
+      }
+      if (dead) break;
+      nk += tiles;
+      if constexpr (!kSum) {
+        // over the warp's keys: 32 columns a time, each lane ends with one's sum
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float* a = acc + 32 * c;
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) {
+            const bool upper = lane & o;
+#pragma unroll
+            for (int j = 0; j < o; ++j) {
+              const float mine = upper ? a[j + o] : a[j], other = upper ? a[j] : a[j + o];
+              a[j] = mine + __shfl_xor_sync(0xffffffffu, other, o);
+            }
+          }
+          S.meet[warp][32 * c + lane] = make_float2(-ref[32 * c + lane], a[0]);
+        }
+        __syncwarp();
+        // over the group's warps
+        group_sync(g);
+        float m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 y = S.meet[4 * g + i][key];
+          if (y.y > 0.f) m = fmaxf(m, y.x);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 y = S.meet[4 * g + i][key];
+          if (y.y > 0.f) l += y.y * ex2(y.x - m);
+        }
+        score_part(A, w, p.seg)[kKeys * g + key] = make_float2(m, l);
+        group_sync(g);
+      }
+      arrive(&S.q_empty);
+    }
+  } else if (warp < kCopyWarp) {
+    // --------------------------------------------------------------- keys
+    // Thread = key.  A's row in tensor memory: 64 columns of hi parts, 64 of lo.
+    tc05::reg_dec<kRegKey>();
+    const int quarter = warp & 3, key = tid & 127, ms = meta_stride(A.compact);
+    const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
+    uint32_t nk = 0, raws = 0;
+    ScorePiece p;
+    for (uint32_t n = 0; next_piece(n, p); ++n) {
+      for (int tile = p.t0; tile < p.t1; ++tile, ++nk) {
+        const uint32_t s = nk & 1, tK = tmem + lanes + kColK + 128u * s;
+        float scale = 0.f;
+        if (tile < p.I) {
+          const int i = kKeys * tile + key;
+          bool ok = i < p.n_int;
+          if (ok) {
+            const int page = __ldcg(A.bt + (size_t)p.b * A.max_pages + (A.sink + i) / kPage);
+            ok = page >= 0 && page < A.num_pages;
+            if (!ok) atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
+          }
+          const uint32_t r = raws % kRaw;
+          if (!wait(&S.raw_full[r], raws / kRaw)) break;
+          ++raws;
+          const uint8_t* raw = S.raw[r][key / kPage];
+          const int slot = key % kPage;
+          uint4 mm;
+          if (A.compact)
+            mm.x = mm.y = mm.z = mm.w = *reinterpret_cast<const uint32_t*>(raw + 512 + ms * slot);
+          else
+            mm = *reinterpret_cast<const uint4*>(raw + 512 + ms * slot);
+          // the four values of each group, over a power of two above the largest
+          const uint32_t pairs[4] = {mm.x, mm.y, mm.z, mm.w};
+          float top = 0.f;
+#pragma unroll
+          for (int G = 0; G < 4; ++G) {
+            const float2 y = unpack_half(pairs[G]);
+            top = fmaxf(top, fmaxf(fabsf(y.y), fabsf(fmaf(3.f, y.x, y.y))));
+          }
+          const int E = min(max((int)(__float_as_uint(top) >> 23) - 126, -60), 60);
+          const float down = __uint_as_float((uint32_t)(127 - E) << 23);
+          if (ok) scale = __uint_as_float((uint32_t)(127 + E) << 23);
+          uint32_t hi[4][2], lo[4][2];
+#pragma unroll
+          for (int G = 0; G < 4; ++G) {
+            const float2 y = unpack_half(pairs[G]);
+            const float sc = y.x * down, mn = y.y * down;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float a = fmaf((float)(2 * e), sc, mn), b = fmaf((float)(2 * e + 1), sc, mn);
+              hi[G][e] = pack_half(a, b);
+              const float2 z = unpack_half(hi[G][e]);
+              lo[G][e] = pack_half(a - z.x, b - z.y);
+            }
+          }
+          if (nk >= 2 && !wait(&S.k_empty[s], nk / 2 - 1)) break;
+#pragma unroll
+          for (int part = 0; part < 4; ++part) {
+            const uint2 word = *reinterpret_cast<const uint2*>(raw + 32 * slot + 8 * part);
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+              const uint32_t x = v ? word.y : word.x;
+              uint32_t pick[8];  // by group and half of its byte
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                // code c of a byte picks bytes 2 c and 2 c + 1 of its group's values
+                const uint32_t a = (x >> (4 * e) & 0x03030303u) * 0x22u + 0x10101010u;
+                const uint32_t b = (x >> (4 * e + 2) & 0x03030303u) * 0x22u + 0x10101010u;
+                pick[e] = __byte_perm(a, b, 0x5140);
+                pick[4 + e] = __byte_perm(a, b, 0x7362);
+                pick[2 + e] = pick[e] >> 16;
+                pick[6 + e] = pick[4 + e] >> 16;
+              }
+              uint32_t y[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) y[e] = __byte_perm(hi[e / 2][0], hi[e / 2][1], pick[e]);
+              tc05::tmem_st8(tK + 16 * part + 8 * v, y);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) y[e] = __byte_perm(lo[e / 2][0], lo[e / 2][1], pick[e]);
+              tc05::tmem_st8(tK + 64 + 16 * part + 8 * v, y);
+            }
+          }
+          arrive(&S.raw_empty[r]);
+        } else {
+          const int i = kKeys * (tile - p.I) + key;
+          if (nk >= 2 && !wait(&S.k_empty[s], nk / 2 - 1)) break;
+          const uint4* src = nullptr;
+          if (i < p.n_win) {
+            scale = 1.f;
+            const int row = win_row(win_pos(i, p.n, A.sink, A.recent), A.sink, A.recent);
+            src = reinterpret_cast<const uint4*>(
+                A.win.win + ((((size_t)p.slot * A.h_kv + p.h) * 2) * (A.sink + A.recent) + row) * kD);
+          }
+#pragma unroll
+          for (int part = 0; part < 4; ++part) {
+            uint32_t y[16];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const uint4 x = src ? __ldcg(src + 4 * part + v) : make_uint4(0u, 0u, 0u, 0u);
+              y[4 * v] = x.x, y[4 * v + 1] = x.y, y[4 * v + 2] = x.z, y[4 * v + 3] = x.w;
+            }
+            tc05::tmem_st16(tK + 16 * part, y);
+          }
+        }
+        S.scale[nk % 4][key] = scale;
+        tc05::tmem_wait_st();
+        tc05::fence_before();
+        arrive(&S.k_full[s]);
+      }
+      if (dead) break;
+    }
+  } else {
+    tc05::reg_dec<kRegIssue>();
+    if (warp == kCopyWarp) {
+      // ------------------------------------------------------------- copies
+      uint32_t raws = 0, nq = 0;
+      ScorePiece p;
+      for (uint32_t n = 0; next_piece(n, p); ++n) {
+        if (n > 0 && !wait(&S.q_empty, n - 1)) break;
+        const uint32_t bytes = (uint32_t)(p.N() + 7) / 8 * 2048, line = (uint32_t)p.N() * 4;
+        if (lane == 0) {
+          const uint8_t* src = qop_of(A, p.seg);
+          const int kinds = win ? 3 : 2;
+          tc05::bar_arrive_expect_tx(&S.q_full, kinds * bytes + (kSum ? 3 : 2) * line);
+          for (int i = 0; i < kinds; ++i) tc05::bulk_g2s(S.q[i], src + (size_t)A.cols * 256 * i, bytes, &S.q_full);
+          const uint8_t* c = src + (size_t)A.cols * 256 * kinds;
+          tc05::bulk_g2s(S.factor, c, line, &S.q_full);
+          tc05::bulk_g2s(S.off, c + (size_t)A.cols * 4, line, &S.q_full);
+          if (kSum) tc05::bulk_g2s(S.ref[0], A.lse + (size_t)p.seg * A.cols, line, &S.q_full);
+        }
+        __syncwarp();
+        ++nq;
+        // lane: page of the tile, codes (0 .. 7) or pairs (8 .. 15); entries a tile ahead
+        auto request = [&](int tile) {
+          const int i = kKeys * tile + kPage * (lane & 7);
+          return tile < min(p.t1, p.I) && lane < 16 && i < p.n_int
+                     ? __ldcg(A.bt + (size_t)p.b * A.max_pages + (A.sink + i) / kPage) : -1;
+        };
+        int page = request(p.t0);
+        for (int tile = p.t0; tile < min(p.t1, p.I); ++tile, ++raws) {
+          const uint32_t r = raws % kRaw;
+          const int ahead = request(tile + 1);
+          if (raws >= kRaw && !wait(&S.raw_empty[r], raws / kRaw - 1)) break;
+          const bool in = page >= 0 && page < A.num_pages;
+          const uint32_t pairs = 16u * meta_stride(A.compact);
+          const uint32_t pages = __popc(__ballot_sync(0xffffffffu, in) & 0xffu);
+          if (lane == 0) tc05::bar_arrive_expect_tx(&S.raw_full[r], pages * (512u + pairs));
+          __syncwarp();
+          if (in) {
+            const uint8_t* src = A.pool + ((size_t)page * A.h_kv + p.h) * chunk_bytes(A.compact);
+            const bool codes = lane < 8;
+            tc05::bulk_g2s(S.raw[r][lane & 7] + (codes ? 0 : 512),
+                           src + (codes ? OPTR_K_CODES_OFFSET : OPTR_K_META_OFFSET), codes ? 512u : pairs,
+                           &S.raw_full[r]);
+          }
+          __syncwarp();
+          page = ahead;
+        }
+        if (dead) break;
+      }
+      // copies in flight land before the CTA exits
+      if (nq) tc05::bar_wait_drain(&S.q_full, (nq - 1) & 1);
+      for (uint32_t x = raws > kRaw ? raws - kRaw : 0; x < raws; ++x)
+        tc05::bar_wait_drain(&S.raw_full[x % kRaw], x / kRaw & 1);
+      __syncwarp();
+    } else if (warp == kMmaWarp) {
+      // ----------------------------------------------------------- products
+      const uint32_t sq = tc05::smem_addr(S.q[0]);
+      uint32_t nk = 0, nd[2] = {0, 0};
+      bool used = false;
+      ScorePiece p;
+      for (uint32_t n = 0; next_piece(n, p); ++n) {
+        const int N = p.N();
+        const bool pair = p.cols() > kKeys;
+        if (!wait(&S.q_full, n)) break;
+        used = true;
+        for (int t = 0; t < p.t1 - p.t0; ++t, ++nk) {
+          const uint32_t s = nk & 1, a = tmem + kColK + 128u * s;
+          const bool exact = p.t0 + t >= p.I;
+          if (!wait(&S.k_full[s], nk / 2)) break;
+          for (int d = 0; d < (pair ? 2 : 1); ++d) {
+            const int D = pair ? d : t & 1;
+            const uint32_t id = tc05::idesc_f16(128, pair && d ? N - kKeys : min(N, kKeys));
+            if (nd[D] > 0 && !wait(&S.d_empty[D], nd[D] - 1)) break;
+            ++nd[D];
+            const uint32_t out = tmem + kColD + 128u * D, b = sq + (uint32_t)d * (kKeys * 256);
+            constexpr uint32_t kPart = kBlockCols * 256;
+            if (exact) {
+              tc05::mma128_ts<16>(out, a, tc05::smem_desc(b + 2 * kPart, 128, 2048), id | tc05::kIdescBf16, 0);
+            } else {
+              // the small parts first: a third of the steps round at the sum's size
+              tc05::mma128_ts<16>(out, a, tc05::smem_desc(b + kPart, 128, 2048), id, 0);
+              tc05::mma128_ts<16>(out, a + 64, tc05::smem_desc(b, 128, 2048), id, 1);
+              tc05::mma128_ts<16>(out, a, tc05::smem_desc(b, 128, 2048), id, 1);
+            }
+            tc05::mma_commit_warp(&S.d_full[D][kSum ? t & 1 : D]);
+          }
+          if (dead) break;
+          tc05::mma_commit_warp(&S.k_empty[s]);
+        }
+        if (dead) break;
+        tc05::mma_commit_warp(&S.q_empty);
+      }
+      if (used) {  // the tensor core is done with tensor memory before it is freed
+        tc05::mma_commit_warp(&S.drained);
+        tc05::bar_wait_drain(&S.drained, 0);
+      }
+      __syncwarp();
+    } else if (warp == kPlanWarp) {
+      // ------------------------------------------------------------- pieces
+      ScoreFinder next;
+      next.start(A, w);
+      bool more = true;
+      for (uint32_t n = 0; more; ++n) {
+        const uint32_t i = n % kPieces;
+        ScorePiece p;
+        p.t0 = p.t1 = 0;
+        if (next.f < next.f1) next.next(A, p);
+        more = p.t1 > p.t0;
+        if (n >= kPieces && !wait(&S.piece_empty[i], n / kPieces - 1)) break;
+        if (lane == 0) {
+          S.piece[i] = p;
+          tc05::bar_arrive(&S.piece_full[i]);
+        }
+        __syncwarp();
+      }
+    }
+  }
+
+  tc05::fence_before();
+  __syncthreads();
+  if (S.abort && tid == 0) atomicOr(A.err, OPTR_DEVERR_TIMEOUT);
+  if (warp == kMmaWarp) {
+    tc05::fence_after();
+    tc05::tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// --------------------------------------------------------- normalisers
+
+// CTA: a segment.  The columns' maxima and sums of the CTAs that had a part in it;
+// minus the log2 of the whole sum, or -infinity for a column of none.
+__global__ void __launch_bounds__(1024) normaliser_kernel(const __grid_constant__ ScoreArgs A) {
+  __shared__ long long sum[32];
+  __shared__ float2 meet[4][kBlockCols];
+  const int seg = blockIdx.x, b = seg / A.h_kv, h = seg % A.h_kv, tid = threadIdx.x;
+  pdl_wait();
+  pdl_trigger();
+  long long before = 0, all = 0;
+  for (int i = tid; i < A.B; i += 1024) {
+    const int t = seq_tiles(score_seq(A, i));
+    all += t;
+    if (i < b) before += t;
+  }
+  auto total = [&](long long x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    __syncthreads();
+    if ((tid & 31) == 0) sum[tid >> 5] = x;
+    __syncthreads();
+    x = 0;
+    for (int i = 0; i < 32; ++i) x += sum[i];
+    return x;
+  };
+  before = total(before);
+  const long long F = total(all) * A.h_kv, W = min((long long)A.W, max(1ll, F));
+  const ScoreSeq s = score_seq(A, b);
+  const int T = seq_tiles(s), cols = 4 * s.rows;
+  if (T == 0) return;
+  const long long f0 = before * A.h_kv + (long long)h * T;
+  // the CTA of a tile f: the largest w with w F / W <= f
+  const int w0 = (int)(((f0 + 1) * W - 1) / F), w1 = (int)(((f0 + T) * W - 1) / F);
+  const int col = tid % kBlockCols, split = tid / kBlockCols;
+  const bool pair = cols > kKeys;
+  float m = -INFINITY, l = 0.f;
+  auto join = [&](float2 x) {
+    if (x.y == 0.f) return;
+    const float mn = fmaxf(m, x.x);
+    l = l * ex2(m - mn) + x.y * ex2(x.x - mn);
+    m = mn;
+  };
+  if (col < cols) {
+#pragma unroll 4
+    for (int w = w0 + split; w <= w1; w += 4) {
+      const float2* part = score_part(A, w, seg);
+      if (pair) {
+        join(__ldcg(part + col));
+      } else {
+        const float2 x = __ldcg(part + col), y = __ldcg(part + kKeys + col);
+        join(x);
+        join(y);
+      }
+    }
+  }
+  meet[split][col] = make_float2(m, l);
+  __syncthreads();
+  if (split != 0 || col >= (cols + 15) / 16 * 16) return;
+  for (int i = 1; i < 4; ++i) join(meet[i][col]);
+  A.lse[(size_t)seg * A.cols + col] = col < cols && l > 0.f ? -(m + log2f(l)) : -INFINITY;
+}
+
+// ---------------------------------------------------------------- host
+
+size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
+
+struct ScoreLayout {
+  size_t part, lse, total;
+  int cols, W;
+};
+
+ScoreLayout score_layout(const optr_params* p, int B, int max_new) {
+  ScoreLayout l;
+  l.cols = (4 * std::min(max_new, kTok) + 15) / 16 * 16;
+  l.W = p->num_sms;
+  const size_t segs = (size_t)B * p->cfg.h_kv;
+  l.part = round_up(segs * qop_bytes(l.cols, p->cfg.sink + p->cfg.recent > 0));
+  l.lse = l.part + round_up((segs + l.W) * 2 * kKeys * sizeof(float2));
+  l.total = l.lse + round_up(segs * l.cols * sizeof(float));
+  return l;
+}
+
+}  // namespace
+}  // namespace optr
+
+using namespace optr;
+
+extern "C" size_t optr_kv_score_workspace_size(const optr_params* p, int n_tok, int B, int max_new,
+                                               int max_pages) {
+  if (!p || n_tok < 0 || B <= 0 || max_new <= 0 || max_pages <= 0) return 0;
+  return score_layout(p, B, max_new).total;
+}
+
+extern "C" optr_status optr_kv_score_win(const optr_params* p, const void* q, int n_tok,
+                                         const int32_t* cu_new, const int32_t* pos0, int max_new,
+                                         const int32_t* block_table, int B, int max_pages,
+                                         const uint8_t* pool, int num_pages, const void* win,
+                                         const int32_t* win_slot, int n_slots, float* score, int n_score,
+                                         void* workspace, size_t ws_bytes, cudaStream_t stream) {
+  if (!p || n_tok < 0 || B <= 0 || max_pages <= 0 || num_pages <= 0 || max_new <= 0 || n_score <= 0)
+    return OPTR_ERR_INVALID_ARG;
+  if (n_tok == 0) return OPTR_OK;
+  if (!q || !cu_new || !pos0 || !block_table || !pool || !score || !aligned(q, 16) || !aligned(pool, 16) ||
+      !aligned(score, 4))
+    return OPTR_ERR_INVALID_ARG;
+  WinArgs w{nullptr, nullptr, 0};
+  if (p->cfg.sink + p->cfg.recent > 0) {
+    if (!win || !win_slot || n_slots <= 0 || !aligned(win, 16)) return OPTR_ERR_INVALID_ARG;
+    w = WinArgs{(__nv_bfloat16*)const_cast<void*>(win), win_slot, n_slots};
+  }
+  if ((long long)B * p->cfg.h_kv > 65535 || (long long)max_pages * kPage > 0x7fffffffll || n_tok > (1 << 24))
+    return OPTR_ERR_OUT_OF_RANGE;
+  const ScoreLayout l = score_layout(p, B, max_new);
+  if (!workspace || ws_bytes < l.total || !aligned(workspace, 256)) return OPTR_ERR_WORKSPACE;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  ScoreArgs A{static_cast<const __nv_bfloat16*>(q), n_tok, cu_new, pos0, max_new, 0, block_table, B, max_pages,
+              pool, num_pages, w, p->cfg.sink, p->cfg.recent, p->cfg.h_kv, p->cfg.group == 4 * kG, p->R_k, p->mu,
+              score, n_score, p->err, l.cols, ws, (float2*)(ws + l.part), (float*)(ws + l.lse), l.W};
+  for (auto fn : {logit_kernel<false>, logit_kernel<true>})
+    if (ensure_dynamic_smem(reinterpret_cast<const void*>(fn), sizeof(Smem)) != cudaSuccess) return OPTR_ERR_CUDA;
+  const unsigned segs = (unsigned)B * p->cfg.h_kv;
+  // a block of tokens a time, in stream order: the sums do not depend on chance
+  cudaError_t e = cudaSuccess;
+  for (A.t0 = 0; A.t0 < max_new && e == cudaSuccess; A.t0 += kTok) {
+    e = launch_pdl(query_kernel, dim3((l.cols + kRotCols - 1) / kRotCols, segs), dim3(kRotThreads), 0, stream, A);
+    if (e == cudaSuccess) e = launch_pdl(logit_kernel<false>, dim3(l.W), dim3(kThreads), sizeof(Smem), stream, A);
+    if (e == cudaSuccess) e = launch_pdl(normaliser_kernel, dim3(segs), dim3(1024), 0, stream, A);
+    if (e == cudaSuccess) e = launch_pdl(logit_kernel<true>, dim3(l.W), dim3(kThreads), sizeof(Smem), stream, A);
+  }
+  return cuda_status(e);
+}
+
+extern "C" optr_status optr_kv_score(const optr_params* p, const void* q, int n_tok, const int32_t* cu_new,
+                                     const int32_t* pos0, int max_new, const int32_t* block_table, int B,
+                                     int max_pages, const uint8_t* pool, int num_pages, float* score,
+                                     int n_score, void* workspace, size_t ws_bytes, cudaStream_t stream) {
+  if (p && (p->cfg.sink > 0 || p->cfg.recent > 0)) return OPTR_ERR_INVALID_ARG;
+  return optr_kv_score_win(p, q, n_tok, cu_new, pos0, max_new, block_table, B, max_pages, pool, num_pages,
+                           nullptr, nullptr, 0, score, n_score, workspace, ws_bytes, stream);
+}

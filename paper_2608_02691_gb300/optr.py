@@ -112,6 +112,10 @@ _SIG = {
     "optr_kv_read": (_I, [_V, _I, _V, _V, _V, _I, _I, _V, _I, _V, _V, _V]),
     "optr_verify_drafts": (_I, [_V, _V, _V, _I, _V, _V, _V, _V, _I, _I, _I, _V, _V, _V]),
     "optr_verify_tree": (_I, [_V, _V, _V, _I, _V, _V, _V, _V, _V, _I, _I, _I, _V, _V, _V, _V]),
+    "optr_kv_score_workspace_size": (ctypes.c_size_t, [_V, _I, _I, _I, _I]),
+    "optr_kv_score": (_I, [_V, _V, _I, _V, _V, _I, _V, _I, _I, _V, _I, _V, _I, _V, ctypes.c_size_t, _V]),
+    "optr_kv_score_win": (_I, [_V, _V, _I, _V, _V, _I, _V, _I, _I, _V, _I, _V, _V, _I, _V, _I, _V,
+                               ctypes.c_size_t, _V]),
     "optr_evict_select": (_I, [_V, _V, _I, _V, _V, _I, _I, _I, _V, _I, _V, _V]),
     "optr_kv_compact": (_I, [_V, _V, _I, _V, _V, _V, _I, _I, _V, _I, _V, _I, _V]),
     "optr_kv_compact_win": (_I, [_V, _V, _I, _V, _V, _V, _I, _I, _V, _I, _V, _V, _I, _V, _I, _V]),
@@ -583,6 +587,49 @@ def _score_rows(p, score, B):
     if score.dim() != 3 or tuple(score.shape[:2]) != (B, p.h_kv):
         raise ValueError("score must be [B][h_kv][positions]")
     return _dev(score, torch.float32, "score"), score.shape[2]
+
+
+def optr_kv_score_workspace_size(p: Params, n_tok: int, B: int, max_new: int, max_pages: int) -> int:
+    return int(lib().optr_kv_score_workspace_size(p.handle, n_tok, B, max_new, max_pages))
+
+
+def new_score_workspace(p: Params, n_tok: int, B: int, max_new: int, max_pages: int, device="cuda"):
+    n = optr_kv_score_workspace_size(p, n_tok, B, max_new, max_pages)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _score_args(p, q, cu_new, pos0, max_new, block_table, pool):
+    i32 = torch.int32
+    B, max_pages = block_table.shape
+    if tuple(q.shape) != (q.shape[0], p.h_q, HEAD_DIM) or cu_new.numel() != B + 1 or pos0.numel() != B:
+        raise ValueError("q must be [n_tok][h_q][128], cu_new [B+1], pos0 [B]")
+    return (_cuda(q, torch.bfloat16, "q"), q.shape[0], _dev(cu_new, i32, "cu_new"), _dev(pos0, i32, "pos0"),
+            max_new, _dev(block_table, i32, "block_table"), B, max_pages, _dev(pool, torch.uint8, "pool"),
+            pool.shape[0])
+
+
+def optr_kv_score(p: Params, q, cu_new, pos0, max_new: int, block_table, pool, score, workspace,
+                  stream=None) -> None:
+    """Add the attention weights of each sequence's new tokens (q bf16 [n_tok][h_q][128], at positions
+    pos0[b] on of the cache, which holds them already) to score float32 [B][h_kv][positions], summed over
+    tokens and a KV head's query heads."""
+    args = _score_args(p, q, cu_new, pos0, max_new, block_table, pool)
+    st = lib().optr_kv_score(p.handle, *args, *_score_rows(p, score, pos0.numel()),
+                             _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
+    if st:
+        raise OptrError(st, "optr_kv_score")
+
+
+def optr_kv_score_win(p: Params, q, cu_new, pos0, max_new: int, block_table, pool, win, win_slot, score,
+                      workspace, stream=None) -> None:
+    """optr_kv_score with the cache's BF16 windows read from win."""
+    args = _score_args(p, q, cu_new, pos0, max_new, block_table, pool)
+    st = lib().optr_kv_score_win(p.handle, *args, *_win_args(p, win, win_slot),
+                                 *_score_rows(p, score, pos0.numel()),
+                                 _dev(workspace, torch.uint8, "workspace"), workspace.numel(),
+                                 _stream(stream))
+    if st:
+        raise OptrError(st, "optr_kv_score_win")
 
 
 def optr_evict_select(p: Params, score, lens, keep, first: int, last: int, kept, n_kept,

@@ -5,7 +5,8 @@ import re
 
 import pytest
 
-NAMES = ("optr_tree_attention", "optr_tree_attention_win", "optr_verify_tree", "optr_evict_select",
+NAMES = ("optr_tree_attention", "optr_tree_attention_win", "optr_verify_tree", "optr_kv_score",
+         "optr_kv_score_win", "optr_evict_select",
          "optr_kv_compact", "optr_kv_compact_win")
 
 
