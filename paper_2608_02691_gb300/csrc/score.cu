@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
       for (int t = 0; t < tiles; ++t) {
         if ((kSum || !pair) && (t & 1) != g) continue;
         const int tile = p.t0 + t;
-        const bool exact = tile >= p.I;  // a window tile
+        const bool exact = tile >= p.I();  // a window tile
         float scale = 0.f, sum = 0.f, old = 0.f;
         int first = 0;                   // the first column that sees the key
         float* at = nullptr;
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           if (!begun) {
             begun = true;
             scale = S.scale[(nk + t) % 4][key];
-            const int i = kKeys * (exact ? tile - p.I : tile) + key;
+            const int i = kKeys * (exact ? tile - p.I() : tile) + key;
             const int pos = exact ? win_pos(i, p.n, A.sink, A.recent) : A.sink + i;
             if (scale != 0.f) {
               const int tok = pos - p.pos0 - A.t0;
@@ -431,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
       for (int tile = p.t0; tile < p.t1; ++tile, ++nk) {
         const uint32_t s = nk & 1, tK = tmem + lanes + kColK + 128u * s;
         float scale = 0.f;
-        if (tile < p.I) {
+        if (tile < p.I()) {
           const int i = kKeys * tile + key;
           bool ok = i < p.n_int;
           if (ok) {
@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           }
           arrive(&S.raw_empty[r]);
         } else {
-          const int i = kKeys * (tile - p.I) + key;
+          const int i = kKeys * (tile - p.I()) + key;
           if (nk >= 2 && !wait(&S.k_empty[s], nk / 2 - 1)) break;
           const uint4* src = nullptr;
           if (i < p.n_win) {
@@ -553,11 +553,11 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         // lane: page of the tile, codes (0 .. 7) or pairs (8 .. 15); entries a tile ahead
         auto request = [&](int tile) {
           const int i = kKeys * tile + kPage * (lane & 7);
-          return tile < min(p.t1, p.I) && lane < 16 && i < p.n_int
+          return tile < min(p.t1, p.I()) && lane < 16 && i < p.n_int
                      ? __ldcg(A.bt + (size_t)p.b * A.max_pages + (A.sink + i) / kPage) : -1;
         };
         int page = request(p.t0);
-        for (int tile = p.t0; tile < min(p.t1, p.I); ++tile, ++raws) {
+        for (int tile = p.t0; tile < min(p.t1, p.I()); ++tile, ++raws) {
           const uint32_t r = raws % kRaw;
           const int ahead = request(tile + 1);
           if (raws >= kRaw && !wait(&S.raw_empty[r], raws / kRaw - 1)) break;
@@ -596,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         used = true;
         for (int t = 0; t < p.t1 - p.t0; ++t, ++nk) {
           const uint32_t s = nk & 1, a = tmem + kColK + 128u * s;
-          const bool exact = p.t0 + t >= p.I;
+          const bool exact = p.t0 + t >= p.I();
           if (!wait(&S.k_full[s], nk / 2)) break;
           for (int d = 0; d < (pair ? 2 : 1); ++d) {
             const int D = pair ? d : t & 1;
@@ -628,8 +628,8 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
       __syncwarp();
     } else if (warp == kPlanWarp) {
       // ------------------------------------------------------------- pieces
-      ScoreFinder next;
-      next.start(A, w);
+      ScoreFinder<Tiles> next;
+      next.start(A, w, A.W);
       bool more = true;
       for (uint32_t n = 0; more; ++n) {
         const uint32_t i = n % kPieces;
@@ -666,30 +666,10 @@ __global__ void __launch_bounds__(1024) normaliser_kernel(const __grid_constant_
   const int seg = blockIdx.x, b = seg / A.h_kv, h = seg % A.h_kv, tid = threadIdx.x;
   pdl_wait();
   pdl_trigger();
-  long long before = 0, all = 0;
-  for (int i = tid; i < A.B; i += 1024) {
-    const int t = seq_tiles(score_seq(A, i));
-    all += t;
-    if (i < b) before += t;
-  }
-  auto total = [&](long long x) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    __syncthreads();
-    if ((tid & 31) == 0) sum[tid >> 5] = x;
-    __syncthreads();
-    x = 0;
-    for (int i = 0; i < 32; ++i) x += sum[i];
-    return x;
-  };
-  before = total(before);
-  const long long F = total(all) * A.h_kv, W = min((long long)A.W, max(1ll, F));
-  const ScoreSeq s = score_seq(A, b);
-  const int T = seq_tiles(s), cols = 4 * s.rows;
-  if (T == 0) return;
-  const long long f0 = before * A.h_kv + (long long)h * T;
-  // the CTA of a tile f: the largest w with w F / W <= f
-  const int w0 = (int)(((f0 + 1) * W - 1) / F), w1 = (int)(((f0 + T) * W - 1) / F);
+  int w0, w1;
+  workers_of<Tiles>(A, b, h, A.W, sum, w0, w1);
+  if (w1 < w0) return;
+  const int cols = 4 * score_seq(A, b).rows;
   const int col = tid % kBlockCols, split = tid / kBlockCols;
   const bool pair = cols > kKeys;
   float m = -INFINITY, l = 0.f;
@@ -747,7 +727,8 @@ using namespace optr;
 extern "C" size_t optr_kv_score_workspace_size(const optr_params* p, int n_tok, int B, int max_new,
                                                int max_pages) {
   if (!p || n_tok < 0 || B <= 0 || max_new <= 0 || max_pages <= 0) return 0;
-  return score_layout(p, B, max_new).total;
+  const size_t n = score_layout(p, B, max_new).total;
+  return few_tokens(p, B, max_new, max_pages) ? std::max(n, few_layout(p, B, max_new, max_pages).total) : n;
 }
 
 extern "C" optr_status optr_kv_score_win(const optr_params* p, const void* q, int n_tok,
@@ -770,11 +751,12 @@ extern "C" optr_status optr_kv_score_win(const optr_params* p, const void* q, in
   if ((long long)B * p->cfg.h_kv > 65535 || (long long)max_pages * kPage > 0x7fffffffll || n_tok > (1 << 24))
     return OPTR_ERR_OUT_OF_RANGE;
   const ScoreLayout l = score_layout(p, B, max_new);
-  if (!workspace || ws_bytes < l.total || !aligned(workspace, 256)) return OPTR_ERR_WORKSPACE;
+  if (!workspace || ws_bytes < optr_kv_score_workspace_size(p, n_tok, B, max_new, max_pages) || !aligned(workspace, 256)) return OPTR_ERR_WORKSPACE;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   ScoreArgs A{static_cast<const __nv_bfloat16*>(q), n_tok, cu_new, pos0, max_new, 0, block_table, B, max_pages,
               pool, num_pages, w, p->cfg.sink, p->cfg.recent, p->cfg.h_kv, p->cfg.group == 4 * kG, p->R_k, p->mu,
               score, n_score, p->err, l.cols, ws, (float2*)(ws + l.part), (float*)(ws + l.lse), l.W};
+  if (few_tokens(p, B, max_new, max_pages)) return cuda_status(launch_score_few(p, A, ws, stream));
   for (auto fn : {logit_kernel<false>, logit_kernel<true>})
     if (ensure_dynamic_smem(reinterpret_cast<const void*>(fn), sizeof(Smem)) != cudaSuccess) return OPTR_ERR_CUDA;
   const unsigned segs = (unsigned)B * p->cfg.h_kv;

@@ -35,6 +35,16 @@ struct ScoreArgs {
   int W;                 // CTAs
 };
 
+// A decode step's few tokens (score_few.cu): its part of the workspace, and the launches.
+constexpr int kFewTok = 4;
+struct FewLayout {
+  size_t part, logits, total;
+  int W;  // warps
+};
+FewLayout few_layout(const optr_params* p, int B, int max_new, int max_pages);
+bool few_tokens(const optr_params* p, int B, int max_new, int max_pages);
+cudaError_t launch_score_few(const optr_params* p, const ScoreArgs& A, uint8_t* ws, cudaStream_t s);
+
 // What one sequence asks for of the query block.
 struct ScoreSeq {
   int c0, pos0, n;       // row of its first token, cached tokens before, and with them
@@ -88,24 +98,30 @@ __device__ __forceinline__ void report_sequences(const ScoreArgs& A) {
   }
 }
 
-// Tiles t0 .. t1-1 of a (sequence, KV head), INT2 tiles first, then the windows'.
+// Units t0 .. t1-1 of a (sequence, KV head), INT2 ones first, then the windows'.
 struct ScorePiece {
   int seg, b, h;
   int c0, pos0, n, rows, n_int, n_win, slot;
-  int I;                 // INT2 tiles
   int t0, t1;
+  __device__ __forceinline__ int I() const { return key_tiles(n_int); }  // INT2 tiles
   __device__ __forceinline__ int cols() const { return 4 * rows; }
   // columns of the products, a multiple of 16
   __device__ __forceinline__ int N() const { return (4 * rows + 15) / 16 * 16; }
 };
 
-// The flat index space orders tiles as (sequence, KV head, tile); CTA w takes
-// [w F / W, (w + 1) F / W).  One warp goes through a CTA's range: lane i holds sequence
+// Units of a (sequence, KV head): tiles of 128 keys.
+struct Tiles {
+  __device__ __forceinline__ static int of(const ScoreSeq& s) { return seq_tiles(s); }
+};
+
+// The flat index space orders units as (sequence, KV head, unit); worker w of W takes
+// [w F / W, (w + 1) F / W).  One warp goes through a range: lane i holds sequence
 // b0 + i.
+template <typename Unit>
 struct ScoreFinder {
   long long f, f1, F;
   int b0;
-  long long base, incl;  // tiles of one head before the 32 held; up to and with the lane's
+  long long base, incl;  // units of one head before the 32 held; up to and with the lane's
   ScoreSeq s;
 
   __device__ __forceinline__ void hold(const ScoreArgs& A, int first) {
@@ -113,7 +129,7 @@ struct ScoreFinder {
     b0 = first;
     s.rows = s.n_int = s.n_win = 0;
     if (b0 + lane < A.B) s = score_seq(A, b0 + lane);
-    incl = seq_tiles(s);
+    incl = Unit::of(s);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const long long y = __shfl_up_sync(0xffffffffu, incl, o);
@@ -121,14 +137,14 @@ struct ScoreFinder {
     }
   }
 
-  __device__ __forceinline__ void start(const ScoreArgs& A, int w) {
+  __device__ __forceinline__ void start(const ScoreArgs& A, int w, int workers) {
     const int lane = threadIdx.x & 31;
     long long sum = 0;
-    for (int b = lane; b < A.B; b += 32) sum += seq_tiles(score_seq(A, b));
+    for (int b = lane; b < A.B; b += 32) sum += Unit::of(score_seq(A, b));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     F = sum * A.h_kv;
-    const long long W = min((long long)A.W, max(1ll, F));  // each has a tile
+    const long long W = min((long long)workers, max(1ll, F));  // each has a unit
     f = w < W ? F * w / W : F;
     f1 = w < W ? F * (w + 1) / W : F;
     base = 0;
@@ -149,12 +165,11 @@ struct ScoreFinder {
     }
     const int l = __ffs(over) - 1;
     auto of = [&](int x) { return __shfl_sync(0xffffffffu, x, l); };
-    const int T = of(seq_tiles(s));
+    const int T = of(Unit::of(s));
     const long long before = base + __shfl_sync(0xffffffffu, incl, l) - T;
     p.b = b0 + l;
     p.c0 = of(s.c0), p.pos0 = of(s.pos0), p.n = of(s.n), p.rows = of(s.rows);
     p.n_int = of(s.n_int), p.n_win = of(s.n_win), p.slot = of(s.slot);
-    p.I = key_tiles(p.n_int);
     const long long r = f - before * A.h_kv;
     p.h = (int)(r / T);
     p.seg = p.b * A.h_kv + p.h;
@@ -163,6 +178,38 @@ struct ScoreFinder {
     f += p.t1 - p.t0;
   }
 };
+
+// What comes before a (sequence, KV head) in the flat order: the workers that have a part
+// in it, w0 .. w1 (none: w1 < w0).  A whole CTA; `sum` has an element a warp.
+template <typename Unit>
+__device__ __forceinline__ void workers_of(const ScoreArgs& A, int b, int h, int workers, long long* sum,
+                                           int& w0, int& w1) {
+  const int threads = blockDim.x, tid = threadIdx.x;
+  long long x[2] = {0, 0};  // units of one head: before b, in all
+  for (int i = tid; i < A.B; i += threads) {
+    const int t = Unit::of(score_seq(A, i));
+    x[1] += t;
+    if (i < b) x[0] += t;
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x[e] += __shfl_xor_sync(0xffffffffu, x[e], o);
+    __syncthreads();
+    if ((tid & 31) == 0) sum[tid >> 5] = x[e];
+    __syncthreads();
+    x[e] = 0;
+    for (int i = 0; i < threads / 32; ++i) x[e] += sum[i];
+  }
+  const long long F = x[1] * A.h_kv, W = min((long long)workers, max(1ll, F));
+  const int T = Unit::of(score_seq(A, b));
+  w0 = 0, w1 = -1;
+  if (T == 0) return;
+  const long long f0 = x[0] * A.h_kv + (long long)h * T;
+  // the worker of a unit f: the largest w with w F / W <= f
+  w0 = (int)(((f0 + 1) * W - 1) / F);
+  w1 = (int)(((f0 + T) * W - 1) / F);
+}
 
 // Operands of a (sequence, KV head)'s query block: hi and lo parts of the rotated
 // queries, the queries as given (with windows), 256 B a column each, then by column the

@@ -1,0 +1,465 @@
+// Attention weights of a decode step's few tokens, summed by position ("optr_kv_score").
+//
+// With one to kFewTok tokens a (sequence, KV head) the keys are read once: their logits, 16
+// bytes a token and position, are kept in the workspace for the second pass.  Three
+// launches: few_query_kernel rotates the queries (as the decode does), few_logit_kernel
+// goes over the keys, a page a step and warp, and few_sum_kernel joins the warps' maxima
+// and sums and adds the weights up.
+//
+// A page's logits are the decode's (decode_tc.cu): m16n8k16 products of the codes, as the
+// fp16 numbers 1024 + code 2^pos that their bits make, with the four query heads in fp16
+// hi and lo parts (eight columns), one accumulator a scale.  Window keys are bf16 as they
+// are, 16 rows a step, which counts as four pages.  All steps of all (sequence, KV head)s
+// stand in one line that is cut into equal ranges, one a warp.
+#include <type_traits>
+
+#include "qrot.cuh"
+#include "score.cuh"
+
+#include <algorithm>
+
+namespace optr {
+namespace {
+
+constexpr int kWarps = 16;
+constexpr int kStages = 6;         // pages on the way to a warp, in pairs
+constexpr int kHalfRec = 768;      // a page's key codes and pairs
+constexpr int kWinCost = 4;
+constexpr int kWinRows = 16;
+// words of a token's query: fragments, offsets, inverse prescales, sums, <q, mu>
+constexpr int kFrag = 0, kOff = 512, kInv = 544, kSum = 548, kMu = 564, kQueryWords = 576;
+
+struct Steps {
+  __device__ __forceinline__ static int pages(int n_int) { return (n_int + kPage - 1) / kPage; }
+  __device__ __forceinline__ static int of(const ScoreSeq& s) {
+    return pages(s.n_int) + kWinCost * ((s.n_win + kWinRows - 1) / kWinRows);
+  }
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Workspace: queries [segments][max_new][kQueryWords], partials [W + segments][16]
+// {maximum, sum}, logits [segments][positions][max_new][4].
+struct FewArgs {
+  ScoreArgs A;
+  uint32_t* query;
+  float2* part;
+  float4* logits;
+  int positions, W;
+  float qscale;
+};
+__device__ __forceinline__ uint32_t* few_query(const FewArgs& F, int seg, int i) {
+  return F.query + ((size_t)seg * F.A.max_new + i) * kQueryWords;
+}
+
+__global__ void __launch_bounds__(kQrotThreads) few_query_kernel(const __grid_constant__ FewArgs F) {
+  __shared__ QrotSmem sm;
+  const ScoreArgs& A = F.A;
+  const int seg = blockIdx.x, b = seg / A.h_kv, h = seg % A.h_kv, tid = threadIdx.x;
+  float rv[32];
+  load_rotation_slice(A.R_k, h, rv);
+  pdl_wait();
+  pdl_trigger();
+  if (seg == 0 && tid < 32) report_sequences(A);
+  const ScoreSeq s = score_seq(A, b);
+  if (Steps::of(s) == 0) return;
+  for (int i = 0; i < s.rows; ++i) {
+    const __nv_bfloat16* q = A.q + (((size_t)s.c0 + i) * A.h_kv + h) * (4 * kD);
+    uint32_t* out = few_query(F, seg, i);
+    rotate_query(sm, q, rv, F.qscale, nullptr, reinterpret_cast<float*>(out + kSum), out + kFrag,
+                 reinterpret_cast<float*>(out + kOff), reinterpret_cast<float*>(out + kInv));
+    if (A.win.win && tid < 128) {  // head tid / 32
+      float d = 0.f;
+      for (int k = tid & 31; k < kD; k += 32)
+        d = fmaf(__bfloat162float(q[(tid >> 5) * kD + k]), __ldg(A.mu + (size_t)h * kD + k), d);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+      if ((tid & 31) == 0) reinterpret_cast<float*>(out + kMu)[tid >> 5] = d * F.qscale;
+    }
+    __syncthreads();
+  }
+}
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                        uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};\n"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                         uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};\n"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <int pos>
+__device__ __forceinline__ uint32_t field(uint32_t x) {  // 1024 + code 2^pos of either half
+  uint32_t y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(x), "n"(0x00030003u << pos), "r"(0x64006400u));
+  return y;
+}
+// The codes of a word whose halves hold a byte of group 2 j (low) and 2 j + 1 (high), as A
+// registers by group parity (code_pos says where each stands).
+__device__ __forceinline__ void fields(uint32_t y, uint32_t (&out)[2][4]) {
+  const uint32_t l = y << 4, r = y >> 6;
+  out[0][0] = field<code_pos(0, 0)>(l);
+  out[0][1] = field<code_pos(0, 1)>(l);
+  out[0][2] = field<code_pos(0, 2)>(y);
+  out[0][3] = field<code_pos(0, 3)>(y);
+  out[1][0] = field<code_pos(1, 0)>(y);
+  out[1][1] = field<code_pos(1, 1)>(r);
+  out[1][2] = field<code_pos(1, 2)>(r);
+  out[1][3] = field<code_pos(1, 3)>(r);
+}
+
+__device__ __forceinline__ float low_half(uint32_t x) {
+  return __low2float(*reinterpret_cast<const __half2*>(&x));
+}
+
+// A token's query as a lane has it: B fragments of its column, what the products start
+// from, the min terms' B fragment, and the inverse prescale of head lane % 4.
+template <bool kCompact>
+struct Query {
+  uint4 frag[kGroups];
+  float start[kGroups][2];
+  uint32_t min;
+  float inv;
+
+  __device__ __forceinline__ void load(const uint32_t* w) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+#pragma unroll
+    for (int G = 0; G < kGroups; ++G)
+      frag[G] = __ldcg(reinterpret_cast<const uint4*>(w + kFrag + lane * 16) + G);
+    const float4* o = reinterpret_cast<const float4*>(w + kOff + c * 8);
+    const float4 a = __ldcg(o), b = __ldcg(o + 1);
+    start[0][0] = -a.x, start[0][1] = -a.y, start[1][0] = -a.z, start[1][1] = -a.w;
+    start[2][0] = -b.x, start[2][1] = -b.y, start[3][0] = -b.z, start[3][1] = -b.w;
+    // column g of the min terms' product: head g / 2, hi or lo part of group c's sum
+    const float s = __uint_as_float(__ldcg(w + kSum + (g >> 1) * kGroups + c));
+    const float hi = __uint_as_float(__float_as_uint(s) & 0xffffe000u);
+    const uint32_t part = __half_as_ushort(__float2half_rn(g & 1 ? s - hi : hi));
+    min = part << 16;
+    inv = __uint_as_float(__ldcg(w + kInv + c));
+  }
+};
+
+// A page's codes and pairs as a lane has them: tokens g and g + 8.
+template <bool kCompact>
+struct Page {
+  uint32_t f[2][2][2][4];  // [row][groups 2 j ..][parity][code]
+  uint32_t w0, w1;         // the min terms' A registers
+  uint4 m0, m1;            // four groups' pairs (the compact record: w0, w1 are the ones)
+
+  __device__ __forceinline__ void load(const uint8_t* st) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const uint2 k0 = *reinterpret_cast<const uint2*>(st + g * 32 + 8 * c);
+    const uint2 k1 = *reinterpret_cast<const uint2*>(st + (g + 8) * 32 + 8 * c);
+    fields(__byte_perm(k0.x, k0.y, 0x5410), f[0][0]);
+    fields(__byte_perm(k0.x, k0.y, 0x7632), f[0][1]);
+    fields(__byte_perm(k1.x, k1.y, 0x5410), f[1][0]);
+    fields(__byte_perm(k1.x, k1.y, 0x7632), f[1][1]);
+    constexpr int ms = meta_stride(kCompact);
+    w0 = *reinterpret_cast<const uint32_t*>(st + 512 + g * ms + (kCompact ? 0 : 4 * c));
+    w1 = *reinterpret_cast<const uint32_t*>(st + 512 + (g + 8) * ms + (kCompact ? 0 : 4 * c));
+    if constexpr (!kCompact) {
+      m0 = *reinterpret_cast<const uint4*>(st + 512 + g * ms);
+      m1 = *reinterpret_cast<const uint4*>(st + 512 + (g + 8) * ms);
+    }
+  }
+
+  // logits of tokens g, g + 8, head c
+  __device__ __forceinline__ float2 logits(const Query<kCompact>& q) const {
+    // an accumulator a group, the compact record's too: in one for all, which starts from
+    // four offsets, a logit is off ten times as far
+    float s[kGroups][4];
+#pragma unroll
+    for (int G = 0; G < kGroups; ++G) {
+      s[G][0] = s[G][2] = q.start[G][0];
+      s[G][1] = s[G][3] = q.start[G][1];
+      const uint32_t (&a)[4] = f[0][G >> 1][G & 1];
+      const uint32_t (&b)[4] = f[1][G >> 1][G & 1];
+      mma_f16(s[G], a[0], b[0], a[1], b[1], q.frag[G].x, q.frag[G].y);
+      mma_f16(s[G], a[2], b[2], a[3], b[3], q.frag[G].z, q.frag[G].w);
+    }
+    float u[4] = {0.f, 0.f, 0.f, 0.f}, t0, t1;
+    mma_f16(u, w0, w1, 0u, 0u, q.min, 0u);
+    if constexpr (kCompact) {
+      t0 = t1 = 0.f;
+#pragma unroll
+      for (int G = 0; G < kGroups; ++G) {
+        t0 += s[G][0] + s[G][1];
+        t1 += s[G][2] + s[G][3];
+      }
+      t0 *= low_half(w0);
+      t1 *= low_half(w1);
+    } else {
+      const uint32_t x[4] = {m0.x, m0.y, m0.z, m0.w}, y[4] = {m1.x, m1.y, m1.z, m1.w};
+      t0 = t1 = 0.f;
+#pragma unroll
+      for (int G = 0; G < kGroups; ++G) {
+        t0 = fmaf(low_half(x[G]), s[G][0] + s[G][1], t0);
+        t1 = fmaf(low_half(y[G]), s[G][2] + s[G][3], t1);
+      }
+    }
+    return make_float2(fmaf(q.inv, t0, u[0] + u[1]), fmaf(q.inv, t1, u[2] + u[3]));
+  }
+};
+
+template <bool kCompact, int kTokens>
+__global__ void __launch_bounds__(kWarps * 32, 1) few_logit_kernel(const __grid_constant__ FewArgs F) {
+  extern __shared__ __align__(16) unsigned char dsm_[];
+  const ScoreArgs& A = F.A;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  uint8_t* stage = dsm_ + (size_t)warp * kStages * kHalfRec;
+  const int w = warp * gridDim.x + blockIdx.x;  // neighbours' ranges on different SMs
+  pdl_wait();
+  pdl_trigger();
+  ScoreFinder<Steps> next;
+  next.start(A, w, F.W);
+  while (next.f < next.f1) {
+    ScorePiece p;
+    next.next(A, p);
+    if (p.t1 <= p.t0) break;
+    const int pages = Steps::pages(p.n_int), last = min(p.t1, pages);
+    const int32_t* table = A.bt + (size_t)p.b * A.max_pages + A.sink / kPage;
+    // lane: the physical page of base + lane
+    int base = p.t0, phys = -1;
+    auto resolve = [&](int from) {
+      base = from;
+      phys = -1;
+      if (from + lane < last) {
+        phys = __ldcg(table + from + lane);
+        if (phys < 0 || phys >= A.num_pages) {
+          phys = -1;
+          atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
+        }
+      }
+    };
+    resolve(p.t0);
+    uint32_t bad = 0;  // stages of pages that are not to be read
+    auto issue = [&](int page, int s) {
+      if (page < last) {
+        if (page - base == 32) resolve(page);
+        const int x = __shfl_sync(0xffffffffu, phys, page - base);
+        bad = x < 0 ? bad | 1u << s : bad & ~(1u << s);
+        const uint8_t* src = A.pool + ((size_t)max(x, 0) * A.h_kv + p.h) * chunk_bytes(kCompact) + 16 * lane;
+        uint8_t* dst = stage + s * kHalfRec + 16 * lane;
+        cp_async16_zfill(dst, src + OPTR_K_CODES_OFFSET, x >= 0);
+        if (lane < meta_stride(kCompact)) cp_async16_zfill(dst + 512, src + OPTR_K_META_OFFSET, x >= 0);
+      }
+    };
+    Query<kCompact> q;
+    if (kTokens == 1 && p.t0 < pages) q.load(few_query(F, p.seg, 0));
+    float m[kTokens], l[kTokens];
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i) m[i] = -1e30f, l[i] = 0.f;
+    float* out = reinterpret_cast<float*>(F.logits) + (size_t)p.seg * F.positions * A.max_new * 4 + c;
+    // two logits of token i, at positions that count if they are seen
+    auto take = [&](int i, int pos0, int pos1, bool in0, bool in1, float x0, float x1) {
+      const int seen = p.pos0 + i;
+      x0 = in0 && pos0 <= seen ? x0 : -INFINITY;
+      x1 = in1 && pos1 <= seen ? x1 : -INFINITY;
+      if (in0) out[((size_t)pos0 * A.max_new + i) * 4] = x0;
+      if (in1) out[((size_t)pos1 * A.max_new + i) * 4] = x1;
+      const float mn = fmaxf(m[i], fmaxf(x0, x1));
+      l[i] = fmaf(l[i], ex2(m[i] - mn), ex2(x0 - mn) + ex2(x1 - mn));
+      m[i] = mn;
+    };
+    constexpr int kPairs = kStages / 2;
+#pragma unroll
+    for (int s = 0; s < kPairs - 1; ++s) {
+      issue(p.t0 + 2 * s, 2 * s);
+      issue(p.t0 + 2 * s + 1, 2 * s + 1);
+      cp_async_commit();
+    }
+    int at = 0;  // the pair's stages
+#pragma unroll 1
+    for (int page = p.t0; page < last; page += 2) {
+      const int to = at == 0 ? kPairs - 1 : at - 1;
+      issue(page + 2 * (kPairs - 1), 2 * to);
+      issue(page + 2 * (kPairs - 1) + 1, 2 * to + 1);
+      cp_async_commit();
+      cp_async_wait<kPairs - 1>();
+      __syncwarp();
+      Page<kCompact> x[2];
+      const int pairs = page + 1 < last ? 2 : 1;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) x[e].load(stage + (2 * at + e) * kHalfRec);
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < kTokens; ++i) {
+        if (i >= p.rows) break;
+        if (kTokens > 1) q.load(few_query(F, p.seg, i));
+        float2 y[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) y[e] = x[e].logits(q);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int k = kPage * (page + e) + g;  // of the INT2 keys
+          const bool ok = !(bad >> (2 * at + e) & 1);
+          const bool in0 = e < pairs && k < p.n_int, in1 = e < pairs && k + 8 < p.n_int;
+          take(i, A.sink + k, A.sink + k + 8, in0, in1, ok ? y[e].x : -INFINITY, ok ? y[e].y : -INFINITY);
+        }
+      }
+      at = at + 1 == kPairs ? 0 : at + 1;
+    }
+    cp_async_wait<0>();
+    // window rows, 16 a step: the warp that has a step's first unit
+    const int first = max(0, p.t0 - pages);
+    for (int u = (first + kWinCost - 1) / kWinCost; pages + kWinCost * u < p.t1; ++u) {
+      const int i0 = kWinRows * u + g, i1 = i0 + 8;
+      const bool in0 = i0 < p.n_win, in1 = i1 < p.n_win;
+      const int pos0 = win_pos(in0 ? i0 : 0, p.n, A.sink, A.recent), pos1 = win_pos(in1 ? i1 : 0, p.n, A.sink, A.recent);
+      const __nv_bfloat16* rows = A.win.win + (((size_t)p.slot * A.h_kv + p.h) * 2) * (A.sink + A.recent) * kD + 8 * c;
+      const __nv_bfloat16 *r0 = rows + (size_t)win_row(pos0, A.sink, A.recent) * kD,
+                          *r1 = rows + (size_t)win_row(pos1, A.sink, A.recent) * kD;
+      uint4 a[4], b[4];
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        a[s] = __ldcg(reinterpret_cast<const uint4*>(r0 + 32 * s));
+        b[s] = __ldcg(reinterpret_cast<const uint4*>(r1 + 32 * s));
+      }
+      for (int i = 0; i < p.rows; ++i) {
+        // (a sum of its own for each step, since a product rounds at its largest term: the
+        // key mean may make one channel's far larger than the logit)
+        float d0 = 0.f, d1 = 0.f;
+        // column g: head g / 2 of the even ones, nothing of the odd ones; the places of
+        // the inner dimension are permuted alike in both operands
+        const __nv_bfloat16* qr = A.q + ((((size_t)p.c0 + i) * A.h_kv + p.h) * 4 + (g >> 1)) * kD + 8 * c;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          uint4 x = make_uint4(0u, 0u, 0u, 0u);
+          if (!(g & 1)) x = __ldcg(reinterpret_cast<const uint4*>(qr + 32 * s));
+          float d[4] = {0.f, 0.f, 0.f, 0.f}, e[4] = {0.f, 0.f, 0.f, 0.f};
+          mma_bf16(d, a[s].x, b[s].x, a[s].y, b[s].y, x.x, x.y);
+          mma_bf16(e, a[s].z, b[s].z, a[s].w, b[s].w, x.z, x.w);
+          d0 += d[0] + e[0];
+          d1 += d[2] + e[2];
+        }
+        const float mu = __uint_as_float(__ldcg(few_query(F, p.seg, i) + kMu + c));
+        const float x0 = fmaf(d0, F.qscale, -mu), x1 = fmaf(d1, F.qscale, -mu);
+#pragma unroll
+        for (int t = 0; t < kTokens; ++t)
+          if (t == i) take(t, pos0, pos1, in0, in1, x0, x1);
+      }
+    }
+    // over the lanes of a head
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i) {
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) {
+        const float om = __shfl_xor_sync(0xffffffffu, m[i], o), ol = __shfl_xor_sync(0xffffffffu, l[i], o);
+        const float mn = fmaxf(m[i], om);
+        l[i] = l[i] * ex2(m[i] - mn) + ol * ex2(om - mn);
+        m[i] = mn;
+      }
+      if (lane < 4) F.part[((size_t)w + p.seg) * (4 * kFewTok) + 4 * i + c] = make_float2(m[i], l[i]);
+    }
+  }
+}
+
+constexpr int kSumThreads = 256, kSumEach = 4;
+
+// CTA (x, seg): 1024 positions' weights.
+__global__ void __launch_bounds__(kSumThreads) few_sum_kernel(const __grid_constant__ FewArgs F) {
+  __shared__ long long sum[kSumThreads / 32];
+  __shared__ float2 meet[16][4 * kFewTok];
+  __shared__ float ref[4 * kFewTok];
+  const ScoreArgs& A = F.A;
+  const int seg = blockIdx.y, b = seg / A.h_kv, h = seg % A.h_kv, tid = threadIdx.x;
+  pdl_wait();
+  pdl_trigger();
+  const ScoreSeq s = score_seq(A, b);
+  const int pos0 = kSumThreads * kSumEach * blockIdx.x;
+  if (pos0 >= s.n || s.rows == 0) return;
+  int w0, w1;
+  workers_of<Steps>(A, b, h, F.W, sum, w0, w1);
+  float m = -INFINITY, l = 0.f;
+  auto join = [&](float2 x) {
+    if (x.y == 0.f) return;
+    const float mn = fmaxf(m, x.x);
+    l = l * ex2(m - mn) + x.y * ex2(x.x - mn);
+    m = mn;
+  };
+  const int col = tid & 15, split = tid >> 4;
+  if (col < 4 * s.rows) {
+#pragma unroll 4
+    for (int w = w0 + split; w <= w1; w += kSumThreads / 16)
+      join(__ldcg(F.part + ((size_t)w + seg) * (4 * kFewTok) + col));
+  }
+  meet[split][col] = make_float2(m, l);
+  __syncthreads();
+  if (tid < 16) {
+    m = -INFINITY, l = 0.f;
+    for (int i = 0; i < kSumThreads / 16; ++i) join(meet[i][tid]);
+    ref[tid] = l > 0.f ? -(m + log2f(l)) : -INFINITY;
+  }
+  __syncthreads();
+  const int end = int2_end(s.n, A.sink, A.recent);
+  const float4* logits = F.logits + (size_t)seg * F.positions * A.max_new;
+  float* score = A.score + (size_t)seg * A.n_score;
+#pragma unroll
+  for (int e = 0; e < kSumEach; ++e) {
+    const int pos = pos0 + kSumThreads * e + tid;
+    // (window positions of a slot out of range have no logits)
+    if (pos >= s.n || (s.n_win == 0 && (pos < A.sink || pos >= end))) continue;
+    float x = 0.f;
+    for (int i = 0; i < s.rows; ++i) {
+      const float4 y = __ldcg(logits + (size_t)pos * A.max_new + i);
+      x += (ex2(y.x + ref[4 * i]) + ex2(y.y + ref[4 * i + 1])) + (ex2(y.z + ref[4 * i + 2]) + ex2(y.w + ref[4 * i + 3]));
+    }
+    score[pos] = __ldcg(score + pos) + x;
+  }
+}
+
+size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
+
+template <int kTokens>
+cudaError_t launch_logits(const optr_params* p, const FewArgs& F, cudaStream_t s) {
+  auto fn = F.A.compact ? few_logit_kernel<true, kTokens> : few_logit_kernel<false, kTokens>;
+  const size_t smem = (size_t)kWarps * kStages * kHalfRec;
+  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), smem);
+  return e != cudaSuccess ? e : launch_pdl(fn, dim3(p->num_sms), dim3(kWarps * 32), smem, s, F);
+}
+
+}  // namespace
+
+FewLayout few_layout(const optr_params* p, int B, int max_new, int max_pages) {
+  FewLayout l;
+  const size_t segs = (size_t)B * p->cfg.h_kv;
+  l.W = p->num_sms * kWarps;
+  l.part = round_up(segs * max_new * kQueryWords * sizeof(uint32_t));
+  l.logits = l.part + round_up((segs + l.W) * 4 * kFewTok * sizeof(float2));
+  l.total = l.logits + round_up(segs * max_pages * kPage * max_new * sizeof(float4));
+  return l;
+}
+
+// Few tokens, and logits that a workspace of 256 MB holds.
+bool few_tokens(const optr_params* p, int B, int max_new, int max_pages) {
+  return max_new <= kFewTok &&
+         (long long)B * p->cfg.h_kv * max_pages * kPage * max_new * (long long)sizeof(float4) <= (256ll << 20);
+}
+
+cudaError_t launch_score_few(const optr_params* p, const ScoreArgs& A, uint8_t* ws, cudaStream_t s) {
+  const FewLayout l = few_layout(p, A.B, A.max_new, A.max_pages);
+  const FewArgs F{A, (uint32_t*)ws, (float2*)(ws + l.part), (float4*)(ws + l.logits), A.max_pages * kPage, l.W,
+                  kLogit};
+  const unsigned segs = (unsigned)A.B * A.h_kv;
+  cudaError_t e = launch_pdl(few_query_kernel, dim3(segs), dim3(kQrotThreads), 0, s, F);
+  if (e == cudaSuccess) e = A.max_new == 1 ? launch_logits<1>(p, F, s) : launch_logits<kFewTok>(p, F, s);
+  const int n = std::min(F.positions, A.n_score), each = kSumThreads * kSumEach;
+  if (e == cudaSuccess)
+    e = launch_pdl(few_sum_kernel, dim3((n + each - 1) / each, segs), dim3(kSumThreads), 0, s, F);
+  return e;
+}
+
+}  // namespace optr
