@@ -30,12 +30,13 @@ struct Smem {
   int count[2];  // this CTA's keys above T, and equal to it
 };
 
-// Unsigned order = the scores' (-0 as 0, NaN above all).
-constexpr uint32_t kZero = 0x80000000u;
+// Unsigned order = the scores' (-0 as 0, NaN above all), between the keys of no position
+// and of one that stays whatever its score.
+constexpr uint32_t kNone = 0u, kZero = 0x80000000u, kNan = 0xfffffffeu, kEnd = 0xffffffffu;
 __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t u = __float_as_uint(__fadd_rn(x, 0.f));
-  if ((u & 0x7fffffffu) > 0x7f800000u) return 0xffffffffu;
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  if ((u & 0x7fffffffu) > 0x7f800000u) return kNan;
+  return u ^ ((uint32_t)((int32_t)u >> 31) | kZero);
 }
 
 // A word of shared memory, over the cluster.
@@ -68,13 +69,13 @@ __device__ __forceinline__ int reach(uint32_t& own, int& rest) {
 
 // kPer: keys of a thread, in registers; 0: as many as there are, read from memory each time.
 template <int kPer>
-__global__ void __launch_bounds__(kThreads, kPer > 16 ? 1 : 2)
+__global__ void __launch_bounds__(kThreads, kPer <= 16 ? 2 : 1)
 select_kernel(const float* __restrict__ score, int n_score, const int32_t* __restrict__ lens,
               const int32_t* __restrict__ keep, int h_kv, int first, int last,
-              int32_t* __restrict__ kept, int n_most, int32_t* __restrict__ n_kept, int cs,
+              int32_t* __restrict__ kept, int n_most, int32_t* __restrict__ n_kept, int log_cs,
               unsigned* err) {
   __shared__ Smem S;
-  const int seg = blockIdx.x / cs, rank = cs > 1 ? cluster_rank_of() : 0, b = seg / h_kv;
+  const int cs = 1 << log_cs, seg = blockIdx.x >> log_cs, rank = cs > 1 ? cluster_rank_of() : 0, b = seg / h_kv;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   for (int i = tid; i < (int)(sizeof(S.bins) / 16); i += kThreads)
     reinterpret_cast<uint4*>(S.bins)[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -96,34 +97,27 @@ select_kernel(const float* __restrict__ score, int n_score, const int32_t* __res
   int32_t* out = kept + (size_t)seg * n_most;
   const bool choose = k > 0 && k < a1 - a0;
   // the warp's part w0 .. w1-1 of the CTA's slice
-  const int lo = (int)((long long)n * rank / cs), hi = (int)((long long)n * (rank + 1) / cs);
+  const int lo = (int)((long long)n * rank >> log_cs), hi = (int)((long long)n * (rank + 1) >> log_cs);
   const int w0 = lo + (int)((long long)(hi - lo) * warp / kWarps),
             w1 = lo + (int)((long long)(hi - lo) * (warp + 1) / kWarps);
+  auto key_at = [&](int i) {
+    uint32_t x = kZero;
+    if (choose && i < w1) x = key_of(__ldcg(row + i));
+    return i >= w1 ? kNone : i < a0 || i >= a1 ? kEnd : x;
+  };
   uint32_t keys[kPer ? kPer : 1];
-  if (kPer && choose) {
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int i = w0 + 32 * j + lane;
-      keys[j] = i < w1 ? key_of(__ldcg(row + i)) : 0u;
-    }
-  }
-  // f(position, key) for each of the lane's, in order
+  for (int j = 0; j < kPer; ++j) keys[j] = key_at(w0 + 32 * j + lane);
+  // f(32 positions, the lane's key) for each of the lane's, in order
   auto each = [&](auto f) {
     if constexpr (kPer > 0) {
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        if (w0 + 32 * j >= w1) break;
-        f(w0 + 32 * j + lane, keys[j]);
-      }
+      for (int j = 0; j < kPer; ++j) f(w0 + 32 * j, keys[j]);
     } else {
-      for (int i0 = w0; i0 < w1; i0 += 32) {
-        const int i = i0 + lane;
-        f(i, choose && i < w1 ? key_of(__ldcg(row + i)) : 0u);
-      }
+      for (int i0 = w0; i0 < w1; i0 += 32) f(i0, key_at(i0 + lane));
     }
   };
-  const int c0 = max(w0, a0), c1 = min(w1, a1);  // of the part, what is chosen from
-  uint32_t T = 0u;
+  uint32_t T = k > 0 ? kNone : kNan;
   int ties = 0;  // of the keys equal to T
   if (choose) {
     __syncthreads();
@@ -132,17 +126,22 @@ select_kernel(const float* __restrict__ score, int n_score, const int32_t* __res
     for (int pass = 0;; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass < 2 ? 11 : 10;
       uint32_t* bins = S.bins + 2048 * pass;
-      // positions that were never attended to are common: their zeros are counted by ballot
+      // positions that were never attended to are common: their zeros are added at once
       if (pass == 0) {
-        each([&](int i, uint32_t x) {
-          const bool in = i >= c0 && i < c1;
-          zeros += __popc(__ballot_sync(0xffffffffu, in && x == kZero));
-          if (in && x != kZero) atomicAdd(&bins[x >> 21], 1u);
+        each([&](int, uint32_t x) {
+          if (x == kZero)
+            ++zeros;
+          else if (x - 1u < kNan)
+            atomicAdd(&bins[x >> 21], 1u);
+        });
+        zeros = __reduce_add_sync(0xffffffffu, zeros);
+      } else if (pass == 1) {
+        each([&](int, uint32_t x) {
+          if (x >> 21 == prefix && x != kZero && x != kEnd) atomicAdd(&bins[x >> 10 & 0x7ffu], 1u);
         });
       } else {
-        each([&](int i, uint32_t x) {
-          if (i >= c0 && i < c1 && x != kZero && x >> (shift + bits) == prefix)
-            atomicAdd(&bins[x >> shift & ((1u << bits) - 1u)], 1u);
+        each([&](int, uint32_t x) {
+          if (x >> 10 == prefix && x != kZero && x != kEnd) atomicAdd(&bins[x & 0x3ffu], 1u);
         });
       }
       if (lane == 0 && zeros > 0 && (pass == 0 || kZero >> (shift + bits) == prefix))
@@ -191,18 +190,14 @@ select_kernel(const float* __restrict__ score, int n_score, const int32_t* __res
     }
   }
   // What lies before each warp's part: kept positions that do not hang on ties, and ties.
-  auto classify = [&](int i, uint32_t x, bool& yes, bool& tie) {
-    const bool in = i >= c0 && i < c1;
-    yes = choose && in ? x > T : i < w1 && (!in || k > 0);
-    tie = choose && in && x == T;
-  };
   int above = 0, equal = 0;
-  each([&](int i, uint32_t x) {
-    bool yes, tie;
-    classify(i, x, yes, tie);
-    above += __popc(__ballot_sync(0xffffffffu, yes));
-    equal += __popc(__ballot_sync(0xffffffffu, tie));
+  each([&](int, uint32_t x) {
+    above += x > T;
+    equal += x == T;
   });
+  above = __reduce_add_sync(0xffffffffu, above);
+  equal = ties > 0 ? __reduce_add_sync(0xffffffffu, equal) : 0;
+  const int mine = equal;
   if (lane == 0) {
     S.above[warp] = above;
     S.equal[warp] = equal;
@@ -228,19 +223,25 @@ select_kernel(const float* __restrict__ score, int n_score, const int32_t* __res
     cluster_arrive();  // no CTA leaves while its shared memory may be read
   }
   const unsigned below = (1u << lane) - 1u;
-  each([&](int i, uint32_t x) {
-    bool yes, tie;
-    classify(i, x, yes, tie);
-    const unsigned t = __ballot_sync(0xffffffffu, tie);
-    // ties before this one are kept as long as there are any to keep
-    const int rank_of = equal + __popc(t & below);
-    const bool stays = yes || (tie && rank_of < ties);
-    const unsigned s = __ballot_sync(0xffffffffu, stays);
-    if (stays) out[above + min(equal, ties) + __popc(s & below)] = i;
-    const int u = __popc(t);
-    above += __popc(s) - (min(equal + u, ties) - min(equal, ties));
-    equal += u;
-  });
+  if (mine == 0) {
+    above += min(equal, ties);
+    each([&](int i, uint32_t x) {
+      const unsigned s = __ballot_sync(0xffffffffu, x > T);
+      if (x > T) out[above + __popc(s & below)] = i + lane;
+      above += __popc(s);
+    });
+  } else {
+    each([&](int i, uint32_t x) {
+      const unsigned t = __ballot_sync(0xffffffffu, x == T);
+      // ties before this one are kept as long as there are any to keep
+      const bool stays = x > T || (x == T && equal + __popc(t & below) < ties);
+      const unsigned s = __ballot_sync(0xffffffffu, stays);
+      if (stays) out[above + min(equal, ties) + __popc(s & below)] = i + lane;
+      const int u = __popc(t);
+      above += __popc(s) - (min(equal + u, ties) - min(equal, ties));
+      equal += u;
+    });
+  }
   if (cs > 1) cluster_wait();
 }
 
@@ -257,12 +258,14 @@ extern "C" optr_status optr_evict_select(const optr_params* p, const float* scor
     return OPTR_ERR_INVALID_ARG;
   const long long rows = (long long)B * p->cfg.h_kv;
   if (rows > (1 << 27) || n_score > (1 << 30)) return OPTR_ERR_OUT_OF_RANGE;
-  // CTAs of a row: as few as leave each 4096 scores or fewer, two per SM in all
-  int cs = 1;
-  while (cs < 8 && n_score > 4096 * cs && rows * 2 * cs <= 2 * p->num_sms) cs *= 2;
+  // CTAs of a row: as few as leave each 4096 scores or fewer, two per SM in all (64 rows of
+  // 32768: clusters of 4 16.4 us; of 8, which are not all resident at once, 35 us)
+  int log_cs = 0;
+  while (log_cs < 3 && n_score > 4096 << log_cs && (rows << log_cs) <= p->num_sms) ++log_cs;
+  const int cs = 1 << log_cs;
   const int per = (n_score - 1) / (cs * kThreads) + 1;
   auto fn = per <= 8 ? select_kernel<8> : per <= 16 ? select_kernel<16> : per <= 32 ? select_kernel<32> : select_kernel<0>;
   return cuda_status(launch_pdl_cluster(fn, dim3((unsigned)(rows * cs)), dim3(kThreads), cs, 0, stream, score,
-                                        n_score, lens, keep, p->cfg.h_kv, first, last, kept, n_most, n_kept, cs,
+                                        n_score, lens, keep, p->cfg.h_kv, first, last, kept, n_most, n_kept, log_cs,
                                         p->err));
 }
