@@ -13,6 +13,7 @@
 // stand in one line that is cut into equal ranges, one a warp.
 #include <type_traits>
 
+#include "cluster.cuh"
 #include "qrot.cuh"
 #include "score.cuh"
 
@@ -86,15 +87,24 @@ __global__ void __launch_bounds__(kQrotThreads) few_query_kernel(const __grid_co
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                         uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
       "{%0,%1,%2,%3};\n"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// d = a b + c
+__device__ __forceinline__ void mma_f16_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                             uint32_t b0, uint32_t b1, const float (&c)[4]) {
+  asm(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%10,%11,%12,%13};\n"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
 __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                          uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
       "{%0,%1,%2,%3};\n"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -125,12 +135,21 @@ __device__ __forceinline__ float low_half(uint32_t x) {
   return __low2float(*reinterpret_cast<const __half2*>(&x));
 }
 
+// A token's query in shared memory: by group the lanes' fragments, then as in the
+// workspace, with the min terms' fragment ready.
+struct FewQuery {
+  uint4 frag[kGroups][32];
+  float off[32];
+  uint32_t min[32];
+  float inv[4], mu[4];
+};
+
 // A token's query as a lane has it: B fragments of its column, what the products start
 // from, the min terms' B fragment, and the inverse prescale of head lane % 4.
 template <bool kCompact>
 struct Query {
   uint4 frag[kGroups];
-  float start[kGroups][2];
+  float start[kGroups][4];
   uint32_t min;
   float inv;
 
@@ -141,14 +160,28 @@ struct Query {
       frag[G] = __ldcg(reinterpret_cast<const uint4*>(w + kFrag + lane * 16) + G);
     const float4* o = reinterpret_cast<const float4*>(w + kOff + c * 8);
     const float4 a = __ldcg(o), b = __ldcg(o + 1);
-    start[0][0] = -a.x, start[0][1] = -a.y, start[1][0] = -a.z, start[1][1] = -a.w;
-    start[2][0] = -b.x, start[2][1] = -b.y, start[3][0] = -b.z, start[3][1] = -b.w;
+    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int G = 0; G < kGroups; ++G) start[G][0] = start[G][2] = -x[2 * G], start[G][1] = start[G][3] = -x[2 * G + 1];
     // column g of the min terms' product: head g / 2, hi or lo part of group c's sum
     const float s = __uint_as_float(__ldcg(w + kSum + (g >> 1) * kGroups + c));
     const float hi = __uint_as_float(__float_as_uint(s) & 0xffffe000u);
     const uint32_t part = __half_as_ushort(__float2half_rn(g & 1 ? s - hi : hi));
     min = part << 16;
     inv = __uint_as_float(__ldcg(w + kInv + c));
+  }
+  // of shared memory
+  __device__ __forceinline__ void load(const FewQuery& w) {
+    const int lane = threadIdx.x & 31, c = lane & 3;
+    const float4 *o = reinterpret_cast<const float4*>(w.off + c * 8), a = o[0], b = o[1];
+    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int G = 0; G < kGroups; ++G) {
+      frag[G] = w.frag[G][lane];
+      start[G][0] = start[G][2] = -x[2 * G], start[G][1] = start[G][3] = -x[2 * G + 1];
+    }
+    min = w.min[lane];
+    inv = w.inv[c];
   }
 };
 
@@ -183,11 +216,9 @@ struct Page {
     float s[kGroups][4];
 #pragma unroll
     for (int G = 0; G < kGroups; ++G) {
-      s[G][0] = s[G][2] = q.start[G][0];
-      s[G][1] = s[G][3] = q.start[G][1];
       const uint32_t (&a)[4] = f[0][G >> 1][G & 1];
       const uint32_t (&b)[4] = f[1][G >> 1][G & 1];
-      mma_f16(s[G], a[0], b[0], a[1], b[1], q.frag[G].x, q.frag[G].y);
+      mma_f16_from(s[G], a[0], b[0], a[1], b[1], q.frag[G].x, q.frag[G].y, q.start[G]);
       mma_f16(s[G], a[2], b[2], a[3], b[3], q.frag[G].z, q.frag[G].w);
     }
     float u[4] = {0.f, 0.f, 0.f, 0.f}, t0, t1;
@@ -213,6 +244,28 @@ struct Page {
     return make_float2(fmaf(q.inv, t0, u[0] + u[1]), fmaf(q.inv, t1, u[2] + u[3]));
   }
 };
+
+// Products of 16 window rows' keys (rows g and g + 8, channels 32 e + 8 c ..) with the four
+// heads of a query (lanes whose column is a head's: `has`), head c of rows g and g + 8.
+__device__ __forceinline__ float2 window_logits(const uint4 (&a)[4], const uint4 (&b)[4], const __nv_bfloat16* qr,
+                                                bool has) {
+  // (a sum of its own for each step, since a product rounds at its largest term: the
+  // key mean may make one channel's far larger than the logit)
+  float d0 = 0.f, d1 = 0.f;
+  // column g: head g / 2 of the even ones, nothing of the odd ones; the places of
+  // the inner dimension are permuted alike in both operands
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    uint4 x = make_uint4(0u, 0u, 0u, 0u);
+    if (has) x = __ldcg(reinterpret_cast<const uint4*>(qr + 32 * s));
+    float d[4] = {0.f, 0.f, 0.f, 0.f}, e[4] = {0.f, 0.f, 0.f, 0.f};
+    mma_bf16(d, a[s].x, b[s].x, a[s].y, b[s].y, x.x, x.y);
+    mma_bf16(e, a[s].z, b[s].z, a[s].w, b[s].w, x.z, x.w);
+    d0 += d[0] + e[0];
+    d1 += d[2] + e[2];
+  }
+  return make_float2(d0, d1);
+}
 
 template <bool kCompact, int kTokens>
 __global__ void __launch_bounds__(kWarps * 32, 1) few_logit_kernel(const __grid_constant__ FewArgs F) {
@@ -329,24 +382,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) few_logit_kernel(const __grid_
         b[s] = __ldcg(reinterpret_cast<const uint4*>(r1 + 32 * s));
       }
       for (int i = 0; i < p.rows; ++i) {
-        // (a sum of its own for each step, since a product rounds at its largest term: the
-        // key mean may make one channel's far larger than the logit)
-        float d0 = 0.f, d1 = 0.f;
-        // column g: head g / 2 of the even ones, nothing of the odd ones; the places of
-        // the inner dimension are permuted alike in both operands
         const __nv_bfloat16* qr = A.q + ((((size_t)p.c0 + i) * A.h_kv + p.h) * 4 + (g >> 1)) * kD + 8 * c;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          uint4 x = make_uint4(0u, 0u, 0u, 0u);
-          if (!(g & 1)) x = __ldcg(reinterpret_cast<const uint4*>(qr + 32 * s));
-          float d[4] = {0.f, 0.f, 0.f, 0.f}, e[4] = {0.f, 0.f, 0.f, 0.f};
-          mma_bf16(d, a[s].x, b[s].x, a[s].y, b[s].y, x.x, x.y);
-          mma_bf16(e, a[s].z, b[s].z, a[s].w, b[s].w, x.z, x.w);
-          d0 += d[0] + e[0];
-          d1 += d[2] + e[2];
-        }
+        const float2 d = window_logits(a, b, qr, !(g & 1));
         const float mu = __uint_as_float(__ldcg(few_query(F, p.seg, i) + kMu + c));
-        const float x0 = fmaf(d0, F.qscale, -mu), x1 = fmaf(d1, F.qscale, -mu);
+        const float x0 = fmaf(d.x, F.qscale, -mu), x1 = fmaf(d.y, F.qscale, -mu);
 #pragma unroll
         for (int t = 0; t < kTokens; ++t)
           if (t == i) take(t, pos0, pos1, in0, in1, x0, x1);
@@ -421,6 +460,283 @@ __global__ void __launch_bounds__(kSumThreads) few_sum_kernel(const __grid_const
   }
 }
 
+// ------------------------------------------------------- a cluster a (sequence, KV head)
+
+constexpr int kOneStages = 6;
+
+// CTA rank r of a cluster of cs: pages P (r) .. P (r + 1) of the INT2 keys and steps
+// of 16 window rows alike, by place: place 16 x + t is token t of the x-th.
+struct OneSmem {
+  union {
+    QrotSmem rot;
+    float4 logits[1];  // [tokens][places]
+  };
+};
+struct OneFixed {
+  FewQuery query[kFewTok];
+  uint32_t frag[512];
+  float sum[16];
+  float top[kWarps][4 * kFewTok], part[kWarps][4 * kFewTok];
+  float2 mine[4 * kFewTok];
+  float ref[4 * kFewTok];
+  alignas(16) uint8_t stage[kWarps][kOneStages][kHalfRec];
+};
+
+template <bool kCompact, int kTokens>
+__global__ void __launch_bounds__(kWarps * 32, 1)
+few_cluster_kernel(const __grid_constant__ ScoreArgs A, int log_cs, int places, float qscale) {
+  extern __shared__ __align__(16) unsigned char dsm_[];
+  OneFixed& S = *reinterpret_cast<OneFixed*>(dsm_);
+  OneSmem& U = *reinterpret_cast<OneSmem*>(dsm_ + sizeof(OneFixed));
+  const int cs = 1 << log_cs, rank = cs > 1 ? cluster_rank_of() : 0;
+  const int seg = blockIdx.x >> log_cs, b = seg / A.h_kv, h = seg % A.h_kv;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+  float rv[32];
+  load_rotation_slice(A.R_k, h, rv);
+  pdl_wait();
+  pdl_trigger();
+  if (blockIdx.x == 0 && warp == 0) report_sequences(A);
+  const ScoreSeq s = score_seq(A, b);
+  if (Steps::of(s) == 0) return;  // the whole cluster
+  const int all = Steps::pages(s.n_int), steps = (s.n_win + kWinRows - 1) / kWinRows;
+  const int P0 = all * rank >> log_cs, P1 = all * (rank + 1) >> log_cs;
+  const int U0 = steps * rank >> log_cs, U1 = steps * (rank + 1) >> log_cs;
+  // this warp's pages
+  const int p0 = P0 + ((P1 - P0) * warp / kWarps), last = P0 + ((P1 - P0) * (warp + 1) / kWarps);
+  const int32_t* table = A.bt + (size_t)b * A.max_pages + A.sink / kPage;
+  // lane: the physical page of base + lane
+  int base = p0, phys = -1;
+  auto resolve = [&](int from) {
+    base = from;
+    phys = -1;
+    if (from + lane < last) {
+      phys = __ldcg(table + from + lane);
+      if (phys < 0 || phys >= A.num_pages) {
+        phys = -1;
+        atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
+      }
+    }
+  };
+  resolve(p0);
+  uint32_t bad = 0;  // stages of pages that are not to be read
+  uint8_t* stage = S.stage[warp][0];
+  auto issue = [&](int page, int st) {
+    if (page < last) {
+      if (page - base == 32) resolve(page);
+      const int x = __shfl_sync(0xffffffffu, phys, page - base);
+      bad = x < 0 ? bad | 1u << st : bad & ~(1u << st);
+      const uint8_t* src = A.pool + ((size_t)max(x, 0) * A.h_kv + h) * chunk_bytes(kCompact) + 16 * lane;
+      uint8_t* dst = stage + st * kHalfRec + 16 * lane;
+      cp_async16_zfill(dst, src + OPTR_K_CODES_OFFSET, x >= 0);
+      if (lane < meta_stride(kCompact)) cp_async16_zfill(dst + 512, src + OPTR_K_META_OFFSET, x >= 0);
+    }
+  };
+  constexpr int kPairs = kOneStages / 2;
+#pragma unroll
+  for (int e = 0; e < kPairs - 1; ++e) {
+    issue(p0 + 2 * e, 2 * e);
+    issue(p0 + 2 * e + 1, 2 * e + 1);
+    cp_async_commit();
+  }
+  // the tokens' queries, while the first pages are on their way
+#pragma unroll 1
+  for (int i = 0; i < s.rows; ++i) {
+    const __nv_bfloat16* q = A.q + (((size_t)s.c0 + i) * A.h_kv + h) * (4 * kD);
+    FewQuery& Q = S.query[i];
+    rotate_query(U.rot, q, rv, qscale, nullptr, S.sum, S.frag, Q.off, Q.inv);
+    __syncthreads();
+    // [lane][group][word] to [group][lane][word]
+    reinterpret_cast<uint32_t*>(Q.frag)[(tid >> 2 & 3) * 128 + (tid >> 4) * 4 + (tid & 3)] = S.frag[tid];
+    if (warp == 0) {
+      // column g of the min terms' product: head g / 2, hi or lo part of group c's sum
+      const float x = S.sum[(g >> 1) * kGroups + c];
+      const float hi = __uint_as_float(__float_as_uint(x) & 0xffffe000u);
+      Q.min[lane] = (uint32_t)__half_as_ushort(__float2half_rn(g & 1 ? x - hi : hi)) << 16;
+    }
+    if (A.win.win && tid < 128) {  // head tid / 32
+      float d = 0.f;
+      for (int k = lane; k < kD; k += 32)
+        d = fmaf(__bfloat162float(q[warp * kD + k]), __ldg(A.mu + (size_t)h * kD + k), d);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+      if (lane == 0) Q.mu[warp] = d * qscale;
+    }
+  }
+  __syncthreads();
+  float m[kTokens];
+#pragma unroll
+  for (int i = 0; i < kTokens; ++i) m[i] = -1e30f;
+  float* logits = reinterpret_cast<float*>(U.logits) + c;
+  Query<kCompact> q;
+  if (kTokens == 1) q.load(S.query[0]);
+  int at = 0;  // the pair's stages
+#pragma unroll 1
+  for (int page = p0; page < last; page += 2) {
+    const int to = at == 0 ? kPairs - 1 : at - 1;
+    issue(page + 2 * (kPairs - 1), 2 * to);
+    issue(page + 2 * (kPairs - 1) + 1, 2 * to + 1);
+    cp_async_commit();
+    cp_async_wait<kPairs - 1>();
+    __syncwarp();
+    Page<kCompact> x[kTokens > 1 ? 2 : 1];
+    if (kTokens > 1) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) x[kTokens > 1 ? e : 0].load(stage + (2 * at + e) * kHalfRec);
+    }
+    const bool whole = !(bad >> (2 * at) & 3) && kPage * (page + 2) <= s.n_int && page + 1 < last;
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i) {
+      if (i >= s.rows) break;
+      if (kTokens > 1) q.load(S.query[i]);
+      float2 y[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (kTokens == 1) x[0].load(stage + (2 * at + e) * kHalfRec);
+        y[e] = x[kTokens > 1 ? e : 0].logits(q);
+      }
+      float* out = logits + ((size_t)i * places + kPage * (page - P0) + g) * 4;
+      // the last page, one that is not to be read, keys that this token does not see
+      const int lim = min(s.n_int, s.pos0 + i + 1 - A.sink);
+      if (!whole || kPage * (page + 2) > lim) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int k = kPage * (page + e) + g;
+          const bool ok = !(bad >> (2 * at + e) & 1);
+          if (!ok || k >= lim) y[e].x = -INFINITY;
+          if (!ok || k + 8 >= lim) y[e].y = -INFINITY;
+        }
+      }
+      out[0] = y[0].x;
+      out[32] = y[0].y;
+      m[i] = fmaxf(m[i], fmaxf(y[0].x, y[0].y));
+      if (page + 1 < last) {
+        out[64] = y[1].x;
+        out[96] = y[1].y;
+        m[i] = fmaxf(m[i], fmaxf(y[1].x, y[1].y));
+      }
+    }
+    __syncwarp();  // the stages are free
+    at = at + 1 == kPairs ? 0 : at + 1;
+  }
+  cp_async_wait<0>();
+  const int w_place = kPage * (P1 - P0);  // of the first window row
+  for (int u = U0 + warp; u < U1; u += kWarps) {
+    const int i0 = kWinRows * u + g, i1 = i0 + 8;
+    const bool in0 = i0 < s.n_win, in1 = i1 < s.n_win;
+    const int pos0 = win_pos(in0 ? i0 : 0, s.n, A.sink, A.recent), pos1 = win_pos(in1 ? i1 : 0, s.n, A.sink, A.recent);
+    const __nv_bfloat16* rows = A.win.win + (((size_t)s.slot * A.h_kv + h) * 2) * (A.sink + A.recent) * kD + 8 * c;
+    const __nv_bfloat16 *r0 = rows + (size_t)win_row(pos0, A.sink, A.recent) * kD,
+                        *r1 = rows + (size_t)win_row(pos1, A.sink, A.recent) * kD;
+    uint4 k0[4], k1[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      k0[e] = __ldcg(reinterpret_cast<const uint4*>(r0 + 32 * e));
+      k1[e] = __ldcg(reinterpret_cast<const uint4*>(r1 + 32 * e));
+    }
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i) {
+      if (i >= s.rows) break;
+      const __nv_bfloat16* qr = A.q + ((((size_t)s.c0 + i) * A.h_kv + h) * 4 + (g >> 1)) * kD + 8 * c;
+      const float2 d = window_logits(k0, k1, qr, !(g & 1));
+      const int seen = s.pos0 + i;
+      const float x0 = in0 && pos0 <= seen ? fmaf(d.x, qscale, -S.query[i].mu[c]) : -INFINITY;
+      const float x1 = in1 && pos1 <= seen ? fmaf(d.y, qscale, -S.query[i].mu[c]) : -INFINITY;
+      float* out = logits + ((size_t)i * places + w_place + kWinRows * (u - U0) + g) * 4;
+      out[0] = x0;
+      out[32] = x1;
+      m[i] = fmaxf(m[i], fmaxf(x0, x1));
+    }
+  }
+  // the CTA's maxima, its sums over those, and the cluster's of both
+  const int cols = 4 * s.rows;
+#pragma unroll
+  for (int i = 0; i < kTokens; ++i) {
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], o));
+    if (lane < 4) S.top[warp][4 * i + c] = m[i];
+  }
+  __syncthreads();
+  auto over_warps = [&](const float (&x)[kWarps][4 * kFewTok], int col, auto join) {
+    float y = x[lane % kWarps][col];
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) y = join(y, __shfl_xor_sync(0xffffffffu, y, o));
+    return y;
+  };
+  const int n_int = min(kPage * (P1 - P0), s.n_int - kPage * P0), n_win = max(0, min(kWinRows * (U1 - U0), s.n_win - kWinRows * U0));
+  const int n_all = n_int + n_win;
+  for (int i = 0; i < s.rows; ++i) {
+    float top[4], l[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      top[j] = over_warps(S.top, 4 * i + j, [](float x, float y) { return fmaxf(x, y); });
+    const float4* x = U.logits + (size_t)i * places;
+#pragma unroll 4
+    for (int k = tid; k < n_all; k += kWarps * 32) {
+      const float4 y = x[k < n_int ? k : k - n_int + w_place];
+      l[0] += ex2(y.x - top[0]);
+      l[1] += ex2(y.y - top[1]);
+      l[2] += ex2(y.z - top[2]);
+      l[3] += ex2(y.w - top[3]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) l[j] += __shfl_xor_sync(0xffffffffu, l[j], o);
+      if (lane == j) {
+        S.part[warp][4 * i + j] = l[j];
+        if (warp == 0) S.mine[4 * i + j].x = top[j];
+      }
+    }
+  }
+  __syncthreads();
+  if (tid < cols) {
+    float l = 0.f;
+    for (int i = 0; i < kWarps; ++i) l += S.part[i][tid];
+    S.mine[tid].y = l;
+  }
+  if (cs > 1) cluster_barrier(); else __syncthreads();
+  if (tid < cols) {
+    float2 y[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      y[r] = make_float2(-1e30f, 0.f);
+      if (r < cs) {
+        if (cs > 1) {
+          const unsigned long long z = cluster_ld64(&S.mine[tid], r);
+          y[r] = make_float2(__uint_as_float((uint32_t)z), __uint_as_float((uint32_t)(z >> 32)));
+        } else {
+          y[r] = S.mine[tid];
+        }
+      }
+    }
+    float top = -1e30f, l = 0.f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) top = fmaxf(top, y[r].x);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) l += y[r].y * ex2(y[r].x - top);
+    S.ref[tid] = l > 0.f ? -(top + log2f(l)) : -INFINITY;
+  }
+  __syncthreads();
+  if (cs > 1) cluster_arrive();  // no CTA leaves while its shared memory may be read
+  float* score = A.score + (size_t)seg * A.n_score;
+#pragma unroll 4
+  for (int k = tid; k < n_all; k += kWarps * 32) {
+    const bool coded = k < n_int;
+    const int place = coded ? k : k - n_int + w_place;
+    const int pos = coded ? A.sink + kPage * P0 + k : win_pos(kWinRows * U0 + k - n_int, s.n, A.sink, A.recent);
+    const float old = __ldcg(score + pos);
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < kTokens; ++i) {
+      if (i >= s.rows) break;
+      const float4 y = U.logits[(size_t)i * places + place], r = *reinterpret_cast<const float4*>(S.ref + 4 * i);
+      x += (ex2(y.x + r.x) + ex2(y.y + r.y)) + (ex2(y.z + r.z) + ex2(y.w + r.w));
+    }
+    score[pos] = old + x;
+  }
+  if (cs > 1) cluster_wait();
+}
+
 size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 
 template <int kTokens>
@@ -429,6 +745,30 @@ cudaError_t launch_logits(const optr_params* p, const FewArgs& F, cudaStream_t s
   const size_t smem = (size_t)kWarps * kStages * kHalfRec;
   const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), smem);
   return e != cudaSuccess ? e : launch_pdl(fn, dim3(p->num_sms), dim3(kWarps * 32), smem, s, F);
+}
+
+// CTAs of a (sequence, KV head) in a cluster, log2, or -1: its logits do not fit, or there
+// are too many (the CTAs of a last, poorly filled round would idle).
+int cluster_log(const optr_params* p, int B, int max_new, int max_pages, int& places, size_t& smem) {
+  const int segs = B * p->cfg.h_kv;
+  int best = -1;
+  for (int l = 0; l < 4; ++l) {
+    // clusters of 4 and 8 do not fill all of the GPU at one CTA an SM (144 and 120 of 152)
+    if (l > 0 && (segs << l) > (l == 1 ? p->num_sms : p->num_sms * 3 / 4)) break;
+    const int units = (max_pages + 2) / (1 << l) + 3;
+    const size_t x = sizeof(OneFixed) + std::max(sizeof(QrotSmem), (size_t)units * kPage * max_new * sizeof(float4));
+    if (x > 227 * 1024) continue;
+    best = l, places = units * kPage, smem = x;
+  }
+  return best;
+}
+
+template <int kTokens>
+cudaError_t launch_cluster(const ScoreArgs& A, int log_cs, int places, size_t smem, cudaStream_t s) {
+  auto fn = A.compact ? few_cluster_kernel<true, kTokens> : few_cluster_kernel<false, kTokens>;
+  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), smem);
+  return e != cudaSuccess ? e : launch_pdl_cluster(fn, dim3((unsigned)(A.B * A.h_kv) << log_cs), dim3(kWarps * 32),
+                                                   1 << log_cs, smem, s, A, log_cs, places, kLogit);
 }
 
 }  // namespace
@@ -450,6 +790,12 @@ bool few_tokens(const optr_params* p, int B, int max_new, int max_pages) {
 }
 
 cudaError_t launch_score_few(const optr_params* p, const ScoreArgs& A, uint8_t* ws, cudaStream_t s) {
+  int places;
+  size_t smem;
+  const int log_cs = cluster_log(p, A.B, A.max_new, A.max_pages, places, smem);
+  if (log_cs >= 0)
+    return A.max_new == 1 ? launch_cluster<1>(A, log_cs, places, smem, s)
+                          : launch_cluster<kFewTok>(A, log_cs, places, smem, s);
   const FewLayout l = few_layout(p, A.B, A.max_new, A.max_pages);
   const FewArgs F{A, (uint32_t*)ws, (float2*)(ws + l.part), (float4*)(ws + l.logits), A.max_pages * kPage, l.W,
                   kLogit};
