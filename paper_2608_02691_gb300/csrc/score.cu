@@ -31,9 +31,11 @@ namespace {
 
 // ------------------------------------------------------------- queries
 
-// Channel at place k of a key row: word w of a slot's codes has, by byte, the four
+// Place of a channel in a key row: word w of a slot's codes has, by byte, the four
 // groups' channels 4 w .. 4 w + 3.
-__host__ __device__ constexpr int key_channel(int k) { return 32 * ((k >> 2) & 3) + 4 * (k >> 4) + (k & 3); }
+__host__ __device__ constexpr int key_place(int channel) {
+  return 16 * ((channel >> 2) & 7) + 4 * (channel >> 5) + (channel & 3);
+}
 
 // Element (n, k) of an operand of n columns, K-major without swizzle: core matrices of
 // 8 columns x 8 of k (128 B), 128 B apart along k and 2048 B along n.
@@ -45,18 +47,30 @@ constexpr int kRotThreads = 256;
 constexpr int kRotCols = 32;  // columns of a CTA: 8 tokens
 
 // CTA (x, seg): columns 32 x .. of the segment's block, rotated in float32.  Thread:
-// place k of the rows, 16 of the columns.
+// channel k of the rows, 16 of the columns.  The rotation comes into shared memory
+// whole, before what the call waits for: its 128 rows' latencies are one.
+struct QuerySmem {
+  float R[kD][kD], q[kRotCols][kD];
+  float top[4][kRotCols], dot[4][kRotCols], sum[4][kRotCols];
+};
 __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constant__ ScoreArgs A) {
-  __shared__ float q[kRotCols][kD];
-  __shared__ float top[4][kRotCols], dot[4][kRotCols];
+  extern __shared__ __align__(1024) unsigned char dsm_[];
+  QuerySmem& S = *reinterpret_cast<QuerySmem*>(dsm_);
+  float (&q)[kRotCols][kD] = S.q;
   const int seg = blockIdx.y, b = seg / A.h_kv, h = seg % A.h_kv, tid = threadIdx.x;
   const int k = tid & 127, part = tid >> 7, lane = tid & 31, quarter = (tid >> 5) & 3;
+  for (int i = tid; i < kD * kD / 4; i += kRotThreads)
+    cp_async16(reinterpret_cast<float4*>(S.R) + i, reinterpret_cast<const float4*>(A.R_k + (size_t)h * kD * kD) + i);
+  cp_async_commit();
   pdl_wait();
   pdl_trigger();
   if (blockIdx.x == 0 && seg == 0 && A.t0 == 0 && tid < 32) report_sequences(A);
   const ScoreSeq s = score_seq(A, b);
   const int c0 = kRotCols * blockIdx.x, N = (4 * s.rows + 15) / 16 * 16;
-  if (c0 >= N || seq_tiles(s) == 0) return;
+  if (c0 >= N || seq_tiles(s) == 0) {
+    cp_async_wait<0>();
+    return;
+  }
   const bool win = A.win.win != nullptr;
   uint8_t* out = qop_of(A, seg);
   for (int i = tid; i < kRotCols * kD / 8; i += kRotThreads) {
@@ -74,37 +88,36 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
     if (win && c0 + c < N)
       *reinterpret_cast<uint4*>(out + (size_t)A.cols * 512 + operand_offset(c0 + c, x)) = y;
   }
+  cp_async_wait<0>();
   __syncthreads();
   constexpr int kMine = kRotCols / 2;
   float acc[kMine] = {};
-  const float* R = A.R_k + (size_t)h * kD * kD + key_channel(k);
-  for (int i0 = 0; i0 < kD; i0 += 16) {
-    float r[16];
+#pragma unroll 4
+  for (int i = 0; i < kD; i += 4) {
+    const float r[4] = {S.R[i][k], S.R[i + 1][k], S.R[i + 2][k], S.R[i + 3][k]};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) r[i] = __ldg(R + (size_t)(i0 + i) * kD);
-#pragma unroll
-    for (int c = 0; c < kMine; ++c)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        const float4 x = *reinterpret_cast<const float4*>(&q[kMine * part + c][i0 + i]);
-        acc[c] = fmaf(x.x, r[i], acc[c]);
-        acc[c] = fmaf(x.y, r[i + 1], acc[c]);
-        acc[c] = fmaf(x.z, r[i + 2], acc[c]);
-        acc[c] = fmaf(x.w, r[i + 3], acc[c]);
-      }
+    for (int c = 0; c < kMine; ++c) {
+      const float4 x = *reinterpret_cast<const float4*>(&q[kMine * part + c][i]);
+      acc[c] = fmaf(x.x, r[0], acc[c]);
+      acc[c] = fmaf(x.y, r[1], acc[c]);
+      acc[c] = fmaf(x.z, r[2], acc[c]);
+      acc[c] = fmaf(x.w, r[3], acc[c]);
+    }
   }
   const float mu = __ldg(A.mu + (size_t)h * kD + k);
 #pragma unroll
   for (int c = 0; c < kMine; ++c) {
-    float m = fabsf(acc[c]), d = q[kMine * part + c][k] * mu;
+    float m = fabsf(acc[c]), d = q[kMine * part + c][k] * mu, t = acc[c];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
       d += __shfl_xor_sync(0xffffffffu, d, o);
+      t += __shfl_xor_sync(0xffffffffu, t, o);
     }
     if (lane == 0) {
-      top[quarter][kMine * part + c] = m;
-      dot[quarter][kMine * part + c] = d;
+      S.top[quarter][kMine * part + c] = m;
+      S.dot[quarter][kMine * part + c] = d;
+      S.sum[quarter][kMine * part + c] = t;
     }
   }
   __syncthreads();
@@ -112,18 +125,19 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
 #pragma unroll
   for (int c = 0; c < kMine; ++c) {
     const int n = kMine * part + c;
-    const float m = fmaxf(fmaxf(top[0][n], top[1][n]), fmaxf(top[2][n], top[3][n]));
+    const float m = fmaxf(fmaxf(S.top[0][n], S.top[1][n]), fmaxf(S.top[2][n], S.top[3][n]));
     // the row's largest at 2^13 .. 2^14, so that lo parts are normal fp16 down to 2^-17 of it
     const int E = m > 0.f ? max(-100, min(100, 13 - ((int)(__float_as_uint(m) >> 23) - 127))) : 0;
     const float x = acc[c] * __uint_as_float((uint32_t)(127 + E) << 23);
     const __half hi = __float2half_rn(x), lo = __float2half_rn(x - __half2float(hi));
     if (c0 + n >= N) break;
-    const int at = operand_offset(c0 + n, k);
+    const int at = operand_offset(c0 + n, key_place(k));
     *reinterpret_cast<__half*>(out + at) = hi;
     *reinterpret_cast<__half*>(out + (size_t)A.cols * 256 + at) = lo;
     if (k == 0) {
       factor[c0 + n] = __uint_as_float((uint32_t)(127 - E) << 23) * kLogit;
-      factor[A.cols + c0 + n] = kLogit * ((dot[0][n] + dot[1][n]) + (dot[2][n] + dot[3][n]));
+      factor[A.cols + c0 + n] = kLogit * ((S.dot[0][n] + S.dot[1][n]) + (S.dot[2][n] + S.dot[3][n]));
+      factor[2 * A.cols + c0 + n] = kLogit * ((S.sum[0][n] + S.sum[1][n]) + (S.sum[2][n] + S.sum[3][n]));
     }
   }
 }
@@ -136,34 +150,41 @@ constexpr int kKeyWarp = 8, kCopyWarp = 12, kMmaWarp = 13, kPlanWarp = 14;
 constexpr int kThreads = 512;
 constexpr int kRegLaunch = 128, kRegEpi = 208, kRegKey = 56, kRegIssue = 40;
 static_assert(2 * kRegEpi + kRegKey + kRegIssue <= 4 * kRegLaunch, "registers of the launch");
-constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kColD = 0, kColK = 256;  // D[d] at 128 d; keys' hi, lo [s] at 256 + 128 s
+constexpr uint32_t kTmemCols = 512, kColD = 0;
+// D[d] at 128 d, then the keys: two of hi and lo parts, or two of codes and one D more
+template <bool kCompact>
+struct Tmem {
+  static constexpr int kDs = kCompact ? 3 : 2;
+  static constexpr uint32_t kColK = 128u * kDs, kKeyCols = kCompact ? 64u : 128u;
+};
 constexpr int kRaw = 3;        // tiles of records on the way
 constexpr int kPieces = 3;     // pieces found ahead
 constexpr int kConsumers = 14; // warps that take the pieces
 constexpr float kSlack = 60.f; // a column's logits may pass its reference by 2^60
-constexpr int kHalfRec = 768;  // a page's key codes and pairs
 
+template <bool kCompact>
 struct Smem {
   uint8_t q[3][kBlockCols * 256];    // hi, lo, as given
-  uint8_t raw[kRaw][kKeys / kPage][kHalfRec];
-  alignas(16) float factor[kBlockCols], off[kBlockCols];
+  uint8_t raw[kRaw][kKeys / kPage][512 + 16 * meta_stride(kCompact)];  // a page's key codes and pairs
+  alignas(16) float factor[kBlockCols], off[kBlockCols], sum[kCompact ? kBlockCols : 4];
   // minus the columns' references: pass 0 by warp, pass 1 the normalisers
   alignas(16) float ref[8][kKeys];
   float2 meet[8][kKeys];             // pass 0: the warps' parts of a piece
-  // a key's power of two, 0 where it does not count.  Read between the tile's logits
-  // and its D being free; written for tile t + 4 once the products of t + 2 are done,
-  // which waited for that.
-  float scale[4][kKeys];
+  // A key's power of two, or its pair, and whether it counts.  Read between a tile's
+  // logits and its last D being free; written for tile t + kRing once the products of
+  // t + kRing - 2 are done, which waited for the Ds before their own.
+  static constexpr int kRing = kCompact ? 8 : 4;
+  uint32_t scale[kRing][kKeys];
+  uint32_t counts[kRing][4];
   ScorePiece piece[kPieces];
   uint64_t raw_full[kRaw], raw_empty[kRaw], k_full[2], k_empty[2];
-  uint64_t d_full[2][2], d_empty[2];  // by D and the epilogue group that takes it
+  uint64_t d_full[3][2], d_empty[3];  // by D and the epilogue group that takes it
   uint64_t piece_full[kPieces], piece_empty[kPieces], q_full, q_empty, drained;
   uint32_t tmem;
   int abort;
 };
 
-static_assert(sizeof(Smem) <= 232448, "shared memory of a CTA");
+static_assert(sizeof(Smem<false>) <= 232448 && sizeof(Smem<true>) <= 232448, "shared memory of a CTA");
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -177,6 +198,14 @@ __device__ __forceinline__ uint32_t pack_half(float a, float b) {  // a in the l
 }
 __device__ __forceinline__ float2 unpack_half(uint32_t x) {
   return __half22float2(*reinterpret_cast<const __half2*>(&x));
+}
+
+// Registers that a load from tensor memory fills: what uses them stays behind the wait
+// before this.
+template <int n>
+__device__ __forceinline__ void loaded(uint32_t (&x)[n]) {
+#pragma unroll
+  for (int i = 0; i < n; ++i) asm volatile("" : "+r"(x[i]));
 }
 
 // The 128 threads of an epilogue group.
@@ -194,10 +223,13 @@ __device__ __forceinline__ float warp_largest(float x) {
   return __int_as_float(y ^ ((y >> 31) & 0x7fffffff));
 }
 
-template <bool kSum>
+template <bool kSum, bool kCompact>
 __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constant__ ScoreArgs A) {
   extern __shared__ __align__(1024) unsigned char dsm_[];
-  Smem& S = *reinterpret_cast<Smem*>(dsm_);
+  using Tmem = Tmem<kCompact>;
+  constexpr int kDs = Tmem::kDs;
+  Smem<kCompact>& S = *reinterpret_cast<Smem<kCompact>*>(dsm_);
+  constexpr uint32_t kRing = Smem<kCompact>::kRing;
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   if (tid == 0) {
@@ -208,6 +240,8 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
     for (int i = 0; i < 2; ++i) {
       tc05::bar_init(&S.k_full[i], 4);
       tc05::bar_init(&S.k_empty[i], 1);
+    }
+    for (int i = 0; i < 3; ++i) {
       tc05::bar_init(&S.d_empty[i], 4);
       for (int e = 0; e < 2; ++e) tc05::bar_init(&S.d_full[i][e], 1);
     }
@@ -255,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
     tc05::reg_inc<kRegEpi>();
     const int g = warp >> 2, key = 32 * (warp & 3) + lane;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
-    uint32_t nd[2] = {0, 0}, nk = 0;  // phases of d_full[.][g]; key tiles of the CTA
+    uint32_t phases = 0, nk = 0, nu = 0;  // of d_full[.][g], by bit; key tiles and Ds of the CTA
     ScorePiece p;
     for (uint32_t n = 0; next_piece(n, p); ++n) {
       const int tiles = p.t1 - p.t0, cols = p.cols();
@@ -281,20 +315,28 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         if ((kSum || !pair) && (t & 1) != g) continue;
         const int tile = p.t0 + t;
         const bool exact = tile >= p.I();  // a window tile
-        float scale = 0.f, sum = 0.f, old = 0.f;
+        float scale = 0.f, least = 0.f, old = 0.f;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
         int first = 0;                   // the first column that sees the key
         float* at = nullptr;
         bool begun = false;
 #pragma unroll 1
         for (int d = kSum || !pair ? 0 : g; d < (pair && (kSum || g == 1) ? 2 : 1); ++d) {
-          const int D = pair ? d : t & 1;
-          if (!wait(&S.d_full[D][g], nd[D]++)) break;
+          const uint32_t D = (nu + (pair ? 2 * t + d : t)) % kDs;
+          if (!wait(&S.d_full[D][g], phases >> D & 1)) break;
+          phases ^= 1u << D;
           if (!begun) {
             begun = true;
-            scale = S.scale[(nk + t) % 4][key];
+            const uint32_t r = (nk + t) % kRing, word = S.scale[r][key];
+            if (kCompact) {
+              const float2 y = unpack_half(word);
+              scale = y.x, least = y.y;
+            } else {
+              scale = __uint_as_float(word);
+            }
             const int i = kKeys * (exact ? tile - p.I() : tile) + key;
             const int pos = exact ? win_pos(i, p.n, A.sink, A.recent) : A.sink + i;
-            if (scale != 0.f) {
+            if (S.counts[r][warp & 3] >> lane & 1) {
               const int tok = pos - p.pos0 - A.t0;
               first = tok > 0 ? 4 * tok : 0;
               if (kSum) {
@@ -308,19 +350,14 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           const uint32_t tD = tmem + lanes + kColD + 128u * D;
           const int c_lo = kSum ? kKeys * d : cbase;    // the columns' place in the block
           const int n_cols = min(kKeys, cols - c_lo);
-          const float2 scale2 = make_float2(scale, scale);
-#pragma unroll
-          for (int c = 0; c < kKeys / 16; ++c) {
-            if (16 * c >= n_cols) break;
-            uint32_t x[16];
-            tc05::tmem_ld16(tD + 16 * c, x);
-            tc05::tmem_wait_ld();
-            if (16 * (c + 1) >= n_cols) {
-              tc05::fence_before();
-              arrive(&S.d_empty[D]);
-            }
+          const bool masked = __any_sync(0xffffffffu, first > c_lo);
+          auto free_d = [&]() {
+            tc05::fence_before();
+            arrive(&S.d_empty[D]);
+          };
+          // logits of 16 columns, over their references
+          auto logits = [&](int c, const uint32_t* x, float (&y)[16]) {
             const float* r = kSum ? S.ref[0] + c_lo + 16 * c : ref + 16 * c;
-            float y[16];
             if (exact) {
 #pragma unroll
               for (int j = 0; j < 16; j += 4) {
@@ -332,31 +369,71 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
                 y[j + 3] = fmaf(__uint_as_float(x[j + 3]), kLogit, m.w - o.w);
               }
             } else {
+              const float2 scale2 = make_float2(scale, scale), min2 = make_float2(least, least);
 #pragma unroll
               for (int j = 0; j < 16; j += 4) {
                 const float4 f = *reinterpret_cast<const float4*>(&S.factor[c_lo + 16 * c + j]);
                 const float4 m = *reinterpret_cast<const float4*>(r + j);
+                float2 m0 = make_float2(m.x, m.y), m1 = make_float2(m.z, m.w);
+                if (kCompact) {
+                  const float4 q = *reinterpret_cast<const float4*>(&S.sum[c_lo + 16 * c + j]);
+                  m0 = fma2(make_float2(q.x, q.y), min2, m0);
+                  m1 = fma2(make_float2(q.z, q.w), min2, m1);
+                }
                 const float2 f0 = mul2(make_float2(f.x, f.y), scale2), f1 = mul2(make_float2(f.z, f.w), scale2);
-                const float2 u = fma2(make_float2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), f0,
-                                      make_float2(m.x, m.y));
-                const float2 v = fma2(make_float2(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), f1,
-                                      make_float2(m.z, m.w));
+                const float2 u = fma2(make_float2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), f0, m0);
+                const float2 v = fma2(make_float2(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), f1, m1);
                 y[j] = u.x, y[j + 1] = u.y, y[j + 2] = v.x, y[j + 3] = v.y;
               }
             }
-            if (__any_sync(0xffffffffu, first > c_lo + 16 * c)) {
+            if (masked) {
               const int k = first - c_lo - 16 * c;
 #pragma unroll
               for (int j = 0; j < 16; ++j)
                 if (j < k) y[j] = -INFINITY;
             }
-            if constexpr (kSum) {
+          };
+          if constexpr (kSum) {
+            // all of D first: the next products may start
+            uint32_t x[4][32];
 #pragma unroll
-              for (int j = 0; j < 16; ++j) sum += ex2(y[j]);
-            } else {
+            for (int c = 0; c < 4; ++c)
+              if (32 * c < n_cols) tc05::tmem_ld32(tD + 32 * c, x[c]);
+            tc05::tmem_wait_ld();
+#pragma unroll
+            for (int c = 0; c < 4; ++c) loaded(x[c]);
+            free_d();
+#pragma unroll
+            for (int c = 0; c < kKeys / 16; ++c) {
+              if (16 * c >= n_cols) break;
+              float y[16];
+              logits(c, x[c / 2] + 16 * (c & 1), y);
+#pragma unroll
+              for (int j = 0; j < 16; j += 4) {
+                sum.x += ex2(y[j]);
+                sum.y += ex2(y[j + 1]);
+                sum.z += ex2(y[j + 2]);
+                sum.w += ex2(y[j + 3]);
+              }
+            }
+          } else {
+            uint32_t x[2][16];
+            tc05::tmem_ld16(tD, x[0]);
+#pragma unroll
+            for (int c = 0; c < kKeys / 16; ++c) {
+              if (16 * c >= n_cols) break;
+              tc05::tmem_wait_ld();
+              loaded(x[c & 1]);
+              if (16 * (c + 1) < n_cols)
+                tc05::tmem_ld16(tD + 16 * (c + 1), x[(c + 1) & 1]);
+              else
+                free_d();
+              float y[16];
+              logits(c, x[c & 1], y);
               float top = y[0];
 #pragma unroll
-              for (int j = 1; j < 16; ++j) top = fmaxf(top, y[j]);
+              for (int j = 1; j < 15; j += 2) top = fmaxf(top, fmaxf(y[j], y[j + 1]));
+              top = fmaxf(top, y[15]);
               const uint32_t known = set[c / 2] >> (16 * (c & 1)) & 0xffffu;
               if (__any_sync(0xffffffffu, known != 0xffffu || top > kSlack)) {
                 // columns without a reference, or with logits far above it: the warp's
@@ -380,10 +457,11 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           }
         }
         if (dead) break;
-        if (kSum && scale != 0.f) *at = old + sum;
+        if (kSum && at) *at = old + ((sum.x + sum.y) + (sum.z + sum.w));
       }
       if (dead) break;
       nk += tiles;
+      nu += pair ? 2 * tiles : tiles;
       if constexpr (!kSum) {
         // over the warp's keys: 32 columns a time, each lane ends with one's sum
 #pragma unroll
@@ -423,17 +501,19 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
     // --------------------------------------------------------------- keys
     // Thread = key.  A's row in tensor memory: 64 columns of hi parts, 64 of lo.
     tc05::reg_dec<kRegKey>();
-    const int quarter = warp & 3, key = tid & 127, ms = meta_stride(A.compact);
+    constexpr int ms = meta_stride(kCompact);
+    const int quarter = warp & 3, key = tid & 127;
     const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
     uint32_t nk = 0, raws = 0;
     ScorePiece p;
     for (uint32_t n = 0; next_piece(n, p); ++n) {
       for (int tile = p.t0; tile < p.t1; ++tile, ++nk) {
-        const uint32_t s = nk & 1, tK = tmem + lanes + kColK + 128u * s;
-        float scale = 0.f;
+        const uint32_t s = nk & 1, tK = tmem + lanes + Tmem::kColK + Tmem::kKeyCols * s;
+        bool ok;
+        uint32_t scale = 0u;
         if (tile < p.I()) {
           const int i = kKeys * tile + key;
-          bool ok = i < p.n_int;
+          ok = i < p.n_int;
           if (ok) {
             const int page = __ldcg(A.bt + (size_t)p.b * A.max_pages + (A.sink + i) / kPage);
             ok = page >= 0 && page < A.num_pages;
@@ -444,33 +524,36 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           ++raws;
           const uint8_t* raw = S.raw[r][key / kPage];
           const int slot = key % kPage;
-          uint4 mm;
-          if (A.compact)
-            mm.x = mm.y = mm.z = mm.w = *reinterpret_cast<const uint32_t*>(raw + 512 + ms * slot);
-          else
-            mm = *reinterpret_cast<const uint4*>(raw + 512 + ms * slot);
-          // the four values of each group, over a power of two above the largest
-          const uint32_t pairs[4] = {mm.x, mm.y, mm.z, mm.w};
-          float top = 0.f;
+          // the four values of each group, hi and lo; the codes themselves
+          uint32_t hi[kCompact ? 1 : 4][2], lo[kCompact ? 1 : 4][2];
+          if constexpr (kCompact) {
+            scale = *reinterpret_cast<const uint32_t*>(raw + 512 + ms * slot);
+            hi[0][0] = 0x3c000000u;
+            hi[0][1] = 0x42004000u;
+          } else {
+            const uint4 mm = *reinterpret_cast<const uint4*>(raw + 512 + ms * slot);
+            // over a power of two above the largest
+            const uint32_t pairs[4] = {mm.x, mm.y, mm.z, mm.w};
+            float top = 0.f;
 #pragma unroll
-          for (int G = 0; G < 4; ++G) {
-            const float2 y = unpack_half(pairs[G]);
-            top = fmaxf(top, fmaxf(fabsf(y.y), fabsf(fmaf(3.f, y.x, y.y))));
-          }
-          const int E = min(max((int)(__float_as_uint(top) >> 23) - 126, -60), 60);
-          const float down = __uint_as_float((uint32_t)(127 - E) << 23);
-          if (ok) scale = __uint_as_float((uint32_t)(127 + E) << 23);
-          uint32_t hi[4][2], lo[4][2];
+            for (int G = 0; G < 4; ++G) {
+              const float2 y = unpack_half(pairs[G]);
+              top = fmaxf(top, fmaxf(fabsf(y.y), fabsf(fmaf(3.f, y.x, y.y))));
+            }
+            const int E = min(max((int)(__float_as_uint(top) >> 23) - 126, -60), 60);
+            const float down = __uint_as_float((uint32_t)(127 - E) << 23);
+            scale = (uint32_t)(127 + E) << 23;
 #pragma unroll
-          for (int G = 0; G < 4; ++G) {
-            const float2 y = unpack_half(pairs[G]);
-            const float sc = y.x * down, mn = y.y * down;
+            for (int G = 0; G < 4; ++G) {
+              const float2 y = unpack_half(pairs[G]);
+              const float sc = y.x * down, mn = y.y * down;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float a = fmaf((float)(2 * e), sc, mn), b = fmaf((float)(2 * e + 1), sc, mn);
-              hi[G][e] = pack_half(a, b);
-              const float2 z = unpack_half(hi[G][e]);
-              lo[G][e] = pack_half(a - z.x, b - z.y);
+              for (int e = 0; e < 2; ++e) {
+                const float a = fmaf((float)(2 * e), sc, mn), b = fmaf((float)(2 * e + 1), sc, mn);
+                hi[G][e] = pack_half(a, b);
+                const float2 z = unpack_half(hi[G][e]);
+                lo[G][e] = pack_half(a - z.x, b - z.y);
+              }
             }
           }
           if (nk >= 2 && !wait(&S.k_empty[s], nk / 2 - 1)) break;
@@ -493,11 +576,13 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
               }
               uint32_t y[8];
 #pragma unroll
-              for (int e = 0; e < 8; ++e) y[e] = __byte_perm(hi[e / 2][0], hi[e / 2][1], pick[e]);
+              for (int e = 0; e < 8; ++e) y[e] = __byte_perm(hi[kCompact ? 0 : e / 2][0], hi[kCompact ? 0 : e / 2][1], pick[e]);
               tc05::tmem_st8(tK + 16 * part + 8 * v, y);
+              if constexpr (!kCompact) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) y[e] = __byte_perm(lo[e / 2][0], lo[e / 2][1], pick[e]);
-              tc05::tmem_st8(tK + 64 + 16 * part + 8 * v, y);
+                for (int e = 0; e < 8; ++e) y[e] = __byte_perm(lo[e / 2][0], lo[e / 2][1], pick[e]);
+                tc05::tmem_st8(tK + 64 + 16 * part + 8 * v, y);
+              }
             }
           }
           arrive(&S.raw_empty[r]);
@@ -505,8 +590,8 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           const int i = kKeys * (tile - p.I()) + key;
           if (nk >= 2 && !wait(&S.k_empty[s], nk / 2 - 1)) break;
           const uint4* src = nullptr;
-          if (i < p.n_win) {
-            scale = 1.f;
+          ok = i < p.n_win;
+          if (ok) {
             const int row = win_row(win_pos(i, p.n, A.sink, A.recent), A.sink, A.recent);
             src = reinterpret_cast<const uint4*>(
                 A.win.win + ((((size_t)p.slot * A.h_kv + p.h) * 2) * (A.sink + A.recent) + row) * kD);
@@ -522,7 +607,9 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
             tc05::tmem_st16(tK + 16 * part, y);
           }
         }
-        S.scale[nk % 4][key] = scale;
+        S.scale[nk % kRing][key] = scale;
+        const uint32_t counts = __ballot_sync(0xffffffffu, ok);
+        if (lane == 0) S.counts[nk % kRing][quarter] = counts;
         tc05::tmem_wait_st();
         tc05::fence_before();
         arrive(&S.k_full[s]);
@@ -541,11 +628,12 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         if (lane == 0) {
           const uint8_t* src = qop_of(A, p.seg);
           const int kinds = win ? 3 : 2;
-          tc05::bar_arrive_expect_tx(&S.q_full, kinds * bytes + (kSum ? 3 : 2) * line);
+          tc05::bar_arrive_expect_tx(&S.q_full, kinds * bytes + (2 + kSum + kCompact) * line);
           for (int i = 0; i < kinds; ++i) tc05::bulk_g2s(S.q[i], src + (size_t)A.cols * 256 * i, bytes, &S.q_full);
           const uint8_t* c = src + (size_t)A.cols * 256 * kinds;
           tc05::bulk_g2s(S.factor, c, line, &S.q_full);
           tc05::bulk_g2s(S.off, c + (size_t)A.cols * 4, line, &S.q_full);
+          if (kCompact) tc05::bulk_g2s(S.sum, c + (size_t)A.cols * 8, line, &S.q_full);
           if (kSum) tc05::bulk_g2s(S.ref[0], A.lse + (size_t)p.seg * A.cols, line, &S.q_full);
         }
         __syncwarp();
@@ -562,12 +650,12 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           const int ahead = request(tile + 1);
           if (raws >= kRaw && !wait(&S.raw_empty[r], raws / kRaw - 1)) break;
           const bool in = page >= 0 && page < A.num_pages;
-          const uint32_t pairs = 16u * meta_stride(A.compact);
+          constexpr uint32_t pairs = 16u * meta_stride(kCompact);
           const uint32_t pages = __popc(__ballot_sync(0xffffffffu, in) & 0xffu);
           if (lane == 0) tc05::bar_arrive_expect_tx(&S.raw_full[r], pages * (512u + pairs));
           __syncwarp();
           if (in) {
-            const uint8_t* src = A.pool + ((size_t)page * A.h_kv + p.h) * chunk_bytes(A.compact);
+            const uint8_t* src = A.pool + ((size_t)page * A.h_kv + p.h) * chunk_bytes(kCompact);
             const bool codes = lane < 8;
             tc05::bulk_g2s(S.raw[r][lane & 7] + (codes ? 0 : 512),
                            src + (codes ? OPTR_K_CODES_OFFSET : OPTR_K_META_OFFSET), codes ? 512u : pairs,
@@ -586,7 +674,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
     } else if (warp == kMmaWarp) {
       // ----------------------------------------------------------- products
       const uint32_t sq = tc05::smem_addr(S.q[0]);
-      uint32_t nk = 0, nd[2] = {0, 0};
+      uint32_t nk = 0, nu = 0;
       bool used = false;
       ScorePiece p;
       for (uint32_t n = 0; next_piece(n, p); ++n) {
@@ -595,25 +683,28 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         if (!wait(&S.q_full, n)) break;
         used = true;
         for (int t = 0; t < p.t1 - p.t0; ++t, ++nk) {
-          const uint32_t s = nk & 1, a = tmem + kColK + 128u * s;
+          const uint32_t s = nk & 1, a = tmem + Tmem::kColK + Tmem::kKeyCols * s;
           const bool exact = p.t0 + t >= p.I();
           if (!wait(&S.k_full[s], nk / 2)) break;
           for (int d = 0; d < (pair ? 2 : 1); ++d) {
-            const int D = pair ? d : t & 1;
+            const uint32_t D = nu % kDs;
             const uint32_t id = tc05::idesc_f16(128, pair && d ? N - kKeys : min(N, kKeys));
-            if (nd[D] > 0 && !wait(&S.d_empty[D], nd[D] - 1)) break;
-            ++nd[D];
+            if (nu >= kDs && !wait(&S.d_empty[D], nu / kDs - 1)) break;
+            ++nu;
             const uint32_t out = tmem + kColD + 128u * D, b = sq + (uint32_t)d * (kKeys * 256);
             constexpr uint32_t kPart = kBlockCols * 256;
             if (exact) {
               tc05::mma128_ts<16>(out, a, tc05::smem_desc(b + 2 * kPart, 128, 2048), id | tc05::kIdescBf16, 0);
+            } else if (kCompact) {
+              tc05::mma128_ts<16>(out, a, tc05::smem_desc(b + kPart, 128, 2048), id, 0);
+              tc05::mma128_ts<16>(out, a, tc05::smem_desc(b, 128, 2048), id, 1);
             } else {
               // the small parts first: a third of the steps round at the sum's size
               tc05::mma128_ts<16>(out, a, tc05::smem_desc(b + kPart, 128, 2048), id, 0);
               tc05::mma128_ts<16>(out, a + 64, tc05::smem_desc(b, 128, 2048), id, 1);
               tc05::mma128_ts<16>(out, a, tc05::smem_desc(b, 128, 2048), id, 1);
             }
-            tc05::mma_commit_warp(&S.d_full[D][kSum ? t & 1 : D]);
+            tc05::mma_commit_warp(&S.d_full[D][kSum || !pair ? t & 1 : d]);
           }
           if (dead) break;
           tc05::mma_commit_warp(&S.k_empty[s]);
@@ -757,16 +848,21 @@ extern "C" optr_status optr_kv_score_win(const optr_params* p, const void* q, in
               pool, num_pages, w, p->cfg.sink, p->cfg.recent, p->cfg.h_kv, p->cfg.group == 4 * kG, p->R_k, p->mu,
               score, n_score, p->err, l.cols, ws, (float2*)(ws + l.part), (float*)(ws + l.lse), l.W};
   if (few_tokens(p, B, max_new, max_pages)) return cuda_status(launch_score_few(p, A, ws, stream));
-  for (auto fn : {logit_kernel<false>, logit_kernel<true>})
-    if (ensure_dynamic_smem(reinterpret_cast<const void*>(fn), sizeof(Smem)) != cudaSuccess) return OPTR_ERR_CUDA;
+  auto first = A.compact ? logit_kernel<false, true> : logit_kernel<false, false>;
+  auto second = A.compact ? logit_kernel<true, true> : logit_kernel<true, false>;
+  const size_t smem = A.compact ? sizeof(Smem<true>) : sizeof(Smem<false>);
+  if (ensure_dynamic_smem(reinterpret_cast<const void*>(query_kernel), sizeof(QuerySmem)) != cudaSuccess ||
+      ensure_dynamic_smem(reinterpret_cast<const void*>(first), smem) != cudaSuccess ||
+      ensure_dynamic_smem(reinterpret_cast<const void*>(second), smem) != cudaSuccess)
+    return OPTR_ERR_CUDA;
   const unsigned segs = (unsigned)B * p->cfg.h_kv;
   // a block of tokens a time, in stream order: the sums do not depend on chance
   cudaError_t e = cudaSuccess;
   for (A.t0 = 0; A.t0 < max_new && e == cudaSuccess; A.t0 += kTok) {
-    e = launch_pdl(query_kernel, dim3((l.cols + kRotCols - 1) / kRotCols, segs), dim3(kRotThreads), 0, stream, A);
-    if (e == cudaSuccess) e = launch_pdl(logit_kernel<false>, dim3(l.W), dim3(kThreads), sizeof(Smem), stream, A);
+    e = launch_pdl(query_kernel, dim3((l.cols + kRotCols - 1) / kRotCols, segs), dim3(kRotThreads), sizeof(QuerySmem), stream, A);
+    if (e == cudaSuccess) e = launch_pdl(first, dim3(l.W), dim3(kThreads), smem, stream, A);
     if (e == cudaSuccess) e = launch_pdl(normaliser_kernel, dim3(segs), dim3(1024), 0, stream, A);
-    if (e == cudaSuccess) e = launch_pdl(logit_kernel<true>, dim3(l.W), dim3(kThreads), sizeof(Smem), stream, A);
+    if (e == cudaSuccess) e = launch_pdl(second, dim3(l.W), dim3(kThreads), smem, stream, A);
   }
   return cuda_status(e);
 }
