@@ -16,15 +16,18 @@
 //
 // Rounding.  The sums are float32, and a weight moves by what its logit does: rounding
 // queries or keys to 16 bits would move it by some 3e-4.  So both go in as fp16 hi + lo
-// parts (22 bits; queries over a power of two by row, keys over one by key), and a tile
+// parts (22 bits; queries over a power of two by block, keys over one by key), and a tile
 // takes the products hi hi + hi lo + lo hi.  A group of a slot has four values, so the
 // parts of 16 values are computed in float32 and the codes pick among them by byte
-// permutes.  Window keys and their queries are bf16 as they are, one product.
+// permutes.  With one pair a slot the codes go in as they are, its scale and minimum are
+// the epilogue's, and two products do.  Window keys and their queries are bf16 as they are, one product.
+#include "cluster.cuh"
 #include "f32x2.cuh"
 #include "score.cuh"
 #include "tc05.cuh"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace optr {
 namespace {
@@ -51,8 +54,26 @@ constexpr int kRotCols = 32;  // columns of a CTA: 8 tokens
 // whole, before what the call waits for: its 128 rows' latencies are one.
 struct QuerySmem {
   float R[kD][kD], q[kRotCols][kD];
-  float top[4][kRotCols], dot[4][kRotCols], sum[4][kRotCols];
+  float top[4][kRotCols], dot[4][kRotCols], sum[4][kRotCols], size[4][kRotCols];
+  float most[2];  // the CTA's largest element, and sum of magnitudes
 };
+
+// Over the warp's lanes, of 16 values each: value lane / 2 (in both lanes).
+template <typename Join>
+__device__ __forceinline__ float over_lanes(float (&x)[16], Join join) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 16; o > 1; o >>= 1) {
+    const bool upper = lane & o;
+#pragma unroll
+    for (int j = 0; j < o / 2; ++j) {
+      const float mine = upper ? x[j + o / 2] : x[j], other = upper ? x[j] : x[j + o / 2];
+      x[j] = join(mine, __shfl_xor_sync(0xffffffffu, other, o));
+    }
+  }
+  return join(x[0], __shfl_xor_sync(0xffffffffu, x[0], 1));
+}
+
 __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constant__ ScoreArgs A) {
   extern __shared__ __align__(1024) unsigned char dsm_[];
   QuerySmem& S = *reinterpret_cast<QuerySmem*>(dsm_);
@@ -67,79 +88,112 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
   if (blockIdx.x == 0 && seg == 0 && A.t0 == 0 && tid < 32) report_sequences(A);
   const ScoreSeq s = score_seq(A, b);
   const int c0 = kRotCols * blockIdx.x, N = (4 * s.rows + 15) / 16 * 16;
-  if (c0 >= N || seq_tiles(s) == 0) {
+  if (seq_tiles(s) == 0) {  // the whole cluster
     cp_async_wait<0>();
     return;
   }
   const bool win = A.win.win != nullptr;
   uint8_t* out = qop_of(A, seg);
-  for (int i = tid; i < kRotCols * kD / 8; i += kRotThreads) {
-    const int c = i / (kD / 8), x = 8 * (i % (kD / 8)), tok = (c0 + c) / 4;
-    uint4 y = make_uint4(0u, 0u, 0u, 0u);
-    if (tok < s.rows)
-      y = __ldcg(reinterpret_cast<const uint4*>(
-          A.q + (((size_t)s.c0 + A.t0 + tok) * A.h_kv + h) * (4 * kD) + (c & 3) * kD + x));
-    const uint32_t word[4] = {y.x, y.y, y.z, y.w};
+  constexpr int kMine = kRotCols / 2;
+  float acc[kMine] = {};
+  if (c0 < N) {
+    for (int i = tid; i < kRotCols * kD / 8; i += kRotThreads) {
+      const int c = i / (kD / 8), x = 8 * (i % (kD / 8)), tok = (c0 + c) / 4;
+      uint4 y = make_uint4(0u, 0u, 0u, 0u);
+      if (tok < s.rows)
+        y = __ldcg(reinterpret_cast<const uint4*>(
+            A.q + (((size_t)s.c0 + A.t0 + tok) * A.h_kv + h) * (4 * kD) + (c & 3) * kD + x));
+      const uint32_t word[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      q[c][x + 2 * e] = __uint_as_float(word[e] << 16);
-      q[c][x + 2 * e + 1] = __uint_as_float(word[e] & 0xffff0000u);
+      for (int e = 0; e < 4; ++e) {
+        q[c][x + 2 * e] = __uint_as_float(word[e] << 16);
+        q[c][x + 2 * e + 1] = __uint_as_float(word[e] & 0xffff0000u);
+      }
+      if (win && c0 + c < N)
+        *reinterpret_cast<uint4*>(out + (size_t)A.cols * 512 + operand_offset(c0 + c, x)) = y;
     }
-    if (win && c0 + c < N)
-      *reinterpret_cast<uint4*>(out + (size_t)A.cols * 512 + operand_offset(c0 + c, x)) = y;
   }
   cp_async_wait<0>();
   __syncthreads();
-  constexpr int kMine = kRotCols / 2;
-  float acc[kMine] = {};
+  if (c0 < N) {
 #pragma unroll 4
-  for (int i = 0; i < kD; i += 4) {
-    const float r[4] = {S.R[i][k], S.R[i + 1][k], S.R[i + 2][k], S.R[i + 3][k]};
+    for (int i = 0; i < kD; i += 4) {
+      const float r[4] = {S.R[i][k], S.R[i + 1][k], S.R[i + 2][k], S.R[i + 3][k]};
 #pragma unroll
-    for (int c = 0; c < kMine; ++c) {
-      const float4 x = *reinterpret_cast<const float4*>(&q[kMine * part + c][i]);
-      acc[c] = fmaf(x.x, r[0], acc[c]);
-      acc[c] = fmaf(x.y, r[1], acc[c]);
-      acc[c] = fmaf(x.z, r[2], acc[c]);
-      acc[c] = fmaf(x.w, r[3], acc[c]);
+      for (int c = 0; c < kMine; ++c) {
+        const float4 x = *reinterpret_cast<const float4*>(&q[kMine * part + c][i]);
+        acc[c] = fmaf(x.x, r[0], acc[c]);
+        acc[c] = fmaf(x.y, r[1], acc[c]);
+        acc[c] = fmaf(x.z, r[2], acc[c]);
+        acc[c] = fmaf(x.w, r[3], acc[c]);
+      }
     }
-  }
-  const float mu = __ldg(A.mu + (size_t)h * kD + k);
+    const float mu = __ldg(A.mu + (size_t)h * kD + k);
+    auto add = [](float x, float y) { return x + y; };
+    float x[kMine];
+    const int at = kMine * part + (lane >> 1);
 #pragma unroll
-  for (int c = 0; c < kMine; ++c) {
-    float m = fabsf(acc[c]), d = q[kMine * part + c][k] * mu, t = acc[c];
+    for (int c = 0; c < kMine; ++c) x[c] = fabsf(acc[c]);
+    S.top[quarter][at] = over_lanes(x, [](float x, float y) { return fmaxf(x, y); });
+#pragma unroll
+    for (int c = 0; c < kMine; ++c) x[c] = fabsf(acc[c]);
+    S.size[quarter][at] = over_lanes(x, add);
+#pragma unroll
+    for (int c = 0; c < kMine; ++c) x[c] = acc[c];
+    S.sum[quarter][at] = over_lanes(x, add);
+#pragma unroll
+    for (int c = 0; c < kMine; ++c) x[c] = q[kMine * part + c][k] * mu;
+    S.dot[quarter][at] = over_lanes(x, add);
+  }
+  __syncthreads();
+  auto quarters = [&](const float (&x)[4][kRotCols], int n) { return (x[0][n] + x[1][n]) + (x[2][n] + x[3][n]); };
+  if (tid < 32) {
+    float m = 0.f, l = 0.f;
+    if (c0 < N) {
+      m = fmaxf(fmaxf(S.top[0][lane], S.top[1][lane]), fmaxf(S.top[2][lane], S.top[3][lane]));
+      l = quarters(S.size, lane);
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      d += __shfl_xor_sync(0xffffffffu, d, o);
-      t += __shfl_xor_sync(0xffffffffu, t, o);
+      l = fmaxf(l, __shfl_xor_sync(0xffffffffu, l, o));
     }
-    if (lane == 0) {
-      S.top[quarter][kMine * part + c] = m;
-      S.dot[quarter][kMine * part + c] = d;
-      S.sum[quarter][kMine * part + c] = t;
-    }
+    if (lane == 0) S.most[0] = m, S.most[1] = l;
   }
-  __syncthreads();
-  float* factor = reinterpret_cast<float*>(out + (size_t)A.cols * (win ? 768 : 512));
-#pragma unroll
-  for (int c = 0; c < kMine; ++c) {
-    const int n = kMine * part + c;
-    const float m = fmaxf(fmaxf(S.top[0][n], S.top[1][n]), fmaxf(S.top[2][n], S.top[3][n]));
-    // the row's largest at 2^13 .. 2^14, so that lo parts are normal fp16 down to 2^-17 of it
+  const int cs = gridDim.x;  // a cluster has the block's columns
+  if (cs > 1) cluster_barrier(); else __syncthreads();
+  float m = S.most[0], l = S.most[1];
+  if (cs > 1) {
+    for (int r = 0; r < cs; ++r) {
+      m = fmaxf(m, __uint_as_float(cluster_ld32(&S.most[0], r)));
+      l = fmaxf(l, __uint_as_float(cluster_ld32(&S.most[1], r)));
+    }
+    cluster_arrive();  // no CTA leaves while its shared memory may be read
+  }
+  if (c0 < N) {
+    // The block's largest at 2^13 .. 2^14: an element has 22 bits down to 2^-17 of that, and
+    // below it is known to 2^-39 of the largest.
     const int E = m > 0.f ? max(-100, min(100, 13 - ((int)(__float_as_uint(m) >> 23) - 127))) : 0;
-    const float x = acc[c] * __uint_as_float((uint32_t)(127 + E) << 23);
-    const __half hi = __float2half_rn(x), lo = __float2half_rn(x - __half2float(hi));
-    if (c0 + n >= N) break;
-    const int at = operand_offset(c0 + n, key_place(k));
-    *reinterpret_cast<__half*>(out + at) = hi;
-    *reinterpret_cast<__half*>(out + (size_t)A.cols * 256 + at) = lo;
-    if (k == 0) {
-      factor[c0 + n] = __uint_as_float((uint32_t)(127 - E) << 23) * kLogit;
-      factor[A.cols + c0 + n] = kLogit * ((S.dot[0][n] + S.dot[1][n]) + (S.dot[2][n] + S.dot[3][n]));
-      factor[2 * A.cols + c0 + n] = kLogit * ((S.sum[0][n] + S.sum[1][n]) + (S.sum[2][n] + S.sum[3][n]));
+    float* line = reinterpret_cast<float*>(out + (size_t)A.cols * (win ? 768 : 512));
+#pragma unroll
+    for (int c = 0; c < kMine; ++c) {
+      const int n = kMine * part + c;
+      const float x = acc[c] * __uint_as_float((uint32_t)(127 + E) << 23);
+      const __half hi = __float2half_rn(x), lo = __float2half_rn(x - __half2float(hi));
+      if (c0 + n >= N) break;
+      const int at = operand_offset(c0 + n, key_place(k));
+      *reinterpret_cast<__half*>(out + at) = hi;
+      *reinterpret_cast<__half*>(out + (size_t)A.cols * 256 + at) = lo;
+      if (k == 0) {
+        line[c0 + n] = kLogit * quarters(S.dot, n);
+        line[A.cols + c0 + n] = kLogit * quarters(S.sum, n);
+      }
     }
+    if (blockIdx.x == 0 && tid == 0)
+      *reinterpret_cast<float4*>(line + 2 * A.cols) =
+          make_float4(__uint_as_float((uint32_t)(127 - E) << 23) * kLogit, kLogit * l, 0.f, 0.f);
   }
+  if (cs > 1) cluster_wait();
 }
 
 // -------------------------------------------------------------- logits
@@ -160,16 +214,18 @@ struct Tmem {
 constexpr int kRaw = 3;        // tiles of records on the way
 constexpr int kPieces = 3;     // pieces found ahead
 constexpr int kConsumers = 14; // warps that take the pieces
-constexpr float kSlack = 60.f; // a column's logits may pass its reference by 2^60
+constexpr float kSlack = 60.f; // a column's logits may pass its reference by 2^60 unseen,
+constexpr float kMost = 100.f; // and are looked at where they may by 2^100
 
 template <bool kCompact>
 struct Smem {
   uint8_t q[3][kBlockCols * 256];    // hi, lo, as given
   uint8_t raw[kRaw][kKeys / kPage][512 + 16 * meta_stride(kCompact)];  // a page's key codes and pairs
-  alignas(16) float factor[kBlockCols], off[kBlockCols], sum[kCompact ? kBlockCols : 4];
+  alignas(16) float off[kBlockCols], sum[kCompact ? kBlockCols : 4];
+  float4 block;  // the block's factor, and its largest sum of magnitudes
   // minus the columns' references: pass 0 by warp, pass 1 the normalisers
   alignas(16) float ref[8][kKeys];
-  float2 meet[8][kKeys];             // pass 0: the warps' parts of a piece
+  float2 meet[8][kKeys];             // pass 0: the warps' parts of a piece (and, on the way, factors)
   // A key's power of two, or its pair, and whether it counts.  Read between a tile's
   // logits and its last D being free; written for tile t + kRing once the products of
   // t + kRing - 2 are done, which waited for the Ds before their own.
@@ -297,25 +353,24 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
       if (!wait(&S.q_full, n)) break;
       float* ref = kSum ? S.ref[0] : S.ref[warp];
       const int cbase = !kSum && pair ? kKeys * g : 0;  // first column of the group's
+      const float factor = S.block.x, size = S.block.y;
       float acc[kSum ? 1 : kKeys];
-      uint32_t set[kSum ? 1 : 4];
+      uint32_t known = 0;     // bit c: column 16 c + lane % 16 has a reference, or is none
+      float least = INFINITY; // no reference has been lower
       if constexpr (!kSum) {
 #pragma unroll
         for (int c = 0; c < kKeys; ++c) acc[c] = 0.f;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          // columns that are none need no reference
-          const int some = cols - cbase - 32 * c;
-          set[c] = some >= 32 ? 0u : some <= 0 ? ~0u : ~0u << some;
-          ref[32 * c + lane] = 0.f;
-        }
+        for (int c = 0; c < 4; ++c) ref[32 * c + lane] = 0.f;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) known |= (cbase + 16 * c + (lane & 15) >= cols ? 1u : 0u) << c;
         __syncwarp();
       }
       for (int t = 0; t < tiles; ++t) {
         if ((kSum || !pair) && (t & 1) != g) continue;
         const int tile = p.t0 + t;
         const bool exact = tile >= p.I();  // a window tile
-        float scale = 0.f, least = 0.f, old = 0.f;
+        float scale = 0.f, low = 0.f, old = 0.f;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
         int first = 0;                   // the first column that sees the key
         float* at = nullptr;
@@ -330,9 +385,9 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
             const uint32_t r = (nk + t) % kRing, word = S.scale[r][key];
             if (kCompact) {
               const float2 y = unpack_half(word);
-              scale = y.x, least = y.y;
+              scale = y.x * factor, low = y.y;
             } else {
-              scale = __uint_as_float(word);
+              scale = __uint_as_float(word) * factor;
             }
             const int i = kKeys * (exact ? tile - p.I() : tile) + key;
             const int pos = exact ? win_pos(i, p.n, A.sink, A.recent) : A.sink + i;
@@ -355,43 +410,47 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
             tc05::fence_before();
             arrive(&S.d_empty[D]);
           };
-          // logits of 16 columns, over their references
-          auto logits = [&](int c, const uint32_t* x, float (&y)[16]) {
+          // logits of 16 columns, over their references.  What a tile is stands in the
+          // type, since branches within made this loop half as long again: it has to
+          // stay small in the instruction cache.
+          auto logits = [&](int c, const uint32_t* x, float (&y)[16], auto exact_tile, auto masked_tile) {
             const float* r = kSum ? S.ref[0] + c_lo + 16 * c : ref + 16 * c;
-            if (exact) {
+            const float2 scale2 = make_float2(scale, scale), low2 = make_float2(low, low);
 #pragma unroll
-              for (int j = 0; j < 16; j += 4) {
+            for (int j = 0; j < 16; j += 4) {
+              const float4 m = *reinterpret_cast<const float4*>(r + j);
+              if constexpr (decltype(exact_tile)::value) {
                 const float4 o = *reinterpret_cast<const float4*>(&S.off[c_lo + 16 * c + j]);
-                const float4 m = *reinterpret_cast<const float4*>(r + j);
                 y[j] = fmaf(__uint_as_float(x[j]), kLogit, m.x - o.x);
                 y[j + 1] = fmaf(__uint_as_float(x[j + 1]), kLogit, m.y - o.y);
                 y[j + 2] = fmaf(__uint_as_float(x[j + 2]), kLogit, m.z - o.z);
                 y[j + 3] = fmaf(__uint_as_float(x[j + 3]), kLogit, m.w - o.w);
-              }
-            } else {
-              const float2 scale2 = make_float2(scale, scale), min2 = make_float2(least, least);
-#pragma unroll
-              for (int j = 0; j < 16; j += 4) {
-                const float4 f = *reinterpret_cast<const float4*>(&S.factor[c_lo + 16 * c + j]);
-                const float4 m = *reinterpret_cast<const float4*>(r + j);
+              } else {
                 float2 m0 = make_float2(m.x, m.y), m1 = make_float2(m.z, m.w);
-                if (kCompact) {
+                if constexpr (kCompact) {
                   const float4 q = *reinterpret_cast<const float4*>(&S.sum[c_lo + 16 * c + j]);
-                  m0 = fma2(make_float2(q.x, q.y), min2, m0);
-                  m1 = fma2(make_float2(q.z, q.w), min2, m1);
+                  m0 = fma2(make_float2(q.x, q.y), low2, m0);
+                  m1 = fma2(make_float2(q.z, q.w), low2, m1);
                 }
-                const float2 f0 = mul2(make_float2(f.x, f.y), scale2), f1 = mul2(make_float2(f.z, f.w), scale2);
-                const float2 u = fma2(make_float2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), f0, m0);
-                const float2 v = fma2(make_float2(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), f1, m1);
-                y[j] = u.x, y[j + 1] = u.y, y[j + 2] = v.x, y[j + 3] = v.y;
+                m0 = fma2(make_float2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), scale2, m0);
+                m1 = fma2(make_float2(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), scale2, m1);
+                y[j] = m0.x, y[j + 1] = m0.y, y[j + 2] = m1.x, y[j + 3] = m1.y;
               }
             }
-            if (masked) {
+            if constexpr (decltype(masked_tile)::value) {
               const int k = first - c_lo - 16 * c;
 #pragma unroll
               for (int j = 0; j < 16; ++j)
                 if (j < k) y[j] = -INFINITY;
             }
+          };
+          auto by_tile = [&](auto f) {
+            if (exact)
+              f(std::true_type{}, std::true_type{});
+            else if (masked)
+              f(std::false_type{}, std::true_type{});
+            else
+              f(std::false_type{}, std::false_type{});
           };
           if constexpr (kSum) {
             // all of D first: the next products may start
@@ -403,57 +462,89 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
 #pragma unroll
             for (int c = 0; c < 4; ++c) loaded(x[c]);
             free_d();
+            by_tile([&](auto exact_tile, auto masked_tile) {
 #pragma unroll
-            for (int c = 0; c < kKeys / 16; ++c) {
-              if (16 * c >= n_cols) break;
-              float y[16];
-              logits(c, x[c / 2] + 16 * (c & 1), y);
+              for (int c = 0; c < kKeys / 16; ++c) {
+                if (16 * c >= n_cols) break;
+                float y[16];
+                logits(c, x[c / 2] + 16 * (c & 1), y, exact_tile, masked_tile);
 #pragma unroll
-              for (int j = 0; j < 16; j += 4) {
-                sum.x += ex2(y[j]);
-                sum.y += ex2(y[j + 1]);
-                sum.z += ex2(y[j + 2]);
-                sum.w += ex2(y[j + 3]);
+                for (int j = 0; j < 16; j += 4) {
+                  sum.x += ex2(y[j]);
+                  sum.y += ex2(y[j + 1]);
+                  sum.z += ex2(y[j + 2]);
+                  sum.w += ex2(y[j + 3]);
+                }
               }
-            }
+            });
           } else {
-            uint32_t x[2][16];
-            tc05::tmem_ld16(tD, x[0]);
-#pragma unroll
-            for (int c = 0; c < kKeys / 16; ++c) {
-              if (16 * c >= n_cols) break;
-              tc05::tmem_wait_ld();
-              loaded(x[c & 1]);
-              if (16 * (c + 1) < n_cols)
-                tc05::tmem_ld16(tD + 16 * (c + 1), x[(c + 1) & 1]);
-              else
-                free_d();
-              float y[16];
-              logits(c, x[c & 1], y);
-              float top = y[0];
-#pragma unroll
-              for (int j = 1; j < 15; j += 2) top = fmaxf(top, fmaxf(y[j], y[j + 1]));
-              top = fmaxf(top, y[15]);
-              const uint32_t known = set[c / 2] >> (16 * (c & 1)) & 0xffffu;
-              if (__any_sync(0xffffffffu, known != 0xffffu || top > kSlack)) {
-                // columns without a reference, or with logits far above it: the warp's
-                // largest becomes it
+            // Columns without a reference, and such whose logits pass theirs by far, take the
+            // warp's largest.  That the logits cannot, of keys whose values are top at most, the
+            // queries' sums of magnitudes say; window keys are always looked at.
+            const float top = kCompact ? fmaxf(fabsf(low), fabsf(fmaf(3.f, scale / factor, low))) : scale / factor;
+            if (__any_sync(0xffffffffu, exact || known != 0xffu || (first < cols && size * top > least + kMost))) {
+              float* by = reinterpret_cast<float*>(S.meet[warp]);  // by what a column's sum shrinks
+              bool shrink = false;
+#pragma unroll 1
+              for (int c = 0; c < kKeys / 16; ++c) {
+                if (16 * c >= n_cols) break;
+                uint32_t x[16];
+                tc05::tmem_ld16(tD + 16 * c, x);
+                tc05::tmem_wait_ld();
+                loaded(x);
+                float y[16], m = -INFINITY;
+                if (exact)
+                  logits(c, x, y, std::true_type{}, std::true_type{});
+                else
+                  logits(c, x, y, std::false_type{}, std::true_type{});
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                  const float m = warp_largest(y[j]);
-                  const bool fresh = !(known >> j & 1);
-                  if (m > kSlack || (fresh && m > -INFINITY)) {
-                    acc[16 * c + j] = fresh ? 0.f : acc[16 * c + j] * ex2(-m);
-                    y[j] -= m;
-                    set[c / 2] |= 1u << (16 * (c & 1) + j);
-                    if (lane == 0) ref[16 * c + j] -= m;
-                  }
+                  const float z = warp_largest(y[j]);
+                  if ((lane & 15) == j) m = z;
+                }
+                const bool fresh = !(known >> c & 1);
+                const bool moves = m > (fresh ? -INFINITY : kSlack);
+                if (moves) {
+                  known |= 1u << c;
+                  least = fminf(least, m - ref[16 * c + (lane & 15)]);
+                }
+                __syncwarp();
+                if (lane < 16) {
+                  if (moves) ref[16 * c + lane] -= m;
+                  by[16 * c + lane] = moves && !fresh ? ex2(-m) : 1.f;
+                }
+                shrink |= moves && !fresh;
+              }
+              least = -warp_largest(-least);
+              __syncwarp();
+              if (__any_sync(0xffffffffu, shrink)) {
+#pragma unroll
+                for (int c = 0; c < kKeys; c += 4) {
+                  if (c >= n_cols) break;
+                  const float4 f = *reinterpret_cast<const float4*>(by + c);
+                  acc[c] *= f.x, acc[c + 1] *= f.y, acc[c + 2] *= f.z, acc[c + 3] *= f.w;
                 }
                 __syncwarp();
               }
-#pragma unroll
-              for (int j = 0; j < 16; ++j) acc[16 * c + j] += ex2(y[j]);
             }
+            by_tile([&](auto exact_tile, auto masked_tile) {
+              uint32_t x[2][16];
+              tc05::tmem_ld16(tD, x[0]);
+#pragma unroll
+              for (int c = 0; c < kKeys / 16; ++c) {
+                if (16 * c >= n_cols) break;
+                tc05::tmem_wait_ld();
+                loaded(x[c & 1]);
+                if (16 * (c + 1) < n_cols)
+                  tc05::tmem_ld16(tD + 16 * (c + 1), x[(c + 1) & 1]);
+                else
+                  free_d();
+                float y[16];
+                logits(c, x[c & 1], y, exact_tile, masked_tile);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[16 * c + j] += ex2(y[j]);
+              }
+            });
           }
         }
         if (dead) break;
@@ -628,12 +719,12 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         if (lane == 0) {
           const uint8_t* src = qop_of(A, p.seg);
           const int kinds = win ? 3 : 2;
-          tc05::bar_arrive_expect_tx(&S.q_full, kinds * bytes + (2 + kSum + kCompact) * line);
+          tc05::bar_arrive_expect_tx(&S.q_full, kinds * bytes + (1 + kSum + kCompact) * line + 16);
           for (int i = 0; i < kinds; ++i) tc05::bulk_g2s(S.q[i], src + (size_t)A.cols * 256 * i, bytes, &S.q_full);
           const uint8_t* c = src + (size_t)A.cols * 256 * kinds;
-          tc05::bulk_g2s(S.factor, c, line, &S.q_full);
-          tc05::bulk_g2s(S.off, c + (size_t)A.cols * 4, line, &S.q_full);
-          if (kCompact) tc05::bulk_g2s(S.sum, c + (size_t)A.cols * 8, line, &S.q_full);
+          tc05::bulk_g2s(S.off, c, line, &S.q_full);
+          if (kCompact) tc05::bulk_g2s(S.sum, c + (size_t)A.cols * 4, line, &S.q_full);
+          tc05::bulk_g2s(&S.block, c + (size_t)A.cols * 8, 16, &S.q_full);
           if (kSum) tc05::bulk_g2s(S.ref[0], A.lse + (size_t)p.seg * A.cols, line, &S.q_full);
         }
         __syncwarp();
@@ -859,7 +950,8 @@ extern "C" optr_status optr_kv_score_win(const optr_params* p, const void* q, in
   // a block of tokens a time, in stream order: the sums do not depend on chance
   cudaError_t e = cudaSuccess;
   for (A.t0 = 0; A.t0 < max_new && e == cudaSuccess; A.t0 += kTok) {
-    e = launch_pdl(query_kernel, dim3((l.cols + kRotCols - 1) / kRotCols, segs), dim3(kRotThreads), sizeof(QuerySmem), stream, A);
+    const int parts = (l.cols + kRotCols - 1) / kRotCols;
+    e = launch_pdl_cluster(query_kernel, dim3(parts, segs), dim3(kRotThreads), parts, sizeof(QuerySmem), stream, A);
     if (e == cudaSuccess) e = launch_pdl(first, dim3(l.W), dim3(kThreads), smem, stream, A);
     if (e == cudaSuccess) e = launch_pdl(normaliser_kernel, dim3(segs), dim3(1024), 0, stream, A);
     if (e == cudaSuccess) e = launch_pdl(second, dim3(l.W), dim3(kThreads), smem, stream, A);

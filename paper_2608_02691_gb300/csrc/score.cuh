@@ -212,11 +212,11 @@ __device__ __forceinline__ void workers_of(const ScoreArgs& A, int b, int h, int
 }
 
 // Operands of a (sequence, KV head)'s query block: hi and lo parts of the rotated
-// queries, the queries as given (with windows), 256 B a column each, then by column the
-// factor that brings a product with the rotated ones to log2 units, <q, mu>, and the
-// rotated queries' sum.
+// queries, the queries as given (with windows), 256 B a column each, then by column
+// <q, mu> and the rotated query's sum, then for the block the factor that brings a product
+// with the rotated ones to log2 units, and the largest sum of a column's magnitudes.
 __host__ __device__ __forceinline__ size_t qop_bytes(int cols, bool win) {
-  return (size_t)cols * (256 * (win ? 3 : 2) + 12);
+  return (size_t)cols * (256 * (win ? 3 : 2) + 8) + 16;
 }
 __device__ __forceinline__ uint8_t* qop_of(const ScoreArgs& A, int seg) {
   return A.qop + (size_t)seg * qop_bytes(A.cols, A.win.win != nullptr);
