@@ -355,7 +355,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
       const int cbase = !kSum && pair ? kKeys * g : 0;  // first column of the group's
       const float factor = S.block.x, size = S.block.y;
       float acc[kSum ? 1 : kKeys];
-      uint32_t known = 0;     // bit c: column 16 c + lane % 16 has a reference, or is none
+      uint32_t known = 0;     // bit c: column 16 c + lane / 2 has a reference, or is none
       float least = INFINITY; // no reference has been lower
       if constexpr (!kSum) {
 #pragma unroll
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
 #pragma unroll
         for (int c = 0; c < 4; ++c) ref[32 * c + lane] = 0.f;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) known |= (cbase + 16 * c + (lane & 15) >= cols ? 1u : 0u) << c;
+        for (int c = 0; c < 8; ++c) known |= (cbase + 16 * c + (lane >> 1) >= cols ? 1u : 0u) << c;
         __syncwarp();
       }
       for (int t = 0; t < tiles; ++t) {
@@ -492,26 +492,23 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
                 tc05::tmem_ld16(tD + 16 * c, x);
                 tc05::tmem_wait_ld();
                 loaded(x);
-                float y[16], m = -INFINITY;
+                float y[16];
                 if (exact)
                   logits(c, x, y, std::true_type{}, std::true_type{});
                 else
                   logits(c, x, y, std::false_type{}, std::true_type{});
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                  const float z = warp_largest(y[j]);
-                  if ((lane & 15) == j) m = z;
-                }
+                // (column 16 c + lane / 2)
+                const float m = over_lanes(y, [](float a, float b) { return fmaxf(a, b); });
                 const bool fresh = !(known >> c & 1);
                 const bool moves = m > (fresh ? -INFINITY : kSlack);
                 if (moves) {
                   known |= 1u << c;
-                  least = fminf(least, m - ref[16 * c + (lane & 15)]);
+                  least = fminf(least, m - ref[16 * c + (lane >> 1)]);
                 }
                 __syncwarp();
-                if (lane < 16) {
-                  if (moves) ref[16 * c + lane] -= m;
-                  by[16 * c + lane] = moves && !fresh ? ex2(-m) : 1.f;
+                if (lane & 1) {
+                  if (moves) ref[16 * c + (lane >> 1)] -= m;
+                  by[16 * c + (lane >> 1)] = moves && !fresh ? ex2(-m) : 1.f;
                 }
                 shrink |= moves && !fresh;
               }
@@ -528,19 +525,16 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
               }
             }
             by_tile([&](auto exact_tile, auto masked_tile) {
-              uint32_t x[2][16];
-              tc05::tmem_ld16(tD, x[0]);
 #pragma unroll
               for (int c = 0; c < kKeys / 16; ++c) {
                 if (16 * c >= n_cols) break;
+                uint32_t x[16];
+                tc05::tmem_ld16(tD + 16 * c, x);
                 tc05::tmem_wait_ld();
-                loaded(x[c & 1]);
-                if (16 * (c + 1) < n_cols)
-                  tc05::tmem_ld16(tD + 16 * (c + 1), x[(c + 1) & 1]);
-                else
-                  free_d();
+                loaded(x);
+                if (16 * (c + 1) >= n_cols) free_d();
                 float y[16];
-                logits(c, x[c & 1], y, exact_tile, masked_tile);
+                logits(c, x, y, exact_tile, masked_tile);
 #pragma unroll
                 for (int j = 0; j < 16; ++j) acc[16 * c + j] += ex2(y[j]);
               }
