@@ -49,14 +49,33 @@ __device__ __forceinline__ int operand_offset(int n, int k) {
 constexpr int kRotThreads = 256;
 constexpr int kRotCols = 32;  // columns of a CTA: 8 tokens
 
-// CTA (x, seg): columns 32 x .. of the segment's block, rotated in float32.  Thread:
-// channel k of the rows, 16 of the columns.  The rotation comes into shared memory
-// whole, before what the call waits for: its 128 rows' latencies are one.
+// CTA (x, seg): columns 32 x .. of the segment's block, rotated.  The queries are bf16, so
+// products with three bf16 parts of the rotation's elements are as good as float32's:
+// m16n8k16, a warp has 16 channels of the 32 columns.  The rotation comes into shared
+// memory whole, before what the call waits for: its 128 rows' latencies are one.
+constexpr int kRotPad = kD + 4, kQueryPad = kD + 8;  // rows in different banks
 struct QuerySmem {
-  float R[kD][kD], q[kRotCols][kD];
-  float top[4][kRotCols], dot[4][kRotCols], sum[4][kRotCols], size[4][kRotCols];
+  float R[kD][kRotPad];
+  __nv_bfloat16 q[kRotCols][kQueryPad];
+  // of the columns: by warp the largest element, the sum and the sum of magnitudes; <q, mu>
+  float top[8][kRotCols], sum[8][kRotCols], size[8][kRotCols], dot[kRotCols];
   float most[2];  // the CTA's largest element, and sum of magnitudes
 };
+
+__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};\n"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// The bf16 parts of two numbers: their rounded values are taken off x and y.
+__device__ __forceinline__ uint32_t bf16_part(float& x, float& y) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(y), "f"(x));
+  x -= __uint_as_float(r << 16);
+  y -= __uint_as_float(r & 0xffff0000u);
+  return r;
+}
 
 // Over the warp's lanes, of 16 values each: value lane / 2 (in both lanes).
 template <typename Join>
@@ -77,11 +96,10 @@ __device__ __forceinline__ float over_lanes(float (&x)[16], Join join) {
 __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constant__ ScoreArgs A) {
   extern __shared__ __align__(1024) unsigned char dsm_[];
   QuerySmem& S = *reinterpret_cast<QuerySmem*>(dsm_);
-  float (&q)[kRotCols][kD] = S.q;
   const int seg = blockIdx.y, b = seg / A.h_kv, h = seg % A.h_kv, tid = threadIdx.x;
-  const int k = tid & 127, part = tid >> 7, lane = tid & 31, quarter = (tid >> 5) & 3;
+  const int warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
   for (int i = tid; i < kD * kD / 4; i += kRotThreads)
-    cp_async16(reinterpret_cast<float4*>(S.R) + i, reinterpret_cast<const float4*>(A.R_k + (size_t)h * kD * kD) + i);
+    cp_async16(&S.R[i / (kD / 4)][4 * (i % (kD / 4))], A.R_k + (size_t)h * kD * kD + 4 * i);
   cp_async_commit();
   pdl_wait();
   pdl_trigger();
@@ -94,64 +112,79 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
   }
   const bool win = A.win.win != nullptr;
   uint8_t* out = qop_of(A, seg);
-  constexpr int kMine = kRotCols / 2;
-  float acc[kMine] = {};
   if (c0 < N) {
     for (int i = tid; i < kRotCols * kD / 8; i += kRotThreads) {
-      const int c = i / (kD / 8), x = 8 * (i % (kD / 8)), tok = (c0 + c) / 4;
+      const int n = i / (kD / 8), x = 8 * (i % (kD / 8)), tok = (c0 + n) / 4;
       uint4 y = make_uint4(0u, 0u, 0u, 0u);
       if (tok < s.rows)
         y = __ldcg(reinterpret_cast<const uint4*>(
-            A.q + (((size_t)s.c0 + A.t0 + tok) * A.h_kv + h) * (4 * kD) + (c & 3) * kD + x));
-      const uint32_t word[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        q[c][x + 2 * e] = __uint_as_float(word[e] << 16);
-        q[c][x + 2 * e + 1] = __uint_as_float(word[e] & 0xffff0000u);
-      }
-      if (win && c0 + c < N)
-        *reinterpret_cast<uint4*>(out + (size_t)A.cols * 512 + operand_offset(c0 + c, x)) = y;
+            A.q + (((size_t)s.c0 + A.t0 + tok) * A.h_kv + h) * (4 * kD) + (n & 3) * kD + x));
+      *reinterpret_cast<uint4*>(&S.q[n][x]) = y;
+      if (win && c0 + n < N)
+        *reinterpret_cast<uint4*>(out + (size_t)A.cols * 512 + operand_offset(c0 + n, x)) = y;
     }
   }
   cp_async_wait<0>();
   __syncthreads();
+  float acc[2][2][4] = {};  // columns 16 i + g, + 8; channels 16 warp + 8 j + 2 c, + 1
   if (c0 < N) {
-#pragma unroll 4
-    for (int i = 0; i < kD; i += 4) {
-      const float r[4] = {S.R[i][k], S.R[i + 1][k], S.R[i + 2][k], S.R[i + 3][k]};
+#pragma unroll 2
+    for (int k = 0; k < kD; k += 16) {
+      uint32_t a[2][4];
 #pragma unroll
-      for (int c = 0; c < kMine; ++c) {
-        const float4 x = *reinterpret_cast<const float4*>(&q[kMine * part + c][i]);
-        acc[c] = fmaf(x.x, r[0], acc[c]);
-        acc[c] = fmaf(x.y, r[1], acc[c]);
-        acc[c] = fmaf(x.z, r[2], acc[c]);
-        acc[c] = fmaf(x.w, r[3], acc[c]);
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          a[i][e] = *reinterpret_cast<const uint32_t*>(&S.q[16 * i + g + 8 * (e & 1)][k + 2 * c + 8 * (e >> 1)]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int n = 16 * warp + 8 * j + g;
+        float x[4] = {S.R[k + 2 * c][n], S.R[k + 2 * c + 1][n], S.R[k + 2 * c + 8][n], S.R[k + 2 * c + 9][n]};
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+          const uint32_t b0 = bf16_part(x[0], x[1]), b1 = bf16_part(x[2], x[3]);
+          mma_bf16(acc[0][j], a[0], b0, b1);
+          mma_bf16(acc[1][j], a[1], b0, b1);
+        }
       }
     }
-    const float mu = __ldg(A.mu + (size_t)h * kD + k);
-    auto add = [](float x, float y) { return x + y; };
-    float x[kMine];
-    const int at = kMine * part + (lane >> 1);
 #pragma unroll
-    for (int c = 0; c < kMine; ++c) x[c] = fabsf(acc[c]);
-    S.top[quarter][at] = over_lanes(x, [](float x, float y) { return fmaxf(x, y); });
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int c = 0; c < kMine; ++c) x[c] = fabsf(acc[c]);
-    S.size[quarter][at] = over_lanes(x, add);
+      for (int e = 0; e < 2; ++e) {
+        const float x[4] = {acc[i][0][2 * e], acc[i][0][2 * e + 1], acc[i][1][2 * e], acc[i][1][2 * e + 1]};
+        float m = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
+        float t = (x[0] + x[1]) + (x[2] + x[3]), l = (fabsf(x[0]) + fabsf(x[1])) + (fabsf(x[2]) + fabsf(x[3]));
 #pragma unroll
-    for (int c = 0; c < kMine; ++c) x[c] = acc[c];
-    S.sum[quarter][at] = over_lanes(x, add);
+        for (int o = 1; o < 4; o <<= 1) {
+          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+          t += __shfl_xor_sync(0xffffffffu, t, o);
+          l += __shfl_xor_sync(0xffffffffu, l, o);
+        }
+        if (c == 0) {
+          const int n = 16 * i + 8 * e + g;
+          S.top[warp][n] = m;
+          S.sum[warp][n] = t;
+          S.size[warp][n] = l;
+        }
+      }
+    // <q, mu>: eight lanes a column
+    float d = 0.f;
+    for (int x = lane & 7; x < kD; x += 8)
+      d = fmaf(__bfloat162float(S.q[tid >> 3][x]), __ldg(A.mu + (size_t)h * kD + x), d);
 #pragma unroll
-    for (int c = 0; c < kMine; ++c) x[c] = q[kMine * part + c][k] * mu;
-    S.dot[quarter][at] = over_lanes(x, add);
+    for (int o = 1; o < 8; o <<= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+    if ((lane & 7) == 0) S.dot[tid >> 3] = d;
   }
   __syncthreads();
-  auto quarters = [&](const float (&x)[4][kRotCols], int n) { return (x[0][n] + x[1][n]) + (x[2][n] + x[3][n]); };
+  auto warps = [&](const float (&x)[8][kRotCols], int n) {
+    return ((x[0][n] + x[1][n]) + (x[2][n] + x[3][n])) + ((x[4][n] + x[5][n]) + (x[6][n] + x[7][n]));
+  };
   if (tid < 32) {
     float m = 0.f, l = 0.f;
     if (c0 < N) {
-      m = fmaxf(fmaxf(S.top[0][lane], S.top[1][lane]), fmaxf(S.top[2][lane], S.top[3][lane]));
-      l = quarters(S.size, lane);
+      for (int w = 0; w < 8; ++w) m = fmaxf(m, S.top[w][lane]);
+      l = warps(S.size, lane);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -175,19 +208,25 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
     // below it is known to 2^-39 of the largest.
     const int E = m > 0.f ? max(-100, min(100, 13 - ((int)(__float_as_uint(m) >> 23) - 127))) : 0;
     float* line = reinterpret_cast<float*>(out + (size_t)A.cols * (win ? 768 : 512));
+    const float up = __uint_as_float((uint32_t)(127 + E) << 23);
 #pragma unroll
-    for (int c = 0; c < kMine; ++c) {
-      const int n = kMine * part + c;
-      const float x = acc[c] * __uint_as_float((uint32_t)(127 + E) << 23);
-      const __half hi = __float2half_rn(x), lo = __float2half_rn(x - __half2float(hi));
-      if (c0 + n >= N) break;
-      const int at = operand_offset(c0 + n, key_place(k));
-      *reinterpret_cast<__half*>(out + at) = hi;
-      *reinterpret_cast<__half*>(out + (size_t)A.cols * 256 + at) = lo;
-      if (k == 0) {
-        line[c0 + n] = kLogit * quarters(S.dot, n);
-        line[A.cols + c0 + n] = kLogit * quarters(S.sum, n);
-      }
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int n = c0 + 16 * i + 8 * e + g;
+          if (n >= N) continue;
+          const int at = operand_offset(n, key_place(16 * warp + 8 * j + 2 * c));
+          const float x = acc[i][j][2 * e] * up, y = acc[i][j][2 * e + 1] * up;
+          const __half2 hi = __floats2half2_rn(x, y);
+          const float2 z = __half22float2(hi);
+          *reinterpret_cast<__half2*>(out + at) = hi;
+          *reinterpret_cast<__half2*>(out + (size_t)A.cols * 256 + at) = __floats2half2_rn(x - z.x, y - z.y);
+        }
+    if (tid < kRotCols && c0 + tid < N) {
+      line[c0 + tid] = kLogit * S.dot[tid];
+      line[A.cols + c0 + tid] = kLogit * warps(S.sum, tid);
     }
     if (blockIdx.x == 0 && tid == 0)
       *reinterpret_cast<float4*>(line + 2 * A.cols) =
@@ -214,8 +253,7 @@ struct Tmem {
 constexpr int kRaw = 3;        // tiles of records on the way
 constexpr int kPieces = 3;     // pieces found ahead
 constexpr int kConsumers = 14; // warps that take the pieces
-constexpr float kSlack = 60.f; // a column's logits may pass its reference by 2^60 unseen,
-constexpr float kMost = 100.f; // and are looked at where they may by 2^100
+constexpr float kSlack = 60.f; // a column's logits may pass its reference by 2^60
 
 template <bool kCompact>
 struct Smem {
@@ -355,6 +393,8 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
       const int cbase = !kSum && pair ? kKeys * g : 0;  // first column of the group's
       const float factor = S.block.x, size = S.block.y;
       float acc[kSum ? 1 : kKeys];
+      // what they may pass it by unseen: a piece's sum over its keys is below 2^128
+      const float most = 119.f - (32 - __clz(tiles));
       uint32_t known = 0;     // bit c: column 16 c + lane / 2 has a reference, or is none
       float least = INFINITY; // no reference has been lower
       if constexpr (!kSum) {
@@ -482,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
             // warp's largest.  That the logits cannot, of keys whose values are top at most, the
             // queries' sums of magnitudes say; window keys are always looked at.
             const float top = kCompact ? fmaxf(fabsf(low), fabsf(fmaf(3.f, scale / factor, low))) : scale / factor;
-            if (__any_sync(0xffffffffu, exact || known != 0xffu || (first < cols && size * top > least + kMost))) {
+            if (__any_sync(0xffffffffu, exact || known != 0xffu || (first < cols && size * top > least + most))) {
               float* by = reinterpret_cast<float*>(S.meet[warp]);  // by what a column's sum shrinks
               bool shrink = false;
 #pragma unroll 1
