@@ -14,7 +14,7 @@
 // loaded at once into shared memory; each CTA walks down the tree by itself (one
 // warp, in shared memory) until a sum S or the final draw needs the vocabulary.  Of
 // that each CTA has a slice; w is not stored but computed from p, q and the S so
-// far, and the CTAs' sums meet in shared memory across the cluster, in rank order
+// far, and the warps' sums meet in shared memory across the cluster, in a fixed order
 // (equal calls give equal bits).
 #include "cluster.cuh"
 #include "optr_internal.cuh"
@@ -43,10 +43,9 @@ struct Smem {
   uint32_t cut[kRows];
   int16_t path[kRows];
   Walk walk;
-  double wsum[kWarps];
-  double sum[2];                    // this CTA's, by pass
-  unsigned long long wbest[kWarps];
-  unsigned long long best[2];
+  double sum[2][kWarps];                 // the warps' sums, by pass,
+  unsigned long long best[2][kWarps];    // and their largest ratios
+  unsigned long long all;
 };
 
 __device__ __forceinline__ float as_float(float x) { return x; }
@@ -82,6 +81,36 @@ __device__ __forceinline__ float left(float w, float S, float q) {
 __device__ __forceinline__ unsigned long long ranked(float value, int token) {
   return (unsigned long long)__float_as_uint(__fadd_rn(value, 0.f)) << 32 | (0xffffffffu - (unsigned)token);
 }
+
+// One warp: the 16 words of each CTA of the cluster (8 at most), four a lane; the lanes of
+// CTAs that there are not get `none`.
+__device__ __forceinline__ void cluster_words(const void* x, int cs, unsigned long long none,
+                                              unsigned long long (&y)[4]) {
+  static_assert(kWarps == 16, "four words a lane, four lanes a CTA");
+  const int lane = threadIdx.x & 31, rank = lane >> 2;
+  const unsigned long long* at = static_cast<const unsigned long long*>(x) + 4 * (lane & 3);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = rank < cs ? (cs > 1 ? cluster_ld64(at + i, rank) : at[i]) : none;
+}
+
+// x / e where it may pass the largest ratio so far.  Most cannot: the reciprocal's estimate
+// says so (to 2^-20; estimates near nothing and what is not a number say nothing).
+struct Largest {
+  float top = -1.f, limit = -1.f;
+  int at = 0;
+  __device__ __forceinline__ void take(float x, float e, int token) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e));
+    const float guess = x * r;
+    if (guess < limit && (guess > 1e-30f || x == 0.f)) return;
+    const float exact = __fdiv_rn(x, e);
+    if (exact > top) {
+      top = exact;
+      limit = exact * 0.999999f;
+      at = token;
+    }
+  }
+};
 
 // One warp: down from S.walk until a sum or the draw is needed.
 __device__ __forceinline__ void descend(Smem& S, int n, bool probs) {
@@ -182,14 +211,18 @@ verify_tree_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
     S.walk = Walk{0, 0, 0, 0, false};
     S.path[0] = 0;
   }
-  __syncthreads();
   const int n_vec = V / kVec;
   const int lo = (int)((long long)n_vec * rank / cs), hi = (int)((long long)n_vec * (rank + 1) / cs);
+  const float* e = noise + (size_t)b * V;
+  // the noise is wanted in any case: it comes into L2 while the walk goes on
+  for (int v = lo + (128 / (4 * kVec)) * tid; v < hi; v += (128 / (4 * kVec)) * kTreeThreads)
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(e + (size_t)v * kVec));
+  __syncthreads();
+  if (warp == 0) descend(S, n, dp != nullptr);
+  __syncthreads();
   // Sums until the walk ends
   Walk w;
   for (int pass = 0;; ++pass) {
-    if (warp == 0) descend(S, n, dp != nullptr);
-    __syncthreads();
     w = S.walk;
     if (w.draw) break;
     const T* p = tp + ((size_t)c0 + w.row) * V;
@@ -211,31 +244,30 @@ verify_tree_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
     double total = sum;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    if (lane == 0) S.wsum[warp] = total;
-    __syncthreads();
-    if (tid == 0) {
-      total = 0.;
-      for (int i = 0; i < kWarps; ++i) total += S.wsum[i];
-      S.sum[pass & 1] = total;
-    }
+    if (lane == 0) S.sum[pass & 1][warp] = total;
     if (cs > 1) cluster_barrier(); else __syncthreads();
-    total = 0.;
-    for (int r = 0; r < cs; ++r)
-      total += cs > 1 ? __longlong_as_double((long long)cluster_ld64(&S.sum[pass & 1], r)) : S.sum[pass & 1];
-    // (the mass that the next child is measured against, where descend() looks for it)
-    if (tid == 0) S.cut[w.n_cut] = __float_as_uint((float)total);
+    if (warp == 0) {
+      unsigned long long y[4];
+      cluster_words(S.sum[pass & 1], cs, 0ull, y);
+      total = (__longlong_as_double((long long)y[0]) + __longlong_as_double((long long)y[1])) +
+              (__longlong_as_double((long long)y[2]) + __longlong_as_double((long long)y[3]));
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      // (the mass that the next child is measured against, where descend() looks for it)
+      if (lane == 0) S.cut[w.n_cut] = __float_as_uint((float)total);
+      __syncwarp();
+      descend(S, n, true);
+    }
     __syncthreads();
   }
   // The next token: first maximum of w / e; of p / e where w is zero everywhere
   const T* p = tp + ((size_t)c0 + w.row) * V;
   const T* q = dp ? dp + ((size_t)c0 + w.row) * V : nullptr;
-  const float* e = noise + (size_t)b * V;
   unsigned long long all = 0;
   for (int pass = 0; pass < 2; ++pass) {
     const int n_cut = pass == 0 ? w.n_cut : 0;
-    float top = -1.f;
-    int at = 0;
-#pragma unroll 2
+    Largest best;
+#pragma unroll 4
     for (int v = lo + tid; v < hi; v += kTreeThreads) {
       float x[kVec], z[kVec], y[kVec];
       fetch(p + (size_t)v * kVec, x);
@@ -252,35 +284,33 @@ verify_tree_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
         }
       }
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        const float r = __fdiv_rn(x[i], z[i]);
-        if (r > top) {
-          top = r;
-          at = v * kVec + i;
-        }
-      }
+      for (int i = 0; i < kVec; ++i) best.take(x[i], z[i], v * kVec + i);
     }
-    unsigned long long c = top >= 0.f ? ranked(top, at) : 0ull;
+    unsigned long long c = best.top >= 0.f ? ranked(best.top, best.at) : 0ull;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       const unsigned long long y = __shfl_xor_sync(0xffffffffu, c, o);
       c = y > c ? y : c;
     }
-    if (lane == 0) S.wbest[warp] = c;
-    __syncthreads();
-    if (tid == 0) {
-      for (int i = 1; i < kWarps; ++i) c = S.wbest[i] > c ? S.wbest[i] : c;
-      S.best[pass] = c;
-    }
+    if (lane == 0) S.best[pass][warp] = c;
     if (cs > 1) cluster_barrier(); else __syncthreads();
-    all = S.best[pass];
-    if (cs > 1)
-      for (int r = 0; r < cs; ++r) {
-        const unsigned long long y = cluster_ld64(&S.best[pass], r);
-        all = y > all ? y : all;
+    if (warp == 0) {
+      unsigned long long y[4];
+      cluster_words(S.best[pass], cs, 0ull, y);
+#pragma unroll
+      for (int i = 1; i < 4; ++i) y[0] = y[i] > y[0] ? y[i] : y[0];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const unsigned long long z = __shfl_xor_sync(0xffffffffu, y[0], o);
+        y[0] = z > y[0] ? z : y[0];
       }
+      if (lane == 0) S.all = y[0];
+    }
+    __syncthreads();
+    all = S.all;
     if ((uint32_t)(all >> 32) != 0u) break;  // the same in the whole cluster
   }
+  if (cs > 1) cluster_arrive();  // no CTA leaves while its shared memory may be read
   if (rank == 0) {
     const int token = (int)(0xffffffffu - (unsigned)all);
     if (tid == 0) accepted[b] = w.depth;
@@ -289,7 +319,7 @@ verify_tree_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
       next[c0 + i] = i < w.depth ? S.node[S.path[i + 1]].token : i == w.depth ? token : -1;
     }
   }
-  if (cs > 1) cluster_barrier();  // no CTA leaves while its shared memory may be read
+  if (cs > 1) cluster_wait();
 }
 
 template <typename T>
