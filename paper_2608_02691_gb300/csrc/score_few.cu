@@ -538,6 +538,10 @@ few_cluster_kernel(const __grid_constant__ ScoreArgs A, int log_cs, int places, 
     issue(p0 + 2 * e + 1, 2 * e + 1);
     cp_async_commit();
   }
+  float* score = A.score + (size_t)seg * A.n_score;
+  // (the sums so far, a line of 32 a thread)
+  if (32 * tid < kPage * (P1 - P0))
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(score + min(A.sink + kPage * P0 + 32 * tid, s.n - 1)));
   // the tokens' queries, while the first pages are on their way
 #pragma unroll 1
   for (int i = 0; i < s.rows; ++i) {
@@ -670,7 +674,7 @@ few_cluster_kernel(const __grid_constant__ ScoreArgs A, int log_cs, int places, 
     for (int j = 0; j < 4; ++j)
       top[j] = over_warps(S.top, 4 * i + j, [](float x, float y) { return fmaxf(x, y); });
     const float4* x = U.logits + (size_t)i * places;
-#pragma unroll 4
+#pragma unroll 8
     for (int k = tid; k < n_all; k += kWarps * 32) {
       const float4 y = x[k < n_int ? k : k - n_int + w_place];
       l[0] += ex2(y.x - top[0]);
@@ -694,6 +698,20 @@ few_cluster_kernel(const __grid_constant__ ScoreArgs A, int log_cs, int places, 
     for (int i = 0; i < kWarps; ++i) l += S.part[i][tid];
     S.mine[tid].y = l;
   }
+  // the sums so far, kEach positions of a thread at a time: on their way before they are wanted
+  constexpr int kEach = 8;
+  float old[kEach];
+  auto pos_of = [&](int k) {
+    return k < n_int ? A.sink + kPage * P0 + k : win_pos(kWinRows * U0 + k - n_int, s.n, A.sink, A.recent);
+  };
+  auto fetch = [&](int k0) {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int k = k0 + e * kWarps * 32;
+      old[e] = k < n_all ? __ldcg(score + pos_of(k)) : 0.f;
+    }
+  };
+  fetch(tid);
   if (cs > 1) cluster_barrier(); else __syncthreads();
   if (tid < cols) {
     float2 y[8];
@@ -718,21 +736,22 @@ few_cluster_kernel(const __grid_constant__ ScoreArgs A, int log_cs, int places, 
   }
   __syncthreads();
   if (cs > 1) cluster_arrive();  // no CTA leaves while its shared memory may be read
-  float* score = A.score + (size_t)seg * A.n_score;
-#pragma unroll 4
-  for (int k = tid; k < n_all; k += kWarps * 32) {
-    const bool coded = k < n_int;
-    const int place = coded ? k : k - n_int + w_place;
-    const int pos = coded ? A.sink + kPage * P0 + k : win_pos(kWinRows * U0 + k - n_int, s.n, A.sink, A.recent);
-    const float old = __ldcg(score + pos);
-    float x = 0.f;
+  for (int k0 = tid; k0 < n_all; k0 += kEach * kWarps * 32) {
 #pragma unroll
-    for (int i = 0; i < kTokens; ++i) {
-      if (i >= s.rows) break;
-      const float4 y = U.logits[(size_t)i * places + place], r = *reinterpret_cast<const float4*>(S.ref + 4 * i);
-      x += (ex2(y.x + r.x) + ex2(y.y + r.y)) + (ex2(y.z + r.z) + ex2(y.w + r.w));
+    for (int e = 0; e < kEach; ++e) {
+      const int k = k0 + e * kWarps * 32;
+      if (k >= n_all) break;
+      const int place = k < n_int ? k : k - n_int + w_place;
+      float x = 0.f;
+#pragma unroll
+      for (int i = 0; i < kTokens; ++i) {
+        if (i >= s.rows) break;
+        const float4 y = U.logits[(size_t)i * places + place], r = *reinterpret_cast<const float4*>(S.ref + 4 * i);
+        x += (ex2(y.x + r.x) + ex2(y.y + r.y)) + (ex2(y.z + r.z) + ex2(y.w + r.w));
+      }
+      score[pos_of(k)] = old[e] + x;
     }
-    score[pos] = old + x;
+    fetch(k0 + kEach * kWarps * 32);
   }
   if (cs > 1) cluster_wait();
 }
