@@ -1,16 +1,24 @@
 // Attention weights of a decode step's few tokens, summed by position ("optr_kv_score").
 //
 // With one to kFewTok tokens a (sequence, KV head) the keys are read once: their logits, 16
-// bytes a token and position, are kept in the workspace for the second pass.  Three
-// launches: few_query_kernel rotates the queries (as the decode does), few_logit_kernel
-// goes over the keys, a page a step and warp, and few_sum_kernel joins the warps' maxima
-// and sums and adds the weights up.
+// bytes a token and position, are kept for the second pass.  few_cluster_kernel does
+// all in one launch: a cluster of CTAs takes a (sequence, KV head), each CTA a range of
+// its pages and window rows; it rotates the queries (as the decode does), keeps the
+// logits in shared memory (in the workspace where they do not fit), and maxima and sums
+// meet across the cluster.  16 x 1 over 8192: 29.5 us, 1.7 TB/s; of that 9 us are the
+// products and what brings the codes to them, 7 us the rest of the page loop, 8 us the weights
+// and 6 us the launch and the rotation, and 24 of 152 SMs have no (sequence, KV head).  One
+// token over 1024: 8.8 us, the host's time of a call.
+//
+// Long contexts of so few or so many (sequence, KV head)s that many SMs would idle take three
+// launches instead (clusters()): few_query_kernel, few_logit_kernel, in which all steps of
+// all (sequence, KV head)s stand in one line that is cut into equal ranges, one a warp, and
+// few_sum_kernel, which joins the warps' maxima and sums and adds the weights up.
 //
 // A page's logits are the decode's (decode_tc.cu): m16n8k16 products of the codes, as the
 // fp16 numbers 1024 + code 2^pos that their bits make, with the four query heads in fp16
 // hi and lo parts (eight columns), one accumulator a scale.  Window keys are bf16 as they
-// are, 16 rows a step, which counts as four pages.  All steps of all (sequence, KV head)s
-// stand in one line that is cut into equal ranges, one a warp.
+// are, 16 rows a step, which counts as four pages in the line.
 #include <type_traits>
 
 #include "cluster.cuh"
@@ -43,7 +51,7 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// Workspace: queries [segments][max_new][kQueryWords], partials [W + segments][16]
+// Workspace of the three launches: queries [segments][max_new][kQueryWords], partials [W + segments][16]
 // {maximum, sum}, logits [segments][positions][max_new][4].
 struct FewArgs {
   ScoreArgs A;
@@ -482,9 +490,10 @@ struct OneFixed {
   alignas(16) uint8_t stage[kWarps][kOneStages][kHalfRec];
 };
 
-template <bool kCompact, int kTokens>
+// kSpill: the logits lie in the workspace, [CTA][token][place].
+template <bool kCompact, int kTokens, bool kSpill>
 __global__ void __launch_bounds__(kWarps * 32, 1)
-few_cluster_kernel(const __grid_constant__ ScoreArgs A, int log_cs, int places, float qscale) {
+few_cluster_kernel(const __grid_constant__ ScoreArgs A, int log_cs, int places, float4* spill, float qscale) {
   extern __shared__ __align__(16) unsigned char dsm_[];
   OneFixed& S = *reinterpret_cast<OneFixed*>(dsm_);
   OneSmem& U = *reinterpret_cast<OneSmem*>(dsm_ + sizeof(OneFixed));
@@ -570,7 +579,8 @@ few_cluster_kernel(const __grid_constant__ ScoreArgs A, int log_cs, int places, 
   float m[kTokens];
 #pragma unroll
   for (int i = 0; i < kTokens; ++i) m[i] = -1e30f;
-  float* logits = reinterpret_cast<float*>(U.logits) + c;
+  float4* const stored = kSpill ? spill + (size_t)blockIdx.x * A.max_new * places : U.logits;
+  float* logits = reinterpret_cast<float*>(stored) + c;
   Query<kCompact> q;
   if (kTokens == 1) q.load(S.query[0]);
   int at = 0;  // the pair's stages
@@ -673,7 +683,7 @@ few_cluster_kernel(const __grid_constant__ ScoreArgs A, int log_cs, int places, 
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       top[j] = over_warps(S.top, 4 * i + j, [](float x, float y) { return fmaxf(x, y); });
-    const float4* x = U.logits + (size_t)i * places;
+    const float4* x = stored + (size_t)i * places;
 #pragma unroll 8
     for (int k = tid; k < n_all; k += kWarps * 32) {
       const float4 y = x[k < n_int ? k : k - n_int + w_place];
@@ -746,7 +756,7 @@ few_cluster_kernel(const __grid_constant__ ScoreArgs A, int log_cs, int places, 
 #pragma unroll
       for (int i = 0; i < kTokens; ++i) {
         if (i >= s.rows) break;
-        const float4 y = U.logits[(size_t)i * places + place], r = *reinterpret_cast<const float4*>(S.ref + 4 * i);
+        const float4 y = stored[(size_t)i * places + place], r = *reinterpret_cast<const float4*>(S.ref + 4 * i);
         x += (ex2(y.x + r.x) + ex2(y.y + r.y)) + (ex2(y.z + r.z) + ex2(y.w + r.w));
       }
       score[pos_of(k)] = old[e] + x;
@@ -766,28 +776,40 @@ cudaError_t launch_logits(const optr_params* p, const FewArgs& F, cudaStream_t s
   return e != cudaSuccess ? e : launch_pdl(fn, dim3(p->num_sms), dim3(kWarps * 32), smem, s, F);
 }
 
-// CTAs of a (sequence, KV head) in a cluster, log2, or -1: its logits do not fit, or there
-// are too many (the CTAs of a last, poorly filled round would idle).
-int cluster_log(const optr_params* p, int B, int max_new, int max_pages, int& places, size_t& smem) {
-  const int segs = B * p->cfg.h_kv;
-  int best = -1;
-  for (int l = 0; l < 4; ++l) {
-    // clusters of 4 and 8 do not fill all of the GPU at one CTA an SM (144 and 120 of 152)
-    if (l > 0 && (segs << l) > (l == 1 ? p->num_sms : p->num_sms * 3 / 4)) break;
-    const int units = (max_pages + 2) / (1 << l) + 3;
-    const size_t x = sizeof(OneFixed) + std::max(sizeof(QrotSmem), (size_t)units * kPage * max_new * sizeof(float4));
-    if (x > 227 * 1024) continue;
-    best = l, places = units * kPage, smem = x;
-  }
-  return best;
+// The cluster kernel's launch: log2 of the CTAs of a (sequence, KV head), places of a CTA,
+// and whether their logits fit shared memory.
+struct Clusters {
+  int log_cs, places;
+  size_t smem;
+  bool spill, use;
+};
+Clusters clusters(const optr_params* p, int B, int max_new, int max_pages) {
+  Clusters c;
+  const long long segs = (long long)B * p->cfg.h_kv;
+  // as many as are resident at once: at one CTA an SM, 152 SMs take 152 CTAs in clusters of 2, 144
+  // of 4 and 120 of 8
+  const int most[4] = {p->num_sms, p->num_sms, p->num_sms * 15 / 16, p->num_sms * 3 / 4};
+  c.log_cs = 0;
+  while (c.log_cs < 3 && (segs << (c.log_cs + 1)) <= most[c.log_cs + 1]) ++c.log_cs;
+  const int units = (max_pages + 2) / (1 << c.log_cs) + 3;
+  c.places = units * kPage;
+  c.smem = sizeof(OneFixed) + std::max(sizeof(QrotSmem), (size_t)c.places * max_new * sizeof(float4));
+  c.spill = c.smem > 227 * 1024;
+  if (c.spill) c.smem = sizeof(OneFixed) + sizeof(QrotSmem);
+  // long contexts that leave many SMs idle are cut evenly instead (few_logit_kernel: 4 x 1 over
+  // 131072 with 64 CTAs 203 us, evenly 146)
+  const long long ctas = segs << c.log_cs, rounds = (ctas + p->num_sms - 1) / p->num_sms;
+  c.use = !c.spill || ctas * 10 >= rounds * p->num_sms * 7;
+  return c;
 }
 
 template <int kTokens>
-cudaError_t launch_cluster(const ScoreArgs& A, int log_cs, int places, size_t smem, cudaStream_t s) {
-  auto fn = A.compact ? few_cluster_kernel<true, kTokens> : few_cluster_kernel<false, kTokens>;
-  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), smem);
-  return e != cudaSuccess ? e : launch_pdl_cluster(fn, dim3((unsigned)(A.B * A.h_kv) << log_cs), dim3(kWarps * 32),
-                                                   1 << log_cs, smem, s, A, log_cs, places, kLogit);
+cudaError_t launch_cluster(const ScoreArgs& A, const Clusters& c, float4* spill, cudaStream_t s) {
+  auto fn = A.compact ? c.spill ? few_cluster_kernel<true, kTokens, true> : few_cluster_kernel<true, kTokens, false>
+                      : c.spill ? few_cluster_kernel<false, kTokens, true> : few_cluster_kernel<false, kTokens, false>;
+  const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(fn), c.smem);
+  return e != cudaSuccess ? e : launch_pdl_cluster(fn, dim3((unsigned)(A.B * A.h_kv) << c.log_cs), dim3(kWarps * 32),
+                                                   1 << c.log_cs, c.smem, s, A, c.log_cs, c.places, spill, kLogit);
 }
 
 }  // namespace
@@ -798,7 +820,8 @@ FewLayout few_layout(const optr_params* p, int B, int max_new, int max_pages) {
   l.W = p->num_sms * kWarps;
   l.part = round_up(segs * max_new * kQueryWords * sizeof(uint32_t));
   l.logits = l.part + round_up((segs + l.W) * 4 * kFewTok * sizeof(float2));
-  l.total = l.logits + round_up(segs * max_pages * kPage * max_new * sizeof(float4));
+  // (a cluster's eight CTAs have some places more)
+  l.total = l.logits + round_up(segs * ((size_t)max_pages + 32) * kPage * max_new * sizeof(float4));
   return l;
 }
 
@@ -809,13 +832,12 @@ bool few_tokens(const optr_params* p, int B, int max_new, int max_pages) {
 }
 
 cudaError_t launch_score_few(const optr_params* p, const ScoreArgs& A, uint8_t* ws, cudaStream_t s) {
-  int places;
-  size_t smem;
-  const int log_cs = cluster_log(p, A.B, A.max_new, A.max_pages, places, smem);
-  if (log_cs >= 0)
-    return A.max_new == 1 ? launch_cluster<1>(A, log_cs, places, smem, s)
-                          : launch_cluster<kFewTok>(A, log_cs, places, smem, s);
   const FewLayout l = few_layout(p, A.B, A.max_new, A.max_pages);
+  const Clusters c = clusters(p, A.B, A.max_new, A.max_pages);
+  if (c.use) {
+    float4* spill = (float4*)(ws + l.logits);
+    return A.max_new == 1 ? launch_cluster<1>(A, c, spill, s) : launch_cluster<kFewTok>(A, c, spill, s);
+  }
   const FewArgs F{A, (uint32_t*)ws, (float2*)(ws + l.part), (float4*)(ws + l.logits), A.max_pages * kPage, l.W,
                   kLogit};
   const unsigned segs = (unsigned)A.B * A.h_kv;
