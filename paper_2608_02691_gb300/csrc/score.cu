@@ -19,8 +19,9 @@
 // parts (22 bits; queries over a power of two by block, keys over one by key), and a tile
 // takes the products hi hi + hi lo + lo hi.  A group of a slot has four values, so the
 // parts of 16 values are computed in float32 and the codes pick among them by byte
-// permutes.  With one pair a slot the codes go in as they are, its scale and minimum are
-// the epilogue's, and two products do.  Window keys and their queries are bf16 as they are, one product.
+// permutes.  With one pair a slot the codes go in as subnormal numbers, code
+// 2^-16 (lower bits cost the sums precision: products are aligned as if their operands
+// were normal), its scale and minimum are the epilogue's, and two products do.  Window keys and their queries are bf16 as they are, one product.
 #include "cluster.cuh"
 #include "f32x2.cuh"
 #include "score.cuh"
@@ -35,9 +36,11 @@ namespace {
 // ------------------------------------------------------------- queries
 
 // Place of a channel in a key row: word w of a slot's codes has, by byte, the four
-// groups' channels 4 w .. 4 w + 3.
-__host__ __device__ constexpr int key_place(int channel) {
-  return 16 * ((channel >> 2) & 7) + 4 * (channel >> 5) + (channel & 3);
+// groups' channels 4 w .. 4 w + 3.  Codes that go in as they are: a register has the same
+// two bits of either half of the word.
+__host__ __device__ constexpr int key_place(int channel, bool codes) {
+  const int w = (channel >> 2) & 7, G = channel >> 5, e = channel & 3;
+  return codes ? 16 * w + 2 * (4 * (G & 1) + e) + (G >> 1) : 16 * w + 4 * G + e;
 }
 
 // Element (n, k) of an operand of n columns, K-major without swizzle: core matrices of
@@ -217,12 +220,20 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
         for (int e = 0; e < 2; ++e) {
           const int n = c0 + 16 * i + 8 * e + g;
           if (n >= N) continue;
-          const int at = operand_offset(n, key_place(16 * warp + 8 * j + 2 * c));
+          const int ch = 16 * warp + 8 * j + 2 * c;
           const float x = acc[i][j][2 * e] * up, y = acc[i][j][2 * e + 1] * up;
           const __half2 hi = __floats2half2_rn(x, y);
           const float2 z = __half22float2(hi);
-          *reinterpret_cast<__half2*>(out + at) = hi;
-          *reinterpret_cast<__half2*>(out + (size_t)A.cols * 256 + at) = __floats2half2_rn(x - z.x, y - z.y);
+          const __half2 lo = __floats2half2_rn(x - z.x, y - z.y);
+          __half* at = reinterpret_cast<__half*>(out + operand_offset(n, key_place(ch, A.compact)));
+          if (A.compact) {  // (the second channel's place is two on)
+            at[0] = __low2half(hi), at[2] = __high2half(hi);
+            at += A.cols * 128;
+            at[0] = __low2half(lo), at[2] = __high2half(lo);
+          } else {
+            *reinterpret_cast<__half2*>(at) = hi;
+            *reinterpret_cast<__half2*>(at + A.cols * 128) = lo;
+          }
         }
     if (tid < kRotCols && c0 + tid < N) {
       line[c0 + tid] = kLogit * S.dot[tid];
@@ -230,7 +241,7 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
     }
     if (blockIdx.x == 0 && tid == 0)
       *reinterpret_cast<float4*>(line + 2 * A.cols) =
-          make_float4(__uint_as_float((uint32_t)(127 - E) << 23) * kLogit, kLogit * l, 0.f, 0.f);
+          make_float4(__uint_as_float((uint32_t)(127 - E) << 23) * (A.compact ? 0x1p16f * kLogit : kLogit), kLogit * l, 0.f, 0.f);
   }
   if (cs > 1) cluster_wait();
 }
@@ -270,6 +281,7 @@ struct Smem {
   static constexpr int kRing = kCompact ? 8 : 4;
   uint32_t scale[kRing][kKeys];
   uint32_t counts[kRing][4];
+  uint32_t pages[kRaw];              // a raw tile's pages that are in range
   ScorePiece piece[kPieces];
   uint64_t raw_full[kRaw], raw_empty[kRaw], k_full[2], k_empty[2];
   uint64_t d_full[3][2], d_empty[3];  // by D and the epilogue group that takes it
@@ -637,24 +649,15 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         bool ok;
         uint32_t scale = 0u;
         if (tile < p.I()) {
-          const int i = kKeys * tile + key;
-          ok = i < p.n_int;
-          if (ok) {
-            const int page = __ldcg(A.bt + (size_t)p.b * A.max_pages + (A.sink + i) / kPage);
-            ok = page >= 0 && page < A.num_pages;
-            if (!ok) atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
-          }
           const uint32_t r = raws % kRaw;
           if (!wait(&S.raw_full[r], raws / kRaw)) break;
           ++raws;
+          ok = kKeys * tile + key < p.n_int && (S.pages[r] >> (key / kPage) & 1);
           const uint8_t* raw = S.raw[r][key / kPage];
           const int slot = key % kPage;
-          // the four values of each group, hi and lo; the codes themselves
-          uint32_t hi[kCompact ? 1 : 4][2], lo[kCompact ? 1 : 4][2];
+          [[maybe_unused]] uint32_t hi[4][2], lo[4][2];  // the four values of each group
           if constexpr (kCompact) {
             scale = *reinterpret_cast<const uint32_t*>(raw + 512 + ms * slot);
-            hi[0][0] = 0x3c000000u;
-            hi[0][1] = 0x42004000u;
           } else {
             const uint4 mm = *reinterpret_cast<const uint4*>(raw + 512 + ms * slot);
             // over a power of two above the largest
@@ -688,22 +691,26 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
               const uint32_t x = v ? word.y : word.x;
-              uint32_t pick[8];  // by group and half of its byte
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                // code c of a byte picks bytes 2 c and 2 c + 1 of its group's values
-                const uint32_t a = (x >> (4 * e) & 0x03030303u) * 0x22u + 0x10101010u;
-                const uint32_t b = (x >> (4 * e + 2) & 0x03030303u) * 0x22u + 0x10101010u;
-                pick[e] = __byte_perm(a, b, 0x5140);
-                pick[4 + e] = __byte_perm(a, b, 0x7362);
-                pick[2 + e] = pick[e] >> 16;
-                pick[6 + e] = pick[4 + e] >> 16;
-              }
               uint32_t y[8];
+              if constexpr (kCompact) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) y[e] = __byte_perm(hi[kCompact ? 0 : e / 2][0], hi[kCompact ? 0 : e / 2][1], pick[e]);
-              tc05::tmem_st8(tK + 16 * part + 8 * v, y);
-              if constexpr (!kCompact) {
+                for (int e = 0; e < 8; ++e) y[e] = (e < 4 ? x << (8 - 2 * e) : x >> (2 * e - 8)) & 0x03000300u;
+                tc05::tmem_st8(tK + 16 * part + 8 * v, y);
+              } else {
+                uint32_t pick[8];  // by group and half of its byte
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  // code c of a byte picks bytes 2 c and 2 c + 1 of its group's values
+                  const uint32_t a = (x >> (4 * e) & 0x03030303u) * 0x22u + 0x10101010u;
+                  const uint32_t b = (x >> (4 * e + 2) & 0x03030303u) * 0x22u + 0x10101010u;
+                  pick[e] = __byte_perm(a, b, 0x5140);
+                  pick[4 + e] = __byte_perm(a, b, 0x7362);
+                  pick[2 + e] = pick[e] >> 16;
+                  pick[6 + e] = pick[4 + e] >> 16;
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = __byte_perm(hi[e / 2][0], hi[e / 2][1], pick[e]);
+                tc05::tmem_st8(tK + 16 * part + 8 * v, y);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] = __byte_perm(lo[e / 2][0], lo[e / 2][1], pick[e]);
                 tc05::tmem_st8(tK + 64 + 16 * part + 8 * v, y);
@@ -776,8 +783,12 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           if (raws >= kRaw && !wait(&S.raw_empty[r], raws / kRaw - 1)) break;
           const bool in = page >= 0 && page < A.num_pages;
           constexpr uint32_t pairs = 16u * meta_stride(kCompact);
-          const uint32_t pages = __popc(__ballot_sync(0xffffffffu, in) & 0xffu);
-          if (lane == 0) tc05::bar_arrive_expect_tx(&S.raw_full[r], pages * (512u + pairs));
+          const uint32_t pages = __ballot_sync(0xffffffffu, in) & 0xffu;
+          if (lane == 0) {
+            S.pages[r] = pages;
+            tc05::bar_arrive_expect_tx(&S.raw_full[r], __popc(pages) * (512u + pairs));
+          }
+          if (!in && lane < 8 && kKeys * tile + kPage * lane < p.n_int) atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
           __syncwarp();
           if (in) {
             const uint8_t* src = A.pool + ((size_t)page * A.h_kv + p.h) * chunk_bytes(kCompact);
