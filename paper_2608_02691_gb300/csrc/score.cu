@@ -4,8 +4,8 @@
 // The sum over rows needs each row's normaliser first, and the logits are too many to
 // be kept (a row of 32768 floats for each of 64 tokens x 4 heads), so they are computed
 // twice: query_kernel rotates the queries, logit_kernel<false> finds each row's maximum
-// and sum by CTA, normaliser_kernel joins those, logit_kernel<true> computes the logits
-// again and adds exp2(l - lse) up.
+// and sum by CTA, logit_kernel<true> joins those, computes the logits again and adds
+// exp2(l - lse) up.
 //
 // Layout.  A tile is 128 keys times the block's columns (64 tokens x 4 heads at most):
 // D[key][column] = K Q^T on the tensor core, K in tensor memory (written there by the
@@ -61,8 +61,8 @@ struct QuerySmem {
   float R[kD][kRotPad];
   __nv_bfloat16 q[kRotCols][kQueryPad];
   // of the columns: by warp the largest element, the sum and the sum of magnitudes; <q, mu>
-  float top[8][kRotCols], sum[8][kRotCols], size[8][kRotCols], dot[kRotCols];
-  float most[2];  // the CTA's largest element, and sum of magnitudes
+  float top[8][kRotCols], sum[8][kRotCols], size[8][kRotCols], dot[kRotCols], given[kRotCols];
+  float most[3];  // the CTA's largest element, and sums of magnitudes, rotated and as given
 };
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -172,20 +172,27 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
         }
       }
     // <q, mu>: eight lanes a column
-    float d = 0.f;
-    for (int x = lane & 7; x < kD; x += 8)
-      d = fmaf(__bfloat162float(S.q[tid >> 3][x]), __ldg(A.mu + (size_t)h * kD + x), d);
+    float d = 0.f, l = 0.f;
+    for (int x = lane & 7; x < kD; x += 8) {
+      const float y = __bfloat162float(S.q[tid >> 3][x]);
+      d = fmaf(y, __ldg(A.mu + (size_t)h * kD + x), d);
+      l += fabsf(y);
+    }
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
-    if ((lane & 7) == 0) S.dot[tid >> 3] = d;
+    for (int o = 1; o < 8; o <<= 1) {
+      d += __shfl_xor_sync(0xffffffffu, d, o);
+      l += __shfl_xor_sync(0xffffffffu, l, o);
+    }
+    if ((lane & 7) == 0) S.dot[tid >> 3] = d, S.given[tid >> 3] = l;
   }
   __syncthreads();
   auto warps = [&](const float (&x)[8][kRotCols], int n) {
     return ((x[0][n] + x[1][n]) + (x[2][n] + x[3][n])) + ((x[4][n] + x[5][n]) + (x[6][n] + x[7][n]));
   };
   if (tid < 32) {
-    float m = 0.f, l = 0.f;
+    float m = 0.f, l = 0.f, given = 0.f;
     if (c0 < N) {
+      given = S.given[lane];
       for (int w = 0; w < 8; ++w) m = fmaxf(m, S.top[w][lane]);
       l = warps(S.size, lane);
     }
@@ -193,16 +200,18 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
     for (int o = 16; o > 0; o >>= 1) {
       m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
       l = fmaxf(l, __shfl_xor_sync(0xffffffffu, l, o));
+      given = fmaxf(given, __shfl_xor_sync(0xffffffffu, given, o));
     }
-    if (lane == 0) S.most[0] = m, S.most[1] = l;
+    if (lane == 0) S.most[0] = m, S.most[1] = l, S.most[2] = given;
   }
   const int cs = gridDim.x;  // a cluster has the block's columns
   if (cs > 1) cluster_barrier(); else __syncthreads();
-  float m = S.most[0], l = S.most[1];
+  float m = S.most[0], l = S.most[1], given = S.most[2];
   if (cs > 1) {
     for (int r = 0; r < cs; ++r) {
       m = fmaxf(m, __uint_as_float(cluster_ld32(&S.most[0], r)));
       l = fmaxf(l, __uint_as_float(cluster_ld32(&S.most[1], r)));
+      given = fmaxf(given, __uint_as_float(cluster_ld32(&S.most[2], r)));
     }
     cluster_arrive();  // no CTA leaves while its shared memory may be read
   }
@@ -241,7 +250,7 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
     }
     if (blockIdx.x == 0 && tid == 0)
       *reinterpret_cast<float4*>(line + 2 * A.cols) =
-          make_float4(__uint_as_float((uint32_t)(127 - E) << 23) * (A.compact ? 0x1p16f * kLogit : kLogit), kLogit * l, 0.f, 0.f);
+          make_float4(__uint_as_float((uint32_t)(127 - E) << 23) * (A.compact ? 0x1p16f * kLogit : kLogit), kLogit * l, kLogit * given, 0.f);
   }
   if (cs > 1) cluster_wait();
 }
@@ -271,7 +280,7 @@ struct Smem {
   uint8_t q[3][kBlockCols * 256];    // hi, lo, as given
   uint8_t raw[kRaw][kKeys / kPage][512 + 16 * meta_stride(kCompact)];  // a page's key codes and pairs
   alignas(16) float off[kBlockCols], sum[kCompact ? kBlockCols : 4];
-  float4 block;  // the block's factor, and its largest sum of magnitudes
+  float4 block;  // the block's factor, and its largest sums of magnitudes
   // minus the columns' references: pass 0 by warp, pass 1 the normalisers
   alignas(16) float ref[8][kKeys];
   float2 meet[8][kKeys];             // pass 0: the warps' parts of a piece (and, on the way, factors)
@@ -286,6 +295,8 @@ struct Smem {
   uint64_t raw_full[kRaw], raw_empty[kRaw], k_full[2], k_empty[2];
   uint64_t d_full[3][2], d_empty[3];  // by D and the epilogue group that takes it
   uint64_t piece_full[kPieces], piece_empty[kPieces], q_full, q_empty, drained;
+  // a piece's meeting of a group's warps (pass 0), and normalisers (pass 1, of all)
+  uint64_t meet_full[2], meet_empty[2];
   uint32_t tmem;
   int abort;
 };
@@ -312,14 +323,6 @@ template <int n>
 __device__ __forceinline__ void loaded(uint32_t (&x)[n]) {
 #pragma unroll
   for (int i = 0; i < n; ++i) asm volatile("" : "+r"(x[i]));
-}
-
-// The 128 threads of an epilogue group.
-__device__ __forceinline__ void group_sync(int g) {
-  if (g == 0)
-    asm volatile("bar.sync 1, 128;" ::: "memory");
-  else
-    asm volatile("bar.sync 2, 128;" ::: "memory");
 }
 
 // Largest of x over the warp (x is not NaN).
@@ -358,6 +361,10 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
     tc05::bar_init(&S.q_full, 1);
     tc05::bar_init(&S.q_empty, 9);  // the products, and the epilogue's warps
     tc05::bar_init(&S.drained, 1);
+    for (int i = 0; i < 2; ++i) {
+      tc05::bar_init(&S.meet_full[i], kSum ? 8 : 4);
+      tc05::bar_init(&S.meet_empty[i], kSum ? 8 : 4);
+    }
     S.abort = 0;
     tc05::bar_init_fence();
   }
@@ -400,15 +407,44 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
     for (uint32_t n = 0; next_piece(n, p); ++n) {
       const int tiles = p.t1 - p.t0, cols = p.cols();
       const bool pair = cols > kKeys;
+      if constexpr (kSum) {
+        // minus the columns' normalisers, from the parts of the CTAs that had keys of the segment
+        arrive(&S.meet_empty[0]);  // (the piece before has been read)
+        if (!wait(&S.meet_empty[0], n)) break;
+        const int col = tid;
+        float m = -INFINITY, l = 0.f;
+        auto join = [&](float2 x) {
+          const float mn = fmaxf(m, x.x);
+          if (x.y > 0.f) l = l * ex2(m - mn) + x.y * ex2(x.x - mn), m = mn;
+        };
+        if (col < cols) {
+          const int halves = pair ? 1 : 2;  // both groups' parts where they share the columns
+#pragma unroll 1
+          for (int i0 = 0; i0 < halves * (p.w1 - p.w0 + 1); i0 += 8) {
+            float2 x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int j = i0 + i, w = p.w0 + (pair ? j : j >> 1);
+              x[i] = w <= p.w1 ? __ldcg(score_part(A, w, p.seg) + (pair ? 0 : (j & 1) * kKeys) + col)
+                               : make_float2(0.f, 0.f);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) join(x[i]);
+          }
+        }
+        S.ref[0][col] = l > 0.f ? -(m + log2f(l)) : -INFINITY;
+        arrive(&S.meet_full[0]);
+        if (!wait(&S.meet_full[0], n)) break;
+      }
       if (!wait(&S.q_full, n)) break;
       float* ref = kSum ? S.ref[0] : S.ref[warp];
       const int cbase = !kSum && pair ? kKeys * g : 0;  // first column of the group's
-      const float factor = S.block.x, size = S.block.y;
+      const float factor = S.block.x;
       float acc[kSum ? 1 : kKeys];
       // what they may pass it by unseen: a piece's sum over its keys is below 2^128
       const float most = 119.f - (32 - __clz(tiles));
-      uint32_t known = 0;     // bit c: column 16 c + lane / 2 has a reference, or is none
-      float least = INFINITY; // no reference has been lower
+      uint32_t known = 0;     // bit c: column 16 c + lane / 2 has keys in its sum, or is none
+      float least = 0.f;      // no reference has been lower
       if constexpr (!kSum) {
 #pragma unroll
         for (int c = 0; c < kKeys; ++c) acc[c] = 0.f;
@@ -435,7 +471,9 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           if (!begun) {
             begun = true;
             const uint32_t r = (nk + t) % kRing, word = S.scale[r][key];
-            if (kCompact) {
+            if (exact) {
+              low = __uint_as_float(word);
+            } else if (kCompact) {
               const float2 y = unpack_half(word);
               scale = y.x * factor, low = y.y;
             } else {
@@ -530,11 +568,15 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
               }
             });
           } else {
-            // Columns without a reference, and such whose logits pass theirs by far, take the
-            // warp's largest.  That the logits cannot, of keys whose values are top at most, the
-            // queries' sums of magnitudes say; window keys are always looked at.
-            const float top = kCompact ? fmaxf(fabsf(low), fabsf(fmaf(3.f, scale / factor, low))) : scale / factor;
-            if (__any_sync(0xffffffffu, exact || known != 0xffu || (first < cols && size * top > least + most))) {
+            // References are 0 as long as no logit lies far from it: that none can, of keys whose
+            // values are top at most, the queries' sums of magnitudes say.  Else columns that
+            // have no keys yet, and such whose logits pass their reference by far, take the warp's
+            // largest.
+            const float top = exact ? low : kCompact ? fmaxf(fabsf(low), fabsf(fmaf(3.f, scale / factor, low))) : scale / factor;
+            const float size = exact ? S.block.z : S.block.y;
+            if (!__any_sync(0xffffffffu, (masked && known != 0xffu) || (first < cols && !(size * top <= least + most)))) {
+              known = 0xffu;
+            } else {
               float* by = reinterpret_cast<float*>(S.meet[warp]);  // by what a column's sum shrinks
               bool shrink = false;
 #pragma unroll 1
@@ -617,7 +659,8 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         }
         __syncwarp();
         // over the group's warps
-        group_sync(g);
+        arrive(&S.meet_full[g]);
+        if (!wait(&S.meet_full[g], n)) break;
         float m = -INFINITY, l = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -630,7 +673,8 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           if (y.y > 0.f) l += y.y * ex2(y.x - m);
         }
         score_part(A, w, p.seg)[kKeys * g + key] = make_float2(m, l);
-        group_sync(g);
+        arrive(&S.meet_empty[g]);
+        if (!wait(&S.meet_empty[g], n)) break;
       }
       arrive(&S.q_empty);
     }
@@ -728,16 +772,28 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
             src = reinterpret_cast<const uint4*>(
                 A.win.win + ((((size_t)p.slot * A.h_kv + p.h) * 2) * (A.sink + A.recent) + row) * kD);
           }
+          float top = 0.f;  // of the centered key
+#pragma unroll 1
+          for (int part = 0; part < 2; ++part) {
+            uint4 x[8];  // all on their way at once
 #pragma unroll
-          for (int part = 0; part < 4; ++part) {
-            uint32_t y[16];
+            for (int v = 0; v < 8; ++v) x[v] = src ? __ldcg(src + 8 * part + v) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              const uint4 x = src ? __ldcg(src + 4 * part + v) : make_uint4(0u, 0u, 0u, 0u);
-              y[4 * v] = x.x, y[4 * v + 1] = x.y, y[4 * v + 2] = x.z, y[4 * v + 3] = x.w;
+            for (int v = 0; v < 8; v += 2) {
+              const uint32_t y[8] = {x[v].x, x[v].y, x[v].z, x[v].w, x[v + 1].x, x[v + 1].y, x[v + 1].z, x[v + 1].w};
+              tc05::tmem_st8(tK + 32 * part + 4 * v, y);
+              if (!kSum) {
+                const float2* mu = reinterpret_cast<const float2*>(A.mu + (size_t)p.h * kD + 64 * part + 8 * v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                  const float2 m = __ldg(mu + e);
+                  top = fmaxf(top, fmaxf(fabsf(__uint_as_float(y[e] << 16) - m.x),
+                                         fabsf(__uint_as_float(y[e] & 0xffff0000u) - m.y)));
+                }
+              }
             }
-            tc05::tmem_st16(tK + 16 * part, y);
           }
+          scale = __float_as_uint(top);
         }
         S.scale[nk % kRing][key] = scale;
         const uint32_t counts = __ballot_sync(0xffffffffu, ok);
@@ -759,14 +815,13 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         const uint32_t bytes = (uint32_t)(p.N() + 7) / 8 * 2048, line = (uint32_t)p.N() * 4;
         if (lane == 0) {
           const uint8_t* src = qop_of(A, p.seg);
-          const int kinds = win ? 3 : 2;
-          tc05::bar_arrive_expect_tx(&S.q_full, kinds * bytes + (1 + kSum + kCompact) * line + 16);
+          const int all = win ? 3 : 2, kinds = p.t1 > p.I() ? 3 : 2;  // as given for window tiles
+          tc05::bar_arrive_expect_tx(&S.q_full, kinds * bytes + (1 + kCompact) * line + 16);
           for (int i = 0; i < kinds; ++i) tc05::bulk_g2s(S.q[i], src + (size_t)A.cols * 256 * i, bytes, &S.q_full);
-          const uint8_t* c = src + (size_t)A.cols * 256 * kinds;
+          const uint8_t* c = src + (size_t)A.cols * 256 * all;
           tc05::bulk_g2s(S.off, c, line, &S.q_full);
           if (kCompact) tc05::bulk_g2s(S.sum, c + (size_t)A.cols * 4, line, &S.q_full);
           tc05::bulk_g2s(&S.block, c + (size_t)A.cols * 8, 16, &S.q_full);
-          if (kSum) tc05::bulk_g2s(S.ref[0], A.lse + (size_t)p.seg * A.cols, line, &S.q_full);
         }
         __syncwarp();
         ++nq;
@@ -863,6 +918,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         ScorePiece p;
         p.t0 = p.t1 = 0;
         if (next.f < next.f1) next.next(A, p);
+        if (kSum) next.workers(A, p);
         more = p.t1 > p.t0;
         if (n >= kPieces && !wait(&S.piece_empty[i], n / kPieces - 1)) break;
         if (lane == 0) {
@@ -883,55 +939,12 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
   }
 }
 
-// --------------------------------------------------------- normalisers
-
-// CTA: a segment.  The columns' maxima and sums of the CTAs that had a part in it;
-// minus the log2 of the whole sum, or -infinity for a column of none.
-__global__ void __launch_bounds__(1024) normaliser_kernel(const __grid_constant__ ScoreArgs A) {
-  __shared__ long long sum[32];
-  __shared__ float2 meet[4][kBlockCols];
-  const int seg = blockIdx.x, b = seg / A.h_kv, h = seg % A.h_kv, tid = threadIdx.x;
-  pdl_wait();
-  pdl_trigger();
-  int w0, w1;
-  workers_of<Tiles>(A, b, h, A.W, sum, w0, w1);
-  if (w1 < w0) return;
-  const int cols = 4 * score_seq(A, b).rows;
-  const int col = tid % kBlockCols, split = tid / kBlockCols;
-  const bool pair = cols > kKeys;
-  float m = -INFINITY, l = 0.f;
-  auto join = [&](float2 x) {
-    if (x.y == 0.f) return;
-    const float mn = fmaxf(m, x.x);
-    l = l * ex2(m - mn) + x.y * ex2(x.x - mn);
-    m = mn;
-  };
-  if (col < cols) {
-#pragma unroll 4
-    for (int w = w0 + split; w <= w1; w += 4) {
-      const float2* part = score_part(A, w, seg);
-      if (pair) {
-        join(__ldcg(part + col));
-      } else {
-        const float2 x = __ldcg(part + col), y = __ldcg(part + kKeys + col);
-        join(x);
-        join(y);
-      }
-    }
-  }
-  meet[split][col] = make_float2(m, l);
-  __syncthreads();
-  if (split != 0 || col >= (cols + 15) / 16 * 16) return;
-  for (int i = 1; i < 4; ++i) join(meet[i][col]);
-  A.lse[(size_t)seg * A.cols + col] = col < cols && l > 0.f ? -(m + log2f(l)) : -INFINITY;
-}
-
 // ---------------------------------------------------------------- host
 
 size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 
 struct ScoreLayout {
-  size_t part, lse, total;
+  size_t part, total;
   int cols, W;
 };
 
@@ -941,8 +954,7 @@ ScoreLayout score_layout(const optr_params* p, int B, int max_new) {
   l.W = p->num_sms;
   const size_t segs = (size_t)B * p->cfg.h_kv;
   l.part = round_up(segs * qop_bytes(l.cols, p->cfg.sink + p->cfg.recent > 0));
-  l.lse = l.part + round_up((segs + l.W) * 2 * kKeys * sizeof(float2));
-  l.total = l.lse + round_up(segs * l.cols * sizeof(float));
+  l.total = l.part + round_up((segs + l.W) * 2 * kKeys * sizeof(float2));
   return l;
 }
 
@@ -982,7 +994,7 @@ extern "C" optr_status optr_kv_score_win(const optr_params* p, const void* q, in
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   ScoreArgs A{static_cast<const __nv_bfloat16*>(q), n_tok, cu_new, pos0, max_new, 0, block_table, B, max_pages,
               pool, num_pages, w, p->cfg.sink, p->cfg.recent, p->cfg.h_kv, p->cfg.group == 4 * kG, p->R_k, p->mu,
-              score, n_score, p->err, l.cols, ws, (float2*)(ws + l.part), (float*)(ws + l.lse), l.W};
+              score, n_score, p->err, l.cols, ws, (float2*)(ws + l.part), l.W};
   if (few_tokens(p, B, max_new, max_pages)) return cuda_status(launch_score_few(p, A, ws, stream));
   auto first = A.compact ? logit_kernel<false, true> : logit_kernel<false, false>;
   auto second = A.compact ? logit_kernel<true, true> : logit_kernel<true, false>;
@@ -998,7 +1010,6 @@ extern "C" optr_status optr_kv_score_win(const optr_params* p, const void* q, in
     const int parts = (l.cols + kRotCols - 1) / kRotCols;
     e = launch_pdl_cluster(query_kernel, dim3(parts, segs), dim3(kRotThreads), parts, sizeof(QuerySmem), stream, A);
     if (e == cudaSuccess) e = launch_pdl(first, dim3(l.W), dim3(kThreads), smem, stream, A);
-    if (e == cudaSuccess) e = launch_pdl(normaliser_kernel, dim3(segs), dim3(1024), 0, stream, A);
     if (e == cudaSuccess) e = launch_pdl(second, dim3(l.W), dim3(kThreads), smem, stream, A);
   }
   return cuda_status(e);

@@ -31,7 +31,6 @@ struct ScoreArgs {
   int cols;              // columns kept for a block
   uint8_t* qop;          // query operands, by (sequence, KV head)
   float2* part;          // [W + segments][2][kKeys] maxima and sums of a CTA
-  float* lse;            // [segments][cols]
   int W;                 // CTAs
 };
 
@@ -103,6 +102,7 @@ struct ScorePiece {
   int seg, b, h;
   int c0, pos0, n, rows, n_int, n_win, slot;
   int t0, t1;
+  int w0, w1;  // the workers that have a part in the segment
   __device__ __forceinline__ int I() const { return key_tiles(n_int); }  // INT2 tiles
   __device__ __forceinline__ int cols() const { return 4 * rows; }
   // columns of the products, a multiple of 16
@@ -119,7 +119,7 @@ struct Tiles {
 // b0 + i.
 template <typename Unit>
 struct ScoreFinder {
-  long long f, f1, F;
+  long long f, f1, F, W;
   int b0;
   long long base, incl;  // units of one head before the 32 held; up to and with the lane's
   ScoreSeq s;
@@ -144,7 +144,7 @@ struct ScoreFinder {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     F = sum * A.h_kv;
-    const long long W = min((long long)workers, max(1ll, F));  // each has a unit
+    W = min((long long)workers, max(1ll, F));  // each has a unit
     f = w < W ? F * w / W : F;
     f1 = w < W ? F * (w + 1) / W : F;
     base = 0;
@@ -175,7 +175,17 @@ struct ScoreFinder {
     p.seg = p.b * A.h_kv + p.h;
     p.t0 = (int)(r - (long long)p.h * T);
     p.t1 = (int)min((long long)T, p.t0 + (f1 - f));
+    p.w0 = 0, p.w1 = T;
     f += p.t1 - p.t0;
+  }
+
+  // The workers of the piece's segment (after next()).
+  __device__ __forceinline__ void workers(const ScoreArgs& A, ScorePiece& p) {
+    if (p.t1 <= p.t0) return;
+    const long long f0 = f - p.t1, T = p.w1;  // the segment's first unit, and its units
+    // the worker of a unit f: the largest w with w F / W <= f
+    p.w0 = (int)(((f0 + 1) * W - 1) / F);
+    p.w1 = (int)(((f0 + T) * W - 1) / F);
   }
 };
 
@@ -214,7 +224,8 @@ __device__ __forceinline__ void workers_of(const ScoreArgs& A, int b, int h, int
 // Operands of a (sequence, KV head)'s query block: hi and lo parts of the rotated
 // queries, the queries as given (with windows), 256 B a column each, then by column
 // <q, mu> and the rotated query's sum, then for the block the factor that brings a product
-// with the rotated ones to log2 units, and the largest sum of a column's magnitudes.
+// with the rotated ones to log2 units, and the largest sums of a column's magnitudes,
+// rotated and as given.
 __host__ __device__ __forceinline__ size_t qop_bytes(int cols, bool win) {
   return (size_t)cols * (256 * (win ? 3 : 2) + 8) + 16;
 }
