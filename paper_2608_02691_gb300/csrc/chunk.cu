@@ -938,14 +938,17 @@ __global__ void __launch_bounds__(256) chunk_combine_kernel(const __grid_constan
     o = make_float4(o.x * u + y.x * v, o.y * u + y.y * v, o.z * u + y.z * v, o.w * u + y.w * v);
   };
   constexpr int kAhead = 4;  // partials requested at a time
-  for (int x0 = w + split; x0 < seg.W && seg.F * x0 / seg.W < seg.end; x0 += kAhead * kSplit) {
+  // the last CTA whose range F x / W .. begins before `end` (one division: they were half of
+  // this kernel's instructions)
+  const int last = (int)min(seg.W - 1ll, (seg.end * seg.W - 1) / seg.F);
+  for (int x0 = w + split; x0 <= last; x0 += kAhead * kSplit) {
     float m[kAhead], l[kAhead];
     float4 y[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int x = x0 + k * kSplit;
       l[k] = 0.f;
-      if (in && x < seg.W && seg.F * x / seg.W < seg.end) {
+      if (in && x <= last) {
         const float* part = part_of(A, x, x != w);
         m[k] = __ldcg(part + (size_t)A.rows * kD + r);
         l[k] = __ldcg(part + (size_t)A.rows * (kD + 1) + r);
