@@ -651,7 +651,8 @@ optr_status optr_verify_tree(const optr_params* p, const void* target_probs,
  *   workspace   device, optr_kv_score_workspace_size bytes, 256-byte aligned, scratch as
  *               in optr_decode_attention.
  * Logits are good to some 2^-20 of |q||k| / sqrt(128) (queries and keys of 22 bits,
- * float32 sums); sums of a position are added in a fixed order.  Queries must be finite.  A
+ * float32 sums; of more than four tokens a query element is known to 2^-38 of the
+ * largest among 64 tokens besides); sums of a position are added in a fixed order.  Queries must be finite.  A
  * sequence with pos0 < 0, or n past max_pages * 16 or n_score (OPTR_DEVERR_SEQ_LEN), more
  * than max_new tokens or inconsistent cu_new (OPTR_DEVERR_CU_NEW) adds nothing.  Positions of
  * an out-of-range page (OPTR_DEVERR_PAGE_ID) or window slot (OPTR_DEVERR_WIN_SLOT) are

@@ -10,6 +10,10 @@
 // chunk's destinations).  Addresses come from the list and the table a chunk earlier
 // still.  Bound by memory: a record is read and written in pieces of 16 bytes, two lanes
 // to a slot's 32 code bytes.
+// Where every second of 8192 records stays, all of the cache is read (memory gives 64
+// bytes at a time, a piece is 32 or 16) and half written: 16 x 8192 to 4096 take 31.5 us,
+// 4.9 TB/s of those bytes.  Records brought into L2 three chunks ahead took 38.5, clusters
+// of 8 CTAs with one chunk each 36.9.
 //
 // Windows.  A ring of r rows turns by n - n' rows: CTAs of their own take 64 bytes of
 // each row of a (sequence, KV head, kind), load all r pieces and store them.

@@ -5,7 +5,7 @@
 // all in one launch: a cluster of CTAs takes a (sequence, KV head), each CTA a range of
 // its pages and window rows; it rotates the queries (as the decode does), keeps the
 // logits in shared memory (in the workspace where they do not fit), and maxima and sums
-// meet across the cluster.  16 x 1 over 8192: 29.5 us, 1.7 TB/s; of that 9 us are the
+// meet across the cluster.  16 x 1 over 8192: 29.5 us, 1.7 TB/s; of that some 9 us are the
 // products and what brings the codes to them, 7 us the rest of the page loop, 8 us the weights
 // and 6 us the launch and the rotation, and 24 of 152 SMs have no (sequence, KV head).  One
 // token over 1024: 8.8 us, the host's time of a call.

@@ -65,8 +65,8 @@ def test_tiles(new, opts):
 @pytest.mark.parametrize("new", [[4], [60]])
 @pytest.mark.parametrize("opts", [dict(), dict(group=128), PAPER])
 def test_queries_of_very_different_sizes(new, opts):
-    """The tensor core's form has one power of two for a block's queries.  An element is known to 2^-39 of
-    the block's largest, so a logit of any row to 2^-39 |k| / sqrt(128) times 128 of those: under 2^-24 here."""
+    """The tensor core's form has one power of two for a block's queries.  An element is known to 2^-38 of
+    the block's largest, so a logit of any row to 2^-38 |k| / sqrt(128) times 128 of those: under 2^-23 here."""
     c = Score(new, [600], seed=55, **opts)
     size = torch.tensor([1.0, 1e-3, 0.0, 1e-6, 0.3], device="cuda")[torch.arange(new[0], device="cuda") % 5]
     c.q.mul_(size[:, None, None])
