@@ -14,8 +14,8 @@
 // is a sum along its registers, and the sum over keys of the first pass is kept per
 // column in registers too and meets the other lanes' once a piece.
 //
-// Bound.  A tile's products: 1.3 us for one pair a slot (two products), 2 us for four
-// (three), at 256 columns; with 32 columns the keys' way into tensor memory, 1.4 us.
+// Bound.  A tile's products: 1.3 us at 256 columns (two products); with 32 columns the keys'
+// way into tensor memory.
 // 2 x 64 tokens over some 32000 positions take 140 us: 70 and 66 for the two passes (26
 // tiles an SM each, the tensor pipe 50% busy; without exponentials 66 and 61, without half
 // of the products 60 and 58), the rest the query kernel and the launches.  What is left
@@ -27,13 +27,14 @@
 // and no maximum is looked for (70 us; with one for each column 95).
 //
 // Rounding.  The sums are float32, and a weight moves by what its logit does: rounding
-// queries or keys to 16 bits would move it by some 3e-4.  So both go in as fp16 hi + lo
-// parts (22 bits; queries over a power of two by block, keys over one by key), and a tile
-// takes the products hi hi + hi lo + lo hi.  A group of a slot has four values, so the
-// parts of 16 values are computed in float32 and the codes pick among them by byte
-// permutes.  With one pair a slot the codes go in as subnormal numbers, code
-// 2^-16 (lower bits cost the sums precision: products are aligned as if their operands
-// were normal), its scale and minimum are the epilogue's, and two products do.  Window keys and their queries are bf16 as they are, one product.
+// queries or keys to 16 bits would move it by some 3e-4.  So queries go in as fp16 hi + lo
+// parts (22 bits, over a power of two by block), and keys without a rounding.  With one
+// pair a slot the codes are the operand, as subnormal numbers, code 2^-16 (lower bits cost
+// the sums precision: products are aligned as if their operands were normal), and scale
+// and minimum are the epilogue's.  With four pairs a value is (code - 1) scale, four numbers
+// of a group that fp16 holds (over a power of two by key; the codes pick among them by byte
+// permutes), plus minimum + scale of its group, which meets the query's sum over the group in one
+// step more, both as hi + lo.  Window keys and their queries are bf16 as they are, one product.
 #include "cluster.cuh"
 #include "f32x2.cuh"
 #include "score.cuh"
@@ -60,6 +61,10 @@ __host__ __device__ constexpr int key_place(int channel, bool codes) {
 __device__ __forceinline__ int operand_offset(int n, int k) {
   return (n / 8) * 2048 + (k / 8) * 128 + (n % 8) * 16 + (k % 8) * 2;
 }
+
+// An operand of 16 inner elements: two core matrices, 128 B apart, of 8 columns each; the
+// first element of column n (the ninth is 128 B on).
+__device__ __forceinline__ int ext_offset(int n) { return (n / 8) * 256 + (n % 8) * 16; }
 
 constexpr int kRotThreads = 256;
 constexpr int kRotCols = 32;  // columns of a CTA: 8 tokens
@@ -231,7 +236,7 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
     // The block's largest at 2^13 .. 2^14: an element has 22 bits down to 2^-17 of that, and
     // below it is known to 2^-38 of the largest.
     const int E = m > 0.f ? max(-100, min(100, 13 - ((int)(__float_as_uint(m) >> 23) - 127))) : 0;
-    float* line = reinterpret_cast<float*>(out + (size_t)A.cols * (win ? 768 : 512));
+    float* line = reinterpret_cast<float*>(out + qop_lines(A.cols, win, A.compact));
     const float up = __uint_as_float((uint32_t)(127 + E) << 23);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -256,6 +261,15 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
             *reinterpret_cast<__half2*>(at + A.cols * 128) = lo;
           }
         }
+    // Beside four pairs a slot: the groups' sums, over 2^5 (32 channels), as the parts that meet
+    // a key's minima: hi, lo, hi
+    if (!A.compact && tid < 128 && c0 + lane < N) {
+      const int n = c0 + lane;
+      const float x = (S.sum[2 * warp][lane] + S.sum[2 * warp + 1][lane]) * (up * 0x1p-5f);
+      const __half hi = __float2half_rn(x), lo = __float2half_rn(x - __half2float(hi));
+      __half* at = reinterpret_cast<__half*>(out + (size_t)A.cols * (win ? 768 : 512) + ext_offset(n)) + warp;
+      at[0] = hi, at[4] = lo, at[64] = hi, at[68] = __float2half_rn(0.f);
+    }
     if (tid < kRotCols && c0 + tid < N) {
       line[c0 + tid] = kLogit * S.dot[tid];
       line[A.cols + c0 + tid] = kLogit * warps(S.sum, tid);
@@ -276,26 +290,28 @@ constexpr int kThreads = 512;
 constexpr int kRegLaunch = 128, kRegEpi = 208, kRegKey = 56, kRegIssue = 40;
 static_assert(2 * kRegEpi + kRegKey + kRegIssue <= 4 * kRegLaunch, "registers of the launch");
 constexpr uint32_t kTmemCols = 512, kColD = 0;
-// D[d] at 128 d, then the keys: two of hi and lo parts, or two of codes and one D more
+// D[d] at 128 d, then two tiles of keys: 64 columns, and 8 for the minima of four pairs a slot;
+// without those there is room for a D more
 template <bool kCompact>
 struct Tmem {
   static constexpr int kDs = kCompact ? 3 : 2;
-  static constexpr uint32_t kColK = 128u * kDs, kKeyCols = kCompact ? 64u : 128u;
+  static constexpr uint32_t kColK = 128u * kDs, kKeyCols = kCompact ? 64u : 80u;
 };
-constexpr int kRaw = 3;        // tiles of records on the way
 constexpr int kPieces = 3;     // pieces found ahead
 constexpr int kConsumers = 14; // warps that take the pieces
 constexpr float kSlack = 60.f; // a column's logits may pass its reference by 2^60
 
 template <bool kCompact>
 struct Smem {
+  static constexpr int kRaw = kCompact ? 3 : 2;  // tiles of records on the way
   uint8_t q[3][kBlockCols * 256];    // hi, lo, as given
   uint8_t raw[kRaw][kKeys / kPage][512 + 16 * meta_stride(kCompact)];  // a page's key codes and pairs
   alignas(16) float off[kBlockCols], sum[kCompact ? kBlockCols : 4];
+  alignas(16) uint8_t ext[kCompact ? 16 : kBlockCols * 32];  // the groups' sums
   float4 block;  // the block's factor, and its largest sums of magnitudes
   // minus the columns' references: pass 0 by warp, pass 1 the normalisers
   alignas(16) float ref[8][kKeys];
-  float2 meet[8][kKeys];             // pass 0: the warps' parts of a piece (and, on the way, factors)
+  float meet[8][kKeys];              // pass 0: the warps' sums of a piece (and, on the way, factors)
   // A key's power of two, or its pair, and whether it counts.  Read between a tile's
   // logits and its last D being free; written for tile t + kRing once the products of
   // t + kRing - 2 are done, which waited for the Ds before their own.
@@ -351,6 +367,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
   constexpr int kDs = Tmem::kDs;
   Smem<kCompact>& S = *reinterpret_cast<Smem<kCompact>*>(dsm_);
   constexpr uint32_t kRing = Smem<kCompact>::kRing;
+  constexpr int kRaw = Smem<kCompact>::kRaw;
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   if (tid == 0) {
@@ -589,7 +606,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
             if (!__any_sync(0xffffffffu, (masked && known != 0xffu) || (first < cols && !(size * top <= least + most)))) {
               known = 0xffu;
             } else {
-              float* by = reinterpret_cast<float*>(S.meet[warp]);  // by what a column's sum shrinks
+              float* by = S.meet[warp];  // by what a column's sum shrinks
               bool shrink = false;
 #pragma unroll 1
               for (int c = 0; c < kKeys / 16; ++c) {
@@ -667,7 +684,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
               a[j] = mine + __shfl_xor_sync(0xffffffffu, other, o);
             }
           }
-          S.meet[warp][32 * c + lane] = make_float2(-ref[32 * c + lane], a[0]);
+          S.meet[warp][32 * c + lane] = a[0];
         }
         __syncwarp();
         // over the group's warps
@@ -676,13 +693,12 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         float m = -INFINITY, l = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float2 y = S.meet[4 * g + i][key];
-          if (y.y > 0.f) m = fmaxf(m, y.x);
+          if (S.meet[4 * g + i][key] > 0.f) m = fmaxf(m, -S.ref[4 * g + i][key]);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float2 y = S.meet[4 * g + i][key];
-          if (y.y > 0.f) l += y.y * ex2(y.x - m);
+          const float y = S.meet[4 * g + i][key];
+          if (y > 0.f) l += y * ex2(-S.ref[4 * g + i][key] - m);
         }
         score_part(A, w, p.seg)[kKeys * g + key] = make_float2(m, l);
         arrive(&S.meet_empty[g]);
@@ -711,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           ok = kKeys * tile + key < p.n_int && (S.pages[r] >> (key / kPage) & 1);
           const uint8_t* raw = S.raw[r][key / kPage];
           const int slot = key % kPage;
-          [[maybe_unused]] uint32_t hi[4][2], lo[4][2];  // the four values of each group
+          [[maybe_unused]] uint32_t value[4][2], least[2][4];  // of each group; minima's parts
           if constexpr (kCompact) {
             scale = *reinterpret_cast<const uint32_t*>(raw + 512 + ms * slot);
           } else {
@@ -727,17 +743,22 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
             const int E = min(max((int)(__float_as_uint(top) >> 23) - 126, -60), 60);
             const float down = __uint_as_float((uint32_t)(127 - E) << 23);
             scale = (uint32_t)(127 + E) << 23;
+            // a value is (code - 1) scale, which fp16 holds, and the rest of its group's
+            float x[4];
 #pragma unroll
             for (int G = 0; G < 4; ++G) {
               const float2 y = unpack_half(pairs[G]);
-              const float sc = y.x * down, mn = y.y * down;
+              const float sc = y.x * down;
+              value[G][0] = pack_half(-sc, 0.f);
+              value[G][1] = pack_half(sc, 2.f * sc);
+              x[G] = (y.x + y.y) * down * 32.f;
+            }
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const float a = fmaf((float)(2 * e), sc, mn), b = fmaf((float)(2 * e + 1), sc, mn);
-                hi[G][e] = pack_half(a, b);
-                const float2 z = unpack_half(hi[G][e]);
-                lo[G][e] = pack_half(a - z.x, b - z.y);
-              }
+            for (int i = 0; i < 2; ++i) {
+              least[0][i] = least[0][2 + i] = pack_half(x[2 * i], x[2 * i + 1]);
+              const float2 z = unpack_half(least[0][i]);
+              least[1][i] = pack_half(x[2 * i] - z.x, x[2 * i + 1] - z.y);
+              least[1][2 + i] = 0u;
             }
           }
           if (nk >= 2 && !wait(&S.k_empty[s], nk / 2 - 1)) break;
@@ -765,13 +786,15 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
                   pick[6 + e] = pick[4 + e] >> 16;
                 }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = __byte_perm(hi[e / 2][0], hi[e / 2][1], pick[e]);
+                for (int e = 0; e < 8; ++e) y[e] = __byte_perm(value[e / 2][0], value[e / 2][1], pick[e]);
                 tc05::tmem_st8(tK + 16 * part + 8 * v, y);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = __byte_perm(lo[e / 2][0], lo[e / 2][1], pick[e]);
-                tc05::tmem_st8(tK + 64 + 16 * part + 8 * v, y);
               }
             }
+          }
+          if constexpr (!kCompact) {
+            const uint32_t y[8] = {least[0][0], least[0][1], least[0][2], least[0][3],
+                                   least[1][0], least[1][1], least[1][2], least[1][3]};
+            tc05::tmem_st8(tK + 64, y);
           }
           arrive(&S.raw_empty[r]);
         } else {
@@ -828,9 +851,11 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         if (lane == 0) {
           const uint8_t* src = qop_of(A, p.seg);
           const int all = win ? 3 : 2, kinds = p.t1 > p.I() ? 3 : 2;  // as given for window tiles
-          tc05::bar_arrive_expect_tx(&S.q_full, kinds * bytes + (1 + kCompact) * line + 16);
+          const uint32_t ext = kCompact ? 0u : (uint32_t)(p.N() + 7) / 8 * 256;
+          tc05::bar_arrive_expect_tx(&S.q_full, kinds * bytes + ext + (1 + kCompact) * line + 16);
           for (int i = 0; i < kinds; ++i) tc05::bulk_g2s(S.q[i], src + (size_t)A.cols * 256 * i, bytes, &S.q_full);
-          const uint8_t* c = src + (size_t)A.cols * 256 * all;
+          if (!kCompact) tc05::bulk_g2s(S.ext, src + (size_t)A.cols * 256 * all, ext, &S.q_full);
+          const uint8_t* c = src + qop_lines(A.cols, win, kCompact);
           tc05::bulk_g2s(S.off, c, line, &S.q_full);
           if (kCompact) tc05::bulk_g2s(S.sum, c + (size_t)A.cols * 4, line, &S.q_full);
           tc05::bulk_g2s(&S.block, c + (size_t)A.cols * 8, 16, &S.q_full);
@@ -876,7 +901,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
       __syncwarp();
     } else if (warp == kMmaWarp) {
       // ----------------------------------------------------------- products
-      const uint32_t sq = tc05::smem_addr(S.q[0]);
+      const uint32_t sq = tc05::smem_addr(S.q[0]), ext = tc05::smem_addr(S.ext);
       uint32_t nk = 0, nu = 0;
       bool used = false;
       ScorePiece p;
@@ -902,9 +927,9 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
               tc05::mma128_ts<16>(out, a, tc05::smem_desc(b + kPart, 128, 2048), id, 0);
               tc05::mma128_ts<16>(out, a, tc05::smem_desc(b, 128, 2048), id, 1);
             } else {
-              // the small parts first: a third of the steps round at the sum's size
+              // the small parts first: half of the steps round at the sum's size
               tc05::mma128_ts<16>(out, a, tc05::smem_desc(b + kPart, 128, 2048), id, 0);
-              tc05::mma128_ts<16>(out, a + 64, tc05::smem_desc(b, 128, 2048), id, 1);
+              tc05::mma16_ts(out, a + 64, tc05::smem_desc(ext + (uint32_t)d * (kKeys * 32), 128, 256), id, 1);
               tc05::mma128_ts<16>(out, a, tc05::smem_desc(b, 128, 2048), id, 1);
             }
             tc05::mma_commit_warp(&S.d_full[D][kSum || !pair ? t & 1 : d]);
@@ -965,7 +990,7 @@ ScoreLayout score_layout(const optr_params* p, int B, int max_new) {
   l.cols = (4 * std::min(max_new, kTok) + 15) / 16 * 16;
   l.W = p->num_sms;
   const size_t segs = (size_t)B * p->cfg.h_kv;
-  l.part = round_up(segs * qop_bytes(l.cols, p->cfg.sink + p->cfg.recent > 0));
+  l.part = round_up(segs * qop_bytes(l.cols, p->cfg.sink + p->cfg.recent > 0, p->cfg.group == 4 * kG));
   l.total = l.part + round_up((segs + l.W) * 2 * kKeys * sizeof(float2));
   return l;
 }

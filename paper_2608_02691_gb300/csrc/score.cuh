@@ -222,15 +222,18 @@ __device__ __forceinline__ void workers_of(const ScoreArgs& A, int b, int h, int
 }
 
 // Operands of a (sequence, KV head)'s query block: hi and lo parts of the rotated
-// queries, the queries as given (with windows), 256 B a column each, then by column
-// <q, mu> and the rotated query's sum, then for the block the factor that brings a product
-// with the rotated ones to log2 units, and the largest sums of a column's magnitudes,
-// rotated and as given.
-__host__ __device__ __forceinline__ size_t qop_bytes(int cols, bool win) {
-  return (size_t)cols * (256 * (win ? 3 : 2) + 8) + 16;
+// queries, the queries as given (with windows), 256 B a column each, and of four pairs a
+// slot the groups' sums of the rotated ones, 32 B a column; then by column <q, mu> and the
+// rotated query's sum, and for the block the factor that brings a product with the rotated
+// ones to log2 units, and the largest sums of a column's magnitudes, rotated and as given.
+__host__ __device__ __forceinline__ size_t qop_lines(int cols, bool win, bool compact) {
+  return (size_t)cols * (256 * (win ? 3 : 2) + (compact ? 0 : 32));
+}
+__host__ __device__ __forceinline__ size_t qop_bytes(int cols, bool win, bool compact) {
+  return qop_lines(cols, win, compact) + (size_t)cols * 8 + 16;
 }
 __device__ __forceinline__ uint8_t* qop_of(const ScoreArgs& A, int seg) {
-  return A.qop + (size_t)seg * qop_bytes(A.cols, A.win.win != nullptr);
+  return A.qop + (size_t)seg * qop_bytes(A.cols, A.win.win != nullptr, A.compact);
 }
 // a CTA's partial of a segment: (CTA, segment) pairs lie on a staircase, so their sum is
 // a slot of its own
