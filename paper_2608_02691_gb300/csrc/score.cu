@@ -312,7 +312,7 @@ struct Smem {
   // minus the columns' references: pass 0 by warp, pass 1 the normalisers
   alignas(16) float ref[8][kKeys];
   float meet[8][kKeys];              // pass 0: the warps' sums of a piece (and, on the way, factors)
-  // A key's power of two, or its pair, and whether it counts.  Read between a tile's
+  // A key's largest value, or its pair, and whether it counts.  Read between a tile's
   // logits and its last D being free; written for tile t + kRing once the products of
   // t + kRing - 2 are done, which waited for the Ds before their own.
   static constexpr int kRing = kCompact ? 8 : 4;
@@ -352,6 +352,9 @@ __device__ __forceinline__ void loaded(uint32_t (&x)[n]) {
 #pragma unroll
   for (int i = 0; i < n; ++i) asm volatile("" : "+r"(x[i]));
 }
+
+// The power of two that a key is divided by, of its largest value's bits.
+__device__ __forceinline__ int key_power(uint32_t top) { return min(max((int)(top >> 23) - 126, -60), 60); }
 
 // Largest of x over the warp (x is not NaN).
 __device__ __forceinline__ float warp_largest(float x) {
@@ -506,7 +509,8 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
               const float2 y = unpack_half(word);
               scale = y.x * factor, low = y.y;
             } else {
-              scale = __uint_as_float(word) * factor;
+              scale = __uint_as_float((uint32_t)(127 + key_power(word)) << 23) * factor;
+              low = __uint_as_float(word);
             }
             const int i = kKeys * (exact ? tile - p.I() : tile) + key;
             const int pos = exact ? win_pos(i, p.n, A.sink, A.recent) : A.sink + i;
@@ -601,7 +605,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
             // values are top at most, the queries' sums of magnitudes say.  Else columns that
             // have no keys yet, and such whose logits pass their reference by far, take the warp's
             // largest.
-            const float top = exact ? low : kCompact ? fmaxf(fabsf(low), fabsf(fmaf(3.f, scale / factor, low))) : scale / factor;
+            const float top = exact || !kCompact ? low : fmaxf(fabsf(low), fabsf(fmaf(3.f, scale / factor, low)));
             const float size = exact ? S.block.z : S.block.y;
             if (!__any_sync(0xffffffffu, (masked && known != 0xffu) || (first < cols && !(size * top <= least + most)))) {
               known = 0xffu;
@@ -740,9 +744,8 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
               const float2 y = unpack_half(pairs[G]);
               top = fmaxf(top, fmaxf(fabsf(y.y), fabsf(fmaf(3.f, y.x, y.y))));
             }
-            const int E = min(max((int)(__float_as_uint(top) >> 23) - 126, -60), 60);
-            const float down = __uint_as_float((uint32_t)(127 - E) << 23);
-            scale = (uint32_t)(127 + E) << 23;
+            scale = __float_as_uint(top);
+            const float down = __uint_as_float((uint32_t)(127 - key_power(scale)) << 23);
             // a value is (code - 1) scale, which fp16 holds, and the rest of its group's
             float x[4];
 #pragma unroll
