@@ -266,11 +266,14 @@ extern "C" optr_status optr_kv_compact_win(const optr_params* p, const int32_t* 
   // CTAs of a (sequence, KV head): two per SM in all, each a chunk at least
   int cs = 1;
   while (cs < 8 && segs * 2 * cs <= 2 * p->num_sms && n_most > cs * kRecords) cs *= 2;
+  // few long lists: 16 (one of 131072 to 30000, 8 heads: 39.9 -> 29.6 us)
+  if (cs == 8 && segs * 16 <= p->num_sms && n_most > 16 * kRecords) cs = 16;
   const bool turn = w.win && p->cfg.recent > 0;
   const long long n_rec = segs * cs, units = turn ? (segs * 2 * kSlices + cs - 1) / cs * cs : 0;
   const CompactArgs A{kept, n_kept, lens, block_table, n_most, max_pages, num_pages, p->cfg.h_kv, B,
                       pool, score, n_score, w, p->cfg.sink, p->cfg.recent, cs, (int)n_rec, p->err};
   auto fn = p->cfg.group == 4 * kG ? compact_kernel<true> : compact_kernel<false>;
+  if (cs > 8 && ensure_wide_clusters(reinterpret_cast<const void*>(fn)) != cudaSuccess) return OPTR_ERR_CUDA;
   return cuda_status(launch_pdl_cluster(fn, dim3((unsigned)(n_rec + units)), dim3(kThreads), cs, 0, stream, A));
 }
 

@@ -262,13 +262,20 @@ extern "C" optr_status optr_evict_select(const optr_params* p, const float* scor
     return OPTR_ERR_INVALID_ARG;
   const long long rows = (long long)B * p->cfg.h_kv;
   if (rows > (1 << 27) || n_score > (1 << 30)) return OPTR_ERR_OUT_OF_RANGE;
-  // CTAs of a row: as few as leave each 4096 scores or fewer, two per SM in all (64 rows of
-  // 32768: clusters of 4 16.4 us; of 8, which are not all resident at once, 35 us)
+  // CTAs of a row: as few as leave each 4096 scores or fewer, one per SM in all (16 x 8 rows of
+  // 8192: one CTA each 8.6 us, two 12.4), and as many as are resident at once (64 rows of 32768
+  // in clusters of 8: 35 us, of 2 16.4)
   int log_cs = 0;
-  while (log_cs < 3 && n_score > 4096 << log_cs && (rows << log_cs) <= p->num_sms) ++log_cs;
+  while (log_cs < 3 && n_score > 4096 << log_cs &&
+         (rows << (log_cs + 1)) <= (log_cs < 2 ? p->num_sms : p->num_sms * 3 / 4))
+    ++log_cs;
   const int cs = 1 << log_cs;
   const int per = (n_score - 1) / (cs * kThreads) + 1;
-  auto fn = per <= 8 ? select_kernel<8> : per <= 16 ? select_kernel<16> : per <= 32 ? select_kernel<32> : select_kernel<0>;
+  auto fn = per <= 8    ? select_kernel<8>
+            : per <= 16 ? select_kernel<16>
+            : per <= 32 ? select_kernel<32>
+            : per <= 64 ? select_kernel<64>
+                        : select_kernel<0>;
   return cuda_status(launch_pdl_cluster(fn, dim3((unsigned)(rows * cs)), dim3(kThreads), cs, 0, stream, score,
                                         n_score, lens, keep, p->cfg.h_kv, first, last, kept, n_most, n_kept, log_cs,
                                         p->err));

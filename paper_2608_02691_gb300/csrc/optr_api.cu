@@ -69,11 +69,13 @@ bool io_pointer(const void* ptr, const void** dev, bool* host) {
   return false;
 }
 
-cudaError_t ensure_dynamic_smem(const void* kernel, size_t bytes) {
+// An attribute of a kernel on the current device, set once to a value as large as `least`.
+static cudaError_t ensure_attribute(const void* kernel, cudaFuncAttribute attribute, size_t least) {
   struct Entry {
     const void* kernel;
     int device;
-    size_t bytes;
+    cudaFuncAttribute attribute;
+    size_t value;
   };
   static std::mutex mu;
   static std::vector<Entry> done;
@@ -83,16 +85,23 @@ cudaError_t ensure_dynamic_smem(const void* kernel, size_t bytes) {
   std::lock_guard<std::mutex> lock(mu);
   Entry* hit = nullptr;
   for (Entry& x : done)
-    if (x.kernel == kernel && x.device == dev) hit = &x;
-  if (hit && hit->bytes >= bytes) return cudaSuccess;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           (int)bytes);
+    if (x.kernel == kernel && x.device == dev && x.attribute == attribute) hit = &x;
+  if (hit && hit->value >= least) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, attribute, (int)least);
   if (e != cudaSuccess) return e;
   if (hit)
-    hit->bytes = bytes;
+    hit->value = least;
   else
-    done.push_back(Entry{kernel, dev, bytes});
+    done.push_back(Entry{kernel, dev, attribute, least});
   return cudaSuccess;
+}
+
+cudaError_t ensure_dynamic_smem(const void* kernel, size_t bytes) {
+  return ensure_attribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+cudaError_t ensure_wide_clusters(const void* kernel) {
+  return ensure_attribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
 }
 
 // Workspace of one decode call (all offsets 256-byte aligned):

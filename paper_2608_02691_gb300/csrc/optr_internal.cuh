@@ -100,6 +100,7 @@ cudaError_t noalloc_scratch_address(void** out);
 // after this opt-in).  Cached per (kernel, device) under a lock, so the
 // runtime call is made once per new maximum.
 cudaError_t ensure_dynamic_smem(const void* kernel, size_t bytes);
+cudaError_t ensure_wide_clusters(const void* kernel);  // of 16 CTAs
 
 // Programmatic dependent launch.  Every kernel of the library is launched
 // with launch_pdl(), so the GPU may schedule it while the previous kernel in

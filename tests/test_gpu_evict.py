@@ -390,3 +390,32 @@ def test_choice_and_move_in_a_graph():
         g.replay()
         c.check(want)
     assert optr.optr_device_error(c.p) == 0
+
+
+@pytest.mark.parametrize("n,counts,opts", [(20000, 9001, dict()), (9000, 8700, dict(group=128)), (33000, 32000, PAPER)])
+def test_long_lists_of_one_sequence(n, counts, opts):
+    """More chunks than one, in clusters of every width (16 CTAs from 8193 places on)."""
+    c = Cache([n], seed=n % 7, **opts)
+    kept = c.lists([counts])
+    want = c.plain(kept, [counts])
+    c.run(kept, [counts])
+    c.check(want)
+    assert optr.optr_device_error(c.p) == 0
+
+
+@pytest.mark.parametrize("B,n,h", [(16, 4097, 8), (19, 8192, 8), (5, 70000, 4), (4, 131072, 4)])
+def test_choice_in_every_split(B, n, h):
+    """Rows that one CTA takes, and clusters of 2, 4 and 8 with up to 64 scores a thread."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    p = params(h)
+    score = torch.rand(B, h, n, device="cuda", generator=g)
+    score[:, :, ::3] = 0.0
+    k = n // 3 + 7
+    kept = torch.full((B, h, k), -1, dtype=torch.int32, device="cuda")
+    count = i32([0] * B)
+    optr.optr_evict_select(p, score, i32([n] * B), i32([k] * B), 4, 64, kept, count)
+    key = score.clone()
+    key[:, :, :4] = 2.0
+    key[:, :, -64:] = 2.0
+    order = key.sort(dim=2, descending=True, stable=True).indices[:, :, :k]
+    assert torch.equal(kept.long(), order.sort(dim=2).values) and count.tolist() == [k] * B
