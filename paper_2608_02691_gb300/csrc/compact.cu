@@ -15,8 +15,9 @@
 // 4.9 TB/s of those bytes.  Records brought into L2 three chunks ahead took 38.5, clusters
 // of 8 CTAs with one chunk each 36.9.
 //
-// Windows.  A ring of r rows turns by n - n' rows: CTAs of their own take 64 bytes of
-// each row of a (sequence, KV head, kind), load all r pieces and store them.
+// Windows.  A ring of r rows turns by n - n' rows: CTAs of their own take the rows of a
+// (sequence, KV head, kind), all bytes or a half or quarter of them, load 64 KB and
+// store them.
 #include "cluster.cuh"
 #include "optr_internal.cuh"
 
@@ -27,7 +28,6 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kRecords = 512;  // of a chunk, by CTA
-constexpr int kSlices = 4;     // column slices of a window row
 
 struct CompactArgs {
   const int32_t *kept, *n_kept, *lens, *bt;
@@ -38,6 +38,7 @@ struct CompactArgs {
   WinArgs win;
   int sink, recent;
   int cs, n_rec;  // CTAs of a (sequence, KV head); of them in all
+  int slices;     // of a window row: 1, 2 or 4
   unsigned* err;
 };
 
@@ -202,7 +203,8 @@ __device__ void move_records(const CompactArgs& A, Smem& S) {
 }
 
 __device__ void turn_ring(const CompactArgs& A, int unit) {
-  const int slice = unit % kSlices, kind = unit / kSlices % 2, seg = unit / (2 * kSlices);
+  const int slice = unit % A.slices, kind = unit / A.slices % 2, seg = unit / (2 * A.slices);
+  const int pieces = 16 / A.slices;  // of 16 bytes, of a row
   const int b = seg / A.h_kv, h = seg % A.h_kv, tid = threadIdx.x;
   if (b >= A.B) return;
   const Job job = job_of(A, b, h);
@@ -210,21 +212,21 @@ __device__ void turn_ring(const CompactArgs& A, int unit) {
   if (d == 0 || d % A.recent == 0) return;
   uint8_t* base = reinterpret_cast<uint8_t*>(A.win.win) +
                   (((size_t)__ldcg(A.win.slot + b) * A.h_kv + h) * 2 + kind) * (size_t)rows * (2 * kD) +
-                  64 * slice + 16 * (tid & 3);
+                  16 * (pieces * slice + tid % pieces);
   // position n - recent + j, at row sink + (n - recent + j - sink) % recent
   const int old0 = (job.n - A.sink) % A.recent, new0 = (job.m - A.sink) % A.recent;
-  constexpr int kMost = 1024 * 4 / kThreads;  // the longest ring's pieces
+  constexpr int kMost = 8;  // pieces of a thread
   uint4 x[kMost];
 #pragma unroll
   for (int e = 0; e < kMost; ++e) {
-    const int j = (kThreads / 4) * e + tid / 4;
+    const int j = (kThreads * e + tid) / pieces;
     if (j < A.recent)
       x[e] = __ldcg(reinterpret_cast<const uint4*>(base + (size_t)(A.sink + (old0 + j) % A.recent) * (2 * kD)));
   }
   __syncthreads();
 #pragma unroll
   for (int e = 0; e < kMost; ++e) {
-    const int j = (kThreads / 4) * e + tid / 4;
+    const int j = (kThreads * e + tid) / pieces;
     if (j < A.recent)
       *reinterpret_cast<uint4*>(base + (size_t)(A.sink + (new0 + j) % A.recent) * (2 * kD)) = x[e];
   }
@@ -269,9 +271,10 @@ extern "C" optr_status optr_kv_compact_win(const optr_params* p, const int32_t* 
   // few long lists: 16 (one of 131072 to 30000, 8 heads: 39.9 -> 29.6 us)
   if (cs == 8 && segs * 16 <= p->num_sms && n_most > 16 * kRecords) cs = 16;
   const bool turn = w.win && p->cfg.recent > 0;
-  const long long n_rec = segs * cs, units = turn ? (segs * 2 * kSlices + cs - 1) / cs * cs : 0;
+  const int slices = p->cfg.recent <= 256 ? 1 : p->cfg.recent <= 512 ? 2 : 4;  // 8 pieces a thread
+  const long long n_rec = segs * cs, units = turn ? (segs * 2 * slices + cs - 1) / cs * cs : 0;
   const CompactArgs A{kept, n_kept, lens, block_table, n_most, max_pages, num_pages, p->cfg.h_kv, B,
-                      pool, score, n_score, w, p->cfg.sink, p->cfg.recent, cs, (int)n_rec, p->err};
+                      pool, score, n_score, w, p->cfg.sink, p->cfg.recent, cs, (int)n_rec, slices, p->err};
   auto fn = p->cfg.group == 4 * kG ? compact_kernel<true> : compact_kernel<false>;
   if (cs > 8 && ensure_wide_clusters(reinterpret_cast<const void*>(fn)) != cudaSuccess) return OPTR_ERR_CUDA;
   return cuda_status(launch_pdl_cluster(fn, dim3((unsigned)(n_rec + units)), dim3(kThreads), cs, 0, stream, A));
