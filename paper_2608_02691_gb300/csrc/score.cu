@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
       const int cbase = !kSum && pair ? kKeys * g : 0;  // first column of the group's
       const float factor = S.block.x;
       float acc[kSum ? 1 : kKeys];
-      // what they may pass it by unseen: a piece's sum over its keys is below 2^128
+      // what they may pass it by unseen: a group's sum over the piece stays below 2^126
       const float most = 119.f - (32 - __clz(tiles));
       uint32_t known = 0;     // bit c: column 16 c + lane / 2 has keys in its sum, or is none
       float least = 0.f;      // no reference has been lower
@@ -703,6 +703,11 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         for (int i = 0; i < 4; ++i) {
           const float y = S.meet[4 * g + i][key];
           if (y > 0.f) l += y * ex2(-S.ref[4 * g + i][key] - m);
+        }
+        if (l > 0x1p64f) {  // the CTAs' parts are summed over references like this one
+          const int e = (int)(__float_as_uint(l) >> 23) - 127;
+          m += (float)e;
+          l *= __uint_as_float((uint32_t)(127 - e) << 23);
         }
         score_part(A, w, p.seg)[kKeys * g + key] = make_float2(m, l);
         arrive(&S.meet_empty[g]);

@@ -97,3 +97,35 @@ def test_the_workspace_holds_every_form():
             optr.optr_kv_score_win(*args, c.win, c.slots, out, ws[:n])
         c.check(out)
         assert (ws[n:] == 0x5A).all()
+
+
+@pytest.mark.parametrize("new", [[4], [6], [40]])
+@pytest.mark.parametrize("size", [-6.4, 6.4, -40.0, 40.0])
+@pytest.mark.parametrize("opts", [dict(), dict(group=128), dict(sink=16, recent=100)])
+def test_all_logits_alike_and_far_from_zero(new, size, opts):
+    """Every key the same row of +-1 in the rotated basis, every query `size` times it: log2 logits of 16.3
+    size, 105 at 6.4 and 653 at 40, above and below zero, as large as sums of magnitudes allow.  All weights
+    are 1 / n: keys of equal bits have equal logits, so only the normaliser's sum counts; window keys are
+    bf16 of the same row, whose logit differs by 2^-8 of the rest, so only their sums are compared there.
+    A logit and a normaliser of 653 are rounded to 2^-15 each, a weight by ln 2 of their sum: 4.3e-5; its
+    sums and exponentials add less than 1e-5 to that, and 1e-4 is allowed."""
+    c = Score(new, [3000], h_kv=1, seed=58, **opts)
+    g = torch.Generator(device="cuda").manual_seed(59)
+    row = torch.randn(128, device="cuda", generator=g).sign().double()
+    n = c.n[0]
+    k = (c.R_k[0] @ row + c.mu[0]).bfloat16().view(1, 1, 128).expand(n, 1, 128).contiguous()
+    args = (c.p, k, k, i32([0, n]), i32([0]), c.bt, c.pool)
+    if c.win is None:
+        optr.optr_kv_append(*args)
+    else:
+        optr.optr_kv_append_win(*args, c.win, c.slots)
+    c.q.copy_((size * (c.R_k[0] @ row)).bfloat16().expand_as(c.q))
+    c.score.zero_()
+    got = c.run().double()[0, 0, :n]
+    if c.win is None:
+        want = torch.zeros(n, dtype=torch.float64, device="cuda")
+        for i in range(new[0]):
+            seen = c.past[0] + i + 1
+            want[:seen] += 4 / seen
+        assert ((got - want).abs() <= 1e-4 * want).all()
+    assert abs(float(got.sum()) - 4 * new[0]) <= 1e-4 * 4 * new[0] and torch.isfinite(got).all()
