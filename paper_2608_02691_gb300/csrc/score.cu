@@ -14,8 +14,8 @@
 // is a sum along its registers, and the sum over keys of the first pass is kept per
 // column in registers too and meets the other lanes' once a piece.
 //
-// Bound.  A tile's products: 1.3 us at 256 columns (two products); with 32 columns the keys'
-// way into tensor memory.
+// Bound.  A tile's products: 1.3 us at 256 columns (two products); with 32 columns the
+// records' and the keys' way, 0.7 us.
 // 2 x 64 tokens over some 32000 positions take 140 us: 70 and 66 for the two passes (26
 // tiles an SM each, the tensor pipe 50% busy; without exponentials 66 and 61, without half
 // of the products 60 and 58), the rest the query kernel and the launches.  What is left
@@ -284,43 +284,58 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
 // -------------------------------------------------------------- logits
 
 // Warps: two epilogue groups of four, four that write keys, one each for the copies, the
-// products and the pieces.  Registers a thread after the split, of the launch's 512 x 128.
-constexpr int kKeyWarp = 8, kCopyWarp = 12, kMmaWarp = 13, kPlanWarp = 14;
-constexpr int kThreads = 512;
-constexpr int kRegLaunch = 128, kRegEpi = 208, kRegKey = 56, kRegIssue = 40;
-static_assert(2 * kRegEpi + kRegKey + kRegIssue <= 4 * kRegLaunch, "registers of the launch");
+// products and the pieces.  Registers a thread after the split, of the launch's.
+// kNarrow: blocks of 16 tokens at most.  A tile of theirs is bound by its keys' way into tensor
+// memory, so two groups write keys, in tiles of their parity, and four tiles of keys
+// stand there (16 x 8 over 8192: 123 -> 119 us).  A group skips the phases of a record buffer
+// that the other takes, so that a phase may not be taken for the next but one: by when a
+// group waits for the tile eight behind, the products of the sixth before it are done, so
+// that tile's records have been there.
+template <bool kNarrow>
+struct Roles {
+  static constexpr int kThreads = kNarrow ? 640 : 512;
+  static constexpr int kKeyWarp = 8, kKeyGroups = kNarrow ? 2 : 1, kCopyWarp = kKeyWarp + 4 * kKeyGroups;
+  static constexpr int kMmaWarp = kCopyWarp + 1, kPlanWarp = kCopyWarp + 2;
+  static constexpr int kConsumers = kCopyWarp + 2;  // warps that take the pieces
+  static constexpr int kLaunch = kNarrow ? 96 : 128, kEpi = kNarrow ? 136 : 208;
+  static constexpr int kKey = kNarrow ? 72 : 56, kIssue = kNarrow ? 64 : 40;
+  static_assert(2 * kEpi + kKeyGroups * kKey + kIssue <= kThreads / 128 * kLaunch, "registers of the launch");
+  static constexpr int kCols = kNarrow ? 64 : 128;  // columns of a D
+};
 constexpr uint32_t kTmemCols = 512, kColD = 0;
-// D[d] at 128 d, then two tiles of keys: 64 columns, and 8 for the minima of four pairs a slot;
-// without those there is room for a D more
-template <bool kCompact>
+// D[d] at kCols d, then the tiles of keys: 64 columns, and 8 for the minima of four pairs a
+// slot (with two such tiles and D of 128 columns there is no room for a third D).
+template <bool kCompact, bool kNarrow>
 struct Tmem {
-  static constexpr int kDs = kCompact ? 3 : 2;
-  static constexpr uint32_t kColK = 128u * kDs, kKeyCols = kCompact ? 64u : 80u;
+  static constexpr int kDs = kCompact || kNarrow ? 3 : 2, kKs = kNarrow ? 4 : 2;
+  static constexpr uint32_t kDCols = Roles<kNarrow>::kCols, kColK = kDCols * kDs, kKeyCols = kCompact ? 64u : 80u;
+  static_assert(kColK + kKs * kKeyCols <= kTmemCols, "tensor memory");
 };
 constexpr int kPieces = 3;     // pieces found ahead
-constexpr int kConsumers = 14; // warps that take the pieces
 constexpr float kSlack = 60.f; // a column's logits may pass its reference by 2^60
 
-template <bool kCompact>
+template <bool kCompact, bool kNarrow>
 struct Smem {
-  static constexpr int kRaw = kCompact ? 3 : 2;  // tiles of records on the way
-  uint8_t q[3][kBlockCols * 256];    // hi, lo, as given
+  static constexpr int kCols = kNarrow ? kBlockCols / 4 : kBlockCols;
+    static constexpr int kRaw = kNarrow ? 8 : kCompact ? 3 : 2;  // tiles of records on the way
+  static_assert(!kNarrow || kRaw >= 8, "see Roles");
+  uint8_t q[3][kCols * 256];    // hi, lo, as given
   uint8_t raw[kRaw][kKeys / kPage][512 + 16 * meta_stride(kCompact)];  // a page's key codes and pairs
-  alignas(16) float off[kBlockCols], sum[kCompact ? kBlockCols : 4];
-  alignas(16) uint8_t ext[kCompact ? 16 : kBlockCols * 32];  // the groups' sums
+  alignas(16) float off[kCols], sum[kCompact ? kCols : 4];
+  alignas(16) uint8_t ext[kCompact ? 16 : kCols * 32];  // the groups' sums
   float4 block;  // the block's factor, and its largest sums of magnitudes
   // minus the columns' references: pass 0 by warp, pass 1 the normalisers
   alignas(16) float ref[8][kKeys];
   float meet[8][kKeys];              // pass 0: the warps' sums of a piece (and, on the way, factors)
   // A key's largest value, or its pair, and whether it counts.  Read between a tile's
   // logits and its last D being free; written for tile t + kRing once the products of
-  // t + kRing - 2 are done, which waited for the Ds before their own.
-  static constexpr int kRing = kCompact ? 8 : 4;
+  // t + kRing less the tiles of keys are done, which waited for the Ds before their own.
+  static constexpr int kRing = kCompact || kNarrow ? 8 : 4;
   uint32_t scale[kRing][kKeys];
   uint32_t counts[kRing][4];
   uint32_t pages[kRaw];              // a raw tile's pages that are in range
   ScorePiece piece[kPieces];
-  uint64_t raw_full[kRaw], raw_empty[kRaw], k_full[2], k_empty[2];
+  uint64_t raw_full[kRaw], raw_empty[kRaw], k_full[4], k_empty[4];
   uint64_t d_full[3][2], d_empty[3];  // by D and the epilogue group that takes it
   uint64_t piece_full[kPieces], piece_empty[kPieces], q_full, q_empty, drained;
   // a piece's meeting of a group's warps (pass 0), and normalisers (pass 1, of all)
@@ -329,7 +344,8 @@ struct Smem {
   int abort;
 };
 
-static_assert(sizeof(Smem<false>) <= 232448 && sizeof(Smem<true>) <= 232448, "shared memory of a CTA");
+static_assert(sizeof(Smem<false, false>) <= 232448 && sizeof(Smem<true, false>) <= 232448 &&
+                  sizeof(Smem<false, true>) <= 232448, "shared memory of a CTA");
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -363,22 +379,27 @@ __device__ __forceinline__ float warp_largest(float x) {
   return __int_as_float(y ^ ((y >> 31) & 0x7fffffff));
 }
 
-template <bool kSum, bool kCompact>
-__global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constant__ ScoreArgs A) {
+template <bool kSum, bool kCompact, bool kNarrow>
+__global__ void __launch_bounds__(Roles<kNarrow>::kThreads, 1) logit_kernel(const __grid_constant__ ScoreArgs A) {
   extern __shared__ __align__(1024) unsigned char dsm_[];
-  using Tmem = Tmem<kCompact>;
+  using Tmem = Tmem<kCompact, kNarrow>;
+  using Roles = Roles<kNarrow>;
   constexpr int kDs = Tmem::kDs;
-  Smem<kCompact>& S = *reinterpret_cast<Smem<kCompact>*>(dsm_);
-  constexpr uint32_t kRing = Smem<kCompact>::kRing;
-  constexpr int kRaw = Smem<kCompact>::kRaw;
+  constexpr uint32_t kKs = Tmem::kKs;
+  constexpr int kKeyWarp = Roles::kKeyWarp, kCopyWarp = Roles::kCopyWarp, kMmaWarp = Roles::kMmaWarp;
+  constexpr int kPlanWarp = Roles::kPlanWarp, kCols = Roles::kCols;
+  using Smem = Smem<kCompact, kNarrow>;
+  Smem& S = *reinterpret_cast<Smem*>(dsm_);
+  constexpr uint32_t kRing = Smem::kRing;
+  constexpr int kRaw = Smem::kRaw;
   const int tid = threadIdx.x, lane = tid & 31;
   const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   if (tid == 0) {
     for (int i = 0; i < kRaw; ++i) {
-      tc05::bar_init(&S.raw_full[i], 1);
+      tc05::bar_init(&S.raw_full[i], kNarrow ? 33 : 1);  // (the lanes' copies, and the tile's pages)
       tc05::bar_init(&S.raw_empty[i], 4);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       tc05::bar_init(&S.k_full[i], 4);
       tc05::bar_init(&S.k_empty[i], 1);
     }
@@ -388,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
     }
     for (int i = 0; i < kPieces; ++i) {
       tc05::bar_init(&S.piece_full[i], 1);
-      tc05::bar_init(&S.piece_empty[i], kConsumers);
+      tc05::bar_init(&S.piece_empty[i], Roles::kConsumers);
     }
     tc05::bar_init(&S.q_full, 1);
     tc05::bar_init(&S.q_empty, 9);  // the products, and the epilogue's warps
@@ -431,14 +452,14 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
     // ------------------------------------------------------------ epilogue
     // Columns beyond 128 have a D of their own.  Maxima and sums: group g takes its D
     // (pair), or the tiles of its parity; weights: the tiles of its parity, both D.
-    tc05::reg_inc<kRegEpi>();
+    tc05::reg_inc<Roles::kEpi>();
     const int g = warp >> 2, key = 32 * (warp & 3) + lane;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     uint32_t phases = 0, nk = 0, nu = 0;  // of d_full[.][g], by bit; key tiles and Ds of the CTA
     ScorePiece p;
     for (uint32_t n = 0; next_piece(n, p); ++n) {
       const int tiles = p.t1 - p.t0, cols = p.cols();
-      const bool pair = cols > kKeys;
+      const bool pair = !kNarrow && cols > kKeys;
       if constexpr (kSum) {
         // minus the columns' normalisers, from the parts of the CTAs that had keys of the segment
         arrive(&S.meet_empty[0]);  // (the piece before has been read)
@@ -472,16 +493,16 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
       float* ref = kSum ? S.ref[0] : S.ref[warp];
       const int cbase = !kSum && pair ? kKeys * g : 0;  // first column of the group's
       const float factor = S.block.x;
-      float acc[kSum ? 1 : kKeys];
+      float acc[kSum ? 1 : kCols];
       // what they may pass it by unseen: a group's sum over the piece stays below 2^126
       const float most = 119.f - (32 - __clz(tiles));
       uint32_t known = 0;     // bit c: column 16 c + lane / 2 has keys in its sum, or is none
       float least = 0.f;      // no reference has been lower
       if constexpr (!kSum) {
 #pragma unroll
-        for (int c = 0; c < kKeys; ++c) acc[c] = 0.f;
+        for (int c = 0; c < kCols; ++c) acc[c] = 0.f;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) ref[32 * c + lane] = 0.f;
+        for (int c = 0; c < kCols / 32; ++c) ref[32 * c + lane] = 0.f;
 #pragma unroll
         for (int c = 0; c < 8; ++c) known |= (cbase + 16 * c + (lane >> 1) >= cols ? 1u : 0u) << c;
         __syncwarp();
@@ -525,7 +546,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
               first = 1 << 20;
             }
           }
-          const uint32_t tD = tmem + lanes + kColD + 128u * D;
+          const uint32_t tD = tmem + lanes + kColD + Tmem::kDCols * D;
           const int c_lo = kSum ? kKeys * d : cbase;    // the columns' place in the block
           const int n_cols = min(kKeys, cols - c_lo);
           const bool masked = __any_sync(0xffffffffu, first > c_lo);
@@ -577,17 +598,17 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           };
           if constexpr (kSum) {
             // all of D first: the next products may start
-            uint32_t x[4][32];
+            uint32_t x[kCols / 32][32];
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < kCols / 32; ++c)
               if (32 * c < n_cols) tc05::tmem_ld32(tD + 32 * c, x[c]);
             tc05::tmem_wait_ld();
 #pragma unroll
-            for (int c = 0; c < 4; ++c) loaded(x[c]);
+            for (int c = 0; c < kCols / 32; ++c) loaded(x[c]);
             free_d();
             by_tile([&](auto exact_tile, auto masked_tile) {
 #pragma unroll
-              for (int c = 0; c < kKeys / 16; ++c) {
+              for (int c = 0; c < kCols / 16; ++c) {
                 if (16 * c >= n_cols) break;
                 float y[16];
                 logits(c, x[c / 2] + 16 * (c & 1), y, exact_tile, masked_tile);
@@ -613,7 +634,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
               float* by = S.meet[warp];  // by what a column's sum shrinks
               bool shrink = false;
 #pragma unroll 1
-              for (int c = 0; c < kKeys / 16; ++c) {
+              for (int c = 0; c < kCols / 16; ++c) {
                 if (16 * c >= n_cols) break;
                 uint32_t x[16];
                 tc05::tmem_ld16(tD + 16 * c, x);
@@ -643,7 +664,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
               __syncwarp();
               if (__any_sync(0xffffffffu, shrink)) {
 #pragma unroll
-                for (int c = 0; c < kKeys; c += 4) {
+                for (int c = 0; c < kCols; c += 4) {
                   if (c >= n_cols) break;
                   const float4 f = *reinterpret_cast<const float4*>(by + c);
                   acc[c] *= f.x, acc[c + 1] *= f.y, acc[c + 2] *= f.z, acc[c + 3] *= f.w;
@@ -653,7 +674,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
             }
             by_tile([&](auto exact_tile, auto masked_tile) {
 #pragma unroll
-              for (int c = 0; c < kKeys / 16; ++c) {
+              for (int c = 0; c < kCols / 16; ++c) {
                 if (16 * c >= n_cols) break;
                 uint32_t x[16];
                 tc05::tmem_ld16(tD + 16 * c, x);
@@ -677,7 +698,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
       if constexpr (!kSum) {
         // over the warp's keys: 32 columns a time, each lane ends with one's sum
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < kCols / 32; ++c) {
           float* a = acc + 32 * c;
 #pragma unroll
           for (int o = 16; o > 0; o >>= 1) {
@@ -695,21 +716,22 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
         arrive(&S.meet_full[g]);
         if (!wait(&S.meet_full[g], n)) break;
         float m = -INFINITY, l = 0.f;
+        if (key < kCols) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (S.meet[4 * g + i][key] > 0.f) m = fmaxf(m, -S.ref[4 * g + i][key]);
-        }
+          for (int i = 0; i < 4; ++i)
+            if (S.meet[4 * g + i][key] > 0.f) m = fmaxf(m, -S.ref[4 * g + i][key]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float y = S.meet[4 * g + i][key];
-          if (y > 0.f) l += y * ex2(-S.ref[4 * g + i][key] - m);
+          for (int i = 0; i < 4; ++i) {
+            const float y = S.meet[4 * g + i][key];
+            if (y > 0.f) l += y * ex2(-S.ref[4 * g + i][key] - m);
+          }
+          if (l > 0x1p64f) {  // the CTAs' parts are summed over references like this one
+            const int e = (int)(__float_as_uint(l) >> 23) - 127;
+            m += (float)e;
+            l *= __uint_as_float((uint32_t)(127 - e) << 23);
+          }
+          score_part(A, w, p.seg)[kKeys * g + key] = make_float2(m, l);
         }
-        if (l > 0x1p64f) {  // the CTAs' parts are summed over references like this one
-          const int e = (int)(__float_as_uint(l) >> 23) - 127;
-          m += (float)e;
-          l *= __uint_as_float((uint32_t)(127 - e) << 23);
-        }
-        score_part(A, w, p.seg)[kKeys * g + key] = make_float2(m, l);
         arrive(&S.meet_empty[g]);
         if (!wait(&S.meet_empty[g], n)) break;
       }
@@ -718,7 +740,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
   } else if (warp < kCopyWarp) {
     // --------------------------------------------------------------- keys
     // Thread = key.  A's row in tensor memory: 64 columns of hi parts, 64 of lo.
-    tc05::reg_dec<kRegKey>();
+    tc05::reg_dec<Roles::kKey>();
     constexpr int ms = meta_stride(kCompact);
     const int quarter = warp & 3, key = tid & 127;
     const uint32_t lanes = (uint32_t)(32 * quarter) << 16;
@@ -726,7 +748,11 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
     ScorePiece p;
     for (uint32_t n = 0; next_piece(n, p); ++n) {
       for (int tile = p.t0; tile < p.t1; ++tile, ++nk) {
-        const uint32_t s = nk & 1, tK = tmem + lanes + Tmem::kColK + Tmem::kKeyCols * s;
+        if (Roles::kKeyGroups > 1 && (nk & 1) != (uint32_t)((warp - kKeyWarp) >> 2)) {  // the other group's
+          raws += tile < p.I();
+          continue;
+        }
+        const uint32_t s = nk % kKs, tK = tmem + lanes + Tmem::kColK + Tmem::kKeyCols * s;
         bool ok;
         uint32_t scale = 0u;
         if (tile < p.I()) {
@@ -769,7 +795,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
               least[1][2 + i] = 0u;
             }
           }
-          if (nk >= 2 && !wait(&S.k_empty[s], nk / 2 - 1)) break;
+          if (nk >= kKs && !wait(&S.k_empty[s], nk / kKs - 1)) break;
 #pragma unroll
           for (int part = 0; part < 4; ++part) {
             const uint2 word = *reinterpret_cast<const uint2*>(raw + 32 * slot + 8 * part);
@@ -807,7 +833,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           arrive(&S.raw_empty[r]);
         } else {
           const int i = kKeys * (tile - p.I()) + key;
-          if (nk >= 2 && !wait(&S.k_empty[s], nk / 2 - 1)) break;
+          if (nk >= kKs && !wait(&S.k_empty[s], nk / kKs - 1)) break;
           const uint4* src = nullptr;
           ok = i < p.n_win;
           if (ok) {
@@ -848,7 +874,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
       if (dead) break;
     }
   } else {
-    tc05::reg_dec<kRegIssue>();
+    tc05::reg_dec<Roles::kIssue>();
     if (warp == kCopyWarp) {
       // ------------------------------------------------------------- copies
       uint32_t raws = 0, nq = 0;
@@ -882,19 +908,39 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
           const int ahead = request(tile + 1);
           if (raws >= kRaw && !wait(&S.raw_empty[r], raws / kRaw - 1)) break;
           const bool in = page >= 0 && page < A.num_pages;
-          constexpr uint32_t pairs = 16u * meta_stride(kCompact);
           const uint32_t pages = __ballot_sync(0xffffffffu, in) & 0xffu;
+          constexpr int kLanes = meta_stride(kCompact);  // 16-byte pieces of a page's pairs
           if (lane == 0) {
             S.pages[r] = pages;
-            tc05::bar_arrive_expect_tx(&S.raw_full[r], __popc(pages) * (512u + pairs));
+            if (kNarrow)
+              tc05::bar_arrive(&S.raw_full[r]);
+            else
+              tc05::bar_arrive_expect_tx(&S.raw_full[r], __popc(pages) * (512u + 16u * kLanes));
           }
           if (!in && lane < 8 && kKeys * tile + kPage * lane < p.n_int) atomicOr(A.err, OPTR_DEVERR_PAGE_ID);
           __syncwarp();
-          if (in) {
+          if constexpr (kNarrow) {
+            // Plain asynchronous copies.  As bulk copies, 16 small ones a tile, they take 0.8 us: more
+            // than all else of a narrow tile (16 x 8 over 8192: 119 us, so 100), less than a wide one
+            // (16 x 32: 164 us, so 172).
+            auto copy = [&](int x, uint32_t to, uint32_t from) {
+              const int phys = __shfl_sync(0xffffffffu, page, x);
+              const bool ok = pages >> x & 1;
+              cp_async16_zfill(S.raw[r][x] + to,
+                               A.pool + ((size_t)(ok ? phys : 0) * A.h_kv + p.h) * chunk_bytes(kCompact) + from, ok);
+            };
+#pragma unroll
+            for (int x = 0; x < 8; ++x) copy(x, 16 * lane, OPTR_K_CODES_OFFSET + 16 * lane);
+#pragma unroll
+            for (int x = 0; x < 8 * kLanes / 32; ++x)
+              copy(x * (32 / kLanes) + lane / kLanes, 512 + 16 * (lane % kLanes),
+                   OPTR_K_META_OFFSET + 16 * (lane % kLanes));
+            tc05::bar_arrive_copies(&S.raw_full[r]);
+          } else if (in) {
             const uint8_t* src = A.pool + ((size_t)page * A.h_kv + p.h) * chunk_bytes(kCompact);
             const bool codes = lane < 8;
             tc05::bulk_g2s(S.raw[r][lane & 7] + (codes ? 0 : 512),
-                           src + (codes ? OPTR_K_CODES_OFFSET : OPTR_K_META_OFFSET), codes ? 512u : pairs,
+                           src + (codes ? OPTR_K_CODES_OFFSET : OPTR_K_META_OFFSET), codes ? 512u : 16u * kLanes,
                            &S.raw_full[r]);
           }
           __syncwarp();
@@ -904,6 +950,7 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
       }
       // copies in flight land before the CTA exits
       if (nq) tc05::bar_wait_drain(&S.q_full, (nq - 1) & 1);
+      if (kNarrow) cp_async_commit(), cp_async_wait<0>();
       for (uint32_t x = raws > kRaw ? raws - kRaw : 0; x < raws; ++x)
         tc05::bar_wait_drain(&S.raw_full[x % kRaw], x / kRaw & 1);
       __syncwarp();
@@ -915,20 +962,20 @@ __global__ void __launch_bounds__(kThreads, 1) logit_kernel(const __grid_constan
       ScorePiece p;
       for (uint32_t n = 0; next_piece(n, p); ++n) {
         const int N = p.N();
-        const bool pair = p.cols() > kKeys;
+        const bool pair = !kNarrow && p.cols() > kKeys;
         if (!wait(&S.q_full, n)) break;
         used = true;
         for (int t = 0; t < p.t1 - p.t0; ++t, ++nk) {
-          const uint32_t s = nk & 1, a = tmem + Tmem::kColK + Tmem::kKeyCols * s;
+          const uint32_t s = nk % kKs, a = tmem + Tmem::kColK + Tmem::kKeyCols * s;
           const bool exact = p.t0 + t >= p.I();
-          if (!wait(&S.k_full[s], nk / 2)) break;
+          if (!wait(&S.k_full[s], nk / kKs)) break;
           for (int d = 0; d < (pair ? 2 : 1); ++d) {
             const uint32_t D = nu % kDs;
             const uint32_t id = tc05::idesc_f16(128, pair && d ? N - kKeys : min(N, kKeys));
             if (nu >= kDs && !wait(&S.d_empty[D], nu / kDs - 1)) break;
             ++nu;
-            const uint32_t out = tmem + kColD + 128u * D, b = sq + (uint32_t)d * (kKeys * 256);
-            constexpr uint32_t kPart = kBlockCols * 256;
+            const uint32_t out = tmem + kColD + Tmem::kDCols * D, b = sq + (uint32_t)d * (kKeys * 256);
+            constexpr uint32_t kPart = Smem::kCols * 256;
             if (exact) {
               tc05::mma128_ts<16>(out, a, tc05::smem_desc(b + 2 * kPart, 128, 2048), id | tc05::kIdescBf16, 0);
             } else if (kCompact) {
@@ -1041,9 +1088,16 @@ extern "C" optr_status optr_kv_score_win(const optr_params* p, const void* q, in
               pool, num_pages, w, p->cfg.sink, p->cfg.recent, p->cfg.h_kv, p->cfg.group == 4 * kG, p->R_k, p->mu,
               score, n_score, p->err, l.cols, ws, (float2*)(ws + l.part), l.W};
   if (few_tokens(p, B, max_new, max_pages)) return cuda_status(launch_score_few(p, A, ws, stream));
-  auto first = A.compact ? logit_kernel<false, true> : logit_kernel<false, false>;
-  auto second = A.compact ? logit_kernel<true, true> : logit_kernel<true, false>;
-  const size_t smem = A.compact ? sizeof(Smem<true>) : sizeof(Smem<false>);
+  const bool narrow = 4 * max_new <= Smem<false, true>::kCols;
+  auto first = A.compact ? logit_kernel<false, true, false> : logit_kernel<false, false, false>;
+  auto second = A.compact ? logit_kernel<true, true, false> : logit_kernel<true, false, false>;
+  const int threads = narrow ? Roles<true>::kThreads : Roles<false>::kThreads;
+  size_t smem = A.compact ? sizeof(Smem<true, false>) : sizeof(Smem<false, false>);
+  if (narrow) {
+    first = A.compact ? logit_kernel<false, true, true> : logit_kernel<false, false, true>;
+    second = A.compact ? logit_kernel<true, true, true> : logit_kernel<true, false, true>;
+    smem = A.compact ? sizeof(Smem<true, true>) : sizeof(Smem<false, true>);
+  }
   if (ensure_dynamic_smem(reinterpret_cast<const void*>(query_kernel), sizeof(QuerySmem)) != cudaSuccess ||
       ensure_dynamic_smem(reinterpret_cast<const void*>(first), smem) != cudaSuccess ||
       ensure_dynamic_smem(reinterpret_cast<const void*>(second), smem) != cudaSuccess)
@@ -1054,8 +1108,8 @@ extern "C" optr_status optr_kv_score_win(const optr_params* p, const void* q, in
   for (A.t0 = 0; A.t0 < max_new && e == cudaSuccess; A.t0 += kTok) {
     const int parts = (l.cols + kRotCols - 1) / kRotCols;
     e = launch_pdl_cluster(query_kernel, dim3(parts, segs), dim3(kRotThreads), parts, sizeof(QuerySmem), stream, A);
-    if (e == cudaSuccess) e = launch_pdl(first, dim3(l.W), dim3(kThreads), smem, stream, A);
-    if (e == cudaSuccess) e = launch_pdl(second, dim3(l.W), dim3(kThreads), smem, stream, A);
+    if (e == cudaSuccess) e = launch_pdl(first, dim3(l.W), dim3(threads), smem, stream, A);
+    if (e == cudaSuccess) e = launch_pdl(second, dim3(l.W), dim3(threads), smem, stream, A);
   }
   return cuda_status(e);
 }
