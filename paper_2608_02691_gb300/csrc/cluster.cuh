@@ -31,15 +31,6 @@ __device__ __forceinline__ uint32_t cluster_ld32(const void* x, int rank) {
                : "=r"(v) : "r"((uint32_t)__cvta_generic_to_shared(x)), "r"(rank) : "memory");
   return v;
 }
-// 16 bytes of it.
-__device__ __forceinline__ uint4 cluster_ld128(const void* x, int rank) {
-  uint4 v;
-  asm volatile("{\n .reg .u32 r;\n mapa.shared::cluster.u32 r, %4, %5;\n"
-               " ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [r];\n}\n"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "r"((uint32_t)__cvta_generic_to_shared(x)), "r"(rank) : "memory");
-  return v;
-}
 __device__ __forceinline__ unsigned long long cluster_ld64(const void* x, int rank) {
   unsigned long long v;
   asm volatile("{\n .reg .u32 r;\n mapa.shared::cluster.u32 r, %1, %2;\n"
