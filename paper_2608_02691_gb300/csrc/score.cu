@@ -190,10 +190,20 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
       }
     // <q, mu>: eight lanes a column
     float d = 0.f, l = 0.f;
-    for (int x = lane & 7; x < kD; x += 8) {
-      const float y = __bfloat162float(S.q[tid >> 3][x]);
-      d = fmaf(y, __ldg(A.mu + (size_t)h * kD + x), d);
-      l += fabsf(y);
+#pragma unroll
+    for (int x = 8 * (lane & 7); x < kD; x += 64) {
+      const uint4 y = *reinterpret_cast<const uint4*>(&S.q[tid >> 3][x]);
+      const float4* mu = reinterpret_cast<const float4*>(A.mu + (size_t)h * kD + x);
+      const float4 m0 = __ldg(mu), m1 = __ldg(mu + 1);
+      const uint32_t word[4] = {y.x, y.y, y.z, y.w};
+      const float m[8] = {m0.x, m0.y, m0.z, m0.w, m1.x, m1.y, m1.z, m1.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float a = __uint_as_float(word[e] << 16), b = __uint_as_float(word[e] & 0xffff0000u);
+        d = fmaf(a, m[2 * e], d);
+        d = fmaf(b, m[2 * e + 1], d);
+        l += fabsf(a) + fabsf(b);
+      }
     }
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) {
@@ -225,10 +235,15 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
   if (cs > 1) cluster_barrier(); else __syncthreads();
   float m = S.most[0], l = S.most[1], given = S.most[2];
   if (cs > 1) {
-    for (int r = 0; r < cs; ++r) {
-      m = fmaxf(m, __uint_as_float(cluster_ld32(&S.most[0], r)));
-      l = fmaxf(l, __uint_as_float(cluster_ld32(&S.most[1], r)));
-      given = fmaxf(given, __uint_as_float(cluster_ld32(&S.most[2], r)));
+    const int r = lane % cs;  // a CTA a lane
+    m = __uint_as_float(cluster_ld32(&S.most[0], r));
+    l = __uint_as_float(cluster_ld32(&S.most[1], r));
+    given = __uint_as_float(cluster_ld32(&S.most[2], r));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      l = fmaxf(l, __shfl_xor_sync(0xffffffffu, l, o));
+      given = fmaxf(given, __shfl_xor_sync(0xffffffffu, given, o));
     }
     cluster_arrive();  // no CTA leaves while its shared memory may be read
   }
@@ -238,29 +253,36 @@ __global__ void __launch_bounds__(kRotThreads) query_kernel(const __grid_constan
     const int E = m > 0.f ? max(-100, min(100, 13 - ((int)(__float_as_uint(m) >> 23) - 127))) : 0;
     float* line = reinterpret_cast<float*>(out + qop_lines(A.cols, win, A.compact));
     const float up = __uint_as_float((uint32_t)(127 + E) << 23);
+    __half* stage = reinterpret_cast<__half*>(S.R);  // the rotation has been used
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int n = c0 + 16 * i + 8 * e + g;
-          if (n >= N) continue;
+          const int n = 16 * i + 8 * e + g;
           const int ch = 16 * warp + 8 * j + 2 * c;
           const float x = acc[i][j][2 * e] * up, y = acc[i][j][2 * e + 1] * up;
           const __half2 hi = __floats2half2_rn(x, y);
           const float2 z = __half22float2(hi);
           const __half2 lo = __floats2half2_rn(x - z.x, y - z.y);
-          __half* at = reinterpret_cast<__half*>(out + operand_offset(n, key_place(ch, A.compact)));
+          __half* at = stage + operand_offset(n, key_place(ch, A.compact)) / 2;
           if (A.compact) {  // (the second channel's place is two on)
             at[0] = __low2half(hi), at[2] = __high2half(hi);
-            at += A.cols * 128;
+            at += kRotCols * kD;
             at[0] = __low2half(lo), at[2] = __high2half(lo);
           } else {
             *reinterpret_cast<__half2*>(at) = hi;
-            *reinterpret_cast<__half2*>(at + A.cols * 128) = lo;
+            *reinterpret_cast<__half2*>(at + kRotCols * kD) = lo;
           }
         }
+    __syncthreads();
+    // (as they lie in memory: eight columns are 2 KB)
+    for (int i = tid; i < min(kRotCols, N - c0) / 8 * 128; i += kRotThreads) {
+      uint4* to = reinterpret_cast<uint4*>(out + (size_t)c0 * 256) + i;
+      to[0] = reinterpret_cast<const uint4*>(stage)[i];
+      to[A.cols * 16] = reinterpret_cast<const uint4*>(stage + kRotCols * kD)[i];
+    }
     // Beside four pairs a slot: the groups' sums, over 2^5 (32 channels), as the parts that meet
     // a key's minima: hi, lo, hi
     if (!A.compact && tid < 128 && c0 + lane < N) {
