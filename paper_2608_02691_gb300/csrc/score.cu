@@ -16,7 +16,7 @@
 //
 // Bound.  A tile's products: 1.3 us at 256 columns (two products); with 32 columns the
 // records' and the keys' way, 0.7 us.
-// 2 x 64 tokens over some 32000 positions take 140 us: 70 and 66 for the two passes (26
+// 2 x 64 tokens over some 32000 positions take 137 us: 70 and 65 for the two passes (26
 // tiles an SM each, the tensor pipe 50% busy; without exponentials 66 and 61, without half
 // of the products 60 and 58), the rest the query kernel and the launches.  What is left
 // lies between the tiles: starts, the query operand's 128 KB, and the few SMs whose
