@@ -24,7 +24,10 @@
 //
 // References.  A sum over keys needs none as long as 2^l neither overflows nor vanishes, and
 // |l| <= max |k| * sum |q| holds for every tile of ordinary inputs: then the reference is 0
-// and no maximum is looked for (70 us; with one for each column 95).
+// and no maximum is looked for (70 us; with one for each column 95).  A sum over reference 0
+// may be as small as 2^-118, beside which a later tile's terms below 2^-126 are nothing to a
+// float and yet count: before the first tile that needs a look, such sums are brought near 1,
+// their references with them.  So are all before those of warps and CTAs are joined.
 //
 // Rounding.  The sums are float32, and a weight moves by what its logit does: rounding
 // queries or keys to 16 bits would move it by some 3e-4.  So queries go in as fp16 hi + lo
@@ -520,6 +523,7 @@ __global__ void __launch_bounds__(Roles<kNarrow>::kThreads, 1) logit_kernel(cons
       const float most = 119.f - (32 - __clz(tiles));
       uint32_t known = 0;     // bit c: column 16 c + lane / 2 has keys in its sum, or is none
       float least = 0.f;      // no reference has been lower
+      bool unseen = false, near = false;  // sums of unseen logits: there are, have been brought near 1
       if constexpr (!kSum) {
 #pragma unroll
         for (int c = 0; c < kCols; ++c) acc[c] = 0.f;
@@ -652,8 +656,29 @@ __global__ void __launch_bounds__(Roles<kNarrow>::kThreads, 1) logit_kernel(cons
             const float size = exact ? S.block.z : S.block.y;
             if (!__any_sync(0xffffffffu, (masked && known != 0xffu) || (first < cols && !(size * top <= least + most)))) {
               known = 0xffu;
+              unseen = true;
             } else {
-              float* by = S.meet[warp];  // by what a column's sum shrinks
+              if (unseen && !near) {
+                near = true;  // (all columns have keys: it is not needed again)
+#pragma unroll
+                for (int c = 0; c < kCols; c += 32) {
+                  if (c >= n_cols) break;
+                  uint32_t mine = 0u;
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) {
+                    const uint32_t e = __reduce_max_sync(0xffffffffu, __float_as_uint(acc[c + j])) & 0x7f800000u;
+                    acc[c + j] *= __uint_as_float((254u << 23) - e);
+                    mine = lane == j ? e : mine;
+                  }
+                  const float e = (float)(mine >> 23) - 127.f;
+                  if (c + lane < n_cols) {
+                    least = fminf(least, e);  // (the warp's, below)
+                    ref[c + lane] -= e;
+                  }
+                }
+                __syncwarp();
+              }
+              float* by = S.meet[warp];  // by what a column's sum shrinks, twice (2^-m may be 0)
               bool shrink = false;
 #pragma unroll 1
               for (int c = 0; c < kCols / 16; ++c) {
@@ -678,7 +703,7 @@ __global__ void __launch_bounds__(Roles<kNarrow>::kThreads, 1) logit_kernel(cons
                 __syncwarp();
                 if (lane & 1) {
                   if (moves) ref[16 * c + (lane >> 1)] -= m;
-                  by[16 * c + (lane >> 1)] = moves && !fresh ? ex2(-m) : 1.f;
+                  by[16 * c + (lane >> 1)] = moves && !fresh ? ex2(-0.5f * m) : 1.f;
                 }
                 shrink |= moves && !fresh;
               }
@@ -689,6 +714,7 @@ __global__ void __launch_bounds__(Roles<kNarrow>::kThreads, 1) logit_kernel(cons
                 for (int c = 0; c < kCols; c += 4) {
                   if (c >= n_cols) break;
                   const float4 f = *reinterpret_cast<const float4*>(by + c);
+                  acc[c] *= f.x, acc[c + 1] *= f.y, acc[c + 2] *= f.z, acc[c + 3] *= f.w;
                   acc[c] *= f.x, acc[c + 1] *= f.y, acc[c + 2] *= f.z, acc[c + 3] *= f.w;
                 }
                 __syncwarp();
@@ -739,19 +765,19 @@ __global__ void __launch_bounds__(Roles<kNarrow>::kThreads, 1) logit_kernel(cons
         if (!wait(&S.meet_full[g], n)) break;
         float m = -INFINITY, l = 0.f;
         if (key < kCols) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (S.meet[4 * g + i][key] > 0.f) m = fmaxf(m, -S.ref[4 * g + i][key]);
+          // (a sum is y 2^e over its reference)
+          float y[4], e[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float y = S.meet[4 * g + i][key];
-            if (y > 0.f) l += y * ex2(-S.ref[4 * g + i][key] - m);
+            const uint32_t x = __float_as_uint(S.meet[4 * g + i][key]);
+            y[i] = __uint_as_float((x & 0x7fffffu) | 0x3f800000u);
+            e[i] = (float)((int)(x >> 23) - 127);
+            if (x < 1u << 23) y[i] = 0.f;  // none
+            if (y[i] > 0.f) m = fmaxf(m, e[i] - S.ref[4 * g + i][key]);
           }
-          if (l > 0x1p64f) {  // the CTAs' parts are summed over references like this one
-            const int e = (int)(__float_as_uint(l) >> 23) - 127;
-            m += (float)e;
-            l *= __uint_as_float((uint32_t)(127 - e) << 23);
-          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (y[i] > 0.f) l += y[i] * ex2((-S.ref[4 * g + i][key] - m) + e[i]);
           score_part(A, w, p.seg)[kKeys * g + key] = make_float2(m, l);
         }
         arrive(&S.meet_empty[g]);
