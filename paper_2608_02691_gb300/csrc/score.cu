@@ -1136,7 +1136,7 @@ extern "C" optr_status optr_kv_score_win(const optr_params* p, const void* q, in
               pool, num_pages, w, p->cfg.sink, p->cfg.recent, p->cfg.h_kv, p->cfg.group == 4 * kG, p->R_k, p->mu,
               score, n_score, p->err, l.cols, ws, (float2*)(ws + l.part), l.W};
   if (few_tokens(p, B, max_new, max_pages)) return cuda_status(launch_score_few(p, A, ws, stream));
-  const bool narrow = 4 * max_new <= Smem<false, true>::kCols;
+  const bool narrow = l.cols <= Smem<false, true>::kCols;
   auto first = A.compact ? logit_kernel<false, true, false> : logit_kernel<false, false, false>;
   auto second = A.compact ? logit_kernel<true, true, false> : logit_kernel<true, false, false>;
   const int threads = narrow ? Roles<true>::kThreads : Roles<false>::kThreads;
@@ -1153,7 +1153,8 @@ extern "C" optr_status optr_kv_score_win(const optr_params* p, const void* q, in
   const unsigned segs = (unsigned)B * p->cfg.h_kv;
   // a block of tokens a time, in stream order: the sums do not depend on chance
   cudaError_t e = cudaSuccess;
-  for (A.t0 = 0; A.t0 < max_new && e == cudaSuccess; A.t0 += kTok) {
+  const int most = std::min(max_new, n_tok);  // no sequence has more
+  for (A.t0 = 0; A.t0 < most && e == cudaSuccess; A.t0 += kTok) {
     const int parts = (l.cols + kRotCols - 1) / kRotCols;
     e = launch_pdl_cluster(query_kernel, dim3(parts, segs), dim3(kRotThreads), parts, sizeof(QuerySmem), stream, A);
     if (e == cudaSuccess) e = launch_pdl(first, dim3(l.W), dim3(threads), smem, stream, A);
