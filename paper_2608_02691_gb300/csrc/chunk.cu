@@ -1048,7 +1048,7 @@ optr_status attend(
   // rule says no: 80.0, 82.3 with it.
   const bool few = max_new <= 16 && (long long)B * h_kv * 8 <= l.W;
   const int per = few ? 2 : 8;  // rows of a joining CTA
-  const dim3 joins(l.W, (std::min(l.rows, 4 * max_new) + per - 1) / per);
+  const dim3 joins(l.W, (4 * std::min(l.rows / 4, max_new) + per - 1) / per);
   e = launch_pdl(fn, dim3(l.W), dim3(kThreads), smem, stream, mq, mk, mv, mw, A);
   if (e == cudaSuccess)
     e = launch_pdl(few ? chunk_combine_kernel<true> : chunk_combine_kernel<false>, joins, dim3(256), 0,
