@@ -604,8 +604,8 @@ optr_status optr_verify_drafts(const optr_params* p, const void* target_probs,
  * come twice), each token of the text has the target's distribution.  Without
  * draft probabilities q_r is 1 at each child's token: the product is u_c S, and
  * a rejected child takes w(x) off S and leaves w(x) = 0.  The arithmetic is float32,
- * one rounding an operation; S is summed in float32 over some hundred probabilities
- * at most, and those sums in float64.
+ * one rounding an operation; S is summed in float32 over 256 probabilities at most, and
+ * those sums in float64.
  *   target_probs device [n_tok][vocab], float32 or bf16 (probs_dtype).
  *   draft_probs  device [n_tok][vocab] of the same type (read where a row has
  *                children), or NULL: drafted without probabilities.

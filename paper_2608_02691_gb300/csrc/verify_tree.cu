@@ -29,6 +29,7 @@ namespace {
 
 constexpr int kTreeThreads = 512, kWarps = kTreeThreads / 32;
 constexpr int kRows = OPTR_TREE_MAX_ROWS;
+constexpr int kTerms = 256;  // probabilities of a float32 sum: 2^-16 of it at the very worst
 
 struct Node {
   int parent, token;  // parent -2: never reached
@@ -232,21 +233,25 @@ verify_tree_kernel(const T* __restrict__ tp, const T* __restrict__ dp,
     if (w.draw) break;
     const T* p = tp + ((size_t)c0 + w.row) * V;
     const T* q = dp + ((size_t)c0 + w.row) * V;
-    float sum = 0.f;
+    double total = 0.0;
+    for (int v = lo + tid; v < hi;) {
+      float sum = 0.f;
+      const int end = min(hi, v + kTerms / kVec * kTreeThreads);
 #pragma unroll 4
-    for (int v = lo + tid; v < hi; v += kTreeThreads) {
-      float x[kVec], y[kVec];
-      fetch(p + (size_t)v * kVec, x);
-      fetch(q + (size_t)v * kVec, y);
-      for (int j = 0; j < w.n_cut; ++j) {
-        const float m = __uint_as_float(S.cut[j]);
+      for (; v < end; v += kTreeThreads) {
+        float x[kVec], y[kVec];
+        fetch(p + (size_t)v * kVec, x);
+        fetch(q + (size_t)v * kVec, y);
+        for (int j = 0; j < w.n_cut; ++j) {
+          const float m = __uint_as_float(S.cut[j]);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) x[i] = left(x[i], m, y[i]);
+          for (int i = 0; i < kVec; ++i) x[i] = left(x[i], m, y[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) sum += x[i];
       }
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) sum += x[i];
+      total += sum;
     }
-    double total = sum;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
     if (lane == 0) S.sum[pass & 1][warp] = total;
