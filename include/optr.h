@@ -649,7 +649,9 @@ optr_status optr_verify_tree(const optr_params* p, const void* target_probs,
  *   score       device float32 [B][h_kv][n_score], added to at positions below n; it
  *               starts as the caller's (zeros, or what is left of earlier sums).
  *   workspace   device, optr_kv_score_workspace_size bytes, 256-byte aligned, scratch as
- *               in optr_decode_attention.
+ *               in optr_decode_attention.  The size grows with each argument: one of a
+ *               server's largest step serves its smaller ones (it holds the logits of the
+ *               largest of those that has up to four tokens a sequence and 256 MB of them).
  * Logits are good to some 2^-20 of |q||k| / sqrt(128) (queries and keys of 22 bits,
  * float32 sums; of more than four tokens a query element is known to 2^-38 of the
  * largest among 64 tokens besides); sums of a position are added in a fixed order.  Queries must be finite.  A

@@ -1106,8 +1106,9 @@ using namespace optr;
 extern "C" size_t optr_kv_score_workspace_size(const optr_params* p, int n_tok, int B, int max_new,
                                                int max_pages) {
   if (!p || n_tok < 0 || B <= 0 || max_new <= 0 || max_pages <= 0) return 0;
-  const size_t n = score_layout(p, B, max_new).total;
-  return few_tokens(p, B, max_new, max_pages) ? std::max(n, few_layout(p, B, max_new, max_pages).total) : n;
+  // (it holds every smaller call's work, whichever form that takes)
+  return std::max(score_layout(p, B, max_new).total,
+                  few_layout(p, B, std::min(max_new, kFewTok), max_pages).total);
 }
 
 extern "C" optr_status optr_kv_score_win(const optr_params* p, const void* q, int n_tok,

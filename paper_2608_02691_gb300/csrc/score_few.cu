@@ -814,21 +814,28 @@ cudaError_t launch_cluster(const ScoreArgs& A, const Clusters& c, float4* spill,
 
 }  // namespace
 
+// Few tokens' logits: of all positions at most, and of a page's.
+constexpr size_t kMostLogits = 256ull << 20;
+size_t page_logits(int max_new) { return (size_t)kPage * max_new * sizeof(float4); }
+
 FewLayout few_layout(const optr_params* p, int B, int max_new, int max_pages) {
   FewLayout l;
   const size_t segs = (size_t)B * p->cfg.h_kv;
   l.W = p->num_sms * kWarps;
   l.part = round_up(segs * max_new * kQueryWords * sizeof(uint32_t));
   l.logits = l.part + round_up((segs + l.W) * 4 * kFewTok * sizeof(float2));
-  // (a cluster's eight CTAs have some places more)
-  l.total = l.logits + round_up(segs * ((size_t)max_pages + 32) * kPage * max_new * sizeof(float4));
+  // A cluster has up to two pages and three for each of its CTAs beside (clusters()), and more
+  // than one CTA only while all fit the SMs.  Calls of more positions are not of few tokens: the size is
+  // that of the largest smaller call which is.
+  const size_t page = page_logits(max_new);
+  const size_t logits = (size_t)max_pages > kMostLogits / (segs * page) ? kMostLogits : segs * max_pages * page;
+  l.total = l.logits + round_up(logits + (5 * segs + 3 * (size_t)p->num_sms) * page);
   return l;
 }
 
-// Few tokens, and logits that a workspace of 256 MB holds.
+// Few tokens, and logits within kMostLogits.
 bool few_tokens(const optr_params* p, int B, int max_new, int max_pages) {
-  return max_new <= kFewTok &&
-         (long long)B * p->cfg.h_kv * max_pages * kPage * max_new * (long long)sizeof(float4) <= (256ll << 20);
+  return max_new <= kFewTok && (size_t)max_pages <= kMostLogits / ((size_t)B * p->cfg.h_kv * page_logits(max_new));
 }
 
 cudaError_t launch_score_few(const optr_params* p, const ScoreArgs& A, uint8_t* ws, cudaStream_t s) {
