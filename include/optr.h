@@ -653,12 +653,14 @@ optr_status optr_verify_tree(const optr_params* p, const void* target_probs,
  *               server's largest step serves its smaller ones (it holds the logits of the
  *               largest of those that has up to four tokens a sequence and 256 MB of them).
  * Logits are good to some 2^-20 of |q||k| / sqrt(128) (queries and keys of 22 bits,
- * float32 sums; of more than four tokens a query element is known to 2^-38 of the
- * largest among 64 tokens besides); sums of a position are added in a fixed order.  Queries must be finite.  A
- * sequence with pos0 < 0, or n past max_pages * 16 or n_score (OPTR_DEVERR_SEQ_LEN), more
- * than max_new tokens or inconsistent cu_new (OPTR_DEVERR_CU_NEW) adds nothing.  Positions of
- * an out-of-range page (OPTR_DEVERR_PAGE_ID) or window slot (OPTR_DEVERR_WIN_SLOT) are
- * left out of the softmax.  Nothing is allocated or synchronised.
+ * float32 sums; a query element is known to 2^-38 of the largest among 64 tokens besides,
+ * unless max_new is at most four and 256 B h_kv max_pages max_new, the bytes of all
+ * logits, are within 256 MB); sums of a position are added in a fixed order.  Queries
+ * must be finite.  A sequence with pos0 < 0, or n past max_pages * 16 or n_score
+ * (OPTR_DEVERR_SEQ_LEN), more than max_new tokens or inconsistent cu_new
+ * (OPTR_DEVERR_CU_NEW) adds nothing.  Positions of an out-of-range page
+ * (OPTR_DEVERR_PAGE_ID) or window slot (OPTR_DEVERR_WIN_SLOT) are left out of the
+ * softmax.  Nothing is allocated or synchronised.
  */
 size_t optr_kv_score_workspace_size(const optr_params* p, int n_tok, int B, int max_new,
                                     int max_pages);
