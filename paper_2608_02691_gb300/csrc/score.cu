@@ -1128,7 +1128,7 @@ extern "C" optr_status optr_kv_score_win(const optr_params* p, const void* q, in
     if (!win || !win_slot || n_slots <= 0 || !aligned(win, 16)) return OPTR_ERR_INVALID_ARG;
     w = WinArgs{(__nv_bfloat16*)const_cast<void*>(win), win_slot, n_slots};
   }
-  if ((long long)B * p->cfg.h_kv > 65535 || (long long)max_pages * kPage > 0x7fffffffll || n_tok > (1 << 24))
+  if ((long long)B * p->cfg.h_kv > 65535 || (long long)max_pages * kPage > (1LL << 30) || n_tok > (1 << 24))
     return OPTR_ERR_OUT_OF_RANGE;
   const ScoreLayout l = score_layout(p, B, max_new);
   if (!workspace || ws_bytes < optr_kv_score_workspace_size(p, n_tok, B, max_new, max_pages) || !aligned(workspace, 256)) return OPTR_ERR_WORKSPACE;
