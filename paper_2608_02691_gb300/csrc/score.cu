@@ -26,8 +26,9 @@
 // |l| <= max |k| * sum |q| holds for every tile of ordinary inputs: then the reference is 0
 // and no maximum is looked for (70 us; with one for each column 95).  A sum over reference 0
 // may be as small as 2^-118, beside which a later tile's terms below 2^-126 are nothing to a
-// float and yet count: before the first tile that needs a look, such sums are brought near 1,
-// their references with them.  So are all before those of warps and CTAs are joined.
+// float and yet count: where a tile that gets a look lies 2^20 and more below a reference, such
+// sums are brought near 1, their references with them.  So are all before those of warps and CTAs
+// are joined.
 //
 // Rounding.  The sums are float32, and a weight moves by what its logit does: rounding
 // queries or keys to 16 bits would move it by some 3e-4.  So queries go in as fp16 hi + lo
@@ -658,28 +659,8 @@ __global__ void __launch_bounds__(Roles<kNarrow>::kThreads, 1) logit_kernel(cons
               known = 0xffu;
               unseen = true;
             } else {
-              if (unseen && !near) {
-                near = true;  // (all columns have keys: it is not needed again)
-#pragma unroll
-                for (int c = 0; c < kCols; c += 32) {
-                  if (c >= n_cols) break;
-                  uint32_t mine = 0u;
-#pragma unroll
-                  for (int j = 0; j < 32; ++j) {
-                    const uint32_t e = __reduce_max_sync(0xffffffffu, __float_as_uint(acc[c + j])) & 0x7f800000u;
-                    acc[c + j] *= __uint_as_float((254u << 23) - e);
-                    mine = lane == j ? e : mine;
-                  }
-                  const float e = (float)(mine >> 23) - 127.f;
-                  if (c + lane < n_cols) {
-                    least = fminf(least, e);  // (the warp's, below)
-                    ref[c + lane] -= e;
-                  }
-                }
-                __syncwarp();
-              }
               float* by = S.meet[warp];  // by what a column's sum shrinks, twice (2^-m may be 0)
-              bool shrink = false;
+              bool shrink = false, deep = false;
 #pragma unroll 1
               for (int c = 0; c < kCols / 16; ++c) {
                 if (16 * c >= n_cols) break;
@@ -706,6 +687,28 @@ __global__ void __launch_bounds__(Roles<kNarrow>::kThreads, 1) logit_kernel(cons
                   by[16 * c + (lane >> 1)] = moves && !fresh ? ex2(-0.5f * m) : 1.f;
                 }
                 shrink |= moves && !fresh;
+                deep |= !fresh && m < -20.f && m > -INFINITY;
+              }
+              __syncwarp();
+              if (unseen && !near && __any_sync(0xffffffffu, deep)) {
+                // (all columns have keys, and those that move a sum near 1: not needed again)
+                near = shrink = true;
+#pragma unroll
+                for (int c = 0; c < kCols; c += 32) {
+                  if (c >= n_cols) break;
+                  uint32_t largest = 0u;
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) {
+                    const uint32_t x = __reduce_max_sync(0xffffffffu, __float_as_uint(acc[c + j]));
+                    if (lane == j) largest = x;
+                  }
+                  if (c + lane < n_cols && by[c + lane] == 1.f) {
+                    const float e = (float)(largest >> 23) - 127.f;
+                    by[c + lane] = ex2(-0.5f * e);
+                    ref[c + lane] -= e;
+                    least = fminf(least, -ref[c + lane]);
+                  }
+                }
               }
               least = -warp_largest(-least);
               __syncwarp();
