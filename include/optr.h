@@ -502,7 +502,8 @@ optr_status optr_chunk_attention_win(const optr_params* p, const void* q,
  *   max_new     host; at most OPTR_TREE_MAX_ROWS (else OPTR_ERR_OUT_OF_RANGE).
  * Everything else, the workspace's size and the roundings as for
  * optr_chunk_attention; parent[t] = i - 1 gives its result.  A parent out of
- * range sets OPTR_DEVERR_TREE and counts as -1.
+ * range sets OPTR_DEVERR_TREE and counts as -1.  (Any row may have the parent -1 here:
+ * optr_verify_tree takes it for a sequence's first row only.)
  */
 #define OPTR_TREE_MAX_ROWS 1024
 optr_status optr_tree_attention(const optr_params* p, const void* q,

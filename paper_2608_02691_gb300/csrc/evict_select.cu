@@ -13,9 +13,10 @@
 // before a warp's part, counted once and summed over warps and CTAs, is all it needs to
 // write its own in order.
 //
-// Bound by the number of instructions: some 60 a key of 32 lanes over its counts, and some
-// 600 a warp beside, against 6.9 MB read.  64 rows of 20011 .. 32768 take 16.4 us, 8 rows of
-// 2049 4.6 us, less than the host needs to call it (7 us).
+// Bound by a chain: up to three counts by shared atomics, the sums of each behind a barrier of
+// the cluster, one more before the list; some 60 instructions a key of 32 lanes over its
+// counts and 600 a warp beside fill 39% of the issue slots, and 6.9 MB are read.  64 rows of 20011 ..
+// 32768 take 16.4 us, 8 rows of 2049 4.6 us, less than the host needs to call it (7 us).
 #include "cluster.cuh"
 #include "optr_internal.cuh"
 

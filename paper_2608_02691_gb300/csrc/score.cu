@@ -790,7 +790,8 @@ __global__ void __launch_bounds__(Roles<kNarrow>::kThreads, 1) logit_kernel(cons
     }
   } else if (warp < kCopyWarp) {
     // --------------------------------------------------------------- keys
-    // Thread = key.  A's row in tensor memory: 64 columns of hi parts, 64 of lo.
+    // Thread = key.  A's row in tensor memory: 64 columns of its codes as they are, its four groups'
+    // (code - 1) scale with 8 of their minima's parts beside, or a window key's bf16.
     tc05::reg_dec<Roles::kKey>();
     constexpr int ms = meta_stride(kCompact);
     const int quarter = warp & 3, key = tid & 127;
